@@ -57,6 +57,21 @@
  *                        QL_ERR_UNSUPPORTED), scales unused (may be NULL);
  *                        Y = X * W^T on the fp16 path (X shifted to fp16
  *                        exactly, the weights exact, fp32 accumulation)
+ *           QL_FMT_MXFP4: 4-bit floating point with a shared exponent (the
+ *                        OCP microscaling format): packed as q4, a code's bit 3
+ *                        the sign above the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4,
+ *                        6.  scales: one BYTE per block, uint8 [N][K/32]
+ *                        (passed as the same pointer, any alignment), the
+ *                        block's values are code * 2^(byte - 127), 255 is NaN.
+ *                        qlinear_quantize writes byte =
+ *                        clamp(floor(log2 absmax) - 2, -127, 127) + 127 (0 for
+ *                        a block of zeros) and the nearest magnitudes (ties to
+ *                        the even code, at most 6).  The products take the
+ *                        values as they are (exact in bf16, fp32 accumulation;
+ *                        fp32 activations as three bf16 terms): the error is a
+ *                        few fp32 roundings.  Infinite activations, and values
+ *                        from 2^128 (bytes 253 and 254, never written), give
+ *                        infinities or NaN.  qlinear_force_path does not apply
  *   scales  fp16 bit patterns, uint16 [N][K/32]
  *   X       QL_DT_BF16: bf16 bit patterns, uint16 [M][K]; QL_DT_F32: fp32
  *   Y       fp32 [M][N]
@@ -112,8 +127,8 @@ typedef enum {
     QL_ERR_HIP = 6          /* a HIP runtime call or kernel launch failed */
 } ql_status;
 
-typedef enum { QL_FMT_Q4 = 4, QL_FMT_INT8 = 8, QL_FMT_F16 = 16 } ql_fmt;
-                                               /* q4 / int8: block fixed at 32 along K */
+/* block fixed at 32 along K (F16: none) */
+typedef enum { QL_FMT_Q4 = 4, QL_FMT_INT8 = 8, QL_FMT_F16 = 16, QL_FMT_MXFP4 = 20 } ql_fmt;
 typedef enum { QL_DT_F32 = 0, QL_DT_BF16 = 1 } ql_dtype; /* activation dtype; Y is fp32 */
 
 #define QL_BLOCK 32
@@ -186,7 +201,8 @@ int qlinear_block_forward(const ql_linear *lin, int n_lin, hipStream_t stream);
  * rounded to nearest even from the fp32 result; 2-byte aligned Y).
  * residual may be Y itself when ydt is QL_DT_F32 (an in-place residual
  * add); no other aliasing. */
-typedef enum { QL_ACT_NONE = 0, QL_ACT_GELU = 1 } ql_act;
+typedef enum { QL_ACT_NONE = 0, QL_ACT_GELU = 1,
+               QL_ACT_SILU = 2  /* of a gated pair (qlinear_block.h) only */ } ql_act;
 
 typedef struct {
     const float *bias;      /* [N] or NULL */

@@ -1,0 +1,125 @@
+// Activation of a gated feed-forward and its derivative, and the store of the
+// outputs that its kernels share.
+#pragma once
+
+#include "epilogue.h"
+#include "mx.h"
+
+namespace qlk {
+
+// act(g) and act'(g):
+//   identity
+//   GELU  g Phi(g), Phi + g phi   (Phi as in epi_gelu, phi the normal density)
+//   SiLU  g s, s (1 + g (1 - s)),   s = 1 / (1 + exp(-g))
+__device__ inline void gate_act(int act, float g, float &a, float &da)
+{
+    if (act == QL_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+        a = g * s;
+        da = s * __builtin_fmaf(g, 1.0f - s, 1.0f);
+    } else if (act == QL_ACT_GELU) {
+        const float e = __expf(-0.5f * g * g);
+        const float z = __builtin_fabsf(g) * 0.70710678118654752f;
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, z, 1.0f));
+        float q = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
+        q = __builtin_fmaf(t, q, 1.421413741f);
+        q = __builtin_fmaf(t, q, -0.284496736f);
+        q = __builtin_fmaf(t, q, 0.254829592f);
+        q = 0.5f * q * t * e;  // Phi(-|g|)
+        const float phi = g >= 0.0f ? 1.0f - q : q;
+        a = g * phi;
+        da = __builtin_fmaf(g * 0.3989422804014327f, e, phi);
+    } else {
+        a = g;
+        da = 1.0f;
+    }
+}
+
+// columns n .. n + 3 of a row starting at element `row` of an fp32 or bf16
+// output with N columns; vec: whole groups of four at 16- / 8-byte alignment
+__device__ inline void gate_store4(void *Y, bool bf16, int64_t row, int n, int N, const float (&v)[4],
+                                   bool vec)
+{
+    if (bf16) {
+        uint16_t *const o = static_cast<uint16_t *>(Y) + row + n;
+        const uint32_t lo = mx_pack_bf16(v[0], v[1]), hi = mx_pack_bf16(v[2], v[3]);
+        if (vec) {
+            *reinterpret_cast<uint2 *>(o) = make_uint2(lo, hi);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N)
+                    o[e] = (uint16_t)((e < 2 ? lo : hi) >> (16 * (e & 1)));
+        }
+    } else {
+        float *const o = static_cast<float *>(Y) + row + n;
+        if (vec) {
+            *reinterpret_cast<float4 *>(o) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < N)
+                    o[e] = v[e];
+        }
+    }
+}
+
+// The outputs of a gated pair for columns n .. n + 3 of row m (n < N, m < M):
+// g, u the two projections without their biases.  Forward: H = act(g) u.
+// Backward: dU = dH act(g), dG = dH u act'(g), rounded to bf16 as the operands
+// of the products that follow (2^-9 of each).
+__device__ inline void gate_outputs(const GateArgs &t, int M, int N, int m, int n,
+                                    const float (&g4)[4], const float (&u4)[4])
+{
+    const bool whole = n + 3 < N;
+    float g[4], u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int c = min(n + e, N - 1);
+        g[e] = g4[e] + (t.bias[0] ? t.bias[0][c] : 0.0f);
+        u[e] = u4[e] + (t.bias[1] ? t.bias[1][c] : 0.0f);
+    }
+    const int64_t row = (int64_t)m * N;
+    if (!t.dG) {
+        float h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float a, da;
+            gate_act(t.act, g[e], a, da);
+            h[e] = a * u[e];
+        }
+        gate_store4(t.H, t.hbf16, row, n, N, h, t.vec && whole);
+        return;
+    }
+    float dg[4], du[4], dh[4];
+    if (t.dhbf16) {
+        const uint16_t *const p = static_cast<const uint16_t *>(t.dH) + row + n;
+        if (t.vec && whole) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(p);
+            dh[0] = __uint_as_float(w.x << 16);
+            dh[1] = __uint_as_float(w.x & 0xFFFF0000u);
+            dh[2] = __uint_as_float(w.y << 16);
+            dh[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                dh[e] = n + e < N ? __uint_as_float((uint32_t)p[e] << 16) : 0.0f;
+        }
+    } else {
+        const float *const p = static_cast<const float *>(t.dH) + row + n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            dh[e] = n + e < N ? p[e] : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a, da;
+        gate_act(t.act, g[e], a, da);
+        du[e] = dh[e] * a;
+        dg[e] = dh[e] * u[e] * da;
+    }
+    gate_store4(t.dG, true, row, n, N, dg, t.vec && whole);
+    gate_store4(t.dU, true, row, n, N, du, t.vec && whole);
+}
+
+}  // namespace qlk

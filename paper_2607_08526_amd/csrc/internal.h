@@ -252,4 +252,100 @@ double gemv4_int8_us(const LinDesc *d, int n, int cus);
 hipError_t launch_qgemm_stream(int fmt, const StreamPlan &p, const LayerGroup &g,
                                hipStream_t stream);
 
+// MXFP4 (mxquant.hip): quantization of rows * K fp32 or bf16 values, to an
+// error status (weights, fp32) or NaN scales (status nullptr: activations),
+// and code * scale of any quantized format as fp32 or bf16 (lo, if any: the
+// bf16 rest of a bf16 value).
+hipError_t launch_mx_quantize(const void *X, bool bf16, int64_t rows, int64_t K, uint8_t *codes,
+                              uint8_t *scales, int *status, hipStream_t stream);
+hipError_t launch_dequantize(int fmt, const void *codes, const void *scales, int64_t N, int64_t K,
+                             void *W, bool bf16, void *lo, hipStream_t stream);
+
+// Rotary positions (rotary.hip): heads of dh channels next to each other in
+// rows with strides; positions of a row from the array, or start + row % period.
+struct RotaryArgs {
+    const void *x;
+    int64_t ldx;
+    void *o;
+    int64_t ldo;
+    int64_t rows;
+    int heads, dh, rot;
+    const double *freqs;       // [rot / 2], radians per position
+    const int64_t *positions;  // [rows] or nullptr
+    int64_t start, period;
+    float mscale;
+    int bf16, interleaved, adjoint;
+    int copy;                  // o is not x: the other channels are copied
+    int rows_per_wg;           // set by the launch
+};
+hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
+
+// The outputs of a gated pair (gated.h): H, or with dG the gradients of both
+// projections.
+struct GateArgs {
+    const float *bias[2];  // gate, up: [N] or nullptr
+    int act;
+    void *H;               // [M][N]
+    int hbf16;
+    const void *dH;        // [M][N]
+    int dhbf16;
+    uint16_t *dG, *dU;     // bf16 [M][N]; nullptr: forward
+    int vec;               // groups of four columns at 16- (fp32) / 8-byte alignment
+};
+
+// One layer of the few-row kernel (qgemm_rows.hip), K % 32 == 0: MXFP4 weights
+// codes[0], scales[0] on bf16, fp32 or (sx: their scales) MXFP4 activations
+// with an epilogue; or with codes[1] a gated pair in any quantized format on
+// bf16 activations.
+struct RowsArgs {
+    const void *X;
+    const uint8_t *sx;
+    const uint8_t *codes[2];
+    const void *scales[2];
+    float *Y;
+    Epilogue ep;
+    GateArgs gate;
+    int M, N, K;
+};
+struct RowsGroup {
+    RowsArgs d[QL_MAX_GROUP];
+    int begin[QL_MAX_GROUP + 1];
+    int n;
+};
+
+// bf16 products of the backward pass (gemm_bf16.hip): out[R][S] of a problem,
+// S % 8 == 0.  segs > 1: one problem, the reduction over A[0] B[0], A[1] B[1],
+// ...; segs == 1: problem i is A[i] B[0].  Rows of lda (ldb) elements, % 8 ==
+// 0, 16-byte aligned.  parts > 1: fp32 sums part[problem][parts][R][S].
+struct GemmArgs {
+    const uint16_t *A[4], *B[4];
+    int64_t lda, ldb;
+    int R, S, C;  // C: reduction length of a segment
+    int segs, parts;
+    float *part;
+    void *out[2];
+    int outbf16;
+};
+int64_t gemm_tiles(int64_t R, int64_t S);
+int gemm_parts(int64_t tiles, int64_t C, int cus);
+hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream);
+// dbg, dbu (each may be nullptr): column sums of dG, dU [M][N], N % 8 == 0
+hipError_t launch_column_sums(const uint16_t *dG, const uint16_t *dU, float *dbg, float *dbu, int M,
+                              int N, hipStream_t stream);
+
+// workgroups of 256 threads that a launch (of fewer than 2^32 threads) holds
+constexpr int64_t MAX_WORKGROUPS = ((int64_t)1 << 24) - 1;
+
+// What the entry points share (qlinear.hip): the current device's CUs, its
+// workspace for a stream (own: the caller frees it on the stream after its
+// launches), an epilogue's checks and its form for the kernels.
+int current_cus();
+bool stream_workspace(size_t bytes, hipStream_t stream, uint8_t **p, bool *own);
+int epilogue_status(const ql_epilogue &ep, const void *Y);
+Epilogue kernel_epilogue(const ql_epilogue *ep);
+
+// workgroups of a layer at the smallest tile (an upper bound of those launched)
+int64_t rows_tiles(int64_t M, int64_t N, bool gated);
+hipError_t launch_qgemm_rows(int fmt, bool xf32, RowsGroup &g, hipStream_t stream);
+
 }  // namespace qlk

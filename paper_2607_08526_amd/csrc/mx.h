@@ -1,0 +1,68 @@
+// 4-bit microscaled values (MXFP4): a block of 32 shares a scale 2^(s - 127),
+// s one byte (255: NaN), and a code is a sign bit above the magnitudes 0, 0.5,
+// 1, 1.5, 2, 3, 4, 6 (one exponent pair, one mantissa bit).  All conversions
+// here are single gfx950 instructions.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace qlk {
+
+typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t mx_u32x4 __attribute__((ext_vector_type(4)));
+
+// 2^(s - 127) as an fp32: s = 0 is a subnormal, s = 255 NaN
+__device__ inline float mx_scale(uint32_t s)
+{
+    return __uint_as_float(s == 0 ? 0x00400000u : s == 255 ? 0x7FC00000u : s << 23);
+}
+
+// two fp32 values rounded to nearest even bf16, packed (v_cvt_pk_bf16_f32)
+__device__ inline uint32_t mx_pack_bf16(float lo, float hi)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(mx_f32x2{lo, hi}, mx_bf16x2));
+}
+
+// the 8 codes of a word times a power of two, as 8 bf16 in k order.  Exact: a
+// code has two significant bits and bf16 the exponents of the scale byte
+// (magnitudes from 2^128, which only scales that quantization never gives
+// reach, are infinite; those below 2^-126 are bf16 subnormals).
+__device__ inline mx_u32x4 mx_bf16x8(uint32_t word, float scale)
+{
+    return mx_u32x4{
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3))};
+}
+
+// fp32 weights c * s of 8 q4 codes (one word) or int8 codes (two words): exact
+// (the code has at most 8 significant bits and the scale 11)
+__device__ inline void q4_f32x8(uint32_t word, float s, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = (float)((int32_t)(word << (28 - 4 * e)) >> 28) * s;
+}
+__device__ inline void int8_f32x8(uint32_t w0, uint32_t w1, float s, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = (float)((int32_t)((e < 4 ? w0 : w1) << (24 - 8 * (e & 3))) >> 24) * s;
+}
+
+// v as hi + lo, bf16 each and packed: |v - hi - lo| <= 2^-18 |v|
+__device__ inline void split2(const float (&v)[8], mx_u32x4 &hi, mx_u32x4 &lo)
+{
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t h = mx_pack_bf16(v[2 * w], v[2 * w + 1]);
+        hi[w] = h;
+        lo[w] = mx_pack_bf16(v[2 * w] - __uint_as_float(h << 16),
+                             v[2 * w + 1] - __uint_as_float(h & 0xFFFF0000u));
+    }
+}
+
+}  // namespace qlk

@@ -20,7 +20,7 @@ constexpr int64_t I31 = (int64_t)1 << 31;
 
 bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-bool fmt_ok(int f) { return f == QL_FMT_INT8 || f == QL_FMT_Q4; }
+bool fmt_ok(int f) { return f == QL_FMT_INT8 || f == QL_FMT_Q4 || f == QL_FMT_MXFP4; }
 
 // formats the forward product takes: the quantized ones and fp16 weights
 bool fwd_fmt_ok(int f) { return fmt_ok(f) || f == QL_FMT_F16; }
@@ -40,7 +40,7 @@ int check_linear(int fmt, const void *X, int xdt, int64_t M, int64_t K, const vo
         return QL_ERR_UNSUPPORTED;
     if (!codes || (!f16 && !scales) || (M > 0 && (!X || !Y)))
         return QL_ERR_INVALID;
-    if (!aligned(codes, 16) || (!f16 && !aligned(scales, 2)) ||
+    if (!aligned(codes, 16) || (!f16 && fmt != QL_FMT_MXFP4 && !aligned(scales, 2)) ||
         (M > 0 && (!aligned(X, 16) || !aligned(Y, ydt == QL_DT_BF16 ? 2 : 4))))
         return QL_ERR_ALIGN;
     return QL_OK;
@@ -1256,11 +1256,41 @@ GroupPath choose_path(const ql_linear_ep *const *ls, int n, int forced, KgPlan &
     return tall && all_wide ? GroupPath::WIDE : GroupPath::TILED;
 }
 
+// One launch over MXFP4 layers that share xdt (M > 0 each).
+int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t stream)
+{
+    RowsGroup g{};
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        const ql_linear &l = ls[i]->lin;
+        RowsArgs &d = g.d[i];
+        d.X = l.X;
+        d.codes[0] = (const uint8_t *)l.codes;
+        d.scales[0] = l.scales;
+        d.Y = l.Y;
+        d.ep = to_epilogue(ls[i]->ep);
+        d.M = (int)l.M;
+        d.N = (int)l.N;
+        d.K = (int)l.K;
+        tiles += rows_tiles(l.M, l.N, false);
+    }
+    g.n = n;
+    if (tiles > MAX_WORKGROUPS)
+        return QL_ERR_UNSUPPORTED;
+    if (wsrc.dry_run)
+        return QL_OK;
+    return launch_qgemm_rows(QL_FMT_MXFP4, ls[0]->lin.xdt == QL_DT_F32, g, stream) == hipSuccess
+               ? QL_OK
+               : QL_ERR_HIP;
+}
+
 // One grouped launch over layers that share fmt and xdt (M > 0 each).
 int launch_group(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t stream)
 {
     if (n == 0)
         return QL_OK;
+    if (ls[0]->lin.fmt == QL_FMT_MXFP4)
+        return launch_mx(ls, n, wsrc, stream);
     const bool xf32 = ls[0]->lin.xdt == QL_DT_F32;
     const int forced = g_forced_path.load(std::memory_order_relaxed);
     const ql_linear_ep *ord[QL_MAX_GROUP];
@@ -1442,8 +1472,9 @@ int launch_group(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream
 // The layers of a block call, partitioned by (fmt, xdt): each class is one
 // launch_group call.
 struct Classes {
-    const ql_linear_ep *cls[6][QL_MAX_GROUP];
-    int cnt[6];
+    static constexpr int N = 8;
+    const ql_linear_ep *cls[N][QL_MAX_GROUP];
+    int cnt[N];
 };
 
 int classify(const ql_linear_ep *lin, int n_lin, Classes &c)
@@ -1455,12 +1486,15 @@ int classify(const ql_linear_ep *lin, int n_lin, Classes &c)
         if (st != QL_OK)
             return st;
     }
-    std::fill(c.cnt, c.cnt + 6, 0);
+    std::fill(c.cnt, c.cnt + Classes::N, 0);
     for (int i = 0; i < n_lin; ++i) {
         const ql_linear &l = lin[i].lin;
         if (l.M == 0)
             continue;
-        const int f = l.fmt == QL_FMT_Q4 ? 0 : l.fmt == QL_FMT_INT8 ? 1 : 2;
+        const int f = l.fmt == QL_FMT_Q4     ? 0
+                      : l.fmt == QL_FMT_INT8 ? 1
+                      : l.fmt == QL_FMT_F16  ? 2
+                                             : 3;
         const int k = 2 * f + (l.xdt == QL_DT_BF16 ? 1 : 0);
         c.cls[k][c.cnt[k]++] = &lin[i];
     }
@@ -1553,6 +1587,26 @@ private:
 
 }  // namespace
 
+namespace qlk {
+
+int current_cus() { return device_cus(); }
+
+bool stream_workspace(size_t bytes, hipStream_t stream, uint8_t **p, bool *own)
+{
+    Workspace w{};
+    if (!take_workspace(bytes, stream, w))
+        return false;
+    *p = w.ptr;
+    *own = w.own_alloc;
+    return true;
+}
+
+int epilogue_status(const ql_epilogue &ep, const void *Y) { return check_epilogue(ep, Y); }
+
+Epilogue kernel_epilogue(const ql_epilogue *ep) { return to_epilogue(ep ? *ep : NO_EPILOGUE); }
+
+}  // namespace qlk
+
 extern "C" {
 
 size_t qlinear_codes_bytes(int fmt, int64_t N, int64_t K)
@@ -1560,8 +1614,8 @@ size_t qlinear_codes_bytes(int fmt, int64_t N, int64_t K)
     if (!fwd_fmt_ok(fmt) || N <= 0 || K <= 0)
         return 0;
     return fmt == QL_FMT_INT8 ? (size_t)N * (size_t)K
-         : fmt == QL_FMT_Q4   ? (size_t)N * (size_t)(K / 2)
-                              : 2 * (size_t)N * (size_t)K;
+         : fmt == QL_FMT_F16  ? 2 * (size_t)N * (size_t)K
+                              : (size_t)N * (size_t)(K / 2);
 }
 
 size_t qlinear_scales_bytes(int64_t N, int64_t K)
@@ -1582,14 +1636,17 @@ int qlinear_quantize(int fmt, const float *W, int64_t N, int64_t K, void *codes,
         return QL_ERR_UNSUPPORTED;
     if (!W || !codes || !scales)
         return QL_ERR_INVALID;
-    if (!aligned(W, 16) || !aligned(codes, 16) || !aligned(scales, 2))
+    if (!aligned(W, 16) || !aligned(codes, 16) || (fmt != QL_FMT_MXFP4 && !aligned(scales, 2)))
         return QL_ERR_ALIGN;
 
     StatusSlot slot;
     if (!slot.word)
         return QL_ERR_HIP;
     *slot.word = QL_OK;
-    bool ok = launch_quantize(fmt, W, N, K, (uint8_t *)codes, scales, slot.word, stream) ==
+    bool ok = (fmt == QL_FMT_MXFP4
+                   ? launch_mx_quantize(W, false, N, K, (uint8_t *)codes, (uint8_t *)scales,
+                                        slot.word, stream)
+                   : launch_quantize(fmt, W, N, K, (uint8_t *)codes, scales, slot.word, stream)) ==
               hipSuccess;
     // (waited for also after a failed launch: the word is given back below)
     ok = hipStreamSynchronize(stream) == hipSuccess && ok;
@@ -1622,7 +1679,7 @@ int qlinear_block_forward_ep(const ql_linear_ep *lin, int n_lin, hipStream_t str
     const int st = classify(lin, n_lin, c);
     if (st != QL_OK)
         return st;
-    for (int k = 0; k < 6; ++k) {
+    for (int k = 0; k < Classes::N; ++k) {
         WsSource src = pool_source();
         const int s = launch_group(c.cls[k], c.cnt[k], src, stream);
         if (s != QL_OK)
@@ -1643,12 +1700,12 @@ int qlinear_block_forward_ep_noalloc(const ql_linear_ep *lin, int n_lin, hipStre
     // size every class's workspace before anything is enqueued; classes run
     // in stream order, so each reuses the scratch from its start
     WsSource dry{base, SCRATCH_BYTES, true, 0};
-    for (int k = 0; k < 6; ++k)
+    for (int k = 0; k < Classes::N; ++k)
         if ((st = launch_group(c.cls[k], c.cnt[k], dry, stream)) != QL_OK)
             return st;
     if (dry.need > SCRATCH_BYTES)
         return QL_ERR_UNSUPPORTED;
-    for (int k = 0; k < 6; ++k) {
+    for (int k = 0; k < Classes::N; ++k) {
         WsSource src{base, SCRATCH_BYTES, false, 0};
         if ((st = launch_group(c.cls[k], c.cnt[k], src, stream)) != QL_OK)
             return st;

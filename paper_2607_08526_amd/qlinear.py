@@ -1,11 +1,13 @@
-"""Python binding of libqlinear.so (include/qlinear.h).
+"""Python binding of libqlinear.so (include/qlinear.h, include/qlinear_block.h).
 
 Argument marshalling only: every step of quantization and of the forward
 product runs in the library's HIP kernels.  PyTorch provides device memory
 and the current HIP stream.  There is no fallback: if the library is missing
 or the process has no GPU, calls raise.
 """
+import collections
 import ctypes
+import math
 import os
 
 import torch
@@ -15,10 +17,12 @@ from . import build as _build
 FMT_Q4 = 4
 FMT_INT8 = 8
 FMT_F16 = 16  # unquantized fp16 weights (forward only; scales unused)
+FMT_MXFP4 = 20  # 4-bit floating point, one scale byte (a power of two) per block
 DT_F32 = 0
 DT_BF16 = 1
 ACT_NONE = 0
 ACT_GELU = 1  # exact GELU, x * Phi(x)
+ACT_SILU = 2  # x * sigmoid(x), of a gated pair only
 BLOCK = 32
 MAX_GROUP = 8
 
@@ -33,6 +37,9 @@ EXPORTS = [
     "qlinear_block_forward_ep", "qlinear_quantize_act", "qlinear_forward_w8a8",
     "qlinear_steer", "qlinear_attention", "qlinear_status_string",
     "qlinear_force_path", "qlinear_block_forward_ep_noalloc",
+    # include/qlinear_block.h
+    "qlinear_mx_scales_bytes", "qlinear_dequantize", "qlinear_mx_quantize_act",
+    "qlinear_mx_forward", "qlinear_gated_forward", "qlinear_gated_backward", "qlinear_rotary",
 ]
 
 PATH_AUTO, PATH_GEMV, PATH_STREAM, PATH_SKINNY, PATH_TILED, PATH_WIDE, PATH_MID = range(7)
@@ -73,6 +80,39 @@ class _Epilogue(ctypes.Structure):
 
 class _LinearEp(ctypes.Structure):
     _fields_ = [("lin", _Linear), ("ep", _Epilogue)]
+
+
+class _Gated(ctypes.Structure):
+    _fields_ = [
+        ("fmt", ctypes.c_int),
+        ("X", ctypes.c_void_p),
+        ("M", ctypes.c_int64),
+        ("K", ctypes.c_int64),
+        ("N", ctypes.c_int64),
+        ("gate_codes", ctypes.c_void_p),
+        ("gate_scales", ctypes.c_void_p),
+        ("up_codes", ctypes.c_void_p),
+        ("up_scales", ctypes.c_void_p),
+        ("gate_bias", ctypes.c_void_p),
+        ("up_bias", ctypes.c_void_p),
+        ("act", ctypes.c_int),
+    ]
+
+
+class _GatedGrad(ctypes.Structure):
+    _fields_ = [
+        ("dH", ctypes.c_void_p),
+        ("dhdt", ctypes.c_int),
+        ("dG", ctypes.c_void_p),
+        ("dU", ctypes.c_void_p),
+        ("dX", ctypes.c_void_p),
+        ("dxdt", ctypes.c_int),
+        ("dWg", ctypes.c_void_p),
+        ("dWu", ctypes.c_void_p),
+        ("dwdt", ctypes.c_int),
+        ("dbg", ctypes.c_void_p),
+        ("dbu", ctypes.c_void_p),
+    ]
 
 
 _LIB = None
@@ -132,6 +172,22 @@ def load():
     lib.qlinear_attention.argtypes = [vp, i64, vp, i64, vp, i64, i64, i64, i64, i64,
                                       ctypes.c_float, vp, i64, ci, vp]
     lib.qlinear_attention.restype = ci
+    lib.qlinear_mx_scales_bytes.argtypes = [i64, i64]
+    lib.qlinear_mx_scales_bytes.restype = ctypes.c_size_t
+    lib.qlinear_dequantize.argtypes = [ci, vp, vp, i64, i64, vp, ci, vp]
+    lib.qlinear_dequantize.restype = ci
+    lib.qlinear_mx_quantize_act.argtypes = [vp, ci, i64, i64, vp, vp, vp]
+    lib.qlinear_mx_quantize_act.restype = ci
+    lib.qlinear_mx_forward.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp,
+                                       ctypes.POINTER(_Epilogue), vp]
+    lib.qlinear_mx_forward.restype = ci
+    lib.qlinear_gated_forward.argtypes = [ctypes.POINTER(_Gated), vp, ci, vp]
+    lib.qlinear_gated_forward.restype = ci
+    lib.qlinear_gated_backward.argtypes = [ctypes.POINTER(_Gated), ctypes.POINTER(_GatedGrad), vp]
+    lib.qlinear_gated_backward.restype = ci
+    lib.qlinear_rotary.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, i64, vp, vp, i64, i64,
+                                   ctypes.c_float, ci, ci, vp]
+    lib.qlinear_rotary.restype = ci
     lib.qlinear_block_forward.restype = ci
     lib.qlinear_force_path.argtypes = [ci]
     lib.qlinear_force_path.restype = ci
@@ -171,6 +227,7 @@ def _ptr(t):
 # written out of bounds; these checks run before the library is called.
 _TWO_BYTE = (torch.int16, torch.uint16, torch.bfloat16, torch.float16)
 _BF16_BITS = (torch.bfloat16, torch.int16, torch.uint16)
+_QUANTIZED = (FMT_INT8, FMT_Q4, FMT_MXFP4)
 
 
 def _require(t, name, dtypes, shape=None, min_cols=None):
@@ -208,16 +265,26 @@ def _on_device(*tensors):
             raise ValueError("every tensor argument must be a device (cuda) tensor")
 
 
+def _on_current_device(*tensors):
+    """_on_device, and the device that the call's stream belongs to."""
+    _on_device(*tensors)
+    dev = torch.cuda.current_device() if _device is None else _device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"every tensor argument must be on the current device (cuda:{dev}), "
+                             f"not {t.device}")
+
+
 def _require_weights(fmt, codes, scales, N, K):
     if fmt == FMT_F16:
         _require(codes, "codes (fp16 weights)", _TWO_BYTE, (N, K))
         return
-    if fmt not in (FMT_INT8, FMT_Q4):
+    if fmt not in _QUANTIZED:
         raise ValueError(f"unknown weight format {fmt}")
     if K % BLOCK:
         raise ValueError(f"K = {K} is not a multiple of {BLOCK}")
     _require(codes, "codes", (torch.uint8, torch.int8), (N, K if fmt == FMT_INT8 else K // 2))
-    _require(scales, "scales", _TWO_BYTE, (N, K // BLOCK))
+    _require(scales, "scales", (torch.uint8,) if fmt == FMT_MXFP4 else _TWO_BYTE, (N, K // BLOCK))
 
 
 def _require_x(X):
@@ -269,21 +336,23 @@ def empty_codes(fmt, N, K, device="cuda"):
                        device=device)
 
 
-def empty_scales(N, K, device="cuda"):
+def empty_scales(N, K, device="cuda", fmt=None):
+    if fmt == FMT_MXFP4:
+        return torch.empty((N, K // BLOCK), dtype=torch.uint8, device=device)
     # fp16 bit patterns; int16 storage so torch never reinterprets them
     return torch.empty((N, K // BLOCK), dtype=torch.int16, device=device)
 
 
 def quantize(fmt, W, codes=None, scales=None, stream=None):
     """Quantize fp32 W [N][K] (device) -> (codes, scales).  Synchronous."""
-    if fmt not in (FMT_INT8, FMT_Q4):
-        raise ValueError(f"quantize takes FMT_INT8 or FMT_Q4, not {fmt}")
+    if fmt not in _QUANTIZED:
+        raise ValueError(f"quantize takes FMT_INT8, FMT_Q4 or FMT_MXFP4, not {fmt}")
     _require(W, "W", (torch.float32,), (None, None))
     N, K = W.shape
     if K % BLOCK:
         raise ValueError(f"K = {K} is not a multiple of {BLOCK}")
     codes = empty_codes(fmt, N, K, W.device) if codes is None else codes
-    scales = empty_scales(N, K, W.device) if scales is None else scales
+    scales = empty_scales(N, K, W.device, fmt) if scales is None else scales
     _require_weights(fmt, codes, scales, N, K)
     _on_device(W, codes, scales)
     _check(load().qlinear_quantize(fmt, _ptr(W), N, K, _ptr(codes), _ptr(scales),
@@ -505,6 +574,196 @@ def attention(q, k, v, B, T, H, dh=64, scale=None, O=None, odtype=torch.float32,
                                     v.stride(0), B, T, H, dh, float(scale), _ptr(O),
                                     O.stride(0), odt, _stream(stream)))
     return O
+
+
+def dequantize(fmt, codes, scales, dtype=torch.float32, out=None, stream=None):
+    """The values code * scale [N][K] that codes and scales of a quantized format
+    stand for, fp32 (exact) or bf16.  Asynchronous."""
+    if fmt not in _QUANTIZED:
+        raise ValueError(f"dequantize takes FMT_INT8, FMT_Q4 or FMT_MXFP4, not {fmt}")
+    _require(codes, "codes", (torch.uint8, torch.int8), (None, None))
+    N, K = codes.shape[0], codes.shape[1] * (1 if fmt == FMT_INT8 else 2)
+    _require_weights(fmt, codes, scales, N, K)
+    if out is None:
+        out = torch.empty((N, K), dtype=dtype, device=codes.device)
+    _require(out, "out", (torch.float32, torch.bfloat16), (N, K))
+    _on_current_device(codes, scales, out)
+    _check(load().qlinear_dequantize(fmt, _ptr(codes), _ptr(scales), N, K, _ptr(out), _ydt(out),
+                                     _stream(stream)))
+    return out
+
+
+def quantize_act_mx(X, qx=None, sx=None, stream=None):
+    """MXFP4 quantization of activations X [M][K] (fp32 or bf16): returns (qx
+    uint8 [M][K/2], sx uint8 [M][K/32]).  A block with a NaN or Inf becomes NaN.
+    Asynchronous."""
+    M, K = _require_x(X)
+    if K % BLOCK or K == 0:
+        raise ValueError(f"K = {K} is not a positive multiple of {BLOCK}")
+    if qx is None:
+        qx = torch.empty((M, K // 2), dtype=torch.uint8, device=X.device)
+    if sx is None:
+        sx = torch.empty((M, K // BLOCK), dtype=torch.uint8, device=X.device)
+    _require(qx, "qx", (torch.uint8,), (M, K // 2))
+    _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
+    _on_current_device(X, qx, sx)
+    _check(load().qlinear_mx_quantize_act(_ptr(X), _xdt(X), M, K, _ptr(qx), _ptr(sx),
+                                          _stream(stream)))
+    return qx, sx
+
+
+def forward_mx(qx, sx, codes, scales, N, Y=None, bias=None, act=ACT_NONE, residual=None,
+               ydtype=torch.float32, steer=None, stream=None, ycopy=None):
+    """Product of MXFP4 activations (quantize_act_mx) and MXFP4 weights
+    (quantize(FMT_MXFP4, ...)) on the 4-bit matrix cores, with the layer epilogue
+    (arguments as forward_ep).  Asynchronous."""
+    _require(qx, "qx", (torch.uint8,), (None, None))
+    M, K = qx.shape[0], 2 * qx.shape[1]
+    _require_weights(FMT_MXFP4, codes, scales, N, K)
+    _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
+    if Y is None:
+        Y = torch.empty((M, N), dtype=ydtype, device=qx.device)
+    _require_y(Y, M, N, (torch.float32, torch.bfloat16))
+    _require_ep(bias, residual, M, N)
+    _require_steer(steer, N)
+    _require_ycopy(ycopy, Y, M, N)
+    ep = _epilogue(Y, bias, act, residual, steer, ycopy)
+    _on_current_device(qx, sx, codes, scales, Y, bias, residual, ycopy,
+                       *(steer[::2] if steer else ()))
+    _check(load().qlinear_mx_forward(_ptr(qx), _ptr(sx), M, K, _ptr(codes), _ptr(scales), N,
+                                     _ptr(Y), ctypes.byref(ep), _stream(stream)))
+    return Y
+
+
+def _gated(fmt, X, gate, up, bias, act):
+    """(_Gated, M, K, N, tensors) of a gated pair's checked arguments."""
+    _require(X, "X", _BF16_BITS, (None, None))
+    M, K = X.shape
+    if fmt not in _QUANTIZED:
+        raise ValueError(f"a gated pair takes FMT_INT8, FMT_Q4 or FMT_MXFP4 weights, not {fmt}")
+    N = gate[0].shape[0]
+    for codes, scales in (gate, up):
+        _require_weights(fmt, codes, scales, N, K)
+    bg, bu = bias if bias is not None else (None, None)
+    for b in (bg, bu):
+        if b is not None:
+            _require(b, "bias", (torch.float32,), (N,))
+    tensors = (X, *gate, *up, bg, bu)
+    return _Gated(fmt, _ptr(X), M, K, N, _ptr(gate[0]), _ptr(gate[1]), _ptr(up[0]), _ptr(up[1]),
+                  _ptr(bg), _ptr(bu), act), M, K, N, tensors
+
+
+def gated_forward(fmt, X, gate, up, H=None, bias=None, act=ACT_SILU, hdtype=torch.bfloat16,
+                  stream=None):
+    """H [M][N] = act(X . Wg^T + bg) * (X . Wu^T + bu), both projections in one
+    kernel.  X bf16 [M][K]; gate, up: (codes, scales) [N][K] of one quantized
+    format; bias: None or (bg, bu), fp32 [N] or None each; act: ACT_NONE, ACT_GELU
+    or ACT_SILU; H fp32 or bf16 (hdtype, or H's).  The block's second half is
+    forward_ep on H.  Asynchronous."""
+    g, M, K, N, tensors = _gated(fmt, X, gate, up, bias, act)
+    if H is None:
+        H = torch.empty((M, N), dtype=hdtype, device=X.device)
+    _require(H, "H", (torch.float32, torch.bfloat16), (M, N))
+    _on_current_device(H, *tensors)
+    _check(load().qlinear_gated_forward(ctypes.byref(g), _ptr(H), _ydt(H), _stream(stream)))
+    return H
+
+
+# Gradients of a gated pair: of X, of both projections' outputs before the
+# activation (bf16 [M][N]), of the weights' values and of the biases (None where
+# they were not asked for).
+GatedGrads = collections.namedtuple("GatedGrads", "X gate up W_gate W_up b_gate b_up")
+
+
+def gated_backward(fmt, X, gate, up, dH, bias=None, act=ACT_SILU, x_grad=True,
+                   weight_grads=False, bias_grads=False, dtype=torch.bfloat16, stream=None):
+    """The backward pass of gated_forward (its arguments) from dH [M][N], fp32 or
+    bf16: GatedGrads, X's and the weights' of `dtype` (fp32 or bf16), the biases'
+    fp32.  The gradients of weights are those of their values (adapters on frozen
+    weights take `gate` and `up` instead).  N % 8 == 0.  Asynchronous."""
+    g, M, K, N, tensors = _gated(fmt, X, gate, up, bias, act)
+    _require(dH, "dH", (torch.float32, torch.bfloat16), (M, N))
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"gradients are float32 or bfloat16, not {dtype}")
+    if N % 8:
+        raise ValueError(f"N = {N} is not a multiple of 8")
+    new = lambda shape, dt: torch.empty(shape, dtype=dt, device=X.device)
+    both = new((2, M, N), torch.bfloat16)
+    dX = new((M, K), dtype) if x_grad else None
+    dW = new((2, N, K), dtype) if weight_grads else (None, None)
+    db = new((2, N), torch.float32) if bias_grads else (None, None)
+    _on_current_device(dH, *tensors)
+    dt = DT_BF16 if dtype == torch.bfloat16 else DT_F32
+    d = _GatedGrad(_ptr(dH), _ydt(dH), _ptr(both[0]), _ptr(both[1]), _ptr(dX), dt, _ptr(dW[0]),
+                   _ptr(dW[1]), dt, _ptr(db[0]), _ptr(db[1]))
+    _check(load().qlinear_gated_backward(ctypes.byref(g), ctypes.byref(d), _stream(stream)))
+    return GatedGrads(dX, both[0], both[1], dW[0], dW[1], db[0], db[1])
+
+
+def rotary_frequencies(rot, base=10000.0, scaling=None, factor=1.0, context=None, device="cuda"):
+    """(freqs, mscale) for rotary: fp64 [rot/2] radians per position, base^(-2j /
+    rot), and the factor of the rotated channels.  scaling, for contexts `factor`
+    times as long as those trained on: None; "linear" (every frequency divided by
+    factor); "ntk" (the base raised so that the slowest frequency is divided by
+    factor and the fastest kept); "yarn" (frequencies that turn more than 32 times
+    within `context`, the length trained on, kept, those that turn less than once
+    divided by factor, a ramp over j between; mscale 0.1 ln(factor) + 1)."""
+    if rot < 2 or rot % 2:
+        raise ValueError(f"rot = {rot} is not a positive even number")
+    if not factor >= 1.0 or not base > 1.0:
+        raise ValueError("base > 1 and factor >= 1 are required")
+    j = torch.arange(0, rot, 2, dtype=torch.float64) / rot
+    mscale = 1.0
+    if scaling == "ntk":
+        if rot > 2:
+            base = base * factor ** (rot / (rot - 2))
+    freqs = base ** -j
+    if scaling == "linear":
+        freqs = freqs / factor
+    elif scaling == "yarn":
+        if context is None or context <= 0:
+            raise ValueError("yarn scaling needs the context trained on")
+        # the pair index whose frequency turns r times within the context
+        index = lambda r: rot * math.log(context / (2 * math.pi * r)) / (2 * math.log(base))
+        lo, hi = max(0, math.floor(index(32))), min(rot // 2 - 1, math.ceil(index(1)))
+        ramp = ((torch.arange(rot // 2, dtype=torch.float64) - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        freqs = freqs * (1 - ramp) + freqs / factor * ramp
+        mscale = 0.1 * math.log(factor) + 1.0
+    elif scaling not in (None, "ntk"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return freqs.to(device), mscale
+
+
+def rotary(x, heads, freqs, dh=64, positions=None, start=0, T=None, interleaved=False,
+           mscale=1.0, adjoint=False, out=None, stream=None):
+    """Rotary positions of the first 2 * len(freqs) channels of each of `heads`
+    heads of dh channels.  x: fp32 or bf16 2-D row view [rows][>= heads * dh] with
+    unit column stride (e.g. the query and key columns of a fused QKV output);
+    freqs fp64 (rotary_frequencies); positions: int64 [rows], or None for start +
+    row % T (sequences of T rows; None: one sequence).  interleaved: pairs of
+    neighbouring channels, otherwise of channels half the rotated part apart.
+    adjoint: the backward pass.  In place, or into the row view out (no overlap).
+    Returns it.  Asynchronous."""
+    _require(x, "x", (torch.float32, torch.bfloat16), min_cols=heads * dh)
+    _require(freqs, "freqs", (torch.float64,), (None,))
+    rows, rot = x.shape[0], 2 * freqs.shape[0]
+    if positions is not None:
+        _require(positions, "positions", (torch.int64,), (rows,))
+    out = x if out is None else out
+    _require(out, "out", (x.dtype,), min_cols=heads * dh)
+    if out.shape[0] != rows:
+        raise ValueError(f"out has {out.shape[0]} rows, expected {rows}")
+    if heads < 1 or not 2 <= rot <= dh:
+        raise ValueError(f"{heads} heads with {rot} of {dh} channels rotated")
+    if T is not None and T < 1:
+        raise ValueError(f"T = {T} is not positive")
+    _on_current_device(x, freqs, positions, out)
+    # (a single row's stride may be anything: its length serves)
+    ld = lambda t: max(t.stride(0), t.shape[1])
+    _check(load().qlinear_rotary(_ptr(x), ld(x), _ptr(out), ld(out), _ydt(x), rows, heads, dh, rot,
+                                 _ptr(freqs), _ptr(positions), start, T or max(rows, 1),
+                                 float(mscale), interleaved, adjoint, _stream(stream)))
+    return out
 
 
 class forced_path:
