@@ -57,6 +57,22 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
 {
     if (rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
+    if (tile_takes(g.K, g.gate_scales, g.up_scales) &&
+        tile_wins(g.fmt, false, true, g.M, g.N, g.K, current_cus())) {
+        TileArgs a{};
+        a.X = g.X;
+        a.planes = 1;
+        a.codes[0] = (const uint8_t *)g.gate_codes;
+        a.codes[1] = (const uint8_t *)g.up_codes;
+        a.scales[0] = g.gate_scales;
+        a.scales[1] = g.up_scales;
+        a.gate = t;
+        a.M = (int)g.M;
+        a.N = (int)g.N;
+        a.K = (int)g.K;
+        a.parts = 1;
+        return status(launch_qgemm_tile(g.fmt, a, stream));
+    }
     RowsGroup r{};
     RowsArgs &d = r.d[0];
     d.X = g.X;
@@ -142,6 +158,10 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
         return QL_ERR_ALIGN;
     if (M == 0)
         return QL_OK;
+    const Mx4Args t{qx, sx, (const uint8_t *)codes, scales, (float *)Y, kernel_epilogue(ep),
+                    (int)M, (int)N, (int)K};
+    if (mx4_takes(t) && mx4_wins(t, current_cus()))
+        return status(launch_qgemm_mx4(t, stream));
     RowsGroup g{};
     RowsArgs &d = g.d[0];
     d.X = qx;
@@ -149,7 +169,7 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
     d.codes[0] = (const uint8_t *)codes;
     d.scales[0] = scales;
     d.Y = (float *)Y;
-    d.ep = kernel_epilogue(ep);
+    d.ep = t.ep;
     d.M = (int)M;
     d.N = (int)N;
     d.K = (int)K;

@@ -50,6 +50,22 @@ __device__ inline void dma_load4(const void *base, uint32_t off, uint32_t lds)
                  : "memory");
 }
 
+// the same, each lane from its own address
+__device__ inline void dma_load16_at(const void *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                 :
+                 : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory");
+}
+__device__ inline void dma_load4_at(const void *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+                 :
+                 : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory");
+}
+
 // Wait until at most y * LOADS (+ nothing else) of the wavefront's loads
 // are still in flight, y <= Y known at run time.
 template <int LOADS, int Y>
@@ -71,6 +87,20 @@ template <typename T>
 __device__ inline void dma_pin(T &v)
 {
     asm volatile("" : "+v"(v));
+}
+
+
+// The accumulators of a stage, kept where the stage ends: matrix instructions
+// have no side effects, and the compiler would sink those of several stages
+// behind the last one's barrier, with all their operands in registers.
+template <typename T, int A, int B>
+__device__ inline void pin_accumulators(T (&acc)[A][B])
+{
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            dma_pin(acc[i][j]);
 }
 
 }  // namespace qlk

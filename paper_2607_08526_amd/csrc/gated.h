@@ -64,37 +64,38 @@ __device__ inline void gate_store4(void *Y, bool bf16, int64_t row, int n, int N
     }
 }
 
-// The outputs of a gated pair for columns n .. n + 3 of row m (n < N, m < M):
-// g, u the two projections without their biases.  Forward: H = act(g) u.
-// Backward: dU = dH act(g), dG = dH u act'(g), rounded to bf16 as the operands
-// of the products that follow (2^-9 of each).
-__device__ inline void gate_outputs(const GateArgs &t, int M, int N, int m, int n,
-                                    const float (&g4)[4], const float (&u4)[4])
+// both biases of columns n .. n + 3 (columns past N repeat the last one)
+__device__ inline void gate_bias4(const GateArgs &t, int n, int N, float (&bg)[4], float (&bu)[4])
 {
-    const bool whole = n + 3 < N;
-    float g[4], u[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int c = min(n + e, N - 1);
-        g[e] = g4[e] + (t.bias[0] ? t.bias[0][c] : 0.0f);
-        u[e] = u4[e] + (t.bias[1] ? t.bias[1][c] : 0.0f);
+        bg[e] = t.bias[0] ? t.bias[0][c] : 0.0f;
+        bu[e] = t.bias[1] ? t.bias[1][c] : 0.0f;
     }
-    const int64_t row = (int64_t)m * N;
-    if (!t.dG) {
-        float h[4];
+}
+
+// H = act(g) u of columns n .. n + 3 of the row that starts at element `row`; g,
+// u: the two projections with their biases
+__device__ inline void gate_forward(const GateArgs &t, int64_t row, int n, int N,
+                                    const float (&g)[4], const float (&u)[4])
+{
+    float h[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float a, da;
-            gate_act(t.act, g[e], a, da);
-            h[e] = a * u[e];
-        }
-        gate_store4(t.H, t.hbf16, row, n, N, h, t.vec && whole);
-        return;
+    for (int e = 0; e < 4; ++e) {
+        float a, da;
+        gate_act(t.act, g[e], a, da);
+        h[e] = a * u[e];
     }
-    float dg[4], du[4], dh[4];
+    gate_store4(t.H, t.hbf16, row, n, N, h, t.vec && n + 3 < N);
+}
+
+__device__ inline void gate_load_dh(const GateArgs &t, int64_t row, int n, int N, float (&dh)[4])
+{
+    const bool vec = t.vec && n + 3 < N;
     if (t.dhbf16) {
         const uint16_t *const p = static_cast<const uint16_t *>(t.dH) + row + n;
-        if (t.vec && whole) {
+        if (vec) {
             const uint2 w = *reinterpret_cast<const uint2 *>(p);
             dh[0] = __uint_as_float(w.x << 16);
             dh[1] = __uint_as_float(w.x & 0xFFFF0000u);
@@ -107,10 +108,28 @@ __device__ inline void gate_outputs(const GateArgs &t, int M, int N, int m, int 
         }
     } else {
         const float *const p = static_cast<const float *>(t.dH) + row + n;
+        if (vec) {
+            const float4 v = *reinterpret_cast<const float4 *>(p);
+            dh[0] = v.x;
+            dh[1] = v.y;
+            dh[2] = v.z;
+            dh[3] = v.w;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            dh[e] = n + e < N ? p[e] : 0.0f;
+            for (int e = 0; e < 4; ++e)
+                dh[e] = n + e < N ? p[e] : 0.0f;
+        }
     }
+}
+
+// dU = dH act(g), dG = dH u act'(g), rounded to bf16 as the operands of the
+// products that follow (2^-9 of each)
+__device__ inline void gate_backward(const GateArgs &t, int64_t row, int n, int N,
+                                     const float (&g)[4], const float (&u)[4],
+                                     const float (&dh)[4])
+{
+    const bool vec = t.vec && n + 3 < N;
+    float dg[4], du[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         float a, da;
@@ -118,8 +137,8 @@ __device__ inline void gate_outputs(const GateArgs &t, int M, int N, int m, int 
         du[e] = dh[e] * a;
         dg[e] = dh[e] * u[e] * da;
     }
-    gate_store4(t.dG, true, row, n, N, dg, t.vec && whole);
-    gate_store4(t.dU, true, row, n, N, du, t.vec && whole);
+    gate_store4(t.dG, true, row, n, N, dg, vec);
+    gate_store4(t.dU, true, row, n, N, du, vec);
 }
 
 }  // namespace qlk

@@ -49,18 +49,10 @@ constexpr int GROUP_M = 4;
 
 __device__ __align__(16) const uint32_t zeros[4] = {0, 0, 0, 0};
 
-// 16 bytes per lane from its own address to lds + lane * 16
-__device__ inline void dma_load16_at(const void *p, uint32_t lds)
-{
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                 :
-                 : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
-                 : "memory");
-}
-
-// swizzles of 16-byte chunks: rows of 4 chunks (reduction along the row), and
-// rows of 16 or 32 (reduction over rows)
-__device__ inline int swz4(int row) { return ((row >> 1) ^ (row >> 3)) & 3; }
+// swizzles of 16-byte chunks: rows of 4 chunks (reduction along the row; a cycle
+// of a 16-byte read serves rows 0-3, 12-15, 20-27, or the others of 32), and rows
+// of 16 or 32 (reduction over rows)
+__device__ inline int swz4(int row) { return ((row >> 2) & 3) ^ ((row >> 4) & 1) * 3; }
 __device__ inline int swzt(int row) { return (row & 3) << 2; }
 
 // Where the chunk in slot i of an operand's stage comes from: its byte offset

@@ -313,6 +313,44 @@ struct RowsGroup {
     int n;
 };
 
+// One product of the large tiles (qgemm_tile.hip): as RowsArgs on bf16
+// activations, with K % 128 == 0, K < 2^22 and 4-byte aligned scales, X of
+// `planes` bf16 planes plane_bytes apart that are added up; parts > 1 (no gated
+// pair, no epilogue): fp32 sums of `parts` K parts in part[parts][M][N].
+struct TileArgs {
+    const void *X;
+    int64_t plane_bytes;
+    int planes;
+    const uint8_t *codes[2];
+    const void *scales[2];
+    float *Y;
+    Epilogue ep;
+    GateArgs gate;
+    int M, N, K;
+    int parts;
+    float *part;
+};
+int64_t tile_tiles(int64_t M, int64_t N, bool gated);
+// whether a layer's (or a gated pair's) shape and scales allow the tiles, and
+// whether they are estimated to be the faster choice
+bool tile_takes(int64_t K, const void *scales0, const void *scales1);
+bool tile_wins(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus);
+hipError_t launch_qgemm_tile(int fmt, const TileArgs &a, hipStream_t stream);
+// fp32 X (count % 8 == 0 values) as three bf16 planes [3][count]
+hipError_t launch_split3(const float *X, int64_t count, uint16_t *planes, hipStream_t stream);
+
+// The product of MXFP4 activations and weights on the large tiles
+// (qgemm_mx4.hip): K % 128 == 0, K < 2^22, 4-byte aligned scales.
+struct Mx4Args {
+    const uint8_t *qx, *sx, *codes, *scales;
+    float *Y;
+    Epilogue ep;
+    int M, N, K;
+};
+bool mx4_takes(const Mx4Args &a);
+bool mx4_wins(const Mx4Args &a, int cus);
+hipError_t launch_qgemm_mx4(const Mx4Args &a, hipStream_t stream);
+
 // bf16 products of the backward pass (gemm_bf16.hip): out[R][S] of a problem,
 // S % 8 == 0.  segs > 1: one problem, the reduction over A[0] B[0], A[1] B[1],
 // ...; segs == 1: problem i is A[i] B[0].  Rows of lda (ldb) elements, % 8 ==

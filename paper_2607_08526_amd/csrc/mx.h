@@ -65,4 +65,28 @@ __device__ inline void split2(const float (&v)[8], mx_u32x4 &hi, mx_u32x4 &lo)
     }
 }
 
+// v as three bf16 planes, packed, largest first: the first two by truncation, so
+// that every remainder is exact (|v - sum| <= 2^-27 |v|); an infinity or NaN is
+// its own first plane, with nothing behind it
+__device__ inline void split3(const float (&v)[8], mx_u32x4 (&p)[3])
+{
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t t[2], u[2];
+        float r[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float f = v[2 * w + e];
+            const bool fin = __builtin_fabsf(f) < INFINITY;
+            t[e] = fin ? __float_as_uint(f) & 0xFFFF0000u : f != f ? 0x7FC00000u : __float_as_uint(f);
+            const float q = fin ? f - __uint_as_float(t[e]) : 0.0f;
+            u[e] = __float_as_uint(q) & 0xFFFF0000u;
+            r[e] = q - __uint_as_float(u[e]);
+        }
+        p[0][w] = t[0] >> 16 | t[1];
+        p[1][w] = u[0] >> 16 | u[1];
+        p[2][w] = mx_pack_bf16(r[0], r[1]);
+    }
+}
+
 }  // namespace qlk

@@ -129,26 +129,7 @@ __device__ inline void act_planes(const Xt<XK> &x, int j, u32x4 (&p)[P])
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             v[e] = __uint_as_float(x.v[2 * j + (e >> 2)][e & 3]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            // by truncation, so that every remainder is exact; an infinity or
-            // NaN is its own first plane, with nothing behind it
-            uint32_t t[2], u[2];
-            float r[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float f = v[2 * w + e];
-                const bool fin = __builtin_fabsf(f) < INFINITY;
-                t[e] = fin ? __float_as_uint(f) & 0xFFFF0000u
-                           : f != f ? 0x7FC00000u : __float_as_uint(f);
-                const float q = fin ? f - __uint_as_float(t[e]) : 0.0f;
-                u[e] = __float_as_uint(q) & 0xFFFF0000u;
-                r[e] = q - __uint_as_float(u[e]);
-            }
-            p[0][w] = t[0] >> 16 | t[1];
-            p[1][w] = u[0] >> 16 | u[1];
-            p[2][w] = mx_pack_bf16(r[0], r[1]);
-        }
+        split3(v, p);
     }
 }
 
@@ -283,8 +264,22 @@ __global__ __launch_bounds__(THREADS) void qgemm_rows_kernel(const RowsGroup arg
             float gv[4], uv[4];
             total(0, i, gv);
             total(1, i, uv);
-            if (m < M && n < N)
-                gate_outputs(a.gate, M, N, m, n, gv, uv);
+            if (m >= M || n >= N)
+                continue;
+            float bg[4], bu[4], dh[4];
+            gate_bias4(a.gate, n, N, bg, bu);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                gv[e] += bg[e];
+                uv[e] += bu[e];
+            }
+            const int64_t row = (int64_t)m * N;
+            if (a.gate.dG) {
+                gate_load_dh(a.gate, row, n, N, dh);
+                gate_backward(a.gate, row, n, N, gv, uv, dh);
+            } else {
+                gate_forward(a.gate, row, n, N, gv, uv);
+            }
         }
     } else {
         const bool vec = epi_vec_ok(a.ep, a.Y, N);

@@ -1256,14 +1256,44 @@ GroupPath choose_path(const ql_linear_ep *const *ls, int n, int forced, KgPlan &
     return tall && all_wide ? GroupPath::WIDE : GroupPath::TILED;
 }
 
-// One launch over MXFP4 layers that share xdt (M > 0 each).
+// MXFP4 layers that share xdt (M > 0 each): the few-row kernel's in one launch,
+// the large tiles' one after the other (fp32 activations as three bf16 planes
+// in the workspace).
 int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t stream)
 {
+    const bool xf32 = ls[0]->lin.xdt == QL_DT_F32;
+    const int cus = device_cus();
     RowsGroup g{};
+    TileArgs tiled[QL_MAX_GROUP];
+    int nt = 0;
     int64_t tiles = 0;
+    size_t bytes = 0;
     for (int i = 0; i < n; ++i) {
         const ql_linear &l = ls[i]->lin;
-        RowsArgs &d = g.d[i];
+        if (tile_takes(l.K, l.scales, nullptr) &&
+            tile_wins(l.fmt, xf32, false, l.M, l.N, l.K, cus)) {
+            TileArgs &t = tiled[nt++];
+            t = TileArgs{};
+            t.X = l.X;
+            t.planes = 1;
+            t.codes[0] = (const uint8_t *)l.codes;
+            t.scales[0] = l.scales;
+            t.Y = l.Y;
+            t.ep = to_epilogue(ls[i]->ep);
+            t.M = (int)l.M;
+            t.N = (int)l.N;
+            t.K = (int)l.K;
+            t.parts = 1;
+            if (xf32) {
+                t.planes = 3;
+                t.plane_bytes = l.M * l.K * 2;
+                bytes = std::max(bytes, (size_t)t.plane_bytes * 3);
+            }
+            if (tile_tiles(l.M, l.N, false) > MAX_WORKGROUPS)
+                return QL_ERR_UNSUPPORTED;
+            continue;
+        }
+        RowsArgs &d = g.d[g.n++];
         d.X = l.X;
         d.codes[0] = (const uint8_t *)l.codes;
         d.scales[0] = l.scales;
@@ -1274,14 +1304,35 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
         d.K = (int)l.K;
         tiles += rows_tiles(l.M, l.N, false);
     }
-    g.n = n;
     if (tiles > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
-    if (wsrc.dry_run)
+    if (wsrc.dry_run) {
+        wsrc.need = std::max(wsrc.need, bytes);
         return QL_OK;
-    return launch_qgemm_rows(QL_FMT_MXFP4, ls[0]->lin.xdt == QL_DT_F32, g, stream) == hipSuccess
-               ? QL_OK
-               : QL_ERR_HIP;
+    }
+    Workspace ws{};
+    if (bytes && !get_workspace(wsrc, bytes, stream, ws))
+        return wsrc.fixed ? QL_ERR_UNSUPPORTED : QL_ERR_HIP;
+    hipError_t e = hipSuccess;
+    for (int i = 0; i < nt && e == hipSuccess; ++i) {
+        TileArgs &t = tiled[i];
+        if (xf32) {
+            // (layers that read the same X in a row share its planes)
+            if (i == 0 || t.X != tiled[i - 1].X || t.M != tiled[i - 1].M || t.K != tiled[i - 1].K)
+                e = launch_split3((const float *)t.X, (int64_t)t.M * t.K, (uint16_t *)ws.ptr,
+                                  stream);
+        }
+        if (e == hipSuccess) {
+            TileArgs run = t;
+            if (xf32)
+                run.X = ws.ptr;
+            e = launch_qgemm_tile(QL_FMT_MXFP4, run, stream);
+        }
+    }
+    if (g.n && e == hipSuccess)
+        e = launch_qgemm_rows(QL_FMT_MXFP4, xf32, g, stream);
+    const hipError_t ef = ws.own_alloc ? hipFreeAsync(ws.ptr, stream) : hipSuccess;
+    return e == hipSuccess && ef == hipSuccess ? QL_OK : QL_ERR_HIP;
 }
 
 // One grouped launch over layers that share fmt and xdt (M > 0 each).
