@@ -70,7 +70,7 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
         a.M = (int)g.M;
         a.N = (int)g.N;
         a.K = (int)g.K;
-        a.parts = 1;
+        tile_parts(g.fmt, a, 1);
         return status(launch_qgemm_tile(g.fmt, a, stream));
     }
     RowsGroup r{};

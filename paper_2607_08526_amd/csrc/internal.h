@@ -314,7 +314,7 @@ struct RowsGroup {
 };
 
 // One product of the large tiles (qgemm_tile.hip): as RowsArgs on bf16
-// activations, with K % 128 == 0, K < 2^22 and 4-byte aligned scales, X of
+// activations, with K % 128 == 0, 256 <= K < 2^22 and 4-byte aligned scales, X of
 // `planes` bf16 planes plane_bytes apart that are added up; parts > 1 (no gated
 // pair, no epilogue): fp32 sums of `parts` K parts in part[parts][M][N].
 struct TileArgs {
@@ -327,9 +327,11 @@ struct TileArgs {
     Epilogue ep;
     GateArgs gate;
     int M, N, K;
-    int parts;
+    int parts, psteps;  // set by tile_parts: K parts and their 64-k steps
     float *part;
 };
+// cuts the reduction into `parts` parts, or as many as its length allows
+void tile_parts(int fmt, TileArgs &a, int parts);
 int64_t tile_tiles(int64_t M, int64_t N, bool gated);
 // whether a layer's (or a gated pair's) shape and scales allow the tiles, and
 // whether they are estimated to be the faster choice

@@ -10,7 +10,7 @@
 namespace qlk {
 
 typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 mx_bf16x2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t mx_u32x4 __attribute__((ext_vector_type(4)));
 
 // 2^(s - 127) as an fp32: s = 0 is a subnormal, s = 255 NaN
@@ -22,7 +22,7 @@ __device__ inline float mx_scale(uint32_t s)
 // two fp32 values rounded to nearest even bf16, packed (v_cvt_pk_bf16_f32)
 __device__ inline uint32_t mx_pack_bf16(float lo, float hi)
 {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(mx_f32x2{lo, hi}, mx_bf16x2));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(mx_f32x2{lo, hi}, mx_bf16x2_t));
 }
 
 // the 8 codes of a word times a power of two, as 8 bf16 in k order.  Exact: a
@@ -36,6 +36,19 @@ __device__ inline mx_u32x4 mx_bf16x8(uint32_t word, float scale)
         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1)),
         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2)),
         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3))};
+}
+
+// word w of mx_bf16x8 (w known at compile time)
+__device__ inline uint32_t mx_bf16x2(uint32_t word, float scale, int w)
+{
+    mx_bf16x2_t v;
+    switch (w) {
+    case 0: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0); break;
+    case 1: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1); break;
+    case 2: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2); break;
+    default: v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3); break;
+    }
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 // fp32 weights c * s of 8 q4 codes (one word) or int8 codes (two words): exact

@@ -22,9 +22,11 @@
 // activation and the product happen on the accumulators.
 //
 // Memory pipeline: direct-to-LDS loads of activations, codes and scales into a
-// ring of stages of 64 k (three; int8 two), chunks of 16 bytes XOR-swizzled;
-// one barrier per stage, at which a wavefront's own loads of the stage have
-// landed and the slot two stages back is free.  Two workgroups per CU.  Scales:
+// ring of stages of 64 k (three; int8 two), chunks of 16 bytes XOR-swizzled.  The
+// step's barrier sits before its last 16-k chunk: by then a stage is in registers
+// and its slot refilled at once, while that chunk runs and prepares the next
+// stage's first one.  Behind every MFMA goes a share of the next chunk's LDS reads
+// and conversions.  Two workgroups per CU.  Scales:
 // where a row's allow it, 16 bytes (MXFP4: of eight steps, fp16: of four) into
 // one slot that every wavefront copies to registers at the group's start, so that
 // it can be refilled behind them; otherwise dwords, one or two steps at a time (a
@@ -83,16 +85,253 @@ __device__ inline int tile_row(int r)
     return GATED ? (r >> 6) * 32 + (r & 31) : r;
 }
 
+// What a lane needs of a tile, fixed for the whole reduction, and how far the
+// loads have come.
+template <int FMT, bool SWIDE>
+struct Ctx {
+    uint8_t *ring, *sring;
+    uint32_t xoff[Geo<FMT>::XLOADS], coff[Geo<FMT>::CLOADS];
+    const uint8_t *cptr[Geo<FMT>::CLOADS];  // wave-uniform
+    const uint8_t *x;                       // of the next stage to load
+    const uint8_t *sp;                      // this thread's scale row
+    int64_t plane_skip;                     // from one plane's end to the next one
+    int plane_steps, ik, sk;                // steps of a plane; next stage, next scale group
+    int wave, lane;
+};
+
+// Operands carried from one 16-k chunk to the next, across stages too: the
+// step's raw codes and scales, and the fragments of the chunk about to be
+// multiplied.
+template <int FMT>
+struct Ops {
+    uint32_t raw[NS][4 * Geo<FMT>::CCH / 2];
+    float sc[NS];
+    u32x4 grp[NS];  // a scale group's dwords
+    u32x4 a[MS], b[NS][Geo<FMT>::PLANES];
+};
+
+// Loads of the next stage into its slot, and where scales are not SWIDE their
+// dwords (with even steps, or every one).
+template <int FMT, bool SWIDE>
+__device__ inline void issue(Ctx<FMT, SWIDE> &c, int t, int slot)
+{
+    using G = Geo<FMT>;
+    const uint32_t base = dma_lds(c.ring + slot * G::STAGE) + c.wave * 1024;
+#pragma unroll
+    for (int r = 0; r < G::XLOADS; ++r)
+        dma_load16(c.x, c.xoff[r], base + r * THREADS * 16);
+#pragma unroll
+    for (int r = 0; r < G::CLOADS; ++r)
+        dma_load16(c.cptr[r] + c.ik * G::CROW, c.coff[r], base + G::XBYTES + r * THREADS * 16);
+    if (!SWIDE && (G::SSTEPS == 1 || t % 2 == 0))
+        dma_load4_at(c.sp + (c.ik / G::SSTEPS) * 4,
+                     dma_lds(c.sring + t / G::SSTEPS % 3 * G::SBYTES) + c.wave * 256);
+    c.x += 128;
+    if (++c.ik == c.plane_steps) {
+        c.ik = 0;
+        c.x += c.plane_skip;
+    }
+}
+
+// SWIDE: 16 bytes per row, the next scale group (past the last: a group of the
+// row that is not used)
+template <int FMT, bool SWIDE>
+__device__ inline void issue_scales(Ctx<FMT, SWIDE> &c)
+{
+    dma_load16_at(c.sp + (c.sk / Geo<FMT>::SSTEPS) * 4, dma_lds(c.sring) + c.wave * 1024);
+    c.sk += 4 * Geo<FMT>::SSTEPS;
+    if (c.sk == c.plane_steps)
+        c.sk = 0;
+}
+
+template <int FMT>
+__device__ inline u32x4 read_x(const uint8_t *st, int lane, int q, int i)
+{
+    const int row = 32 * i + (lane & 31);
+    return *reinterpret_cast<const u32x4 *>(st + (row * 8 + ((4 * (lane >> 5) + q) ^ xswz(row))) *
+                                                     16);
+}
+
+// codes and scale of step t (from stage st) for fragment j; U = t % 4
+template <int FMT, bool SWIDE, int U>
+__device__ inline void read_weights(const Ctx<FMT, SWIDE> &c, const uint8_t *st, int t, int j,
+                                    Ops<FMT> &op)
+{
+    using G = Geo<FMT>;
+    const int row = c.wave * 64 + 32 * j + (c.lane & 31), g = c.lane >> 5;
+#pragma unroll
+    for (int h = 0; h < G::CCH / 2; ++h) {
+        const int lc = g * (G::CCH / 2) + h;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(
+            st + G::XBYTES + (row * G::CCH + (lc ^ cswz<FMT>(row))) * 16);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            op.raw[j][4 * h + w] = v[w];
+    }
+    if constexpr (SWIDE) {
+        if constexpr (U == 0) {
+            // MXFP4: the second four steps of a group of eight take its other half
+            if (G::SSTEPS == 2 && (t & 4)) {
+                op.grp[j][0] = op.grp[j][2];
+                op.grp[j][1] = op.grp[j][3];
+            } else {
+                op.grp[j] = *reinterpret_cast<const u32x4 *>(c.sring + row * 16);
+            }
+        }
+    } else if (G::SSTEPS == 1 || U % 2 == 0) {
+        op.grp[j][U / G::SSTEPS] = *reinterpret_cast<const uint32_t *>(
+            c.sring + t / G::SSTEPS % 3 * G::SBYTES + row * 4);
+    }
+}
+
+template <int FMT, int U>
+__device__ inline void scale_value(int lane, int j, Ops<FMT> &op)
+{
+    const int g = lane >> 5;
+    const uint32_t d = op.grp[j][U / Geo<FMT>::SSTEPS];
+    if constexpr (FMT == QL_FMT_MXFP4)
+        op.sc[j] = mx_scale(d >> (16 * (U & 1) + 8 * g) & 255u);
+    else
+        op.sc[j] = (float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * g)));
+}
+
+// word w (two k) of fragment j, chunk q
+template <int FMT>
+__device__ inline void weight_word(const Ops<FMT> &op, int j, int q, int w,
+                                   u32x4 (&b)[NS][Geo<FMT>::PLANES])
+{
+    // (pinned to where it is written: the words would otherwise gather behind the
+    // chunk's last MFMA)
+    if constexpr (FMT == QL_FMT_MXFP4) {
+        uint32_t x = mx_bf16x2(op.raw[j][q], op.sc[j], w);
+        dma_pin(x);
+        b[j][0][w] = x;
+    } else {
+        float v0, v1;
+        if constexpr (FMT == QL_FMT_Q4) {
+            v0 = (float)((int32_t)(op.raw[j][q] << (28 - 8 * w)) >> 28);
+            v1 = (float)((int32_t)(op.raw[j][q] << (24 - 8 * w)) >> 28);
+        } else {
+            const uint32_t x = op.raw[j][2 * q + (w >> 1)];
+            v0 = (float)((int32_t)(x << (24 - 16 * (w & 1))) >> 24);
+            v1 = (float)((int32_t)(x << (16 - 16 * (w & 1))) >> 24);
+        }
+        v0 *= op.sc[j];
+        v1 *= op.sc[j];
+        uint32_t h = mx_pack_bf16(v0, v1);
+        uint32_t l = mx_pack_bf16(v0 - __uint_as_float(h << 16),
+                                  v1 - __uint_as_float(h & 0xFFFF0000u));
+        dma_pin(h);
+        dma_pin(l);
+        b[j][0][w] = h;
+        b[j][Geo<FMT>::PLANES - 1][w] = l;
+    }
+}
+
+// The MFMAs of chunk Q of step t (U = t % 4), and behind each, in a group that
+// the compiler keeps together, a share of the next chunk's operands: of this
+// stage (Q < 3) or with NEXT of the next one (nxt).
+template <int FMT, bool SWIDE, int U, int Q, bool NEXT>
+__device__ inline void chunk(const Ctx<FMT, SWIDE> &c, const uint8_t *cur, const uint8_t *nxt,
+                             int t, Ops<FMT> &op, f32x16 (&acc)[MS][NS])
+{
+    constexpr int P = Geo<FMT>::PLANES, KK = MS * NS * P, UN = (U + 1) & 3;
+    constexpr int W0 = Q < 3 ? 0 : KK / 2, PER = (8 + KK - W0 - 1) / (KK - W0);  // words per MFMA
+    static_assert(NS == 2, "8 words");
+    u32x4 an[MS], bn[NS][P];
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+        const int v = P - 1 - k / (MS * NS), i = k / NS % MS, j = k % NS;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, op.a[i]), __builtin_bit_cast(bf16x8, op.b[j][v]), acc[i][j],
+            0, 0, 0);
+        if constexpr (Q < 3 || NEXT) {
+            if (Q == 3 && k < NS)
+                read_weights<FMT, SWIDE, UN>(c, nxt, t + 1, k, op);
+            if (k < 2 * MS && k % 2 == 0)
+                an[k / 2] = read_x<FMT>(Q < 3 ? cur : nxt, c.lane, Q < 3 ? Q + 1 : 0, k / 2);
+            if (Q == 3 && k == W0 - 1) {
+#pragma unroll
+                for (int jj = 0; jj < NS; ++jj)
+                    scale_value<FMT, UN>(c.lane, jj, op);
+            }
+            if (k >= W0) {
+#pragma unroll
+                for (int w = (k - W0) * PER; w < (k - W0 + 1) * PER; ++w)
+                    if (w < 8)
+                        weight_word<FMT>(op, w / 4, Q < 3 ? Q + 1 : 0, w % 4, bn);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (Q < 3 || NEXT) {
+#pragma unroll
+        for (int i = 0; i < MS; ++i)
+            op.a[i] = an[i];
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int v = 0; v < P; ++v)
+                op.b[j][v] = bn[j][v];
+    }
+}
+
+// Step t (U: its place in the loop's four).  TAIL: one of the last four, all
+// conditions known, so that a step is one basic block.  Chunks 0-2 prepare their
+// successors from the stage; then all of the stage is in registers, the next one
+// has landed (loads land in order: what was issued after it may be in flight), and
+// behind the barrier the stage's slot is refilled while chunk 3 runs and prepares
+// the next stage's first one.
+template <int FMT, bool SWIDE, int U, bool TAIL>
+__device__ inline void step(Ctx<FMT, SWIDE> &c, int t, int &slot, Ops<FMT> &op,
+                            f32x16 (&acc)[MS][NS])
+{
+    using G = Geo<FMT>;
+    constexpr int NST = G::NST;
+    constexpr bool LAST = TAIL && U == 3;                   // t + 1 == ns
+    constexpr bool ISSUE = !TAIL || U + NST < 4;            // t + NST < ns
+    constexpr bool YOUNGER = NST == 3 && (!TAIL || U < 2);  // stage t + 2 is in flight
+    const uint8_t *const cur = c.ring + slot * G::STAGE;
+    const int nslot = slot + 1 == NST ? 0 : slot + 1;
+    const uint8_t *const nxt = c.ring + nslot * G::STAGE;
+    chunk<FMT, SWIDE, U, 0, false>(c, cur, nxt, t, op, acc);
+    chunk<FMT, SWIDE, U, 1, false>(c, cur, nxt, t, op, acc);
+    chunk<FMT, SWIDE, U, 2, false>(c, cur, nxt, t, op, acc);
+    if constexpr (!LAST) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        // a group of scales starts every 4 SSTEPS steps; the next one's are issued
+        // behind its first step's barrier, before the stage
+        const bool first = G::SSTEPS == 1 || !(t & 4);
+        if constexpr (YOUNGER) {
+            if (SWIDE && U == 1 && first)
+                __builtin_amdgcn_s_waitcnt(dma_vmcnt(G::LOADS + 1));
+            else
+                __builtin_amdgcn_s_waitcnt(
+                    dma_vmcnt(G::LOADS + (!SWIDE && (G::SSTEPS == 1 || U % 2 == 0))));
+        } else {
+            __builtin_amdgcn_s_waitcnt(dma_vmcnt(0));
+        }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
+        if (SWIDE && U == 0 && first)
+            issue_scales<FMT, SWIDE>(c);
+        if constexpr (ISSUE)
+            issue<FMT, SWIDE>(c, t + NST, slot);
+        chunk<FMT, SWIDE, U, 3, true>(c, cur, nxt, t, op, acc);
+    } else {
+        chunk<FMT, SWIDE, U, 3, false>(c, cur, nxt, t, op, acc);
+    }
+    slot = nslot;
+}
+
 // SWIDE: scales 16 bytes at a time.  EPI: an epilogue beyond the output's type.
 template <int FMT, bool GATED, bool SWIDE, bool EPI>
 __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a)
 {
     using G = Geo<FMT>;
-    constexpr int NST = G::NST, P = G::PLANES;
+    constexpr int NST = G::NST;
     constexpr int COLS = GATED ? BN / 2 : BN;  // output columns of a tile
-    constexpr int SG = SWIDE ? 4 * G::SSTEPS : 2;  // steps of a scale group
     __shared__ __align__(16) uint8_t ring[G::LDS];
-    uint8_t *const sring = ring + NST * G::STAGE;
     const int M = a.M, N = a.N, K = a.K, nb = K >> 5;
     const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + COLS - 1) / COLS;
     // each XCD takes a contiguous range of the tiles, in groups of 4 row tiles
@@ -104,21 +343,27 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     const int gid = tile / (GROUP_M * tiles_n), within = tile - gid * (GROUP_M * tiles_n);
     const int gsz = min(tiles_m - gid * GROUP_M, GROUP_M);
     const int m0 = (gid * GROUP_M + within % gsz) * BM, n0 = within / gsz * COLS;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
 
     const int plane_steps = K >> 6, all_steps = plane_steps * a.planes;
-    // parts of whole scale groups (a plane is some, too)
-    const int per = ((all_steps + a.parts - 1) / a.parts + SG - 1) / SG * SG;
-    const int s0 = part * per, ns = max(0, min(all_steps, s0 + per) - s0);
+    const int s0 = part * a.psteps, ns = min(all_steps, s0 + a.psteps) - s0;
 
+    Ctx<FMT, SWIDE> c;
+    c.ring = ring;
+    c.sring = ring + NST * G::STAGE;
+    c.wave = wave;
+    c.lane = lane;
+    c.plane_steps = plane_steps;
+    const int plane = s0 / plane_steps;
+    c.ik = c.sk = s0 - plane * plane_steps;
+    c.plane_skip = a.plane_bytes - (int64_t)K * 2;
+    c.x = static_cast<const uint8_t *>(a.X) + plane * a.plane_bytes + (int64_t)m0 * K * 2 +
+          (int64_t)c.ik * 128;
     // per-lane offsets within the tile; rows past the end repeat the last one
-    uint32_t xoff[G::XLOADS];
-    const uint8_t *cptr[G::CLOADS];
-    uint32_t coff[G::CLOADS];
 #pragma unroll
     for (int r = 0; r < G::XLOADS; ++r) {
-        const int slot = r * THREADS + tid, row = slot >> 3, lc = (slot & 7) ^ xswz(row);
-        xoff[r] = (uint32_t)((min(m0 + row, M - 1) - m0) * K * 2 + lc * 16);
+        const int i = r * THREADS + tid, row = i >> 3, lc = (i & 7) ^ xswz(row);
+        c.xoff[r] = (uint32_t)((min(m0 + row, M - 1) - m0) * K * 2 + lc * 16);
     }
     const uint8_t *const cbase[2] = {a.codes[0], a.codes[GATED ? 1 : 0]};
     const uint8_t *const sbase[2] = {static_cast<const uint8_t *>(a.scales[0]),
@@ -128,38 +373,15 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     // cover 32 rows of 2 chunks, or 16 of 4)
 #pragma unroll
     for (int r = 0; r < G::CLOADS; ++r) {
-        const int slot = r * THREADS + tid, row = slot / G::CCH, lc = (slot % G::CCH) ^ cswz<FMT>(row);
+        const int i = r * THREADS + tid, row = i / G::CCH, lc = (i % G::CCH) ^ cswz<FMT>(row);
         const int n = min(n0 + tile_row<GATED>(row), N - 1) - n0;
         const int up = GATED ? __builtin_amdgcn_readfirstlane((row >> 5) & 1) : 0;
-        cptr[r] = cbase[up] + (int64_t)n0 * crow;
-        coff[r] = (uint32_t)(n * crow + lc * 16);
+        c.cptr[r] = cbase[up] + (int64_t)n0 * crow;
+        c.coff[r] = (uint32_t)(n * crow + lc * 16);
     }
     // a wavefront's 64 scale rows: of a gated pair, half of each projection
-    const uint8_t *const sp = sbase[GATED ? (tid >> 5) & 1 : 0] +
-                              (int64_t)min(n0 + tile_row<GATED>(tid), N - 1) * srow;
-
-    const uint8_t *const xb = static_cast<const uint8_t *>(a.X) + (int64_t)m0 * K * 2;
-    auto issue = [&](int t) {  // step s0 + t into its slots
-        const int s = s0 + t, plane = s / plane_steps, ks = s - plane * plane_steps;
-        uint8_t *const st = ring + t % NST * G::STAGE;
-        const uint32_t base = dma_lds(st);
-        const uint8_t *const x = xb + plane * a.plane_bytes + (int64_t)ks * 128;
-#pragma unroll
-        for (int r = 0; r < G::XLOADS; ++r)
-            dma_load16(x, xoff[r], base + (r * THREADS + wave * 64) * 16);
-#pragma unroll
-        for (int r = 0; r < G::CLOADS; ++r)
-            dma_load16(cptr[r] + (int64_t)ks * G::CROW, coff[r],
-                       base + G::XBYTES + (r * THREADS + wave * 64) * 16);
-        if (!SWIDE && (G::SSTEPS == 1 || t % 2 == 0))
-            dma_load4_at(sp + (int64_t)(ks / G::SSTEPS) * 4,
-                         dma_lds(sring + t / G::SSTEPS % 3 * G::SBYTES) + wave * 256);
-    };
-
-    auto issue_scales = [&](int t) {  // of the group from step s0 + t (or the last one)
-        const int s = s0 + min(t, ns - SG), ks = s - s / plane_steps * plane_steps;
-        dma_load16_at(sp + (int64_t)(ks / G::SSTEPS) * 4, dma_lds(sring) + wave * 1024);
-    };
+    c.sp = sbase[GATED ? (tid >> 5) & 1 : 0] +
+           (int64_t)min(n0 + tile_row<GATED>(tid), N - 1) * srow;
 
     f32x16 acc[MS][NS];
 #pragma unroll
@@ -170,108 +392,46 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
             for (int r = 0; r < 16; ++r)
                 acc[i][j][r] = 0.f;
 
-    if (SWIDE && ns > 0)
-        issue_scales(0);
+    {
+        if (SWIDE)
+            issue_scales<FMT, SWIDE>(c);
 #pragma unroll
-    for (int t = 0; t < NST - 1; ++t)
-        if (t < ns)
-            issue(t);
-    u32x4 sgrp[NS];  // SWIDE: the group's scales of this lane's rows
-    auto step = [&](int t, auto uc) {
-        constexpr int U = decltype(uc)::value, ODD = U & 1;  // t % SG
-        // loads land in order: with three stages the next one's may be in flight,
-        // and what was issued with it: a scale dword with an even step, the next
-        // group's scales behind the second step's barrier
-        constexpr int EXTRA = SWIDE ? U == 2 : G::SSTEPS == 1 || ODD;
-        if (NST == 3 && t + 1 < ns)
-            __builtin_amdgcn_s_waitcnt(dma_vmcnt(G::LOADS + EXTRA));
-        else
-            __builtin_amdgcn_s_waitcnt(dma_vmcnt(0));
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        for (int t = 0; t < NST; ++t)
+            issue<FMT, SWIDE>(c, t, t);
+        // stage 0: the younger ones may be in flight (ns >= 4 > NST)
+        constexpr int DW = SWIDE ? 0 : G::SSTEPS == 1 ? NST - 1 : (NST - 1) / 2;  // their dwords
+        __builtin_amdgcn_s_waitcnt(dma_vmcnt((NST - 1) * G::LOADS + DW));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
-        if (t + NST - 1 < ns)
-            issue(t + NST - 1);
-        if constexpr (SWIDE && U == 1)
-            issue_scales(t - 1 + SG);
-        const uint8_t *const st = ring + t % NST * G::STAGE;
-        uint32_t raw[NS][4 * G::CCH / 2];
-        float sc[NS];
+        Ops<FMT> op;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-            const int row = wave * 64 + 32 * j + l32;
-            uint32_t d;
-            if constexpr (SWIDE) {
-                if constexpr (U == 0)
-                    sgrp[j] = *reinterpret_cast<const u32x4 *>(sring + row * 16);
-                d = sgrp[j][U / G::SSTEPS];
-            } else {
-                d = *reinterpret_cast<const uint32_t *>(sring + t / G::SSTEPS % 3 * G::SBYTES +
-                                                        row * 4);
-            }
-            if constexpr (FMT == QL_FMT_MXFP4)
-                sc[j] = mx_scale(d >> (16 * ODD + 8 * g) & 255u);
-            else
-                sc[j] = (float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * g)));
-#pragma unroll
-            for (int h = 0; h < G::CCH / 2; ++h) {
-                const int lc = g * (G::CCH / 2) + h;
-                const u32x4 v = *reinterpret_cast<const u32x4 *>(
-                    st + G::XBYTES + (row * G::CCH + (lc ^ cswz<FMT>(row))) * 16);
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    raw[j][4 * h + w] = v[w];
-            }
+            read_weights<FMT, SWIDE, 0>(c, c.ring, 0, j, op);
+            scale_value<FMT, 0>(lane, j, op);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            u32x4 xa[MS], wb[NS][P];
+        for (int i = 0; i < MS; ++i)
+            op.a[i] = read_x<FMT>(c.ring, lane, 0, i);
 #pragma unroll
-            for (int i = 0; i < MS; ++i) {
-                const int row = 32 * i + l32;
-                xa[i] = *reinterpret_cast<const u32x4 *>(
-                    st + (row * 8 + ((4 * g + q) ^ xswz(row))) * 16);
-            }
-#pragma unroll
-            for (int j = 0; j < NS; ++j) {
-                if constexpr (FMT == QL_FMT_MXFP4) {
-                    wb[j][0] = mx_bf16x8(raw[j][q], sc[j]);
-                } else {
-                    float v[8];
-                    if constexpr (FMT == QL_FMT_Q4)
-                        q4_f32x8(raw[j][q], sc[j], v);
-                    else
-                        int8_f32x8(raw[j][2 * q], raw[j][2 * q + 1], sc[j], v);
-                    split2(v, wb[j][0], wb[j][P - 1]);
-                }
-            }
-#pragma unroll
-            for (int v = P - 1; v >= 0; --v)
-#pragma unroll
-                for (int i = 0; i < MS; ++i)
-#pragma unroll
-                    for (int j = 0; j < NS; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(bf16x8, xa[i]),
-                            __builtin_bit_cast(bf16x8, wb[j][v]), acc[i][j], 0, 0, 0);
+        for (int w = 0; w < 8; ++w)
+            weight_word<FMT>(op, w / 4, 0, w % 4, op.b);
+        int slot = 0, t = 0;
+        if (!SWIDE && (ns & 2)) {  // (then ns is 6 at least: the tail follows)
+            step<FMT, SWIDE, 0, false>(c, 0, slot, op, acc);
+            step<FMT, SWIDE, 1, false>(c, 1, slot, op, acc);
+            t = 2;
         }
-        pin_accumulators(acc);
-    };
-    // (ns is a multiple of SG: K % 128 == 0, and whole groups where SWIDE)
 #pragma unroll 1
-    for (int t = 0; t < ns; t += SG) {
-        step(t, std::integral_constant<int, 0>{});
-        step(t + 1, std::integral_constant<int, 1>{});
-        if constexpr (SG >= 4) {
-            step(t + 2, std::integral_constant<int, 2>{});
-            step(t + 3, std::integral_constant<int, 3>{});
+        for (; t + 4 < ns; t += 4) {
+            step<FMT, SWIDE, 0, false>(c, t, slot, op, acc);
+            step<FMT, SWIDE, 1, false>(c, t + 1, slot, op, acc);
+            step<FMT, SWIDE, 2, false>(c, t + 2, slot, op, acc);
+            step<FMT, SWIDE, 3, false>(c, t + 3, slot, op, acc);
         }
-        if constexpr (SG == 8) {
-            step(t + 4, std::integral_constant<int, 4>{});
-            step(t + 5, std::integral_constant<int, 5>{});
-            step(t + 6, std::integral_constant<int, 6>{});
-            step(t + 7, std::integral_constant<int, 7>{});
-        }
+        step<FMT, SWIDE, 0, true>(c, t, slot, op, acc);
+        step<FMT, SWIDE, 1, true>(c, t + 1, slot, op, acc);
+        step<FMT, SWIDE, 2, true>(c, t + 2, slot, op, acc);
+        step<FMT, SWIDE, 3, true>(c, t + 3, slot, op, acc);
     }
     __syncthreads();  // the ring is free: the 32 x 32 tiles turn through patches of it
 
@@ -312,10 +472,36 @@ int64_t tile_tiles(int64_t M, int64_t N, bool gated)
     return (M + BM - 1) / BM * ((N + cols - 1) / cols);
 }
 
+// scales in 16-byte chunks: whole groups in a row, 16-byte aligned
+static bool scales_wide(int fmt, int64_t K, const void *scales0, const void *scales1)
+{
+    return K % (fmt == QL_FMT_MXFP4 ? 512 : 256) == 0 &&
+           (((uintptr_t)scales0 | (uintptr_t)scales1) & 15) == 0;
+}
+
 bool tile_takes(int64_t K, const void *scales0, const void *scales1)
 {
-    return K % 128 == 0 && K < ((int64_t)1 << 22) && ((uintptr_t)scales0 & 3) == 0 &&
+    return K % 128 == 0 && K >= 256 && K < ((int64_t)1 << 22) && ((uintptr_t)scales0 & 3) == 0 &&
            ((uintptr_t)scales1 & 3) == 0;
+}
+
+void tile_parts(int fmt, TileArgs &a, int parts)
+{
+    // whole scale groups and loop rounds in a part; a last part of 4 steps or 6 at
+    // least (what the loop takes)
+    const int all = a.K / 64 * a.planes;
+    const bool wide = scales_wide(fmt, a.K, a.scales[0], a.scales[1]);
+    const int unit = wide && fmt == QL_FMT_MXFP4 ? 8 : 4;
+    for (; parts > 1; --parts) {
+        a.psteps = ((all + parts - 1) / parts + unit - 1) / unit * unit;
+        const int n = (all + a.psteps - 1) / a.psteps, last = all - (n - 1) * a.psteps;
+        if (n > 1 && last >= 4) {
+            a.parts = n;
+            return;
+        }
+    }
+    a.parts = 1;
+    a.psteps = all;
 }
 
 bool tile_wins(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus)
@@ -339,9 +525,7 @@ hipError_t launch_qgemm_tile(int fmt, const TileArgs &a, hipStream_t stream)
     const bool gated = a.codes[1] != nullptr;
     const dim3 grid((unsigned)(tile_tiles(a.M, a.N, gated) * a.parts)), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-    // scales in 16-byte chunks: whole groups in a row, 16-byte aligned
-    const bool swide = a.K % (fmt == QL_FMT_MXFP4 ? 512 : 256) == 0 &&
-                       (((uintptr_t)a.scales[0] | (uintptr_t)a.scales[1]) & 15) == 0;
+    const bool swide = scales_wide(fmt, a.K, a.scales[0], a.scales[1]);
     auto with = [&](auto fmtc, auto gatedc, auto epic) {
         constexpr int F = decltype(fmtc)::value;
         constexpr bool GD = decltype(gatedc)::value, E = decltype(epic)::value;

@@ -1283,12 +1283,12 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
             t.M = (int)l.M;
             t.N = (int)l.N;
             t.K = (int)l.K;
-            t.parts = 1;
             if (xf32) {
                 t.planes = 3;
                 t.plane_bytes = l.M * l.K * 2;
                 bytes = std::max(bytes, (size_t)t.plane_bytes * 3);
             }
+            tile_parts(l.fmt, t, 1);
             if (tile_tiles(l.M, l.N, false) > MAX_WORKGROUPS)
                 return QL_ERR_UNSUPPORTED;
             continue;
