@@ -116,8 +116,8 @@ int qlinear_dequantize(int fmt, const void *codes, const void *scales, int64_t N
         return QL_ERR_INVALID;
     if (!aligned(codes, 16) || !aligned(scales, fmt == QL_FMT_MXFP4 ? 1 : 2) || !aligned(W, 16))
         return QL_ERR_ALIGN;
-    return status(launch_dequantize(fmt, codes, scales, N, K, W, wdt == QL_DT_BF16, nullptr,
-                                    stream));
+    const DequantJob job{codes, scales, W, nullptr};
+    return status(launch_dequantize(fmt, &job, 1, N, K, wdt == QL_DT_BF16, stream));
 }
 
 int qlinear_mx_quantize_act(const void *X, int xdt, int64_t M, int64_t K, uint8_t *qx, uint8_t *sx,
@@ -224,7 +224,7 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
     // sums (the products run one after the other)
     constexpr size_t PART_BYTES = (size_t)256 << 20;
     auto parts = [&](int64_t R, int64_t S, int64_t C, int problems) {
-        const int p = gemm_parts(gemm_tiles(R, S) * problems, C, cus);
+        const int p = gemm_parts(gemm_tiles(R, S) * problems, R * problems, S, C, cus);
         const size_t one = (size_t)problems * R * S * 4;
         return (int)std::max<int64_t>(1, std::min<int64_t>(p, (int64_t)(PART_BYTES / one)));
     };
@@ -281,12 +281,12 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         a.part = part;
         a.out[0] = d->dX;
         a.outbf16 = d->dxdt == QL_DT_BF16;
-        for (int i = 0; i < 2 && s == QL_OK; ++i)
-            s = status(launch_dequantize(g->fmt, i ? g->up_codes : g->gate_codes,
-                                         i ? g->up_scales : g->gate_scales, N, K,
-                                         (void *)a.B[i * planes], true,
-                                         planes == 2 ? (void *)a.B[i * planes + 1] : nullptr,
-                                         stream));
+        const DequantJob jobs[2] = {
+            {g->gate_codes, g->gate_scales, (void *)a.B[0], planes == 2 ? (void *)a.B[1] : nullptr},
+            {g->up_codes, g->up_scales, (void *)a.B[planes],
+             planes == 2 ? (void *)a.B[3] : nullptr}};
+        if (s == QL_OK)
+            s = status(launch_dequantize(g->fmt, jobs, 2, N, K, true, stream));
         if (s == QL_OK)
             s = status(launch_gemm_bf16(false, a, 1, stream));
         if (s == QL_OK && px > 1)

@@ -15,11 +15,12 @@
 // receive 4 rows of one column each), so neither needs a transposed copy.
 //
 // Tile: 4 wavefronts compute 128 x 256, each a strip of 64 columns (4 x 2 MFMA
-// tiles).  Direct-to-LDS loads fill a ring of three stages of 32 c (72 KB, two
-// workgroups per CU); one barrier per stage: at it a wavefront's stage has
-// landed and the slot of the one before is free for the next but one.  Chunks of
-// 16 bytes are XOR-swizzled against bank conflicts.  Reductions that do not
-// divide into whole stages end in one filled up from a page of zeros.
+// tiles).  Direct-to-LDS loads fill a ring of stages of 32 c: three (72 KB, two
+// workgroups per CU), or six where there is no more than a workgroup for each CU.
+// The barrier of a stage sits before its last 16-c chunk; behind every MFMA goes a
+// share of the next chunk's LDS reads.  Chunks of 16 bytes are XOR-swizzled
+// against bank conflicts.  Reductions that do not divide into whole stages end in
+// one filled up from a page of zeros.
 //
 // Few tiles: the reduction is cut into parts whose fp32 sums another launch
 // adds in order (split_sum_kernel).
@@ -28,6 +29,7 @@
 #include "dma.h"
 #include "internal.h"
 #include "mx.h"
+#include "strip.h"
 
 namespace qlk {
 namespace {
@@ -40,7 +42,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-constexpr int BM = 128, BN = 256, BC = 32, NST = 3;
+constexpr int BM = 128, BN = 256, BC = 32;
 constexpr int MS = 4, NS = 2;  // MFMA tiles of a wavefront
 constexpr int ABYTES = BM * BC * 2, BBYTES = BN * BC * 2, STAGE = ABYTES + BBYTES;
 constexpr int ALOADS = ABYTES / 16 / THREADS, BLOADS = BBYTES / 16 / THREADS;
@@ -98,8 +100,85 @@ __device__ inline bf16x8 fragment(const uint8_t *st, int line, int q, int lane)
     }
 }
 
+// What a lane needs of a tile, fixed for the whole reduction, and how far the
+// loads have come.
+struct Ctx {
+    uint8_t *ring;
+    uint32_t aoff[ALOADS], boff[BLOADS];
+    int ac[ALOADS], bc[BLOADS];  // each chunk's first reduction index in its stage
+    const uint8_t *A, *B;        // of the next stage
+    int64_t astep, bstep;        // from one stage to the next
+    int seg, c0;                 // of the next stage
+    int wave, lane;
+};
+
 template <bool TRA>
-__global__ __launch_bounds__(THREADS, 2) void gemm_bf16_kernel(const GemmArgs a)
+__device__ inline void start_segment(const GemmArgs &a, Ctx &c, int prob, int m0, int n0)
+{
+    const bool many = a.segs > 1;
+    c.A = reinterpret_cast<const uint8_t *>(a.A[many ? c.seg : prob] +
+                                            (TRA ? c.c0 * a.lda + m0 : m0 * a.lda + c.c0));
+    c.B = reinterpret_cast<const uint8_t *>(a.B[many ? c.seg : 0] + c.c0 * a.ldb + n0);
+}
+
+template <bool TRA>
+__device__ inline void issue(const GemmArgs &a, Ctx &c, int prob, int m0, int n0, int slot)
+{
+    const uint32_t base = dma_lds(c.ring + slot * STAGE) + c.wave * 1024;
+    if (c.c0 + BC <= a.C) {
+#pragma unroll
+        for (int i = 0; i < ALOADS; ++i)
+            dma_load16(c.A, c.aoff[i], base + i * THREADS * 16);
+#pragma unroll
+        for (int i = 0; i < BLOADS; ++i)
+            dma_load16(c.B, c.boff[i], base + ABYTES + i * THREADS * 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < ALOADS; ++i)
+            dma_load16_at(c.c0 + c.ac[i] < a.C ? c.A + c.aoff[i] : (const uint8_t *)zeros,
+                          base + i * THREADS * 16);
+#pragma unroll
+        for (int i = 0; i < BLOADS; ++i)
+            dma_load16_at(c.c0 + c.bc[i] < a.C ? c.B + c.boff[i] : (const uint8_t *)zeros,
+                          base + ABYTES + i * THREADS * 16);
+    }
+    c.c0 += BC;
+    c.A += c.astep;
+    c.B += c.bstep;
+    if (c.c0 >= a.C && c.seg + 1 < a.segs) {
+        ++c.seg;
+        c.c0 = 0;
+        start_segment<TRA>(a, c, prob, m0, n0);
+    }
+}
+
+// The MFMAs of a 16-c chunk, and behind each, in a group that the compiler keeps
+// together, a share of the operands of chunk QN of stage nxt.
+template <bool TRA, int QN>
+__device__ inline void chunk(const Ctx &c, const uint8_t *nxt, bf16x8 (&av)[MS], bf16x8 (&bv)[NS],
+                             f32x16 (&acc)[MS][NS])
+{
+    bf16x8 an[MS], bn[NS];
+#pragma unroll
+    for (int k = 0; k < MS * NS; ++k) {
+        const int i = k / NS, j = k % NS;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[i], bv[j], acc[i][j], 0, 0, 0);
+        if (k < NS)
+            bn[k] = fragment<true, BN>(nxt + ABYTES, c.wave * 64 + 32 * k, QN, c.lane);
+        else if (k < NS + MS)
+            an[k - NS] = fragment<TRA, BM>(nxt, 32 * (k - NS), QN, c.lane);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < MS; ++i)
+        av[i] = an[i];
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+        bv[j] = bn[j];
+}
+
+template <bool TRA, int NST>
+__global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(const GemmArgs a)
 {
     __shared__ __align__(16) uint8_t ring[NST * STAGE];
     const int tiles_m = (a.R + BM - 1) / BM, tiles_n = (a.S + BN - 1) / BN;
@@ -113,50 +192,12 @@ __global__ __launch_bounds__(THREADS, 2) void gemm_bf16_kernel(const GemmArgs a)
     const int gid = tile / (GROUP_M * tiles_n), within = tile - gid * (GROUP_M * tiles_n);
     const int gsz = min(tiles_m - gid * GROUP_M, GROUP_M);
     const int m0 = (gid * GROUP_M + within % gsz) * BM, n0 = within / gsz * BN;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
 
     // the reduction: `segs` segments of C each, in whole stages of BC
     const int seg_steps = (a.C + BC - 1) / BC, all_steps = seg_steps * a.segs;
     const int per = (all_steps + a.parts - 1) / a.parts;
-    const int s0 = part * per, s1 = min(all_steps, s0 + per);
-
-    uint32_t aoff[ALOADS], boff[BLOADS];
-    int ac[ALOADS], bc[BLOADS];
-#pragma unroll
-    for (int i = 0; i < ALOADS; ++i)
-        aoff[i] = chunk_at<TRA, BM>(i * THREADS + tid, a.R - m0, a.lda, ac[i]);
-#pragma unroll
-    for (int i = 0; i < BLOADS; ++i)
-        boff[i] = chunk_at<true, BN>(i * THREADS + tid, a.S - n0, a.ldb, bc[i]);
-
-    auto issue = [&](int s) {
-        uint8_t *const st = ring + (s - s0) % NST * STAGE;
-        const int seg = s / seg_steps;
-        const int c0 = (s - seg * seg_steps) * BC;
-        const int w = a.segs > 1 ? seg : prob;
-        const uint8_t *const A = reinterpret_cast<const uint8_t *>(
-            a.A[w] + (TRA ? c0 * a.lda + m0 : m0 * a.lda + c0));
-        const uint8_t *const B =
-            reinterpret_cast<const uint8_t *>(a.B[a.segs > 1 ? seg : 0] + c0 * a.ldb + n0);
-        const uint32_t base = dma_lds(st);
-        if (c0 + BC <= a.C) {
-#pragma unroll
-            for (int i = 0; i < ALOADS; ++i)
-                dma_load16(A, aoff[i], base + (i * THREADS + wave * 64) * 16);
-#pragma unroll
-            for (int i = 0; i < BLOADS; ++i)
-                dma_load16(B, boff[i], base + ABYTES + (i * THREADS + wave * 64) * 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < ALOADS; ++i)
-                dma_load16_at(c0 + ac[i] < a.C ? A + aoff[i] : (const uint8_t *)zeros,
-                              base + (i * THREADS + wave * 64) * 16);
-#pragma unroll
-            for (int i = 0; i < BLOADS; ++i)
-                dma_load16_at(c0 + bc[i] < a.C ? B + boff[i] : (const uint8_t *)zeros,
-                              base + ABYTES + (i * THREADS + wave * 64) * 16);
-        }
-    };
+    const int s0 = part * per, ns = min(all_steps, s0 + per) - s0;
 
     f32x16 acc[MS][NS];
 #pragma unroll
@@ -167,70 +208,67 @@ __global__ __launch_bounds__(THREADS, 2) void gemm_bf16_kernel(const GemmArgs a)
             for (int r = 0; r < 16; ++r)
                 acc[i][j][r] = 0.f;
 
-    if (s0 < s1)
-        issue(s0);
-    if (s0 + 1 < s1)
-        issue(s0 + 1);
-    for (int s = s0; s < s1; ++s) {
-        // loads land in order: all but the next stage's
-        if (s + 1 < s1)
-            __builtin_amdgcn_s_waitcnt(dma_vmcnt(LOADS));
-        else
-            __builtin_amdgcn_s_waitcnt(dma_vmcnt(0));
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (ns > 0) {
+        Ctx c;
+        c.ring = ring;
+        c.wave = wave;
+        c.lane = lane;
+#pragma unroll
+        for (int i = 0; i < ALOADS; ++i)
+            c.aoff[i] = chunk_at<TRA, BM>(i * THREADS + tid, a.R - m0, a.lda, c.ac[i]);
+#pragma unroll
+        for (int i = 0; i < BLOADS; ++i)
+            c.boff[i] = chunk_at<true, BN>(i * THREADS + tid, a.S - n0, a.ldb, c.bc[i]);
+        c.astep = (TRA ? BC * a.lda : BC) * 2;
+        c.bstep = BC * a.ldb * 2;
+        c.seg = s0 / seg_steps;
+        c.c0 = (s0 - c.seg * seg_steps) * BC;
+        start_segment<TRA>(a, c, prob, m0, n0);
+#pragma unroll 1
+        for (int t = 0; t < NST && t < ns; ++t)
+            issue<TRA>(a, c, prob, m0, n0, t);
+        dma_wait<LOADS, NST - 1>(min(ns, NST) - 1);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
-        if (s + 2 < s1)
-            issue(s + 2);
-        const uint8_t *const st = ring + (s - s0) % NST * STAGE;
+        bf16x8 av[MS], bv[NS];
 #pragma unroll
-        for (int q = 0; q < BC / 16; ++q) {
-            bf16x8 av[MS], bv[NS];
+        for (int j = 0; j < NS; ++j)
+            bv[j] = fragment<true, BN>(ring + ABYTES, wave * 64 + 32 * j, 0, lane);
 #pragma unroll
-            for (int j = 0; j < NS; ++j)
-                bv[j] = fragment<true, BN>(st + ABYTES, wave * 64 + 32 * j, q, lane);
-#pragma unroll
-            for (int i = 0; i < MS; ++i)
-                av[i] = fragment<TRA, BM>(st, 32 * i, q, lane);
-#pragma unroll
-            for (int i = 0; i < MS; ++i)
-#pragma unroll
-                for (int j = 0; j < NS; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[i], bv[j], acc[i][j],
-                                                                        0, 0, 0);
+        for (int i = 0; i < MS; ++i)
+            av[i] = fragment<TRA, BM>(ring, 32 * i, 0, lane);
+        int slot = 0;
+        for (int t = 0; t < ns; ++t) {
+            uint8_t *const cur = ring + slot * STAGE;
+            const int nslot = slot + 1 == NST ? 0 : slot + 1;
+            chunk<TRA, 1>(c, cur, av, bv, acc);
+            // all of the stage is in registers; the next one has landed where only
+            // those younger than it are in flight (loads land in order); behind the
+            // barrier the stage's slot is refilled while its last chunk runs and
+            // prepares the next stage's first (after the last stage: from whatever
+            // the next slot holds, never multiplied)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            dma_wait<LOADS, NST - 2>(min(ns - 2 - t, NST - 2));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (t + NST < ns)
+                issue<TRA>(a, c, prob, m0, n0, slot);
+            chunk<TRA, 0>(c, ring + nslot * STAGE, av, bv, acc);
+            slot = nslot;
         }
     }
-    __syncthreads();  // the ring is free: every 32 x 32 tile turns through a patch of it
+    __syncthreads();  // the ring is free: the 32 x 32 tiles turn through patches of it
 
-    float *const patch = reinterpret_cast<float *>(ring) + wave * 1024;
     const bool to_part = a.parts > 1;
     const int64_t RS = (int64_t)a.R * a.S;
-    float *const F = to_part ? a.part + ((int64_t)prob * a.parts + part) * RS
+    Epilogue e{};
+    e.ybf16 = !to_part && a.outbf16;
+    float *const Y = to_part ? a.part + ((int64_t)prob * a.parts + part) * RS
                              : static_cast<float *>(a.out[prob]);
-    const bool bf = !to_part && a.outbf16;
-#pragma unroll
-    for (int i = 0; i < MS; ++i)
-#pragma unroll
-        for (int j = 0; j < NS; ++j) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                patch[(8 * (r >> 2) + 4 * g + (r & 3)) * 32 + l32] = acc[i][j][r];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int row = m0 + 32 * i + 8 * t + (lane >> 3);
-                const int col = n0 + wave * 64 + 32 * j + 4 * (lane & 7);
-                const f32x4 v = *reinterpret_cast<const f32x4 *>(patch + (8 * t + (lane >> 3)) * 32 +
-                                                                 4 * (lane & 7));
-                if (row >= a.R || col >= a.S)  // (S % 8 == 0: groups of four are whole)
-                    continue;
-                const int64_t at = (int64_t)row * a.S + col;
-                if (bf)
-                    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.out[prob]) + at) =
-                        u32x2{mx_pack_bf16(v[0], v[1]), mx_pack_bf16(v[2], v[3])};
-                else
-                    *reinterpret_cast<f32x4 *>(F + at) = v;
-            }
-        }
+    // (S % 8 == 0 and aligned outputs: whole groups of four)
+    strip_store<false>(e, Y, a.R, a.S, m0, n0 + wave * 64,
+                       reinterpret_cast<float *>(ring) + wave * STRIP_PATCH, lane, acc, true,
+                       !to_part);
 }
 
 // Column sums of bf16 matrices [M][N] (bias gradients), in a fixed order: a
@@ -270,21 +308,35 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const uint16_t *dG, co
 
 int64_t gemm_tiles(int64_t R, int64_t S) { return (R + BM - 1) / BM * ((S + BN - 1) / BN); }
 
-int gemm_parts(int64_t tiles, int64_t C, int cus)
+int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, int cus)
 {
-    // parts of at least 16 stages that fill the CUs about once
+    // A stage takes a workgroup 0.28 us where CUs have one each, and two on a CU
+    // take turns; a part more costs a sum's round trip through memory at 4 TB/s and
+    // the sum's launch 4 us.
     const int64_t steps = (C + BC - 1) / BC;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cus / std::max<int64_t>(1, tiles),
-                                                       std::min<int64_t>(16, steps / 16)));
+    int best = 1;
+    double us = 0.0;
+    for (int p = 1; p <= 16 && p * 8 <= std::max<int64_t>(8, steps); ++p) {
+        const double rounds = (double)((tiles * p + cus - 1) / cus);
+        const double t = rounds * ((double)((steps + p - 1) / p) * 0.28 + 3.0) +
+                         (p > 1 ? 4.0 + 8.0 * p * (double)(R * S) / 4e6 : 0.0);
+        if (p == 1 || t < us) {
+            best = p;
+            us = t;
+        }
+    }
+    return best;
 }
 
 hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(gemm_tiles(a.R, a.S) * problems * a.parts)), block(THREADS);
-    if (tra)
-        hipLaunchKernelGGL(gemm_bf16_kernel<true>, grid, block, 0, stream, a);
+    const int64_t wgs = gemm_tiles(a.R, a.S) * problems * a.parts;
+    const dim3 grid((unsigned)wgs), block(THREADS);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+    if (wgs <= current_cus())
+        tra ? go(gemm_bf16_kernel<true, 6>) : go(gemm_bf16_kernel<false, 6>);
     else
-        hipLaunchKernelGGL(gemm_bf16_kernel<false>, grid, block, 0, stream, a);
+        tra ? go(gemm_bf16_kernel<true, 3>) : go(gemm_bf16_kernel<false, 3>);
     return hipGetLastError();
 }
 

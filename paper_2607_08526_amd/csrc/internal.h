@@ -254,12 +254,16 @@ hipError_t launch_qgemm_stream(int fmt, const StreamPlan &p, const LayerGroup &g
 
 // MXFP4 (mxquant.hip): quantization of rows * K fp32 or bf16 values, to an
 // error status (weights, fp32) or NaN scales (status nullptr: activations),
-// and code * scale of any quantized format as fp32 or bf16 (lo, if any: the
-// bf16 rest of a bf16 value).
+// and code * scale of n (<= 2) tensors of a quantized format as fp32 or bf16 (lo,
+// if any: the bf16 rest of a bf16 value).
 hipError_t launch_mx_quantize(const void *X, bool bf16, int64_t rows, int64_t K, uint8_t *codes,
                               uint8_t *scales, int *status, hipStream_t stream);
-hipError_t launch_dequantize(int fmt, const void *codes, const void *scales, int64_t N, int64_t K,
-                             void *W, bool bf16, void *lo, hipStream_t stream);
+struct DequantJob {
+    const void *codes, *scales;
+    void *W, *lo;
+};
+hipError_t launch_dequantize(int fmt, const DequantJob *jobs, int n, int64_t N, int64_t K,
+                             bool bf16, hipStream_t stream);
 
 // Rotary positions (rotary.hip): heads of dh channels next to each other in
 // rows with strides; positions of a row from the array, or start + row % period.
@@ -367,7 +371,9 @@ struct GemmArgs {
     int outbf16;
 };
 int64_t gemm_tiles(int64_t R, int64_t S);
-int gemm_parts(int64_t tiles, int64_t C, int cus);
+// parts of the reduction estimated to be fastest, for `tiles` tiles in all and
+// outputs of R * S in all
+int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, int cus);
 hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream);
 // dbg, dbu (each may be nullptr): column sums of dG, dU [M][N], N % 8 == 0
 hipError_t launch_column_sums(const uint16_t *dG, const uint16_t *dU, float *dbg, float *dbu, int M,

@@ -94,12 +94,15 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const void *__restrict
 
 // 8 values of one block per thread: code * scale, exact in fp32 (a bf16 output
 // of q4 / int8 is rounded once, and lo, if any, receives what that leaves)
+struct DequantArgs {
+    DequantJob j[2];
+};
 template <int FMT, bool BF16>
-__global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restrict__ codes,
-                                                         const void *__restrict__ scales,
-                                                         int64_t groups, void *__restrict__ W,
-                                                         void *__restrict__ lo)
+__global__ __launch_bounds__(256) void dequantize_kernel(const DequantArgs a, int64_t groups)
 {
+    const uint8_t *const codes = static_cast<const uint8_t *>(a.j[blockIdx.y].codes);
+    const void *const scales = a.j[blockIdx.y].scales;
+    void *const W = a.j[blockIdx.y].W, *const lo = a.j[blockIdx.y].lo;
     for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups;
          g += (int64_t)gridDim.x * 256) {
         float v[8];
@@ -156,14 +159,16 @@ hipError_t launch_mx_quantize(const void *X, bool bf16, int64_t rows, int64_t K,
     return hipGetLastError();
 }
 
-hipError_t launch_dequantize(int fmt, const void *codes, const void *scales, int64_t N, int64_t K,
-                             void *W, bool bf16, void *lo, hipStream_t stream)
+hipError_t launch_dequantize(int fmt, const DequantJob *jobs, int n, int64_t N, int64_t K,
+                             bool bf16, hipStream_t stream)
 {
     const int64_t groups = N * (K / 8);
-    const dim3 grid((unsigned)std::min<int64_t>((groups + 255) / 256, MAX_GRID)), block(256);
+    DequantArgs a{};
+    for (int i = 0; i < n; ++i)
+        a.j[i] = jobs[i];
+    const dim3 grid((unsigned)std::min<int64_t>((groups + 255) / 256, MAX_GRID), (unsigned)n);
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid, block, 0, stream, static_cast<const uint8_t *>(codes),
-                           scales, groups, W, lo);
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, groups);
     };
     if (fmt == QL_FMT_MXFP4)
         bf16 ? go(dequantize_kernel<QL_FMT_MXFP4, true>) : go(dequantize_kernel<QL_FMT_MXFP4, false>);
