@@ -223,15 +223,21 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
     // workspace: both weights in bf16 (q4, int8: two planes each), then the larger of the products' partial
     // sums (the products run one after the other)
     constexpr size_t PART_BYTES = (size_t)256 << 20;
-    auto parts = [&](int64_t R, int64_t S, int64_t C, int problems) {
-        const int p = gemm_parts(gemm_tiles(R, S) * problems, R * problems, S, C, cus);
+    auto parts = [&](int64_t R, int64_t S, int64_t C, int problems, GemmCost cost) {
+        const int p = gemm_parts(gemm_tiles(R, S) * problems, R * problems, S, C, cost, cus);
         const size_t one = (size_t)problems * R * S * 4;
         return (int)std::max<int64_t>(1, std::min<int64_t>(p, (int64_t)(PART_BYTES / one)));
     };
     const int planes = g->fmt == QL_FMT_MXFP4 ? 1 : 2;
-    const int px = want_x ? parts(M, K, 2 * planes * N, 1) : 1;
-    const int pw = d->dWg ? parts(N, K, M, 2) : 1;
-    const size_t plane = want_x ? round256((size_t)N * K * 2) : 0;
+    // dX straight from the compressed weights up to a few hundred rows, beyond from
+    // a bf16 copy (us of dX at N = 4096, mxfp4 / q4: 128 rows of K = 1536 21.9 / 27.8
+    // against 28.8 / 36.0, 1024 rows of K = 2048 61.6 / 89.2 against 58.2 / 90.6)
+    const bool direct = M <= 512 && dx_takes(K, g->gate_scales, g->up_scales);
+    const int px = !want_x  ? 1
+                   : direct ? parts(M, K, 2 * N, 1, planes == 1 ? GemmCost{0.64, 0.45} : GemmCost{1.2, 1.2})
+                            : parts(M, K, 2 * planes * N, 1, GemmCost{0.5, 0.43});
+    const int pw = d->dWg ? parts(N, K, M, 2, GemmCost{0.5, 0.43}) : 1;
+    const size_t plane = want_x && !direct ? round256((size_t)N * K * 2) : 0;
     const size_t wbytes = 2 * planes * plane;
     const size_t part_bytes = std::max(px > 1 ? (size_t)px * M * K * 4 : 0,
                                        pw > 1 ? (size_t)pw * 2 * N * K * 4 : 0);
@@ -264,7 +270,17 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         }
         return status(launch_split_sum(sums, problems, stream));
     };
-    if (want_x && s == QL_OK) {
+    if (want_x && direct && s == QL_OK) {
+        const DxArgs a{{d->dG, d->dU},
+                       {(const uint8_t *)g->gate_codes, (const uint8_t *)g->up_codes},
+                       {g->gate_scales, g->up_scales},
+                       (int)M, (int)N, (int)K, px, part, d->dX, d->dxdt == QL_DT_BF16};
+        s = status(launch_gemm_dx(g->fmt, a, stream));
+        void *const out[1] = {d->dX};
+        if (s == QL_OK && px > 1)
+            s = sum(1, px, M, K, out, a.outbf16);
+    }
+    if (want_x && !direct && s == QL_OK) {
         GemmArgs a{};
         for (int i = 0; i < 2; ++i)
             for (int q = 0; q < planes; ++q) {

@@ -163,10 +163,15 @@ __device__ inline void chunk(const Ctx &c, const uint8_t *nxt, bf16x8 (&av)[MS],
     for (int k = 0; k < MS * NS; ++k) {
         const int i = k / NS, j = k % NS;
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[i], bv[j], acc[i][j], 0, 0, 0);
-        if (k < NS)
-            bn[k] = fragment<true, BN>(nxt + ABYTES, c.wave * 64 + 32 * k, QN, c.lane);
-        else if (k < NS + MS)
-            an[k - NS] = fragment<TRA, BM>(nxt, 32 * (k - NS), QN, c.lane);
+        // (two fragments at a time: they have to be there by the chunk's end)
+        if (k == 0) {
+#pragma unroll
+            for (int jj = 0; jj < NS; ++jj)
+                bn[jj] = fragment<true, BN>(nxt + ABYTES, c.wave * 64 + 32 * jj, QN, c.lane);
+        } else if (k <= MS / 2) {
+            an[2 * k - 2] = fragment<TRA, BM>(nxt, 32 * (2 * k - 2), QN, c.lane);
+            an[2 * k - 1] = fragment<TRA, BM>(nxt, 32 * (2 * k - 1), QN, c.lane);
+        }
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -248,7 +253,10 @@ __global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(con
             // prepares the next stage's first (after the last stage: from whatever
             // the next slot holds, never multiplied)
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            dma_wait<LOADS, NST - 2>(min(ns - 2 - t, NST - 2));
+            if (t + NST < ns)
+                __builtin_amdgcn_s_waitcnt(dma_vmcnt((NST - 2) * LOADS));
+            else
+                dma_wait<LOADS, NST - 2>(min(ns - 2 - t, NST - 2));
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (t + NST < ns)
@@ -308,18 +316,18 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const uint16_t *dG, co
 
 int64_t gemm_tiles(int64_t R, int64_t S) { return (R + BM - 1) / BM * ((S + BN - 1) / BN); }
 
-int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, int cus)
+int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, int cus)
 {
-    // A stage takes a workgroup 0.28 us where CUs have one each, and two on a CU
-    // take turns; a part more costs a sum's round trip through memory at 4 TB/s and
-    // the sum's launch 4 us.
+    // a part more costs a sum's round trip through memory at 5 TB/s, and the first
+    // one the sum's launch
     const int64_t steps = (C + BC - 1) / BC;
     int best = 1;
     double us = 0.0;
-    for (int p = 1; p <= 16 && p * 8 <= std::max<int64_t>(8, steps); ++p) {
-        const double rounds = (double)((tiles * p + cus - 1) / cus);
-        const double t = rounds * ((double)((steps + p - 1) / p) * 0.28 + 3.0) +
-                         (p > 1 ? 4.0 + 8.0 * p * (double)(R * S) / 4e6 : 0.0);
+    for (int p = 1; p <= 32 && p * 8 <= std::max<int64_t>(8, steps); ++p) {
+        const int64_t rounds = (tiles * p + cus - 1) / cus;
+        const double stage = rounds == 1 ? cost.alone_us : rounds * cost.shared_us;
+        const double t = (double)((steps + p - 1) / p) * stage + 3.0 * rounds +
+                         (p > 1 ? 4.0 + 8.0 * p * (double)(R * S) / 5e6 : 0.0);
         if (p == 1 || t < us) {
             best = p;
             us = t;

@@ -371,10 +371,29 @@ struct GemmArgs {
     int outbf16;
 };
 int64_t gemm_tiles(int64_t R, int64_t S);
-// parts of the reduction estimated to be fastest, for `tiles` tiles in all and
-// outputs of R * S in all
-int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, int cus);
+// parts of the reduction C estimated to be fastest, for `tiles` tiles and R * S
+// outputs in all; us that a stage of 32 takes a workgroup alone on its CU, and each
+// workgroup's share where a CU has several
+struct GemmCost {
+    double alone_us, shared_us;
+};
+int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, int cus);
 hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream);
+// dX of a gated pair from the compressed weights (gemm_dx.hip): d = {dG, dU} bf16
+// [M][N], N % 8 == 0, K % 128 == 0, scales 4-byte aligned (dx_takes); parts > 1:
+// fp32 sums part[parts][M][K].
+struct DxArgs {
+    const uint16_t *d[2];
+    const uint8_t *codes[2];
+    const void *scales[2];
+    int M, N, K;
+    int parts;
+    float *part;
+    void *out;
+    int outbf16;
+};
+bool dx_takes(int64_t K, const void *scales0, const void *scales1);
+hipError_t launch_gemm_dx(int fmt, const DxArgs &a, hipStream_t stream);
 // dbg, dbu (each may be nullptr): column sums of dG, dU [M][N], N % 8 == 0
 hipError_t launch_column_sums(const uint16_t *dG, const uint16_t *dU, float *dbg, float *dbu, int M,
                               int N, hipStream_t stream);

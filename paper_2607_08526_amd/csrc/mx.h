@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "qlinear.h"
+
 namespace qlk {
 
 typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
@@ -64,6 +66,30 @@ __device__ inline void int8_f32x8(uint32_t w0, uint32_t w1, float s, float (&v)[
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         v[e] = (float)((int32_t)((e < 4 ? w0 : w1) << (24 - 8 * (e & 3))) >> 24) * s;
+}
+
+// word w (two k, w known at compile time) of a run of codes as bf16 planes: raw
+// holds 8 codes a word (int8: 4); MXFP4 has one plane, hi
+template <int FMT>
+__device__ inline void decode_word(const uint32_t *raw, int w, float s, uint32_t &hi, uint32_t &lo)
+{
+    if constexpr (FMT == QL_FMT_MXFP4) {
+        hi = mx_bf16x2(raw[w >> 2], s, w & 3);
+        lo = 0;
+    } else {
+        float v0, v1;
+        if constexpr (FMT == QL_FMT_Q4) {
+            v0 = (float)((int32_t)(raw[w >> 2] << (28 - 8 * (w & 3))) >> 28);
+            v1 = (float)((int32_t)(raw[w >> 2] << (24 - 8 * (w & 3))) >> 28);
+        } else {
+            v0 = (float)((int32_t)(raw[w >> 1] << (24 - 16 * (w & 1))) >> 24);
+            v1 = (float)((int32_t)(raw[w >> 1] << (16 - 16 * (w & 1))) >> 24);
+        }
+        v0 *= s;
+        v1 *= s;
+        hi = mx_pack_bf16(v0, v1);
+        lo = mx_pack_bf16(v0 - __uint_as_float(hi << 16), v1 - __uint_as_float(hi & 0xFFFF0000u));
+    }
 }
 
 // v as hi + lo, bf16 each and packed: |v - hi - lo| <= 2^-18 |v|

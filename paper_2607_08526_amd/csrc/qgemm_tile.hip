@@ -202,29 +202,13 @@ __device__ inline void weight_word(const Ops<FMT> &op, int j, int q, int w,
 {
     // (pinned to where it is written: the words would otherwise gather behind the
     // chunk's last MFMA)
-    if constexpr (FMT == QL_FMT_MXFP4) {
-        uint32_t x = mx_bf16x2(op.raw[j][q], op.sc[j], w);
-        dma_pin(x);
-        b[j][0][w] = x;
-    } else {
-        float v0, v1;
-        if constexpr (FMT == QL_FMT_Q4) {
-            v0 = (float)((int32_t)(op.raw[j][q] << (28 - 8 * w)) >> 28);
-            v1 = (float)((int32_t)(op.raw[j][q] << (24 - 8 * w)) >> 28);
-        } else {
-            const uint32_t x = op.raw[j][2 * q + (w >> 1)];
-            v0 = (float)((int32_t)(x << (24 - 16 * (w & 1))) >> 24);
-            v1 = (float)((int32_t)(x << (16 - 16 * (w & 1))) >> 24);
-        }
-        v0 *= op.sc[j];
-        v1 *= op.sc[j];
-        uint32_t h = mx_pack_bf16(v0, v1);
-        uint32_t l = mx_pack_bf16(v0 - __uint_as_float(h << 16),
-                                  v1 - __uint_as_float(h & 0xFFFF0000u));
-        dma_pin(h);
-        dma_pin(l);
-        b[j][0][w] = h;
-        b[j][Geo<FMT>::PLANES - 1][w] = l;
+    uint32_t hi, lo;
+    decode_word<FMT>(op.raw[j], 4 * q + w, op.sc[j], hi, lo);
+    dma_pin(hi);
+    b[j][0][w] = hi;
+    if constexpr (Geo<FMT>::PLANES == 2) {
+        dma_pin(lo);
+        b[j][1][w] = lo;
     }
 }
 
