@@ -17,7 +17,7 @@ SOURCES = ["qlinear.hip", "quantize.hip", "qgemm.hip", "qgemm_wide.hip", "qgemm_
            "qgemm_w8a8.hip", "steer.hip", "attention.hip", "qgemm_mid.hip",
            "qgemm_kg.hip", "block.hip", "mxquant.hip", "rotary.hip", "qgemm_rows.hip",
            "gemm_bf16.hip", "qgemm_tile.hip",
-           "qgemm_mx4.hip", "gemm_dx.hip"]
+           "qgemm_mx4.hip", "gemm_dx.hip", "qgemm_kgm.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -40,7 +40,8 @@ SOURCE_FLAGS = {"qgemm.hip": VGPR_FORM, "qgemm_skinny.hip": VGPR_FORM,
                 "attention.hip": VGPR_FORM, "qgemm_mid.hip": VGPR_FORM,
                 "qgemm_kg.hip": VGPR_FORM, "qgemm_rows.hip": VGPR_FORM,
                 "gemm_bf16.hip": VGPR_FORM, "qgemm_tile.hip": VGPR_FORM,
-                "qgemm_mx4.hip": VGPR_FORM, "gemm_dx.hip": VGPR_FORM}
+                "qgemm_mx4.hip": VGPR_FORM, "gemm_dx.hip": VGPR_FORM,
+                "qgemm_kgm.hip": VGPR_FORM}
 
 
 def _compile(src):

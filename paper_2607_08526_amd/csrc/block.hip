@@ -57,8 +57,10 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
 {
     if (rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
-    if (tile_takes(g.K, g.gate_scales, g.up_scales) &&
-        tile_wins(g.fmt, false, true, g.M, g.N, g.K, current_cus())) {
+    int shape;
+    const RowsKernel kernel = choose_rows(g.fmt, false, true, g.M, g.M, g.N, g.K, g.gate_scales,
+                                          g.up_scales, current_cus(), &shape);
+    if (kernel == ROWS_TILE) {
         TileArgs a{};
         a.X = g.X;
         a.planes = 1;
@@ -70,7 +72,6 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
         a.M = (int)g.M;
         a.N = (int)g.N;
         a.K = (int)g.K;
-        tile_parts(g.fmt, a, 1);
         return status(launch_qgemm_tile(g.fmt, a, stream));
     }
     RowsGroup r{};
@@ -84,8 +85,11 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
     d.M = (int)g.M;
     d.N = (int)g.N;
     d.K = (int)g.K;
+    d.shape = shape;
     r.n = 1;
-    return status(launch_qgemm_rows(g.fmt, false, r, stream));
+    r.maxM = (int)g.M;
+    return status(kernel == ROWS_KGM ? launch_qgemm_kgm(g.fmt, false, r, stream)
+                                     : launch_qgemm_rows(g.fmt, false, r, stream));
 }
 
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -174,6 +178,7 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
     d.N = (int)N;
     d.K = (int)K;
     g.n = 1;
+    g.maxM = (int)M;
     return status(launch_qgemm_rows(QL_FMT_MXFP4, false, g, stream));
 }
 

@@ -15,6 +15,7 @@
 // the group's start, so that it can be refilled behind them; otherwise a dword
 // with each stage (as many memory requests as the codes).  Two workgroups per CU.
 #include <algorithm>
+#include <cmath>
 
 #include "dma.h"
 #include "internal.h"
@@ -203,21 +204,35 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
 
 }  // namespace
 
+static int64_t mx4_tiles(const Mx4Args &a)
+{
+    return ((int64_t)a.M + BM - 1) / BM * (((int64_t)a.N + BN - 1) / BN);
+}
+
 bool mx4_takes(const Mx4Args &a)
 {
     return a.K % 128 == 0 && a.K < (1 << 22) && ((uintptr_t)a.sx & 3) == 0 &&
            ((uintptr_t)a.scales & 3) == 0;
 }
 
+// Estimated us: a stage of a tile takes 0.49 us while few CUs work, 0.62 when all
+// do, two on a CU 0.66 each; a 128-k step of the few-row kernel 0.13 to 0.32 us by
+// its row tile and 0.85 ns per workgroup (6144 x 1536, tiles / few rows: 128 rows
+// 11.5 / 10.0, 256 rows 11.4 / 13.9, 1024 rows 12.8 / 41.7; 1536 x 6144: 256 rows
+// 29.1 / 19.9, 1024 rows 29.7 / 51.5).
 bool mx4_wins(const Mx4Args &a, int cus)
 {
-    return ((int64_t)a.M + BM - 1) / BM * (((int64_t)a.N + BN - 1) / BN) >= cus / 2;
+    const double r = (double)mx4_tiles(a) / cus, up = std::ceil(r), steps = (double)(a.K / 128);
+    const double tile = 5.5 + steps * (r <= 1.0 ? 0.49 + 0.13 * r : 0.66 * (r + 0.4 * (up - r)));
+    const int rows = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
+    const double wgs = (double)((a.M + rows - 1) / rows) * ((a.N + 31) / 32);
+    const double few = 4.5 + steps * ((rows == 16 ? 0.13 : rows == 32 ? 0.19 : 0.32) + 0.00085 * wgs);
+    return tile < few;
 }
 
 hipError_t launch_qgemm_mx4(const Mx4Args &a, hipStream_t stream)
 {
-    const int64_t tiles = ((int64_t)a.M + BM - 1) / BM * (((int64_t)a.N + BN - 1) / BN);
-    const dim3 grid((unsigned)tiles), block(THREADS);
+    const dim3 grid((unsigned)mx4_tiles(a)), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
     const bool epi = !strip_plain(a.ep);
     if (a.K % 512 == 0 && (((uintptr_t)a.sx | (uintptr_t)a.scales) & 15) == 0)

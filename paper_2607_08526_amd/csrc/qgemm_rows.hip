@@ -335,9 +335,7 @@ int64_t rows_tiles(int64_t M, int64_t N, bool gated)
 
 hipError_t launch_qgemm_rows(int fmt, bool xf32, RowsGroup &g, hipStream_t stream)
 {
-    int maxM = 0;
-    for (int i = 0; i < g.n; ++i)
-        maxM = std::max(maxM, g.d[i].M);
+    const int maxM = g.maxM;
     const bool gated = g.d[0].codes[1] != nullptr;
     if (gated) {
         if (fmt == QL_FMT_MXFP4)

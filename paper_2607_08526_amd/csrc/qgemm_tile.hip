@@ -32,6 +32,7 @@
 // it can be refilled behind them; otherwise dwords, one or two steps at a time (a
 // memory request per row each: as many as the codes).
 #include <algorithm>
+#include <cmath>
 
 #include "dma.h"
 #include "internal.h"
@@ -106,7 +107,7 @@ template <int FMT>
 struct Ops {
     uint32_t raw[NS][4 * Geo<FMT>::CCH / 2];
     float sc[NS];
-    u32x4 grp[NS];  // a scale group's dwords
+    u32x4 grp[NS];  // a scale group's dwords (not SWIDE: one)
     u32x4 a[MS], b[NS][Geo<FMT>::PLANES];
 };
 
@@ -179,16 +180,16 @@ __device__ inline void read_weights(const Ctx<FMT, SWIDE> &c, const uint8_t *st,
             }
         }
     } else if (G::SSTEPS == 1 || U % 2 == 0) {
-        op.grp[j][U / G::SSTEPS] = *reinterpret_cast<const uint32_t *>(
+        op.grp[j][0] = *reinterpret_cast<const uint32_t *>(
             c.sring + t / G::SSTEPS % 3 * G::SBYTES + row * 4);
     }
 }
 
-template <int FMT, int U>
+template <int FMT, bool SWIDE, int U>
 __device__ inline void scale_value(int lane, int j, Ops<FMT> &op)
 {
     const int g = lane >> 5;
-    const uint32_t d = op.grp[j][U / Geo<FMT>::SSTEPS];
+    const uint32_t d = op.grp[j][SWIDE ? U / Geo<FMT>::SSTEPS : 0];
     if constexpr (FMT == QL_FMT_MXFP4)
         op.sc[j] = mx_scale(d >> (16 * (U & 1) + 8 * g) & 255u);
     else
@@ -237,7 +238,7 @@ __device__ inline void chunk(const Ctx<FMT, SWIDE> &c, const uint8_t *cur, const
             if (Q == 3 && k == W0 - 1) {
 #pragma unroll
                 for (int jj = 0; jj < NS; ++jj)
-                    scale_value<FMT, UN>(c.lane, jj, op);
+                    scale_value<FMT, SWIDE, UN>(c.lane, jj, op);
             }
             if (k >= W0) {
 #pragma unroll
@@ -319,18 +320,16 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     const int M = a.M, N = a.N, K = a.K, nb = K >> 5;
     const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + COLS - 1) / COLS;
     // each XCD takes a contiguous range of the tiles, in groups of 4 row tiles
-    // walked row tile fastest; the parts of a tile are adjacent
+    // walked row tile fastest
     const int p = (int)blockIdx.x, grid = (int)gridDim.x;
     const int gq = grid >> 3, gr = grid & 7, xcd = p & 7, idx = p >> 3;
-    const int local = xcd < gr ? xcd * (gq + 1) + idx : gr * (gq + 1) + (xcd - gr) * gq + idx;
-    const int part = local % a.parts, tile = local / a.parts;
+    const int tile = xcd < gr ? xcd * (gq + 1) + idx : gr * (gq + 1) + (xcd - gr) * gq + idx;
     const int gid = tile / (GROUP_M * tiles_n), within = tile - gid * (GROUP_M * tiles_n);
     const int gsz = min(tiles_m - gid * GROUP_M, GROUP_M);
     const int m0 = (gid * GROUP_M + within % gsz) * BM, n0 = within / gsz * COLS;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
 
-    const int plane_steps = K >> 6, all_steps = plane_steps * a.planes;
-    const int s0 = part * a.psteps, ns = min(all_steps, s0 + a.psteps) - s0;
+    const int plane_steps = K >> 6, ns = plane_steps * a.planes;
 
     Ctx<FMT, SWIDE> c;
     c.ring = ring;
@@ -338,11 +337,9 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     c.wave = wave;
     c.lane = lane;
     c.plane_steps = plane_steps;
-    const int plane = s0 / plane_steps;
-    c.ik = c.sk = s0 - plane * plane_steps;
+    c.ik = c.sk = 0;
     c.plane_skip = a.plane_bytes - (int64_t)K * 2;
-    c.x = static_cast<const uint8_t *>(a.X) + plane * a.plane_bytes + (int64_t)m0 * K * 2 +
-          (int64_t)c.ik * 128;
+    c.x = static_cast<const uint8_t *>(a.X) + (int64_t)m0 * K * 2;
     // per-lane offsets within the tile; rows past the end repeat the last one
 #pragma unroll
     for (int r = 0; r < G::XLOADS; ++r) {
@@ -391,7 +388,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
             read_weights<FMT, SWIDE, 0>(c, c.ring, 0, j, op);
-            scale_value<FMT, 0>(lane, j, op);
+            scale_value<FMT, SWIDE, 0>(lane, j, op);
         }
 #pragma unroll
         for (int i = 0; i < MS; ++i)
@@ -423,10 +420,8 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     if constexpr (GATED) {
         strip_gated(a.gate, M, N, m0, n0 + wave * 32, patch, lane, acc);
     } else {
-        const bool to_part = a.parts > 1;
-        float *const Y = to_part ? a.part + (int64_t)part * M * N : a.Y;
-        strip_store<EPI>(a.ep, Y, M, N, m0, n0 + wave * 64, patch, lane, acc,
-                         epi_vec_ok(a.ep, Y, N), !to_part);
+        strip_store<EPI>(a.ep, a.Y, M, N, m0, n0 + wave * 64, patch, lane, acc,
+                         epi_vec_ok(a.ep, a.Y, N), true);
     }
 }
 
@@ -469,31 +464,17 @@ bool tile_takes(int64_t K, const void *scales0, const void *scales1)
            ((uintptr_t)scales1 & 3) == 0;
 }
 
-void tile_parts(int fmt, TileArgs &a, int parts)
+// A 64-k step of a tile takes 0.64 us while few CUs work and 0.88 when most do (what
+// a CU gets of the caches' bandwidth and the clock), two on a CU 0.9 each; q4 and
+// int8, with twice the matrix instructions, 1.45 to 1.87.
+double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus)
 {
-    // whole scale groups and loop rounds in a part; a last part of 4 steps or 6 at
-    // least (what the loop takes)
-    const int all = a.K / 64 * a.planes;
-    const bool wide = scales_wide(fmt, a.K, a.scales[0], a.scales[1]);
-    const int unit = wide && fmt == QL_FMT_MXFP4 ? 8 : 4;
-    for (; parts > 1; --parts) {
-        a.psteps = ((all + parts - 1) / parts + unit - 1) / unit * unit;
-        const int n = (all + a.psteps - 1) / a.psteps, last = all - (n - 1) * a.psteps;
-        if (n > 1 && last >= 4) {
-            a.parts = n;
-            return;
-        }
-    }
-    a.parts = 1;
-    a.psteps = all;
-}
-
-bool tile_wins(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus)
-{
-    (void)fmt;
-    (void)xf32;
-    (void)K;
-    return tile_tiles(M, N, gated) >= cus / 2;
+    const bool mx = fmt == QL_FMT_MXFP4;
+    const double r = (double)tile_tiles(M, N, gated) / cus, up = std::ceil(r);
+    const double step = r <= 1.0 ? (mx ? 0.64 : 1.45) + (mx ? 0.24 : 0.4) * std::min(1.0, r / 0.75)
+                                 : (mx ? 0.9 : 1.87) * (r + 0.4 * (up - r));
+    return 5.2 + (double)(K / 64) * (xf32 ? 3 : 1) * step +
+           (xf32 ? 2.0 + 10.0 * (double)M * (double)K / 5e6 : 0.0);
 }
 
 hipError_t launch_split3(const float *X, int64_t count, uint16_t *planes, hipStream_t stream)
@@ -507,7 +488,7 @@ hipError_t launch_split3(const float *X, int64_t count, uint16_t *planes, hipStr
 hipError_t launch_qgemm_tile(int fmt, const TileArgs &a, hipStream_t stream)
 {
     const bool gated = a.codes[1] != nullptr;
-    const dim3 grid((unsigned)(tile_tiles(a.M, a.N, gated) * a.parts)), block(THREADS);
+    const dim3 grid((unsigned)tile_tiles(a.M, a.N, gated)), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
     const bool swide = scales_wide(fmt, a.K, a.scales[0], a.scales[1]);
     auto with = [&](auto fmtc, auto gatedc, auto epic) {

@@ -1256,22 +1256,27 @@ GroupPath choose_path(const ql_linear_ep *const *ls, int n, int forced, KgPlan &
     return tall && all_wide ? GroupPath::WIDE : GroupPath::TILED;
 }
 
-// MXFP4 layers that share xdt (M > 0 each): the few-row kernel's in one launch,
-// the large tiles' one after the other (fp32 activations as three bf16 planes
-// in the workspace).
+// MXFP4 layers that share xdt (M > 0 each): those of the K-group kernel and of the
+// few-row kernel in one launch each, the large tiles' one after the other (fp32
+// activations as three bf16 planes in the workspace).
 int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t stream)
 {
     const bool xf32 = ls[0]->lin.xdt == QL_DT_F32;
     const int cus = device_cus();
-    RowsGroup g{};
+    RowsGroup any{}, kgm{};
     TileArgs tiled[QL_MAX_GROUP];
     int nt = 0;
-    int64_t tiles = 0;
+    int64_t tiles = 0, maxM = 0;
     size_t bytes = 0;
+    for (int i = 0; i < n; ++i)
+        maxM = std::max(maxM, ls[i]->lin.M);
+    any.maxM = kgm.maxM = (int)maxM;
     for (int i = 0; i < n; ++i) {
         const ql_linear &l = ls[i]->lin;
-        if (tile_takes(l.K, l.scales, nullptr) &&
-            tile_wins(l.fmt, xf32, false, l.M, l.N, l.K, cus)) {
+        int shape;
+        const RowsKernel kernel = choose_rows(l.fmt, xf32, false, maxM, l.M, l.N, l.K, l.scales,
+                                              nullptr, cus, &shape);
+        if (kernel == ROWS_TILE) {
             TileArgs &t = tiled[nt++];
             t = TileArgs{};
             t.X = l.X;
@@ -1288,12 +1293,13 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
                 t.plane_bytes = l.M * l.K * 2;
                 bytes = std::max(bytes, (size_t)t.plane_bytes * 3);
             }
-            tile_parts(l.fmt, t, 1);
             if (tile_tiles(l.M, l.N, false) > MAX_WORKGROUPS)
                 return QL_ERR_UNSUPPORTED;
             continue;
         }
+        RowsGroup &g = kernel == ROWS_KGM ? kgm : any;
         RowsArgs &d = g.d[g.n++];
+        d.shape = shape;
         d.X = l.X;
         d.codes[0] = (const uint8_t *)l.codes;
         d.scales[0] = l.scales;
@@ -1329,8 +1335,10 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
             e = launch_qgemm_tile(QL_FMT_MXFP4, run, stream);
         }
     }
-    if (g.n && e == hipSuccess)
-        e = launch_qgemm_rows(QL_FMT_MXFP4, xf32, g, stream);
+    if (kgm.n && e == hipSuccess)
+        e = launch_qgemm_kgm(QL_FMT_MXFP4, xf32, kgm, stream);
+    if (any.n && e == hipSuccess)
+        e = launch_qgemm_rows(QL_FMT_MXFP4, xf32, any, stream);
     const hipError_t ef = ws.own_alloc ? hipFreeAsync(ws.ptr, stream) : hipSuccess;
     return e == hipSuccess && ef == hipSuccess ? QL_OK : QL_ERR_HIP;
 }

@@ -167,9 +167,13 @@ def test_mx_every_scale(gpu):
         np.testing.assert_array_equal(Y, want)
 
 
-SHAPES = [(1, 1, 32), (1, 200, 96), (3, 33, 64), (16, 1000, 160), (17, 64, 1056), (33, 96, 512),
-          (64, 257, 256), (65, 1024, 128), (130, 40, 2048), (300, 520, 384), (513, 768, 1536),
-          (1100, 2064, 640)]
+# from one value to the large tiles: reductions of every residue that the kernels
+# tell apart (32, 128, 256, 512), widths that end inside a tile or a group of four
+SHAPES = [(1, 1, 32), (1, 200, 96), (3, 33, 64), (8, 2000, 128), (16, 1000, 160), (9, 130, 6144),
+          (17, 64, 1056), (33, 96, 512), (40, 300, 384), (64, 257, 256), (65, 1024, 128),
+          (130, 40, 2048), (130, 640, 2176), (256, 1030, 1024), (300, 520, 384), (513, 768, 1536),
+          (520, 2052, 128), (1100, 2064, 640), (1100, 4100, 256), (1100, 4099, 384),
+          (1100, 4100, 512), (1030, 4100, 1152), (1030, 4102, 1536)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -219,7 +223,8 @@ def test_mx_extreme_activations(gpu):
     assert not np.isfinite(Y[2]).any() and np.isnan(Y[3]).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 100, 64), (40, 258, 96), (200, 264, 512), (700, 512, 256)])
+@pytest.mark.parametrize("M,N,K", [(1, 100, 64), (40, 258, 96), (40, 260, 128), (200, 264, 512),
+                                   (700, 512, 256), (1100, 4100, 256), (1100, 4098, 512)])
 @pytest.mark.parametrize("mx", [False, True])
 def test_mx_epilogue(gpu, M, N, K, mx):
     """Bias, GELU, residual, steering, bf16 outputs and copies."""
@@ -282,32 +287,35 @@ def test_mx_groups(gpu):
 
 
 def test_mx_scales_at_any_byte(gpu):
-    """Scale bytes need no alignment: a slice that starts at an odd address."""
+    """Scale bytes need no alignment: slices that start at odd addresses (which other
+    kernels take, that add in another order)."""
     torch, ql = gpu
     rng = np.random.default_rng(9)
     M, N, K = 70, 130, 512
-    codes, scales, _ = R.weight("mxfp4", rng.standard_normal((N, K)).astype(np.float32))
-    X = bf16(torch, rng.standard_normal((M, K)))[0]
+    codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((N, K)).astype(np.float32))
+    X, Xv = bf16(torch, rng.standard_normal((M, K)))
     c, s = dev(torch, codes), dev(torch, scales)
-    buf = torch.empty(s.numel() + 3, dtype=torch.uint8, device="cuda")
-    for off in (1, 2, 3):
-        odd = buf[off: off + s.numel()].view(s.shape)
-        odd.copy_(s)
-        assert torch.equal(ql.forward(ql.FMT_MXFP4, X, c, s, N),
-                           ql.forward(ql.FMT_MXFP4, X, c, odd, N))
-        qx, sx = ql.quantize_act_mx(X)
-        so = torch.empty(sx.numel() + 3, dtype=torch.uint8, device="cuda")[off: off + sx.numel()]
-        so = so.view(sx.shape)
-        so.copy_(sx)
-        assert torch.equal(ql.forward_mx(qx, sx, c, s, N), ql.forward_mx(qx, so, c, odd, N))
-        assert torch.equal(ql.gated_forward(ql.FMT_MXFP4, X, (c, s), (c, s)),
-                           ql.gated_forward(ql.FMT_MXFP4, X, (c, odd), (c, odd)))
+    qx, sx = ql.quantize_act_mx(X)
+    Xq = R.mx_decode(*R.mx_encode(Xv))
+    for off in (0, 1, 2, 3, 4):
+        def shifted(t):
+            v = torch.empty(t.numel() + 4, dtype=torch.uint8, device="cuda")
+            v = v[off: off + t.numel()].view(t.shape)
+            return v.copy_(t)
+        odd = shifted(s)
+        check(ql.forward(ql.FMT_MXFP4, X, c, odd, N), *R.product(Xv, Wv), f"bf16 {off}")
+        check(ql.forward_mx(qx, shifted(sx), c, odd, N), *R.product(Xq, Wv), f"mx {off}")
+        want, e, _ = R.gated(Xv, Wv, Wv, 0, 0, "silu", False)
+        H = torch.empty((M, N), device="cuda")
+        check(ql.gated_forward(ql.FMT_MXFP4, X, (c, odd), (c, odd), H=H), want, e, f"gated {off}")
 
 
 # ---- gated feed-forward -----------------------------------------------------------
 
 GATED = [(1, 8, 32), (1, 1000, 96), (5, 17, 64), (16, 130, 1056), (33, 64, 160), (64, 72, 256),
-         (65, 500, 128), (129, 264, 512), (260, 128, 1536), (700, 640, 384)]
+         (65, 500, 128), (129, 264, 512), (260, 128, 1536), (700, 640, 384), (9, 40, 4096),
+         (20, 1000, 128), (130, 1032, 384), (260, 2048, 256), (1100, 2056, 256), (1100, 2050, 384),
+         (1100, 2056, 512), (1030, 2056, 1152)]
 
 
 def gated_case(torch, fmt, M, N, K, seed, bias):
