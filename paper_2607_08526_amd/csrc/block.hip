@@ -58,8 +58,8 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
     if (rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
     int shape;
-    const RowsKernel kernel = choose_rows(g.fmt, false, true, g.M, g.M, g.N, g.K, g.gate_scales,
-                                          g.up_scales, current_cus(), &shape);
+    const RowsKernel kernel = choose_rows(g.fmt, false, true, g.M, g.M, g.N, g.K, current_cus(),
+                                          &shape);
     if (kernel == ROWS_TILE) {
         TileArgs a{};
         a.X = g.X;

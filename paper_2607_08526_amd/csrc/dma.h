@@ -58,6 +58,21 @@ __device__ inline void dma_load16_at(const void *p, uint32_t lds)
                  : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory");
 }
+// (one or two bytes, zero-extended: lane t's dword lands at lds + t * 4)
+template <int BYTES>
+__device__ inline void dma_load_small_at(const void *p, uint32_t lds)
+{
+    if constexpr (BYTES == 1)
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %0, off"
+                     :
+                     : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ushort %0, off"
+                     :
+                     : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds))
+                     : "memory");
+}
 __device__ inline void dma_load4_at(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"

@@ -11,7 +11,8 @@
 // columns of both projections, whose sums meet in one thread; MXFP4 codes become
 // exact bf16 with their scale in one instruction per pair and accumulate in the
 // matrix cores, with no work per block (q4 and int8: exact codes, then acc += s *
-// partial in fp32); scales travel as dwords, so K % 128 == 0 is enough.
+// partial in fp32); a block's scale travels by itself, so that K % 32 == 0 and scales
+// of any alignment are enough.
 //
 // Memory.  Activations, codes and scales of a stage (256 or 512 k) go to LDS by
 // direct-to-LDS loads, at least 128 contiguous bytes per row but for the scales,
@@ -56,7 +57,7 @@ struct Geo {
     static constexpr int XRB = EB * (XF32 ? 128 : 64), XCH = XRB / 16;  // activation bytes,
                                                                         // chunks per row
     static constexpr int CRB = EB * (I8 ? 32 : 16), CCH = CRB / 16;
-    static constexpr int SD = MX ? EB / 4 : EB / 2;   // scale dwords per weight row
+    static constexpr int SD = EB;                     // scales (a dword each) per weight row
     static constexpr int XBYTES = XR * XRB, CBYTES = TW * CRB, SBYTES = TW * SD * 4;
     // loads in units of one wavefront (1 KB; scales 256 bytes); wavefront w takes
     // units w, w + 16, ..., the last ones repeated so that every wavefront counts the
@@ -115,7 +116,8 @@ __device__ inline void kgm_tile(const RowsArgs &d, int tile, uint8_t *ring)
     const int tiles_m = (M + G::TM - 1) / G::TM;
     const int tn = tile / tiles_m, tm = tile - tn * tiles_m;
     const int m0 = tm * G::TM, n0 = tn * G::TN;
-    const int crow = nb * (G::I8 ? 32 : 16), srow = nb * (G::MX ? 1 : 2);
+    constexpr int SB = G::MX ? 1 : 2;  // bytes of a scale
+    const int crow = nb * (G::I8 ? 32 : 16), srow = nb * SB;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kg = wave / G::WN, wn = wave % G::WN;
@@ -152,17 +154,14 @@ __device__ inline void kgm_tile(const RowsArgs &d, int tile, uint8_t *ring)
             ulim[q] = crow - 16;
             udst[q] = u * 1024;
         } else {
-            // scales: dword-major, [SD][TW]; a pair's rows alternate by 32 within a
-            // unit, so its addresses are formed from the first projection's
+            // scales: [block][TW] of a dword each
             const int slot = ((u - G::XU - G::CU) * 64 + lane) % (G::TW * G::SD);
-            const int row = slot % G::TW;
             ub[q] = nullptr;
             urow[q] = 0;
-            ucol[q] = slot / G::TW * 4;
-            ustep[q] = G::SD * 4;
-            ulim[q] = srow - 4;
+            ucol[q] = slot / G::TW * SB;
+            ustep[q] = G::SD * SB;
+            ulim[q] = srow - SB;
             udst[q] = G::XBYTES + G::CBYTES + (u - G::XU - G::CU) * 256;
-            (void)row;
         }
     }
     // the scale rows of this lane's units (row depends on the unit only through TW)
@@ -182,7 +181,7 @@ __device__ inline void kgm_tile(const RowsArgs &d, int tile, uint8_t *ring)
         if (min(q * WAVES + wave, G::UNITS - 1) < G::XU + G::CU)
             dma_load16(ub[q], urow[q] + col, to);
         else
-            dma_load4_at(sp[q] + col, to);
+            dma_load_small_at<SB>(sp[q] + col, to);
     };
 #pragma unroll
     for (int it = 0; it < G::NST - 1; ++it)
@@ -229,16 +228,14 @@ __device__ inline void kgm_tile(const RowsArgs &d, int tile, uint8_t *ring)
                 const int wr = (wn * NW + w) * 32 + l32;
                 const uint8_t *const wrow = st + G::XBYTES + wr * G::CRB;
                 const uint8_t *const sd = st + G::XBYTES + G::CBYTES;
+                const uint32_t e = *reinterpret_cast<const uint32_t *>(sd + (b * G::TW + wr) * 4);
                 if constexpr (G::MX) {
-                    const uint32_t e = sd[(b / 4 * G::TW + wr) * 4 + b % 4];
                     const float f = mx_scale(e);
                     const u32x2 c = *reinterpret_cast<const u32x2 *>(
                         wrow + (b ^ cswz<G::CCH>(wr)) * 16 + 8 * g);
                     wv[w][0] = mx_bf16x8(c[0], f);
                     wv[w][1] = mx_bf16x8(c[1], f);
                 } else {
-                    const uint32_t e = *reinterpret_cast<const uint16_t *>(
-                        sd + (b / 2 * G::TW + wr) * 4 + b % 2 * 2);
                     s[w] = (float)__builtin_bit_cast(_Float16, (uint16_t)e) *
                            (G::I8 ? 1.0f : 0.0625f);  // exact
                     if constexpr (G::I8) {
@@ -473,11 +470,7 @@ KgTile kgm_tile_shape(int fmt, bool xf32, bool gated, int64_t maxM, int shape)
                        [&](auto s) { return tile_of<decltype(s)>(shape); });
 }
 
-bool kgm_takes(int64_t K, const void *scales0, const void *scales1)
-{
-    return K % 128 == 0 && K < ((int64_t)1 << 22) && ((uintptr_t)scales0 & 3) == 0 &&
-           ((uintptr_t)scales1 & 3) == 0;
-}
+bool kgm_takes(int64_t K) { return K < ((int64_t)1 << 22); }
 
 // us of a workgroup of each shape: fixed, and per 256 k (measured on layers of K =
 // 1024 to 6144, one and many rounds of workgroups).  Products of bf16 and of fp32
@@ -517,7 +510,7 @@ double kgm_us(int fmt, bool xf32, bool gated, int64_t maxM, int64_t M, int64_t N
 }
 
 RowsKernel choose_rows(int fmt, bool xf32, bool gated, int64_t maxM, int64_t M, int64_t N,
-                       int64_t K, const void *scales0, const void *scales1, int cus, int *shape)
+                       int64_t K, int cus, int *shape)
 {
     *shape = 0;
     // few rows of short reductions: the kernel without stages starts faster (us there
@@ -525,10 +518,10 @@ RowsKernel choose_rows(int fmt, bool xf32, bool gated, int64_t maxM, int64_t M, 
     // row, MXFP4 4096 x 1536 5.5 / 6.9, 1536 x 6144 12.7 / 11.3, q4 1024 x 1024 6.0 /
     // 6.6, 6144 x 1536 11.1 / 8.2)
     const bool few = M <= 16 && (gated ? K <= (fmt == QL_FMT_MXFP4 ? 2048 : 1024) : xf32);
-    if (few || !kgm_takes(K, scales0, scales1))
+    if (few || !kgm_takes(K))
         return ROWS_ANY;
     const double us = kgm_us(fmt, xf32, gated, maxM, M, N, K, cus, shape);
-    if (tile_takes(K, scales0, scales1) && tile_us(fmt, xf32, gated, M, N, K, cus) < us)
+    if (tile_takes(K) && tile_us(fmt, xf32, gated, M, N, K, cus) < us)
         return ROWS_TILE;
     return us < 1e30 ? ROWS_KGM : ROWS_ANY;
 }

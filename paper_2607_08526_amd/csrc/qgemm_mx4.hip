@@ -12,8 +12,9 @@
 // directly to LDS through a ring of three, 16-byte chunks XOR-swizzled, one
 // barrier per stage.  Scales of the tile's 384 rows: where a row's allow it, 16
 // bytes (four stages) into one slot that every wavefront copies to registers at
-// the group's start, so that it can be refilled behind them; otherwise a dword
-// with each stage (as many memory requests as the codes).  Two workgroups per CU.
+// the group's start, so that it can be refilled behind them; otherwise each by
+// itself with its stage (more memory requests than the codes), a ring of two.  A
+// stage that K leaves unfilled ends in zeros.  Two workgroups per CU.
 #include <algorithm>
 #include <cmath>
 
@@ -35,10 +36,13 @@ constexpr int BM = 128, BN = 256, MS = 4, NS = 2;
 constexpr int GROUP_M = 4;
 constexpr int ROW = 64;  // code bytes per row and stage (128 k)
 constexpr int XBYTES = BM * ROW, WBYTES = BN * ROW;
-constexpr int STAGE = XBYTES + WBYTES, NST = 3;
-constexpr int SROWS = BM + BN, SLDS = SROWS * 16;  // scales: a slot of 16 bytes, or 3 of 4
+constexpr int STAGE = XBYTES + WBYTES;
+constexpr int SROWS = BM + BN, SLDS = SROWS * 16;  // scales: 16 bytes, or 4 blocks' dwords
 constexpr int XLOADS = XBYTES / 16 / THREADS, WLOADS = WBYTES / 16 / THREADS;
-static_assert(2 * (NST * STAGE + SLDS) <= 160 * 1024, "two workgroups per CU");
+static_assert(2 * (3 * STAGE + SLDS) <= 160 * 1024 && 4 * (STAGE + SLDS) <= 160 * 1024,
+              "two workgroups per CU");
+
+__device__ __align__(16) const uint32_t zeros[4] = {0, 0, 0, 0};
 
 // physical 16-byte chunk = logical ^ swz(row): a cycle of a 16-byte read serves
 // rows 0-3, 12-15, 20-27, or the others of 32, and meets distinct banks
@@ -53,8 +57,8 @@ __device__ inline i32x8 codes8(u32x4 v)
 template <bool SWIDE, bool EPI>
 __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
 {
-    constexpr int SG = SWIDE ? 4 : 1, SB = SWIDE ? 16 : 4;  // stages, bytes of a scale group
-    __shared__ __align__(16) uint8_t ring[NST * STAGE + SLDS];
+    constexpr int SG = SWIDE ? 4 : 1, NST = SWIDE ? 3 : 2;  // stages of a scale group, of the ring
+    __shared__ __align__(16) uint8_t ring[NST * STAGE + (SWIDE ? 1 : NST) * SLDS];
     uint8_t *const sring = ring + NST * STAGE;
     const int M = a.M, N = a.N, nb = a.K >> 5;
     const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
@@ -65,7 +69,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
     const int gsz = min(tiles_m - gid * GROUP_M, GROUP_M);
     const int m0 = (gid * GROUP_M + within % gsz) * BM, n0 = within / gsz * BN;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
-    const int ns = a.K >> 7;
+    const int ns = (nb + 3) >> 2;
 
     // per-lane offsets within the tile; rows past the end repeat the last one
     const int krow = nb * 16;
@@ -84,33 +88,54 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
     const uint32_t xsoff = (uint32_t)((min(m0 + (tid & 127), M - 1) - m0) * nb);
     const uint8_t *const xb = a.qx + (int64_t)m0 * krow, *const wb = a.codes + (int64_t)n0 * krow;
     const uint8_t *const xs = a.sx + (int64_t)m0 * nb, *const ws = a.scales + (int64_t)n0 * nb;
-    // scales of the group that stage s starts: rows of X, then of W.  (X's by the
-    // first two wavefronts; the others repeat them, so that every wavefront counts
-    // the same loads)
+    // scales of the group that stage s starts: rows of X, then of W (not SWIDE: four
+    // of them, one for each block; past K the row's last).  (X's by the first two
+    // wavefronts; SWIDE the others repeat them, so that every wavefront counts the
+    // same loads, otherwise they take every other block.)
     auto issue_scales = [&](int s) {
-        const uint32_t base = dma_lds(sring + (SWIDE ? 0 : s % 3) * (SROWS * 4));
-        const uint32_t xl = base + (wave & 1) * 64 * SB, wl = base + (BM + wave * 64) * SB;
         if constexpr (SWIDE) {
-            dma_load16(ws + (int64_t)s * 4, wsoff, wl);
-            dma_load16(xs + (int64_t)s * 4, xsoff, xl);
+            const uint32_t base = dma_lds(sring);
+            dma_load16(ws + (int64_t)s * 4, wsoff, base + (BM + wave * 64) * 16);
+            dma_load16(xs + (int64_t)s * 4, xsoff, base + (wave & 1) * 64 * 16);
         } else {
-            dma_load4(ws + (int64_t)s * 4, wsoff, wl);
-            dma_load4(xs + (int64_t)s * 4, xsoff, xl);
+            const uint32_t base = dma_lds(sring + s % NST * SLDS);
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                dma_load_small_at<1>(ws + wsoff + min(4 * s + h, nb - 1),
+                                     base + h * (SROWS * 4) + (BM + wave * 64) * 4);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                dma_load_small_at<1>(xs + xsoff + min(4 * s + 2 * h + (wave >> 1), nb - 1),
+                                     base + (2 * h + (wave >> 1)) * (SROWS * 4) +
+                                         (wave & 1) * 64 * 4);
         }
     };
     auto issue = [&](int s) {
-        const uint32_t base = dma_lds(ring + s % NST * STAGE);
+        const uint32_t base = dma_lds(ring + s % NST * STAGE) + wave * 1024;
+        const uint8_t *const x = xb + (int64_t)s * ROW, *const w = wb + (int64_t)s * ROW;
+        if (SWIDE || 4 * s + 4 <= nb) {
 #pragma unroll
-        for (int r = 0; r < XLOADS; ++r)
-            dma_load16(xb + (int64_t)s * ROW, xoff[r], base + (r * THREADS + wave * 64) * 16);
+            for (int r = 0; r < XLOADS; ++r)
+                dma_load16(x, xoff[r], base + r * THREADS * 16);
 #pragma unroll
-        for (int r = 0; r < WLOADS; ++r)
-            dma_load16(wb + (int64_t)s * ROW, woff[r],
-                       base + XBYTES + (r * THREADS + wave * 64) * 16);
+            for (int r = 0; r < WLOADS; ++r)
+                dma_load16(w, woff[r], base + XBYTES + r * THREADS * 16);
+        } else {
+            // (a chunk is a block)
+            auto at = [&](const uint8_t *p, uint32_t off, int i) {
+                return 4 * s + ((i & 3) ^ swz(i >> 2)) < nb ? p + off : (const uint8_t *)zeros;
+            };
+#pragma unroll
+            for (int r = 0; r < XLOADS; ++r)
+                dma_load16_at(at(x, xoff[r], r * THREADS + tid), base + r * THREADS * 16);
+#pragma unroll
+            for (int r = 0; r < WLOADS; ++r)
+                dma_load16_at(at(w, woff[r], r * THREADS + tid), base + XBYTES + r * THREADS * 16);
+        }
         if constexpr (!SWIDE)
             issue_scales(s);
     };
-    constexpr int LOADS = XLOADS + WLOADS + (SWIDE ? 0 : 2);
+    constexpr int LOADS = XLOADS + WLOADS + (SWIDE ? 0 : 6);
 
     f32x16 acc[MS][NS];
 #pragma unroll
@@ -124,34 +149,35 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
     if constexpr (SWIDE)
         issue_scales(0);
     issue(0);
-    if (ns > 1)
+    if (NST == 3 && ns > 1)
         issue(1);
     u32x4 ga[MS], gb[NS];  // SWIDE: the group's scales of this lane's rows
     auto step = [&](int s, auto uc) {
         constexpr int U = decltype(uc)::value;  // s % SG
         // loads land in order: the next stage's may be in flight, and the next
         // group's scales, issued behind the second stage's barrier
-        if (s + 1 < ns)
+        if (NST == 3 && s + 1 < ns)
             __builtin_amdgcn_s_waitcnt(dma_vmcnt(LOADS + (SWIDE && U == 2 ? 2 : 0)));
         else
             __builtin_amdgcn_s_waitcnt(dma_vmcnt(0));
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
-        if (s + 2 < ns)
-            issue(s + 2);
+        if (s + NST - 1 < ns)
+            issue(s + NST - 1);
         if constexpr (SWIDE && U == 1)  // (the last group again at the end)
             issue_scales(min(s - 1 + SG, ns - SG));
         const uint8_t *const st = ring + s % NST * STAGE;
-        const uint8_t *const ss = sring + (SWIDE ? 0 : s % 3) * (SROWS * 4);
-        uint32_t sa[MS], sb[NS];  // byte 2 q: this lane's block of chunk q
+        const uint8_t *const ss = sring + (SWIDE ? 0 : s % NST * SLDS);
+        uint32_t sa[MS], sb[NS];  // byte 2 q: this lane's block (2 q + g) of chunk q
         auto scale = [&](int row, u32x4 &grp) {
             if constexpr (SWIDE) {
                 if constexpr (U == 0)
                     grp = *reinterpret_cast<const u32x4 *>(ss + row * 16);
                 return grp[U] >> (8 * g);
             } else {
-                return *reinterpret_cast<const uint32_t *>(ss + row * 4) >> (8 * g);
+                const uint32_t *const d = reinterpret_cast<const uint32_t *>(ss) + g * SROWS + row;
+                return d[0] | d[2 * SROWS] << 16;
             }
         };
 #pragma unroll
@@ -211,8 +237,7 @@ static int64_t mx4_tiles(const Mx4Args &a)
 
 bool mx4_takes(const Mx4Args &a)
 {
-    return a.K % 128 == 0 && a.K < (1 << 22) && ((uintptr_t)a.sx & 3) == 0 &&
-           ((uintptr_t)a.scales & 3) == 0;
+    return a.K < (1 << 22);
 }
 
 // Estimated us: a stage of a tile takes 0.49 us while few CUs work, 0.62 when all
@@ -222,7 +247,7 @@ bool mx4_takes(const Mx4Args &a)
 // 29.1 / 19.9, 1024 rows 29.7 / 51.5).
 bool mx4_wins(const Mx4Args &a, int cus)
 {
-    const double r = (double)mx4_tiles(a) / cus, up = std::ceil(r), steps = (double)(a.K / 128);
+    const double r = (double)mx4_tiles(a) / cus, up = std::ceil(r), steps = std::ceil(a.K / 128.0);
     const double tile = 5.5 + steps * (r <= 1.0 ? 0.49 + 0.13 * r : 0.66 * (r + 0.4 * (up - r)));
     const int rows = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
     const double wgs = (double)((a.M + rows - 1) / rows) * ((a.N + 31) / 32);

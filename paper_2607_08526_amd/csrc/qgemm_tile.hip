@@ -26,11 +26,12 @@
 // step's barrier sits before its last 16-k chunk: by then a stage is in registers
 // and its slot refilled at once, while that chunk runs and prepares the next
 // stage's first one.  Behind every MFMA goes a share of the next chunk's LDS reads
-// and conversions.  Two workgroups per CU.  Scales:
-// where a row's allow it, 16 bytes (MXFP4: of eight steps, fp16: of four) into
-// one slot that every wavefront copies to registers at the group's start, so that
-// it can be refilled behind them; otherwise dwords, one or two steps at a time (a
-// memory request per row each: as many as the codes).
+// and conversions.  Two workgroups per CU.  Scales: where a row's allow it, 16 bytes
+// (MXFP4: of eight steps, fp16: of four) into one slot that every wavefront copies
+// to registers at the group's start, so that it can be refilled behind them;
+// otherwise each by itself with its step (a memory request each: as many as the
+// codes).  Steps that K leaves unfilled, and those that fill up the loop's rounds,
+// come from a page of zeros.
 #include <algorithm>
 #include <cmath>
 
@@ -55,10 +56,12 @@ template <int FMT>
 struct Geo {
     static constexpr int CROW = FMT == QL_FMT_INT8 ? 64 : 32;  // code bytes per row per step
     static constexpr int CCH = CROW / 16;
-    static constexpr int XBYTES = BM * 128, CBYTES = BN * CROW, SBYTES = BN * 4;
-    static constexpr int SSTEPS = FMT == QL_FMT_MXFP4 ? 2 : 1;  // steps of a scale dword
+    static constexpr int XBYTES = BM * 128, CBYTES = BN * CROW;
+    static constexpr int SB = FMT == QL_FMT_MXFP4 ? 1 : 2;      // bytes of a scale
+    static constexpr int SSTEPS = FMT == QL_FMT_MXFP4 ? 2 : 1;  // steps of a dword of scales
     static constexpr int STAGE = XBYTES + CBYTES;
-    static constexpr int SLDS = 4 * SBYTES;  // a slot of 16 bytes per row, or a ring of 3 dwords
+    static constexpr int SSTEP = 2 * BN * 4;  // a step's scales, a dword each
+    static constexpr int SLDS = 3 * SSTEP;    // (or a slot of 16 bytes per row)
     static constexpr int NST = 2 * (3 * STAGE + SLDS) <= 160 * 1024 ? 3 : 2;
     static constexpr int LDS = NST * STAGE + SLDS;
     static constexpr int XLOADS = XBYTES / 16 / THREADS, CLOADS = CBYTES / 16 / THREADS;
@@ -67,6 +70,8 @@ struct Geo {
     static_assert(2 * LDS <= 160 * 1024, "two workgroups per CU");
     static_assert(BN == THREADS, "one scale dword per thread");
 };
+
+__device__ __align__(16) const uint32_t zeros[4] = {0, 0, 0, 0};
 
 // physical 16-byte chunk = logical ^ swizzle(row), so that the 16 lanes that one
 // cycle of a 16-byte LDS read serves (rows 0-3, 12-15, 20-27, or the others of 32)
@@ -96,7 +101,8 @@ struct Ctx {
     const uint8_t *x;                       // of the next stage to load
     const uint8_t *sp;                      // this thread's scale row
     int64_t plane_skip;                     // from one plane's end to the next one
-    int plane_steps, ik, sk;                // steps of a plane; next stage, next scale group
+    int plane_steps, planes;                // steps of a plane; planes from this one on
+    int nb, ik, sk;                         // blocks of a row; next stage, next scale group
     int wave, lane;
 };
 
@@ -111,24 +117,46 @@ struct Ops {
     u32x4 a[MS], b[NS][Geo<FMT>::PLANES];
 };
 
-// Loads of the next stage into its slot, and where scales are not SWIDE their
-// dwords (with even steps, or every one).
+// Loads of step t, the next stage, into its slot, and where scales are not SWIDE
+// the step's (of blocks past K: the row's last).
 template <int FMT, bool SWIDE>
 __device__ inline void issue(Ctx<FMT, SWIDE> &c, int t, int slot)
 {
     using G = Geo<FMT>;
     const uint32_t base = dma_lds(c.ring + slot * G::STAGE) + c.wave * 1024;
+    const int left = c.nb - 2 * c.ik;  // blocks from this step on
+    if (SWIDE || left >= 2) {
 #pragma unroll
-    for (int r = 0; r < G::XLOADS; ++r)
-        dma_load16(c.x, c.xoff[r], base + r * THREADS * 16);
+        for (int r = 0; r < G::XLOADS; ++r)
+            dma_load16(c.x, c.xoff[r], base + r * THREADS * 16);
 #pragma unroll
-    for (int r = 0; r < G::CLOADS; ++r)
-        dma_load16(c.cptr[r] + c.ik * G::CROW, c.coff[r], base + G::XBYTES + r * THREADS * 16);
-    if (!SWIDE && (G::SSTEPS == 1 || t % 2 == 0))
-        dma_load4_at(c.sp + (c.ik / G::SSTEPS) * 4,
-                     dma_lds(c.sring + t / G::SSTEPS % 3 * G::SBYTES) + c.wave * 256);
+        for (int r = 0; r < G::CLOADS; ++r)
+            dma_load16(c.cptr[r] + c.ik * G::CROW, c.coff[r], base + G::XBYTES + r * THREADS * 16);
+    } else {
+        const int tid = c.wave * 64 + c.lane;
+#pragma unroll
+        for (int r = 0; r < G::XLOADS; ++r) {
+            const int i = r * THREADS + tid, lc = (i & 7) ^ xswz(i >> 3);
+            dma_load16_at(lc / 4 < left ? c.x + c.xoff[r] : (const uint8_t *)zeros,
+                          base + r * THREADS * 16);
+        }
+#pragma unroll
+        for (int r = 0; r < G::CLOADS; ++r) {
+            const int i = r * THREADS + tid, lc = (i % G::CCH) ^ cswz<FMT>(i / G::CCH);
+            dma_load16_at(lc / (G::CCH / 2) < left ? c.cptr[r] + c.ik * G::CROW + c.coff[r]
+                                                   : (const uint8_t *)zeros,
+                          base + G::XBYTES + r * THREADS * 16);
+        }
+    }
+    if constexpr (!SWIDE) {
+        const uint32_t to = dma_lds(c.sring + t % 3 * G::SSTEP) + c.wave * 256;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            dma_load_small_at<G::SB>(c.sp + min(2 * c.ik + h, c.nb - 1) * G::SB, to + h * BN * 4);
+    }
     c.x += 128;
-    if (++c.ik == c.plane_steps) {
+    if (++c.ik == c.plane_steps && c.planes > 1) {
+        --c.planes;
         c.ik = 0;
         c.x += c.plane_skip;
     }
@@ -179,19 +207,20 @@ __device__ inline void read_weights(const Ctx<FMT, SWIDE> &c, const uint8_t *st,
                 op.grp[j] = *reinterpret_cast<const u32x4 *>(c.sring + row * 16);
             }
         }
-    } else if (G::SSTEPS == 1 || U % 2 == 0) {
-        op.grp[j][0] = *reinterpret_cast<const uint32_t *>(
-            c.sring + t / G::SSTEPS % 3 * G::SBYTES + row * 4);
+    } else {
+        op.grp[j][0] = *reinterpret_cast<const uint32_t *>(c.sring + t % 3 * G::SSTEP +
+                                                           g * (BN * 4) + row * 4);
     }
 }
 
 template <int FMT, bool SWIDE, int U>
 __device__ inline void scale_value(int lane, int j, Ops<FMT> &op)
 {
-    const int g = lane >> 5;
+    // SWIDE: this lane half's part of the group's dword; otherwise the scale itself
+    const int g = SWIDE ? lane >> 5 : 0;
     const uint32_t d = op.grp[j][SWIDE ? U / Geo<FMT>::SSTEPS : 0];
     if constexpr (FMT == QL_FMT_MXFP4)
-        op.sc[j] = mx_scale(d >> (16 * (U & 1) + 8 * g) & 255u);
+        op.sc[j] = mx_scale(d >> ((SWIDE ? 16 * (U & 1) : 0) + 8 * g) & 255u);
     else
         op.sc[j] = (float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * g)));
 }
@@ -291,8 +320,7 @@ __device__ inline void step(Ctx<FMT, SWIDE> &c, int t, int &slot, Ops<FMT> &op,
             if (SWIDE && U == 1 && first)
                 __builtin_amdgcn_s_waitcnt(dma_vmcnt(G::LOADS + 1));
             else
-                __builtin_amdgcn_s_waitcnt(
-                    dma_vmcnt(G::LOADS + (!SWIDE && (G::SSTEPS == 1 || U % 2 == 0))));
+                __builtin_amdgcn_s_waitcnt(dma_vmcnt(G::LOADS + (SWIDE ? 0 : 2)));
         } else {
             __builtin_amdgcn_s_waitcnt(dma_vmcnt(0));
         }
@@ -329,7 +357,8 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     const int m0 = (gid * GROUP_M + within % gsz) * BM, n0 = within / gsz * COLS;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
 
-    const int plane_steps = K >> 6, ns = plane_steps * a.planes;
+    // (an odd number of steps gets one of zeros)
+    const int plane_steps = (nb + 1) >> 1, ns = (plane_steps * a.planes + 1) & ~1;
 
     Ctx<FMT, SWIDE> c;
     c.ring = ring;
@@ -337,8 +366,10 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     c.wave = wave;
     c.lane = lane;
     c.plane_steps = plane_steps;
+    c.planes = a.planes;
+    c.nb = nb;
     c.ik = c.sk = 0;
-    c.plane_skip = a.plane_bytes - (int64_t)K * 2;
+    c.plane_skip = a.plane_bytes - (int64_t)plane_steps * 128;
     c.x = static_cast<const uint8_t *>(a.X) + (int64_t)m0 * K * 2;
     // per-lane offsets within the tile; rows past the end repeat the last one
 #pragma unroll
@@ -349,7 +380,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     const uint8_t *const cbase[2] = {a.codes[0], a.codes[GATED ? 1 : 0]};
     const uint8_t *const sbase[2] = {static_cast<const uint8_t *>(a.scales[0]),
                                      static_cast<const uint8_t *>(a.scales[GATED ? 1 : 0])};
-    const int crow = K / 32 * (G::CROW / 2), srow = nb * (FMT == QL_FMT_MXFP4 ? 1 : 2);
+    const int crow = nb * (G::CROW / 2), srow = nb * G::SB;
     // (a wavefront's chunks of one load lie in rows of one projection: 64 lanes
     // cover 32 rows of 2 chunks, or 16 of 4)
 #pragma unroll
@@ -380,8 +411,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
         for (int t = 0; t < NST; ++t)
             issue<FMT, SWIDE>(c, t, t);
         // stage 0: the younger ones may be in flight (ns >= 4 > NST)
-        constexpr int DW = SWIDE ? 0 : G::SSTEPS == 1 ? NST - 1 : (NST - 1) / 2;  // their dwords
-        __builtin_amdgcn_s_waitcnt(dma_vmcnt((NST - 1) * G::LOADS + DW));
+        __builtin_amdgcn_s_waitcnt(dma_vmcnt((NST - 1) * (G::LOADS + (SWIDE ? 0 : 2))));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
         Ops<FMT> op;
@@ -458,11 +488,8 @@ static bool scales_wide(int fmt, int64_t K, const void *scales0, const void *sca
            (((uintptr_t)scales0 | (uintptr_t)scales1) & 15) == 0;
 }
 
-bool tile_takes(int64_t K, const void *scales0, const void *scales1)
-{
-    return K % 128 == 0 && K >= 256 && K < ((int64_t)1 << 22) && ((uintptr_t)scales0 & 3) == 0 &&
-           ((uintptr_t)scales1 & 3) == 0;
-}
+// (four steps at least: the loop's last round)
+bool tile_takes(int64_t K) { return K >= 224 && K < ((int64_t)1 << 22); }
 
 // A 64-k step of a tile takes 0.64 us while few CUs work and 0.88 when most do (what
 // a CU gets of the caches' bandwidth and the clock), two on a CU 0.9 each; q4 and
@@ -473,7 +500,7 @@ double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, 
     const double r = (double)tile_tiles(M, N, gated) / cus, up = std::ceil(r);
     const double step = r <= 1.0 ? (mx ? 0.64 : 1.45) + (mx ? 0.24 : 0.4) * std::min(1.0, r / 0.75)
                                  : (mx ? 0.9 : 1.87) * (r + 0.4 * (up - r));
-    return 5.2 + (double)(K / 64) * (xf32 ? 3 : 1) * step +
+    return 5.2 + (double)((K + 63) / 64) * (xf32 ? 3 : 1) * step +
            (xf32 ? 2.0 + 10.0 * (double)M * (double)K / 5e6 : 0.0);
 }
 

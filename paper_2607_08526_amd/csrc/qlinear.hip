@@ -1274,8 +1274,8 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
     for (int i = 0; i < n; ++i) {
         const ql_linear &l = ls[i]->lin;
         int shape;
-        const RowsKernel kernel = choose_rows(l.fmt, xf32, false, maxM, l.M, l.N, l.K, l.scales,
-                                              nullptr, cus, &shape);
+        const RowsKernel kernel = choose_rows(l.fmt, xf32, false, maxM, l.M, l.N, l.K, cus,
+                                              &shape);
         if (kernel == ROWS_TILE) {
             TileArgs &t = tiled[nt++];
             t = TileArgs{};

@@ -173,7 +173,9 @@ SHAPES = [(1, 1, 32), (1, 200, 96), (3, 33, 64), (8, 2000, 128), (16, 1000, 160)
           (17, 64, 1056), (33, 96, 512), (40, 300, 384), (64, 257, 256), (65, 1024, 128),
           (130, 40, 2048), (130, 640, 2176), (256, 1030, 1024), (300, 520, 384), (513, 768, 1536),
           (520, 2052, 128), (1100, 2064, 640), (1100, 4100, 256), (1100, 4099, 384),
-          (1100, 4100, 512), (1030, 4100, 1152), (1030, 4102, 1536)]
+          (1100, 4100, 512), (1030, 4100, 1152), (1030, 4102, 1536), (130, 1000, 416),
+          (300, 2050, 1056), (1100, 4100, 224), (1100, 4100, 288), (1030, 4100, 1056),
+          (1030, 4098, 864)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -315,7 +317,8 @@ def test_mx_scales_at_any_byte(gpu):
 GATED = [(1, 8, 32), (1, 1000, 96), (5, 17, 64), (16, 130, 1056), (33, 64, 160), (64, 72, 256),
          (65, 500, 128), (129, 264, 512), (260, 128, 1536), (700, 640, 384), (9, 40, 4096),
          (20, 1000, 128), (130, 1032, 384), (260, 2048, 256), (1100, 2056, 256), (1100, 2050, 384),
-         (1100, 2056, 512), (1030, 2056, 1152)]
+         (1100, 2056, 512), (1030, 2056, 1152), (130, 1032, 416), (1100, 2056, 224),
+         (1100, 2056, 288), (1030, 2056, 1056)]
 
 
 def gated_case(torch, fmt, M, N, K, seed, bias):
