@@ -378,7 +378,7 @@ int qlinear_rotary(const void *x, int64_t ldx, void *o, int64_t ldo, int dt, int
     a.interleaved = interleaved != 0;
     a.adjoint = adjoint != 0;
     a.copy = x != o;
-    return status(launch_rotary(a, stream));
+    return status(launch_rotary(a, current_cus(), stream));
 }
 
 }  // extern "C"

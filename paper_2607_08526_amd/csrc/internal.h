@@ -280,9 +280,9 @@ struct RotaryArgs {
     float mscale;
     int bf16, interleaved, adjoint;
     int copy;                  // o is not x: the other channels are copied
-    int rows_per_wg;           // set by the launch
+    int rows_per_wg, heads_per_wg;  // set by the launch
 };
-hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
+hipError_t launch_rotary(RotaryArgs a, int cus, hipStream_t stream);
 
 // The outputs of a gated pair (gated.h): H, or with dG the gradients of both
 // projections.

@@ -4,8 +4,8 @@
 // of four rows.
 //
 // Loads and stores retire in order: a load behind a store waits until memory has
-// taken the store.  So what the epilogue reads is loaded before a row block's
-// first store, and a strip without an epilogue loads nothing.  (With a load,
+// taken the store.  So what the epilogue reads of the next row block is loaded before
+// a row block's first store, and a strip without an epilogue loads nothing.  (With a load,
 // even one that its branch skips, between the stores: 10 us per launch.)
 #pragma once
 
@@ -59,20 +59,25 @@ __device__ inline void strip_store(const Epilogue &e, float *Y, int M, int N, in
     auto read = [&](int u) {
         return *reinterpret_cast<const strip_f32x4 *>(patch + (4 * u + rl) * 64 + cq);
     };
+    // this lane's row of store u of a row block that starts at mb: mb + 4 u
+    strip_f32x4 r[8];
+    auto load_resid = [&](int mb) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (e.resid && mb + 4 * u < M && n < N)
+                r[u] = __builtin_nontemporal_load(reinterpret_cast<const strip_f32x4 *>(
+                    e.resid + (int64_t)(mb + 4 * u) * N + n));
+    };
+    if (EPI && vec) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            r[u] = b4;
+        load_resid(m0 + rl);
+    }
 #pragma unroll 1
     for (int i = 0; i < MS; ++i) {
         static_assert(MS == 4, "row blocks");
-        const int mb = m0 + 32 * i + rl;  // this lane's row of store u: mb + 4 u
-        strip_f32x4 r[8];
-        if (EPI && vec) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                r[u] = b4;
-                if (e.resid && mb + 4 * u < M && n < N)
-                    r[u] = __builtin_nontemporal_load(reinterpret_cast<const strip_f32x4 *>(
-                        e.resid + (int64_t)(mb + 4 * u) * N + n));
-            }
-        }
+        const int mb = m0 + 32 * i + rl;
         if (i == 0)
             put(std::integral_constant<int, 0>{});
         else if (i == 1)
@@ -111,6 +116,8 @@ __device__ inline void strip_store(const Epilogue &e, float *Y, int M, int N, in
                     cp[u] = epi_bf16x4(w[u]);
             }
         }
+        if (EPI && i + 1 < MS)
+            load_resid(mb + 32);
         if (e.ybf16) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) {

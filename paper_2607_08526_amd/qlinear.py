@@ -228,6 +228,8 @@ def _ptr(t):
 _TWO_BYTE = (torch.int16, torch.uint16, torch.bfloat16, torch.float16)
 _BF16_BITS = (torch.bfloat16, torch.int16, torch.uint16)
 _QUANTIZED = (FMT_INT8, FMT_Q4, FMT_MXFP4)
+# weights per byte of codes, and the scales' dtypes
+_LAYOUT = {FMT_INT8: (1, _TWO_BYTE), FMT_Q4: (2, _TWO_BYTE), FMT_MXFP4: (2, (torch.uint8,))}
 
 
 def _require(t, name, dtypes, shape=None, min_cols=None):
@@ -267,10 +269,10 @@ def _on_device(*tensors):
 
 def _on_current_device(*tensors):
     """_on_device, and the device that the call's stream belongs to."""
-    _on_device(*tensors)
-    dev = torch.cuda.current_device() if _device is None else _device()
+    dev = _device() if _device is not None and torch.cuda.is_initialized() else None
     for t in tensors:
-        if t is not None and t.device.index != dev:
+        if t is not None and t.get_device() != dev:
+            _on_device(*tensors)
             raise ValueError(f"every tensor argument must be on the current device (cuda:{dev}), "
                              f"not {t.device}")
 
@@ -278,6 +280,14 @@ def _on_current_device(*tensors):
 def _require_weights(fmt, codes, scales, N, K):
     if fmt == FMT_F16:
         _require(codes, "codes (fp16 weights)", _TWO_BYTE, (N, K))
+        return
+    # the plain case in as few steps as it takes
+    layout = _LAYOUT.get(fmt)
+    if layout is not None and K % BLOCK == 0 and isinstance(codes, torch.Tensor) and \
+            isinstance(scales, torch.Tensor) and codes.dtype is torch.uint8 and \
+            codes.shape == (N, K // layout[0]) and codes.is_contiguous() and \
+            scales.dtype in layout[1] and scales.shape == (N, K // BLOCK) and \
+            scales.is_contiguous():
         return
     if fmt not in _QUANTIZED:
         raise ValueError(f"unknown weight format {fmt}")
@@ -417,7 +427,7 @@ def forward_ep(fmt, X, codes, scales, N, Y=None, bias=None, act=ACT_NONE, residu
     M, K = _require_x(X)
     _require_weights(fmt, codes, scales, N, K)
     if Y is None:
-        Y = torch.empty((M, N), dtype=ydtype, device=X.device)
+        Y = X.new_empty((M, N), dtype=ydtype)
     _require_y(Y, M, N, (torch.float32, torch.bfloat16))
     _require_ep(bias, residual, M, N)
     _require_steer(steer, N)
@@ -529,7 +539,7 @@ def forward_w8a8(qx, sx, codes, scales, N, Y=None, bias=None, act=ACT_NONE, resi
     _require(sx, "sx", _TWO_BYTE, (M,))
     _require_weights(FMT_INT8, codes, scales, N, K)
     if Y is None:
-        Y = torch.empty((M, N), dtype=ydtype, device=qx.device)
+        Y = qx.new_empty((M, N), dtype=ydtype)
     _require_y(Y, M, N, (torch.float32, torch.bfloat16))
     _require_ep(bias, residual, M, N)
     _require_steer(steer, N)
@@ -585,7 +595,7 @@ def dequantize(fmt, codes, scales, dtype=torch.float32, out=None, stream=None):
     N, K = codes.shape[0], codes.shape[1] * (1 if fmt == FMT_INT8 else 2)
     _require_weights(fmt, codes, scales, N, K)
     if out is None:
-        out = torch.empty((N, K), dtype=dtype, device=codes.device)
+        out = codes.new_empty((N, K), dtype=dtype)
     _require(out, "out", (torch.float32, torch.bfloat16), (N, K))
     _on_current_device(codes, scales, out)
     _check(load().qlinear_dequantize(fmt, _ptr(codes), _ptr(scales), N, K, _ptr(out), _ydt(out),
@@ -601,11 +611,13 @@ def quantize_act_mx(X, qx=None, sx=None, stream=None):
     if K % BLOCK or K == 0:
         raise ValueError(f"K = {K} is not a positive multiple of {BLOCK}")
     if qx is None:
-        qx = torch.empty((M, K // 2), dtype=torch.uint8, device=X.device)
+        qx = X.new_empty((M, K // 2), dtype=torch.uint8)
+    else:
+        _require(qx, "qx", (torch.uint8,), (M, K // 2))
     if sx is None:
-        sx = torch.empty((M, K // BLOCK), dtype=torch.uint8, device=X.device)
-    _require(qx, "qx", (torch.uint8,), (M, K // 2))
-    _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
+        sx = X.new_empty((M, K // BLOCK), dtype=torch.uint8)
+    else:
+        _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
     _on_current_device(X, qx, sx)
     _check(load().qlinear_mx_quantize_act(_ptr(X), _xdt(X), M, K, _ptr(qx), _ptr(sx),
                                           _stream(stream)))
@@ -622,7 +634,7 @@ def forward_mx(qx, sx, codes, scales, N, Y=None, bias=None, act=ACT_NONE, residu
     _require_weights(FMT_MXFP4, codes, scales, N, K)
     _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
     if Y is None:
-        Y = torch.empty((M, N), dtype=ydtype, device=qx.device)
+        Y = qx.new_empty((M, N), dtype=ydtype)
     _require_y(Y, M, N, (torch.float32, torch.bfloat16))
     _require_ep(bias, residual, M, N)
     _require_steer(steer, N)
@@ -662,7 +674,7 @@ def gated_forward(fmt, X, gate, up, H=None, bias=None, act=ACT_SILU, hdtype=torc
     forward_ep on H.  Asynchronous."""
     g, M, K, N, tensors = _gated(fmt, X, gate, up, bias, act)
     if H is None:
-        H = torch.empty((M, N), dtype=hdtype, device=X.device)
+        H = X.new_empty((M, N), dtype=hdtype)
     _require(H, "H", (torch.float32, torch.bfloat16), (M, N))
     _on_current_device(H, *tensors)
     _check(load().qlinear_gated_forward(ctypes.byref(g), _ptr(H), _ydt(H), _stream(stream)))
@@ -687,12 +699,12 @@ def gated_backward(fmt, X, gate, up, dH, bias=None, act=ACT_SILU, x_grad=True,
         raise TypeError(f"gradients are float32 or bfloat16, not {dtype}")
     if N % 8:
         raise ValueError(f"N = {N} is not a multiple of 8")
-    new = lambda shape, dt: torch.empty(shape, dtype=dt, device=X.device)
+    _on_current_device(dH, *tensors)
+    new = lambda shape, dt: X.new_empty(shape, dtype=dt)
     both = new((2, M, N), torch.bfloat16)
     dX = new((M, K), dtype) if x_grad else None
     dW = new((2, N, K), dtype) if weight_grads else (None, None)
     db = new((2, N), torch.float32) if bias_grads else (None, None)
-    _on_current_device(dH, *tensors)
     dt = DT_BF16 if dtype == torch.bfloat16 else DT_F32
     d = _GatedGrad(_ptr(dH), _ydt(dH), _ptr(both[0]), _ptr(both[1]), _ptr(dX), dt, _ptr(dW[0]),
                    _ptr(dW[1]), dt, _ptr(db[0]), _ptr(db[1]))

@@ -443,7 +443,7 @@ def test_gated_partial_outputs(gpu):
 ROTARY = [  # rows, heads, dh, rot, extra columns
     (1, 2, 64, 64, 0), (3, 5, 64, 32, 64), (130, 8, 64, 48, 0), (7, 3, 80, 20, 5),
     (2, 1, 6, 2, 1), (65, 48, 64, 64, 1536), (4, 2, 128, 128, 8), (5, 1, 4100, 4100, 0),
-    (3000, 4, 64, 16, 0)]
+    (3000, 4, 64, 16, 0), (9, 160, 128, 128, 8), (1200, 70, 64, 32, 0)]
 
 
 @pytest.mark.parametrize("rows,heads,dh,rot,extra", ROTARY)
