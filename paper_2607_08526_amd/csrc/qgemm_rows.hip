@@ -1,6 +1,7 @@
 // Products with MXFP4 weights, and gated pairs of projections in any of the
-// quantized formats, at few rows and at every size that the tiled kernels do
-// not take:
+// quantized formats, without stages in LDS: fp32 activations and gated pairs at few
+// rows, where nothing else starts as fast, MXFP4 activations below the tiles of
+// qgemm_mx4.hip, and reductions too long for the staged kernels:
 //
 //   P[m][n] = sum_b sum_{k in b} X[m][k] c[n][k] s[n][b]
 //
@@ -307,7 +308,9 @@ __global__ __launch_bounds__(THREADS) void qgemm_rows_kernel(const RowsGroup arg
 template <int FMT, int XK, bool GATED>
 void launch(RowsGroup &g, int maxM, hipStream_t stream)
 {
-    const int mt = maxM <= 16 ? 1 : maxM <= 32 || XK == X_F32 ? 2 : 4;
+    // (more than 16 rows of other activations: only where the reduction is longer
+    // than the staged kernels take)
+    const int mt = XK != X_MX || maxM <= 16 ? 1 : maxM <= 32 ? 2 : 4;
     int64_t total = 0;
     for (int i = 0; i < g.n; ++i) {
         g.begin[i] = (int)total;
@@ -318,12 +321,13 @@ void launch(RowsGroup &g, int maxM, hipStream_t stream)
         g.begin[i] = (int)total;
     const dim3 grid((unsigned)total), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g); };
-    if (mt == 1)
-        go(qgemm_rows_kernel<FMT, XK, GATED, 1>);
-    else if (mt == 2)
-        go(qgemm_rows_kernel<FMT, XK, GATED, 2>);
-    else if constexpr (XK != X_F32)
-        go(qgemm_rows_kernel<FMT, XK, GATED, 4>);
+    if constexpr (XK == X_MX) {
+        if (mt == 2)
+            return go(qgemm_rows_kernel<FMT, XK, GATED, 2>);
+        if (mt == 4)
+            return go(qgemm_rows_kernel<FMT, XK, GATED, 4>);
+    }
+    go(qgemm_rows_kernel<FMT, XK, GATED, 1>);
 }
 
 }  // namespace

@@ -158,17 +158,19 @@ __device__ inline void strip_gated(const GateArgs &t, int M, int N, int m0, int 
         constexpr int i = decltype(ic)::value;
         strip_put(patch, lane, acc[i][0], acc[i][1]);
     };
+    float dh[4][4];
+    auto load_dh = [&](int mb) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (mb + 8 * u < M && n < N)
+                gate_load_dh(t, (int64_t)(mb + 8 * u) * N, n, N, dh[u]);
+    };
+    if (t.dG)
+        load_dh(m0 + rl);
 #pragma unroll 1
     for (int i = 0; i < MS; ++i) {
         static_assert(MS == 4, "row blocks");
         const int mb = m0 + 32 * i + rl;
-        float dh[4][4];
-        if (t.dG) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (mb + 8 * u < M && n < N)
-                    gate_load_dh(t, (int64_t)(mb + 8 * u) * N, n, N, dh[u]);
-        }
         if (i == 0)
             put(std::integral_constant<int, 0>{});
         else if (i == 1)
@@ -186,12 +188,20 @@ __device__ inline void strip_gated(const GateArgs &t, int M, int N, int m0, int 
             }
         };
         if (t.dG) {
+            float dc[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    dc[u][q] = dh[u][q];
+            if (i + 1 < MS)
+                load_dh(mb + 32);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 float g[4], v[4];
                 pair(u, g, v);
                 if (mb + 8 * u < M && n < N)
-                    gate_backward(t, (int64_t)(mb + 8 * u) * N, n, N, g, v, dh[u]);
+                    gate_backward(t, (int64_t)(mb + 8 * u) * N, n, N, g, v, dc[u]);
             }
         } else {
 #pragma unroll
