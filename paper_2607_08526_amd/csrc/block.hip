@@ -55,11 +55,12 @@ GateArgs gate_args(const ql_gated &g)
 // the two projections of a gated pair with the outputs t
 int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
 {
-    if (rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
-        return QL_ERR_UNSUPPORTED;
     int shape;
     const RowsKernel kernel = choose_rows(g.fmt, false, true, g.M, g.M, g.N, g.K, current_cus(),
                                           &shape);
+    if (kernel == ROWS_TILE ? tile_tiles(g.M, g.N, true) > MAX_WORKGROUPS
+                            : kernel == ROWS_ANY && rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
+        return QL_ERR_UNSUPPORTED;
     if (kernel == ROWS_TILE) {
         TileArgs a{};
         a.X = g.X;
@@ -153,7 +154,7 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
     }
     if (M < 0 || N <= 0 || K <= 0 || K % QL_BLOCK)
         return QL_ERR_SHAPE;
-    if (M >= I31 || N >= I31 || K >= I31 || rows_tiles(M, N, false) > MAX_WORKGROUPS)
+    if (M >= I31 || N >= I31 || K >= I31)
         return QL_ERR_UNSUPPORTED;
     if (!codes || !scales || (M > 0 && (!qx || !sx || !Y)))
         return QL_ERR_INVALID;
@@ -165,7 +166,10 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
     const Mx4Args t{qx, sx, (const uint8_t *)codes, scales, (float *)Y, kernel_epilogue(ep),
                     (int)M, (int)N, (int)K};
     if (mx4_takes(t) && mx4_wins(t, current_cus()))
-        return status(launch_qgemm_mx4(t, stream));
+        return mx4_tiles(t) > MAX_WORKGROUPS ? QL_ERR_UNSUPPORTED
+                                             : status(launch_qgemm_mx4(t, stream));
+    if (rows_tiles(M, N, false) > MAX_WORKGROUPS)
+        return QL_ERR_UNSUPPORTED;
     RowsGroup g{};
     RowsArgs &d = g.d[0];
     d.X = qx;
@@ -247,8 +251,7 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
     const size_t part_bytes = std::max(px > 1 ? (size_t)px * M * K * 4 : 0,
                                        pw > 1 ? (size_t)pw * 2 * N * K * 4 : 0);
     if ((want_x && gemm_tiles(M, K) * px > MAX_WORKGROUPS) ||
-        (d->dWg && gemm_tiles(N, K) * 2 * pw > MAX_WORKGROUPS) ||
-        rows_tiles(M, N, true) > MAX_WORKGROUPS)
+        (d->dWg && gemm_tiles(N, K) * 2 * pw > MAX_WORKGROUPS))
         return QL_ERR_UNSUPPORTED;
     uint8_t *ws = nullptr;
     bool own = false;

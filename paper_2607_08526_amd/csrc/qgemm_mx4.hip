@@ -230,7 +230,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
 
 }  // namespace
 
-static int64_t mx4_tiles(const Mx4Args &a)
+int64_t mx4_tiles(const Mx4Args &a)
 {
     return ((int64_t)a.M + BM - 1) / BM * (((int64_t)a.N + BN - 1) / BN);
 }

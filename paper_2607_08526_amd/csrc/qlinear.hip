@@ -1256,9 +1256,19 @@ GroupPath choose_path(const ql_linear_ep *const *ls, int n, int forced, KgPlan &
     return tall && all_wide ? GroupPath::WIDE : GroupPath::TILED;
 }
 
+constexpr int64_t PLANES_BYTES = (int64_t)64 << 20;
+
+// rows of fp32 activations that launch_mx splits into planes at a time: all, or whole
+// tiles' rows that PLANES_BYTES hold
+int64_t plane_rows(int64_t M, int64_t K)
+{
+    return std::min(M, std::max<int64_t>(1, PLANES_BYTES / (768 * K)) * 128);
+}
+
 // MXFP4 layers that share xdt (M > 0 each): those of the K-group kernel and of the
 // few-row kernel in one launch each, the large tiles' one after the other (fp32
-// activations as three bf16 planes in the workspace).
+// activations as three bf16 planes in the workspace, a slice of rows after the other
+// where all of them take more than PLANES_BYTES).
 int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t stream)
 {
     const bool xf32 = ls[0]->lin.xdt == QL_DT_F32;
@@ -1290,8 +1300,7 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
             t.K = (int)l.K;
             if (xf32) {
                 t.planes = 3;
-                t.plane_bytes = l.M * l.K * 2;
-                bytes = std::max(bytes, (size_t)t.plane_bytes * 3);
+                bytes = std::max(bytes, (size_t)(plane_rows(l.M, l.K) * l.K * 6));
             }
             if (tile_tiles(l.M, l.N, false) > MAX_WORKGROUPS)
                 return QL_ERR_UNSUPPORTED;
@@ -1308,7 +1317,8 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
         d.M = (int)l.M;
         d.N = (int)l.N;
         d.K = (int)l.K;
-        tiles += rows_tiles(l.M, l.N, false);
+        if (kernel == ROWS_ANY)
+            tiles += rows_tiles(l.M, l.N, false);
     }
     if (tiles > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
@@ -1321,18 +1331,27 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
         return wsrc.fixed ? QL_ERR_UNSUPPORTED : QL_ERR_HIP;
     hipError_t e = hipSuccess;
     for (int i = 0; i < nt && e == hipSuccess; ++i) {
-        TileArgs &t = tiled[i];
-        if (xf32) {
-            // (layers that read the same X in a row share its planes)
-            if (i == 0 || t.X != tiled[i - 1].X || t.M != tiled[i - 1].M || t.K != tiled[i - 1].K)
-                e = launch_split3((const float *)t.X, (int64_t)t.M * t.K, (uint16_t *)ws.ptr,
-                                  stream);
-        }
-        if (e == hipSuccess) {
+        const TileArgs &t = tiled[i];
+        const int64_t step = xf32 ? plane_rows(t.M, t.K) : t.M;
+        for (int64_t m = 0; m < t.M && e == hipSuccess; m += step) {
             TileArgs run = t;
-            if (xf32)
+            if (xf32) {
+                run.M = (int)std::min(step, t.M - m);
                 run.X = ws.ptr;
-            e = launch_qgemm_tile(QL_FMT_MXFP4, run, stream);
+                run.plane_bytes = (int64_t)run.M * t.K * 2;
+                const int64_t at = m * t.N;
+                run.Y = t.ep.ybf16 ? reinterpret_cast<float *>(reinterpret_cast<uint16_t *>(t.Y) + at)
+                                   : t.Y + at;
+                run.ep.resid = t.ep.resid ? t.ep.resid + at : nullptr;
+                run.ep.ycopy = t.ep.ycopy ? t.ep.ycopy + at : nullptr;
+                // (layers that read the same X in a row share its planes)
+                if (i == 0 || step < t.M || t.X != tiled[i - 1].X || t.M != tiled[i - 1].M ||
+                    t.K != tiled[i - 1].K)
+                    e = launch_split3((const float *)t.X + m * t.K, (int64_t)run.M * t.K,
+                                      (uint16_t *)ws.ptr, stream);
+            }
+            if (e == hipSuccess)
+                e = launch_qgemm_tile(QL_FMT_MXFP4, run, stream);
         }
     }
     if (kgm.n && e == hipSuccess)

@@ -771,7 +771,7 @@ def rotary(x, heads, freqs, dh=64, positions=None, start=0, T=None, interleaved=
         raise ValueError(f"T = {T} is not positive")
     _on_current_device(x, freqs, positions, out)
     # (a single row's stride may be anything: its length serves)
-    ld = lambda t: max(t.stride(0), t.shape[1])
+    ld = lambda t: t.stride(0) if rows > 1 else t.shape[1]
     _check(load().qlinear_rotary(_ptr(x), ld(x), _ptr(out), ld(out), _ydt(x), rows, heads, dh, rot,
                                  _ptr(freqs), _ptr(positions), start, T or max(rows, 1),
                                  float(mscale), interleaved, adjoint, _stream(stream)))

@@ -288,6 +288,67 @@ def test_mx_groups(gpu):
         assert torch.equal(e[5], y)
 
 
+def test_mx_groups_of_many_rows(gpu):
+    """Layers of different kernels and row counts in one call: one row beside the
+    tiles, fp32 layers that share their activations, one whose activations take more
+    than a slice of the workspace; each against its own reference, and the entry point
+    that allocates nothing the same bit for bit."""
+    torch, ql = gpu
+    rng = np.random.default_rng(18)
+    K = 2048
+    codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((520, K)).astype(np.float32) * 0.05)
+    c, s = dev(torch, codes), dev(torch, scales)
+    big = rng.standard_normal((6000, K)).astype(np.float32)
+    tall, few = big[:300], big[:1]
+    resid = dev(torch, rng.standard_normal((6000, 520)).astype(np.float32))
+    copy = torch.empty((6000, 520), dtype=torch.bfloat16, device="cuda")
+    rows = [0, 127, 128, 4999, 5375, 5376, 5377, 5503, 5504, 5999]
+    bigd, talld = dev(torch, big), dev(torch, tall)
+    f = lambda X, N, Y, r=None, y=None: (ql.FMT_MXFP4, X, c[:N], s[:N], N, Y, None, ql.ACT_NONE,
+                                         r, None, y)
+    new = lambda M, N, dt=torch.float32: torch.empty((M, N), dtype=dt, device="cuda")
+    ents = [f(bigd, 520, new(6000, 520), resid, copy), f(dev(torch, few), 100, new(1, 100)),
+            f(talld, 520, new(300, 520)), f(talld, 516, new(300, 516, torch.bfloat16)),
+            f(dev(torch, few).to(torch.bfloat16), 520, new(1, 520)),
+            f(dev(torch, tall).to(torch.bfloat16), 520, new(300, 520))]
+    ql.block_forward_ep(ents)
+    first = [e[5].clone() for e in ents] + [copy.clone()]
+    P, e = R.product(big[rows].astype(np.float64), Wv)
+    want = P + host(resid[rows])
+    check(ents[0][5][rows], want, e + 4 * R.F32 * (np.abs(P) + np.abs(want)), "slices")
+    assert torch.equal(copy, ents[0][5].to(torch.bfloat16))
+    P, e = R.product(tall.astype(np.float64), Wv)
+    check(ents[1][5], P[:1, :100], e[:1, :100], "one row")
+    check(ents[2][5], P, e, "fp32")
+    check(ents[3][5], P[:, :516], (e + R.BF16 * (np.abs(P) + e))[:, :516], "bf16 output")
+    P, e = R.product(bf16(torch, tall)[1], Wv)
+    check(ents[4][5], P[:1], e[:1], "one bf16 row")
+    check(ents[5][5], P, e, "bf16")
+    for t in ents:
+        t[5].fill_(-1)
+    copy.fill_(-1)
+    ql.block_forward_ep_noalloc(ents)
+    for a, b in zip(first, [t[5] for t in ents] + [copy]):
+        assert torch.equal(a, b)
+
+
+# reductions beyond the staged kernels' 2^22
+@pytest.mark.parametrize("M", [1, 21])
+def test_mx_longest_reductions(gpu, M):
+    torch, ql = gpu
+    rng = np.random.default_rng(M)
+    K, N = (1 << 22) + 32, 3
+    codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((N, K)).astype(np.float32) * 0.05)
+    c, s = dev(torch, codes), dev(torch, scales)
+    X = rng.standard_normal((M, K)).astype(np.float32)
+    check(ql.forward(ql.FMT_MXFP4, dev(torch, X), c, s, N),
+          *R.product(X.astype(np.float64), Wv), "fp32")
+    Xb, Xv = bf16(torch, X)
+    check(ql.forward(ql.FMT_MXFP4, Xb, c, s, N), *R.product(Xv, Wv), "bf16")
+    q = ql.quantize_act_mx(Xb)
+    check(ql.forward_mx(*q, c, s, N), *R.product(host(ql.dequantize(ql.FMT_MXFP4, *q)), Wv), "mx")
+
+
 def test_mx_scales_at_any_byte(gpu):
     """Scale bytes need no alignment: slices that start at odd addresses (which other
     kernels take, that add in another order)."""
@@ -490,6 +551,166 @@ def test_rotary_row_positions(gpu):
     assert torch.equal(one, ql.rotary(x, H, freqs, positions=torch.arange(B * T, device="cuda"),
                                       out=torch.empty_like(x)))
     assert ql.rotary(x[:0], H, freqs).shape == (0, H * 64)
+
+
+def test_rotary_overlapping_rows(gpu):
+    """Rows that are longer than their distance: only the heads' channels are read
+    and written."""
+    torch, ql = gpu
+    rows, H = 6, 2
+    flat = torch.randn(rows * 128 + 64, device="cuda")
+    x = flat.as_strided((rows, 192), (128, 1))
+    freqs, _ = ql.rotary_frequencies(32)
+    want = ql.rotary(flat[:rows * 128].view(rows, 128).clone(), H, freqs)
+    out = torch.full((rows, 192), 3.0, device="cuda")
+    ql.rotary(x, H, freqs, out=out)
+    assert torch.equal(out[:, :128], want) and (out[:, 128:] == 3).all()
+    tail = flat[rows * 128:].clone()
+    ql.rotary(x, H, freqs)
+    assert torch.equal(flat[:rows * 128].view(rows, 128), want)
+    assert torch.equal(flat[rows * 128:], tail)
+
+
+# ---- offsets past 32 bits ------------------------------------------------------------
+# The first 64 rows repeat: whatever lies far must come out as they do, bit for bit
+# (the same kernel, and the same order of sums, at another address).
+
+def periodic(torch, t, rows=64):
+    """Every row of t equals the row 64 before it."""
+    for i in range(rows, t.shape[0], 1 << 13):
+        part = t[i: i + (1 << 13)]
+        if not torch.equal(part, t[i - rows: i - rows + part.shape[0]]):
+            return False
+    return True
+
+
+def test_many_rows_past_32_bits(gpu):
+    torch, ql = gpu
+    n, g = 2049, torch.Generator(device="cuda").manual_seed(1)
+    many = lambda t: t.repeat(n, 1)
+    base = torch.randn((64, 32768), generator=g, device="cuda").to(torch.bfloat16)
+    X = many(base)
+    M = X.shape[0]
+    assert X.numel() > 1 << 32
+    q = ql.quantize_act_mx(X)
+    want = ql.quantize_act_mx(base)
+    assert torch.equal(q[0][:64], want[0]) and torch.equal(q[1][:64], want[1])
+    assert periodic(torch, q[0]) and periodic(torch, q[1])
+    back = ql.dequantize(ql.FMT_MXFP4, *q, dtype=torch.bfloat16)
+    assert torch.equal(back[:64], ql.dequantize(ql.FMT_MXFP4, *want, dtype=torch.bfloat16))
+    assert periodic(torch, back)
+    del back, q
+    freqs, _ = ql.rotary_frequencies(64)
+    pos = torch.arange(64, device="cuda").repeat(n)
+    ql.rotary(X, 512, freqs, positions=pos)
+    assert torch.equal(X[:64], ql.rotary(base.clone(), 512, freqs, positions=pos[:64]))
+    assert periodic(torch, X)
+    del X
+
+    N, K = 32776, 256
+    rng = np.random.default_rng(2)
+    codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((N, K)).astype(np.float32) * 0.05)
+    w = dev(torch, codes), dev(torch, scales)
+    x32 = rng.standard_normal((64, K)).astype(np.float32)
+    xb, xv = bf16(torch, x32)
+    Y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    out = lambda P, e: (P, e + R.BF16 * (np.abs(P) + e))
+    for x, values in ((xb, xv), (dev(torch, x32), x32.astype(np.float64))):
+        ql.forward_ep(ql.FMT_MXFP4, many(x), *w, N, Y=Y)
+        check(Y[:64], *out(*R.product(values, Wv)), "product")
+        assert periodic(torch, Y)
+    q = ql.quantize_act_mx(xb)
+    ql.forward_mx(many(q[0]), many(q[1]), *w, N, Y=Y)
+    check(Y[:64], *out(*R.product(host(ql.dequantize(ql.FMT_MXFP4, *q)), Wv)), "4-bit product")
+    assert periodic(torch, Y)
+    X = many(xb)
+    ql.gated_forward(ql.FMT_MXFP4, X, w, w, H=Y)
+    check(Y[:64], *out(*R.gated(xv, Wv, Wv, 0, 0, "silu", False)[:2]), "gated")
+    assert periodic(torch, Y)
+
+    # backward, with the forward's output as dH
+    b = ql.gated_backward(ql.FMT_MXFP4, X, w, w, Y, weight_grads=True, bias_grads=True)
+    H, _, (G, U, eG, eU) = R.gated(xv, Wv, Wv, 0, 0, "silu", False)
+    dG, dU, bG, bU = R.gated_grads(host(Y[:64]), G, U, eG, eU, "silu")
+    check(b.gate[:64], dG, bG, "dG")
+    check(b.up[:64], dU, bU, "dU")
+    assert periodic(torch, b.gate) and periodic(torch, b.up) and periodic(torch, b.X)
+    d = host(b.gate[:64]), host(b.up[:64])
+    dX, S = (d[0] + d[1]) @ Wv, (np.abs(d[0]) + np.abs(d[1])) @ np.abs(Wv)
+    e = S * (2 * N * R.STEP)
+    check(b.X[:64], dX, e + R.BF16 * (np.abs(dX) + e), "dX")
+    for got, v in ((b.W_gate, d[0]), (b.W_up, d[1])):
+        dW = n * v.T @ xv
+        e = M * R.STEP * n * (np.abs(v).T @ np.abs(xv))
+        check(got, dW, e + R.BF16 * (np.abs(dW) + e), "dW")
+    for got, v in ((b.b_gate, d[0]), (b.b_up, d[1])):
+        check(got, n * v.sum(axis=0), M * R.STEP * n * np.abs(v).sum(axis=0), "db")
+
+
+def test_more_rows_than_few_row_tiles(gpu):
+    """More outputs than a launch of the few-row kernel could hold: the tiles take
+    them."""
+    torch, ql = gpu
+    n, N, K = 9376, 16392, 256
+    M = 64 * n
+    assert (M // 16) * (N // 32) >= 1 << 24
+    rng = np.random.default_rng(4)
+    codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((N, K)).astype(np.float32) * 0.05)
+    w = dev(torch, codes), dev(torch, scales)
+    xb, xv = bf16(torch, rng.standard_normal((64, K)))
+    X = xb.repeat(n, 1)
+    Y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    q = ql.quantize_act_mx(X)
+    P, e = R.product(xv, Wv)
+    Pq, eq = R.product(host(ql.dequantize(ql.FMT_MXFP4, q[0][:64], q[1][:64])), Wv)
+    H, eh, _ = R.gated(xv, Wv, Wv, 0, 0, "silu", False)
+    for call, want, bound in (
+            (lambda: ql.forward_ep(ql.FMT_MXFP4, X, *w, N, Y=Y), P, e),
+            (lambda: ql.forward_mx(*q, *w, N, Y=Y), Pq, eq),
+            (lambda: ql.gated_forward(ql.FMT_MXFP4, X, w, w, H=Y), H, eh)):
+        Y.fill_(7)
+        call()
+        check(Y[:64], want, bound + R.BF16 * (np.abs(want) + bound), "first rows")
+        assert periodic(torch, Y)
+
+
+def test_large_weights_past_32_bits(gpu):
+    """Few rows against weights of more than 2^32 bytes of codes."""
+    torch, ql = gpu
+    rng = np.random.default_rng(3)
+    n, K = 16400, 8192
+    N = 64 * n
+    x32 = rng.standard_normal((3, K)).astype(np.float32)
+    xb, xv = bf16(torch, x32)
+    for fmt in ("mxfp4", "int8"):
+        codes, scales, Wv = R.weight(fmt, rng.standard_normal((64, K)).astype(np.float32) * 0.01)
+        w = tuple(dev(torch, t).repeat(n, 1) for t in (codes, scales))
+        assert w[0].numel() > 1 << 32
+        f = fmts(ql)[fmt]
+        if fmt == "mxfp4":
+            for x, values in ((xb, xv), (dev(torch, x32), x32.astype(np.float64))):
+                Y = ql.forward(f, x, *w, N)
+                check(Y[:, :64], *R.product(values, Wv), "product")
+                assert periodic(torch, Y.t())
+            q = ql.quantize_act_mx(xb)
+            Y = ql.forward_mx(*q, *w, N)
+            check(Y[:, :64], *R.product(host(ql.dequantize(f, *q)), Wv), "4-bit product")
+            assert periodic(torch, Y.t())
+        H = torch.empty((3, N), device="cuda")
+        ql.gated_forward(f, xb, w, w, H=H)
+        want, e, (G, U, eG, eU) = R.gated(xv, Wv, Wv, 0, 0, "silu", fmt != "mxfp4")
+        check(H[:, :64], want, e, "gated")
+        assert periodic(torch, H.t())
+        b = ql.gated_backward(f, xb, w, w, H, dtype=torch.float32)
+        dG, dU, bG, bU = R.gated_grads(host(H[:, :64]), G, U, eG, eU, "silu")
+        check(b.gate[:, :64], dG, bG, "dG")
+        check(b.up[:, :64], dU, bU, "dU")
+        assert periodic(torch, b.gate.t()) and periodic(torch, b.up.t())
+        dg, du = host(b.gate[:, :64]), host(b.up[:, :64])
+        S = n * (np.abs(dg) + np.abs(du)) @ np.abs(Wv)
+        check(b.X, n * (dg + du) @ Wv,
+              S * (2 * N * R.STEP * (1 if fmt == "mxfp4" else 2) +
+                   (R.PLANES if fmt != "mxfp4" else 0)), "dX")
 
 
 # ---- together ---------------------------------------------------------------------
