@@ -166,7 +166,7 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
     const Mx4Args t{qx, sx, (const uint8_t *)codes, scales, (float *)Y, kernel_epilogue(ep),
                     (int)M, (int)N, (int)K};
     if (mx4_takes(t) && mx4_wins(t, current_cus()))
-        return mx4_tiles(t) > MAX_WORKGROUPS ? QL_ERR_UNSUPPORTED
+        return mx4_tiles(t, 64) > MAX_WORKGROUPS ? QL_ERR_UNSUPPORTED
                                              : status(launch_qgemm_mx4(t, stream));
     if (rows_tiles(M, N, false) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;

@@ -350,7 +350,7 @@ struct Mx4Args {
     int M, N, K;
 };
 bool mx4_takes(const Mx4Args &a);
-int64_t mx4_tiles(const Mx4Args &a);
+int64_t mx4_tiles(const Mx4Args &a, int rows);
 bool mx4_wins(const Mx4Args &a, int cus);
 hipError_t launch_qgemm_mx4(const Mx4Args &a, hipStream_t stream);
 

@@ -8,13 +8,19 @@
 // 64-k chunk, and that block's scale in one byte of a register.
 //
 // Tile, pipeline and store as in the bf16 tiles (qgemm_tile.hip): 4 wavefronts
-// compute 128 rows x 256 weight rows (strips of 64), stages of 128 k move
-// directly to LDS through a ring of three, 16-byte chunks XOR-swizzled, one
-// barrier per stage.  Scales of the tile's 384 rows: where a row's allow it, 16
+// compute 128 or 64 rows x 256 weight rows (strips of 64 weight rows), stages of 128
+// k move directly to LDS through a ring of three, 16-byte chunks XOR-swizzled, one
+// barrier per stage.  Scales of the tile's rows: where a row's allow it, 16
 // bytes (four stages) into one slot that every wavefront copies to registers at
 // the group's start, so that it can be refilled behind them; otherwise each by
 // itself with its stage (more memory requests than the codes), a ring of two.  A
 // stage that K leaves unfilled ends in zeros.  Two workgroups per CU.
+//
+// Bound: latency where tiles are few (a wavefront per SIMD: hence the 64-row tiles,
+// which are twice as many), the stores and the residual at short reductions, and
+// operand traffic from L2 at long ones: 4096 x 8192 x 8192 (2 M N K = 550 Gflop) 165 to
+// 174 us, 3.2 to 3.3 PFLOP/s.  1290 rows x 6144 x 1536 with bias, GELU and an fp32
+// residual 26.6 us, 24.4 Gflop and 70 MB (14 us of a copy).
 #include <algorithm>
 #include <cmath>
 
@@ -32,15 +38,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-constexpr int BM = 128, BN = 256, MS = 4, NS = 2;
-constexpr int GROUP_M = 4;
+constexpr int BN = 256, NS = 2;
 constexpr int ROW = 64;  // code bytes per row and stage (128 k)
-constexpr int XBYTES = BM * ROW, WBYTES = BN * ROW;
-constexpr int STAGE = XBYTES + WBYTES;
-constexpr int SROWS = BM + BN, SLDS = SROWS * 16;  // scales: 16 bytes, or 4 blocks' dwords
-constexpr int XLOADS = XBYTES / 16 / THREADS, WLOADS = WBYTES / 16 / THREADS;
-static_assert(2 * (3 * STAGE + SLDS) <= 160 * 1024 && 4 * (STAGE + SLDS) <= 160 * 1024,
-              "two workgroups per CU");
 
 __device__ __align__(16) const uint32_t zeros[4] = {0, 0, 0, 0};
 
@@ -54,9 +53,16 @@ __device__ inline i32x8 codes8(u32x4 v)
 }
 
 // SWIDE: scales 16 bytes at a time.  EPI: an epilogue beyond the output's type.
-template <bool SWIDE, bool EPI>
+// MS: blocks of 32 rows of the tile.
+template <int MS, bool SWIDE, bool EPI>
 __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
 {
+    constexpr int BM = 32 * MS, GROUP_M = 16 / MS;
+    constexpr int XBYTES = BM * ROW, WBYTES = BN * ROW, STAGE = XBYTES + WBYTES;
+    constexpr int SROWS = BM + BN, SLDS = SROWS * 16;  // scales: 16 bytes, or 4 blocks' dwords
+    constexpr int XLOADS = XBYTES / 16 / THREADS, WLOADS = WBYTES / 16 / THREADS;
+    static_assert(2 * (3 * STAGE + SLDS) <= 160 * 1024 && 4 * (STAGE + SLDS) <= 160 * 1024,
+                  "two workgroups per CU");
     constexpr int SG = SWIDE ? 4 : 1, NST = SWIDE ? 3 : 2;  // stages of a scale group, of the ring
     __shared__ __align__(16) uint8_t ring[NST * STAGE + (SWIDE ? 1 : NST) * SLDS];
     uint8_t *const sring = ring + NST * STAGE;
@@ -85,18 +91,19 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
         woff[r] = (uint32_t)((min(n0 + row, N - 1) - n0) * krow + lc * 16);
     }
     const uint32_t wsoff = (uint32_t)((min(n0 + tid, N - 1) - n0) * nb);
-    const uint32_t xsoff = (uint32_t)((min(m0 + (tid & 127), M - 1) - m0) * nb);
+    const uint32_t xsoff = (uint32_t)((min(m0 + tid % BM, M - 1) - m0) * nb);
     const uint8_t *const xb = a.qx + (int64_t)m0 * krow, *const wb = a.codes + (int64_t)n0 * krow;
     const uint8_t *const xs = a.sx + (int64_t)m0 * nb, *const ws = a.scales + (int64_t)n0 * nb;
     // scales of the group that stage s starts: rows of X, then of W (not SWIDE: four
-    // of them, one for each block; past K the row's last).  (X's by the first two
+    // of them, one for each block; past K the row's last).  (X's by the first XH
     // wavefronts; SWIDE the others repeat them, so that every wavefront counts the
-    // same loads, otherwise they take every other block.)
+    // same loads, otherwise they take other blocks.)
+    constexpr int XH = BM / 64;
     auto issue_scales = [&](int s) {
         if constexpr (SWIDE) {
             const uint32_t base = dma_lds(sring);
             dma_load16(ws + (int64_t)s * 4, wsoff, base + (BM + wave * 64) * 16);
-            dma_load16(xs + (int64_t)s * 4, xsoff, base + (wave & 1) * 64 * 16);
+            dma_load16(xs + (int64_t)s * 4, xsoff, base + wave % XH * 64 * 16);
         } else {
             const uint32_t base = dma_lds(sring + s % NST * SLDS);
 #pragma unroll
@@ -104,10 +111,11 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
                 dma_load_small_at<1>(ws + wsoff + min(4 * s + h, nb - 1),
                                      base + h * (SROWS * 4) + (BM + wave * 64) * 4);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                dma_load_small_at<1>(xs + xsoff + min(4 * s + 2 * h + (wave >> 1), nb - 1),
-                                     base + (2 * h + (wave >> 1)) * (SROWS * 4) +
-                                         (wave & 1) * 64 * 4);
+            for (int h = 0; h < XH; ++h) {
+                const int b = (4 * h + wave) / XH;
+                dma_load_small_at<1>(xs + xsoff + min(4 * s + b, nb - 1),
+                                     base + b * (SROWS * 4) + wave % XH * 64 * 4);
+            }
         }
     };
     auto issue = [&](int s) {
@@ -135,7 +143,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
         if constexpr (!SWIDE)
             issue_scales(s);
     };
-    constexpr int LOADS = XLOADS + WLOADS + (SWIDE ? 0 : 6);
+    constexpr int LOADS = XLOADS + WLOADS + (SWIDE ? 0 : 4 + XH);
 
     f32x16 acc[MS][NS];
 #pragma unroll
@@ -230,9 +238,9 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_mx4_kernel(const Mx4Args a)
 
 }  // namespace
 
-int64_t mx4_tiles(const Mx4Args &a)
+int64_t mx4_tiles(const Mx4Args &a, int rows)
 {
-    return ((int64_t)a.M + BM - 1) / BM * (((int64_t)a.N + BN - 1) / BN);
+    return ((int64_t)a.M + rows - 1) / rows * (((int64_t)a.N + BN - 1) / BN);
 }
 
 bool mx4_takes(const Mx4Args &a)
@@ -240,30 +248,54 @@ bool mx4_takes(const Mx4Args &a)
     return a.K < (1 << 22);
 }
 
-// Estimated us: a stage of a tile takes 0.49 us while few CUs work, 0.62 when all
-// do, two on a CU 0.66 each; a 128-k step of the few-row kernel 0.13 to 0.32 us by
-// its row tile and 0.85 ns per workgroup (6144 x 1536, tiles / few rows: 128 rows
-// 11.5 / 10.0, 256 rows 11.4 / 13.9, 1024 rows 12.8 / 41.7; 1536 x 6144: 256 rows
-// 29.1 / 19.9, 1024 rows 29.7 / 51.5).
+// Estimated us of tiles of 64 or 128 rows.  A stage of a tile that has a CU to itself
+// takes 0.37 or 0.53 us (latency: rising where most CUs work), one of several on a CU
+// 0.46 or 0.66; an epilogue 4 us, with an activation 8, per 128 rows of a tile.
+// Measured, 64 / 128 rows without an epilogue: 6144 x 1536 at 256 rows 9.3 / 12.8, at
+// 1290 16.2 / 18.9, at 2048 21.2 / 20.3; 1536 x 6144 at 1290 rows 24.0 / 31.8, at 4096
+// 42.4 / 34.1; with bias, GELU and residual 6144 x 1536 at 1290 rows 26.6 / 34.2.
+static double mx4_us(const Mx4Args &a, int rows, int cus)
+{
+    const double r = (double)mx4_tiles(a, rows) / cus, up = std::ceil(r);
+    const double steps = std::ceil(a.K / 128.0), busy = r + 0.4 * (up - r);
+    const double stage = rows == 64 ? (r <= 1.0 ? 0.36 + 0.05 * r : 0.46 * busy)
+                                    : (r <= 1.0 ? 0.49 + 0.13 * r : 0.66 * busy);
+    const double epi = strip_plain(a.ep) ? 0.0 : a.ep.act ? 8.0 : 4.0;
+    return (rows == 64 ? 5.0 : 5.5) + steps * stage +
+           epi * rows / 128 * std::max(1.0, std::min(r, 2.0));
+}
+
+static int mx4_rows(const Mx4Args &a, int cus)
+{
+    return mx4_us(a, 64, cus) < mx4_us(a, 128, cus) ? 64 : 128;
+}
+
+// Against the few-row kernel: a 128-k step there takes 0.13 to 0.32 us by its row tile
+// and 0.85 ns per workgroup.
 bool mx4_wins(const Mx4Args &a, int cus)
 {
-    const double r = (double)mx4_tiles(a) / cus, up = std::ceil(r), steps = std::ceil(a.K / 128.0);
-    const double tile = 5.5 + steps * (r <= 1.0 ? 0.49 + 0.13 * r : 0.66 * (r + 0.4 * (up - r)));
+    const double steps = std::ceil(a.K / 128.0);
     const int rows = a.M <= 16 ? 16 : a.M <= 32 ? 32 : 64;
     const double wgs = (double)((a.M + rows - 1) / rows) * ((a.N + 31) / 32);
     const double few = 4.5 + steps * ((rows == 16 ? 0.13 : rows == 32 ? 0.19 : 0.32) + 0.00085 * wgs);
-    return tile < few;
+    return std::min(mx4_us(a, 64, cus), mx4_us(a, 128, cus)) < few;
 }
 
 hipError_t launch_qgemm_mx4(const Mx4Args &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)mx4_tiles(a)), block(THREADS);
+    const int rows = mx4_rows(a, current_cus());
+    const dim3 grid((unsigned)mx4_tiles(a, rows)), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
     const bool epi = !strip_plain(a.ep);
-    if (a.K % 512 == 0 && (((uintptr_t)a.sx | (uintptr_t)a.scales) & 15) == 0)
-        epi ? go(qgemm_mx4_kernel<true, true>) : go(qgemm_mx4_kernel<true, false>);
-    else
-        epi ? go(qgemm_mx4_kernel<false, true>) : go(qgemm_mx4_kernel<false, false>);
+    const bool swide = a.K % 512 == 0 && (((uintptr_t)a.sx | (uintptr_t)a.scales) & 15) == 0;
+    auto with = [&](auto msc) {
+        constexpr int MS = decltype(msc)::value;
+        if (swide)
+            epi ? go(qgemm_mx4_kernel<MS, true, true>) : go(qgemm_mx4_kernel<MS, true, false>);
+        else
+            epi ? go(qgemm_mx4_kernel<MS, false, true>) : go(qgemm_mx4_kernel<MS, false, false>);
+    };
+    rows == 64 ? with(std::integral_constant<int, 2>{}) : with(std::integral_constant<int, 4>{});
     return hipGetLastError();
 }
 

@@ -76,16 +76,16 @@ __device__ inline void strip_store(const Epilogue &e, float *Y, int M, int N, in
     }
 #pragma unroll 1
     for (int i = 0; i < MS; ++i) {
-        static_assert(MS == 4, "row blocks");
+        static_assert(MS == 2 || MS == 4, "row blocks");
         const int mb = m0 + 32 * i + rl;
         if (i == 0)
             put(std::integral_constant<int, 0>{});
-        else if (i == 1)
+        else if (MS == 2 || i == 1)
             put(std::integral_constant<int, 1>{});
         else if (i == 2)
-            put(std::integral_constant<int, 2>{});
+            put(std::integral_constant<int, MS - 2>{});
         else
-            put(std::integral_constant<int, 3>{});
+            put(std::integral_constant<int, MS - 1>{});
         if (!vec) {
 #pragma unroll 1
             for (int u = 0; u < 8; ++u) {
