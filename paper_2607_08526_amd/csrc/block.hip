@@ -58,8 +58,7 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
     int shape;
     const RowsKernel kernel = choose_rows(g.fmt, false, true, g.M, g.M, g.N, g.K, current_cus(),
                                           &shape);
-    if (kernel == ROWS_TILE ? tile_tiles(g.M, g.N, true) > MAX_WORKGROUPS
-                            : kernel == ROWS_ANY && rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
+    if (kernel == ROWS_ANY && rows_tiles(g.M, g.N, true) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
     if (kernel == ROWS_TILE) {
         TileArgs a{};
@@ -73,6 +72,7 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
         a.M = (int)g.M;
         a.N = (int)g.N;
         a.K = (int)g.K;
+        a.rows = shape;
         return status(launch_qgemm_tile(g.fmt, a, stream));
     }
     RowsGroup r{};

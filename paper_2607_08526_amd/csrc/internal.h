@@ -320,7 +320,8 @@ struct RowsGroup {
 };
 
 // One product of the large tiles (qgemm_tile.hip): as RowsArgs on bf16
-// activations, with 224 <= K < 2^22, X of `planes` bf16 planes plane_bytes apart that are added up.
+// activations, with 224 <= K < 2^22, X of `planes` bf16 planes plane_bytes apart that
+// are added up.
 struct TileArgs {
     const void *X;
     int64_t plane_bytes;
@@ -331,12 +332,12 @@ struct TileArgs {
     Epilogue ep;
     GateArgs gate;
     int M, N, K;
+    int rows;  // of a tile: 128 or 64
 };
-int64_t tile_tiles(int64_t M, int64_t N, bool gated);
-// whether a layer's (or a gated pair's) shape allows the tiles, and their estimated
-// us
+// whether a layer's (or a gated pair's) shape allows the tiles; their estimated us
+// (1e30: more than a launch holds) and the rows of a tile
 bool tile_takes(int64_t K);
-double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus);
+double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus, int *rows);
 hipError_t launch_qgemm_tile(int fmt, const TileArgs &a, hipStream_t stream);
 // fp32 X (count % 8 == 0 values) as three bf16 planes [3][count]
 hipError_t launch_split3(const float *X, int64_t count, uint16_t *planes, hipStream_t stream);
@@ -407,8 +408,8 @@ int epilogue_status(const ql_epilogue &ep, const void *Y);
 Epilogue kernel_epilogue(const ql_epilogue *ep);
 
 // The same layers but for MXFP4 activations on the K-group kernel
-// (qgemm_kgm.hip): K < 2^22.  kgm_tile_shape: rows and columns of a shape's tile in a launch of at most maxM rows ({0, 0}: the
-// launch has no such shape).
+// (qgemm_kgm.hip): K < 2^22.  kgm_tile_shape: rows and columns of a shape's tile in a
+// launch of at most maxM rows ({0, 0}: the launch has no such shape).
 enum KgmShape { KGM_R1W1, KGM_R1W2, KGM_R1W4, KGM_R2W2, KGM_R2W4, KGM_SHAPES };
 KgTile kgm_tile_shape(int fmt, bool xf32, bool gated, int64_t maxM, int shape);
 hipError_t launch_qgemm_kgm(int fmt, bool xf32, RowsGroup &g, hipStream_t stream);
@@ -417,7 +418,8 @@ bool kgm_takes(int64_t K);
 double kgm_us(int fmt, bool xf32, bool gated, int64_t maxM, int64_t M, int64_t N, int64_t K,
               int cus, int *shape);
 // The kernel of a layer (or gated pair) that is not on MXFP4 activations, by what
-// its shape allows and the estimates; shape for ROWS_KGM.
+// its shape allows and the estimates; shape: of ROWS_KGM, or the rows of a tile of
+// ROWS_TILE.
 enum RowsKernel { ROWS_ANY, ROWS_KGM, ROWS_TILE };
 RowsKernel choose_rows(int fmt, bool xf32, bool gated, int64_t maxM, int64_t M, int64_t N,
                        int64_t K, int cus, int *shape);

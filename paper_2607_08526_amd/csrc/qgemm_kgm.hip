@@ -521,8 +521,11 @@ RowsKernel choose_rows(int fmt, bool xf32, bool gated, int64_t maxM, int64_t M, 
     if (few || !kgm_takes(K))
         return ROWS_ANY;
     const double us = kgm_us(fmt, xf32, gated, maxM, M, N, K, cus, shape);
-    if (tile_takes(K) && tile_us(fmt, xf32, gated, M, N, K, cus) < us)
+    int rows = 0;
+    if (tile_takes(K) && tile_us(fmt, xf32, gated, M, N, K, cus, &rows) < us) {
+        *shape = rows;
         return ROWS_TILE;
+    }
     return us < 1e30 ? ROWS_KGM : ROWS_ANY;
 }
 

@@ -16,7 +16,8 @@
 // one scale block, one 16-byte LDS read (int8: two).
 //
 // Tile: 4 wavefronts compute 128 rows x 256 weight rows, each a strip of 64
-// weight rows (4 x 2 MFMA tiles): every converted weight feeds 4 MFMAs.  Of a
+// weight rows (4 x 2 MFMA tiles): every converted weight feeds 4 MFMAs; or 64 rows,
+// where tiles are few: twice as many wavefronts hide the latency that bounds them.  Of a
 // gated pair the strip is 32 rows of the gate and the same 32 of the up
 // projection, so both projections of an output meet in one lane and the
 // activation and the product happen on the accumulators.
@@ -49,11 +50,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-constexpr int BM = 128, BN = 256, MS = 4, NS = 2;
-constexpr int GROUP_M = 4;
+constexpr int BN = 256, NS = 2;
 
-template <int FMT>
+// MS: blocks of 32 rows of the tile.
+template <int FMT, int MS>
 struct Geo {
+    static constexpr int BM = 32 * MS;
     static constexpr int CROW = FMT == QL_FMT_INT8 ? 64 : 32;  // code bytes per row per step
     static constexpr int CCH = CROW / 16;
     static constexpr int XBYTES = BM * 128, CBYTES = BN * CROW;
@@ -93,11 +95,11 @@ __device__ inline int tile_row(int r)
 
 // What a lane needs of a tile, fixed for the whole reduction, and how far the
 // loads have come.
-template <int FMT, bool SWIDE>
+template <int FMT, int MS, bool SWIDE>
 struct Ctx {
     uint8_t *ring, *sring;
-    uint32_t xoff[Geo<FMT>::XLOADS], coff[Geo<FMT>::CLOADS];
-    const uint8_t *cptr[Geo<FMT>::CLOADS];  // wave-uniform
+    uint32_t xoff[Geo<FMT, MS>::XLOADS], coff[Geo<FMT, MS>::CLOADS];
+    const uint8_t *cptr[Geo<FMT, MS>::CLOADS];  // wave-uniform
     const uint8_t *x;                       // of the next stage to load
     const uint8_t *sp;                      // this thread's scale row
     int64_t plane_skip;                     // from one plane's end to the next one
@@ -109,20 +111,20 @@ struct Ctx {
 // Operands carried from one 16-k chunk to the next, across stages too: the
 // step's raw codes and scales, and the fragments of the chunk about to be
 // multiplied.
-template <int FMT>
+template <int FMT, int MS>
 struct Ops {
-    uint32_t raw[NS][4 * Geo<FMT>::CCH / 2];
+    uint32_t raw[NS][4 * Geo<FMT, MS>::CCH / 2];
     float sc[NS];
     u32x4 grp[NS];  // a scale group's dwords (not SWIDE: one)
-    u32x4 a[MS], b[NS][Geo<FMT>::PLANES];
+    u32x4 a[MS], b[NS][Geo<FMT, MS>::PLANES];
 };
 
 // Loads of step t, the next stage, into its slot, and where scales are not SWIDE
 // the step's (of blocks past K: the row's last).
-template <int FMT, bool SWIDE>
-__device__ inline void issue(Ctx<FMT, SWIDE> &c, int t, int slot)
+template <int FMT, int MS, bool SWIDE>
+__device__ inline void issue(Ctx<FMT, MS, SWIDE> &c, int t, int slot)
 {
-    using G = Geo<FMT>;
+    using G = Geo<FMT, MS>;
     const uint32_t base = dma_lds(c.ring + slot * G::STAGE) + c.wave * 1024;
     const int left = c.nb - 2 * c.ik;  // blocks from this step on
     if (SWIDE || left >= 2) {
@@ -164,16 +166,15 @@ __device__ inline void issue(Ctx<FMT, SWIDE> &c, int t, int slot)
 
 // SWIDE: 16 bytes per row, the next scale group (past the last: a group of the
 // row that is not used)
-template <int FMT, bool SWIDE>
-__device__ inline void issue_scales(Ctx<FMT, SWIDE> &c)
+template <int FMT, int MS, bool SWIDE>
+__device__ inline void issue_scales(Ctx<FMT, MS, SWIDE> &c)
 {
-    dma_load16_at(c.sp + (c.sk / Geo<FMT>::SSTEPS) * 4, dma_lds(c.sring) + c.wave * 1024);
-    c.sk += 4 * Geo<FMT>::SSTEPS;
+    dma_load16_at(c.sp + (c.sk / Geo<FMT, MS>::SSTEPS) * 4, dma_lds(c.sring) + c.wave * 1024);
+    c.sk += 4 * Geo<FMT, MS>::SSTEPS;
     if (c.sk == c.plane_steps)
         c.sk = 0;
 }
 
-template <int FMT>
 __device__ inline u32x4 read_x(const uint8_t *st, int lane, int q, int i)
 {
     const int row = 32 * i + (lane & 31);
@@ -182,11 +183,11 @@ __device__ inline u32x4 read_x(const uint8_t *st, int lane, int q, int i)
 }
 
 // codes and scale of step t (from stage st) for fragment j; U = t % 4
-template <int FMT, bool SWIDE, int U>
-__device__ inline void read_weights(const Ctx<FMT, SWIDE> &c, const uint8_t *st, int t, int j,
-                                    Ops<FMT> &op)
+template <int FMT, int MS, bool SWIDE, int U>
+__device__ inline void read_weights(const Ctx<FMT, MS, SWIDE> &c, const uint8_t *st, int t, int j,
+                                    Ops<FMT, MS> &op)
 {
-    using G = Geo<FMT>;
+    using G = Geo<FMT, MS>;
     const int row = c.wave * 64 + 32 * j + (c.lane & 31), g = c.lane >> 5;
 #pragma unroll
     for (int h = 0; h < G::CCH / 2; ++h) {
@@ -213,12 +214,12 @@ __device__ inline void read_weights(const Ctx<FMT, SWIDE> &c, const uint8_t *st,
     }
 }
 
-template <int FMT, bool SWIDE, int U>
-__device__ inline void scale_value(int lane, int j, Ops<FMT> &op)
+template <int FMT, int MS, bool SWIDE, int U>
+__device__ inline void scale_value(int lane, int j, Ops<FMT, MS> &op)
 {
     // SWIDE: this lane half's part of the group's dword; otherwise the scale itself
     const int g = SWIDE ? lane >> 5 : 0;
-    const uint32_t d = op.grp[j][SWIDE ? U / Geo<FMT>::SSTEPS : 0];
+    const uint32_t d = op.grp[j][SWIDE ? U / Geo<FMT, MS>::SSTEPS : 0];
     if constexpr (FMT == QL_FMT_MXFP4)
         op.sc[j] = mx_scale(d >> ((SWIDE ? 16 * (U & 1) : 0) + 8 * g) & 255u);
     else
@@ -226,9 +227,9 @@ __device__ inline void scale_value(int lane, int j, Ops<FMT> &op)
 }
 
 // word w (two k) of fragment j, chunk q
-template <int FMT>
-__device__ inline void weight_word(const Ops<FMT> &op, int j, int q, int w,
-                                   u32x4 (&b)[NS][Geo<FMT>::PLANES])
+template <int FMT, int MS>
+__device__ inline void weight_word(const Ops<FMT, MS> &op, int j, int q, int w,
+                                   u32x4 (&b)[NS][Geo<FMT, MS>::PLANES])
 {
     // (pinned to where it is written: the words would otherwise gather behind the
     // chunk's last MFMA)
@@ -236,7 +237,7 @@ __device__ inline void weight_word(const Ops<FMT> &op, int j, int q, int w,
     decode_word<FMT>(op.raw[j], 4 * q + w, op.sc[j], hi, lo);
     dma_pin(hi);
     b[j][0][w] = hi;
-    if constexpr (Geo<FMT>::PLANES == 2) {
+    if constexpr (Geo<FMT, MS>::PLANES == 2) {
         dma_pin(lo);
         b[j][1][w] = lo;
     }
@@ -245,11 +246,11 @@ __device__ inline void weight_word(const Ops<FMT> &op, int j, int q, int w,
 // The MFMAs of chunk Q of step t (U = t % 4), and behind each, in a group that
 // the compiler keeps together, a share of the next chunk's operands: of this
 // stage (Q < 3) or with NEXT of the next one (nxt).
-template <int FMT, bool SWIDE, int U, int Q, bool NEXT>
-__device__ inline void chunk(const Ctx<FMT, SWIDE> &c, const uint8_t *cur, const uint8_t *nxt,
-                             int t, Ops<FMT> &op, f32x16 (&acc)[MS][NS])
+template <int FMT, int MS, bool SWIDE, int U, int Q, bool NEXT>
+__device__ inline void chunk(const Ctx<FMT, MS, SWIDE> &c, const uint8_t *cur, const uint8_t *nxt,
+                             int t, Ops<FMT, MS> &op, f32x16 (&acc)[MS][NS])
 {
-    constexpr int P = Geo<FMT>::PLANES, KK = MS * NS * P, UN = (U + 1) & 3;
+    constexpr int P = Geo<FMT, MS>::PLANES, KK = MS * NS * P, UN = (U + 1) & 3;
     constexpr int W0 = Q < 3 ? 0 : KK / 2, PER = (8 + KK - W0 - 1) / (KK - W0);  // words per MFMA
     static_assert(NS == 2, "8 words");
     u32x4 an[MS], bn[NS][P];
@@ -261,19 +262,19 @@ __device__ inline void chunk(const Ctx<FMT, SWIDE> &c, const uint8_t *cur, const
             0, 0, 0);
         if constexpr (Q < 3 || NEXT) {
             if (Q == 3 && k < NS)
-                read_weights<FMT, SWIDE, UN>(c, nxt, t + 1, k, op);
+                read_weights<FMT, MS, SWIDE, UN>(c, nxt, t + 1, k, op);
             if (k < 2 * MS && k % 2 == 0)
-                an[k / 2] = read_x<FMT>(Q < 3 ? cur : nxt, c.lane, Q < 3 ? Q + 1 : 0, k / 2);
+                an[k / 2] = read_x(Q < 3 ? cur : nxt, c.lane, Q < 3 ? Q + 1 : 0, k / 2);
             if (Q == 3 && k == W0 - 1) {
 #pragma unroll
                 for (int jj = 0; jj < NS; ++jj)
-                    scale_value<FMT, SWIDE, UN>(c.lane, jj, op);
+                    scale_value<FMT, MS, SWIDE, UN>(c.lane, jj, op);
             }
             if (k >= W0) {
 #pragma unroll
                 for (int w = (k - W0) * PER; w < (k - W0 + 1) * PER; ++w)
                     if (w < 8)
-                        weight_word<FMT>(op, w / 4, Q < 3 ? Q + 1 : 0, w % 4, bn);
+                        weight_word<FMT, MS>(op, w / 4, Q < 3 ? Q + 1 : 0, w % 4, bn);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -296,11 +297,11 @@ __device__ inline void chunk(const Ctx<FMT, SWIDE> &c, const uint8_t *cur, const
 // has landed (loads land in order: what was issued after it may be in flight), and
 // behind the barrier the stage's slot is refilled while chunk 3 runs and prepares
 // the next stage's first one.
-template <int FMT, bool SWIDE, int U, bool TAIL>
-__device__ inline void step(Ctx<FMT, SWIDE> &c, int t, int &slot, Ops<FMT> &op,
+template <int FMT, int MS, bool SWIDE, int U, bool TAIL>
+__device__ inline void step(Ctx<FMT, MS, SWIDE> &c, int t, int &slot, Ops<FMT, MS> &op,
                             f32x16 (&acc)[MS][NS])
 {
-    using G = Geo<FMT>;
+    using G = Geo<FMT, MS>;
     constexpr int NST = G::NST;
     constexpr bool LAST = TAIL && U == 3;                   // t + 1 == ns
     constexpr bool ISSUE = !TAIL || U + NST < 4;            // t + NST < ns
@@ -308,9 +309,9 @@ __device__ inline void step(Ctx<FMT, SWIDE> &c, int t, int &slot, Ops<FMT> &op,
     const uint8_t *const cur = c.ring + slot * G::STAGE;
     const int nslot = slot + 1 == NST ? 0 : slot + 1;
     const uint8_t *const nxt = c.ring + nslot * G::STAGE;
-    chunk<FMT, SWIDE, U, 0, false>(c, cur, nxt, t, op, acc);
-    chunk<FMT, SWIDE, U, 1, false>(c, cur, nxt, t, op, acc);
-    chunk<FMT, SWIDE, U, 2, false>(c, cur, nxt, t, op, acc);
+    chunk<FMT, MS, SWIDE, U, 0, false>(c, cur, nxt, t, op, acc);
+    chunk<FMT, MS, SWIDE, U, 1, false>(c, cur, nxt, t, op, acc);
+    chunk<FMT, MS, SWIDE, U, 2, false>(c, cur, nxt, t, op, acc);
     if constexpr (!LAST) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         // a group of scales starts every 4 SSTEPS steps; the next one's are issued
@@ -327,22 +328,22 @@ __device__ inline void step(Ctx<FMT, SWIDE> &c, int t, int &slot, Ops<FMT> &op,
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
         if (SWIDE && U == 0 && first)
-            issue_scales<FMT, SWIDE>(c);
+            issue_scales<FMT, MS, SWIDE>(c);
         if constexpr (ISSUE)
-            issue<FMT, SWIDE>(c, t + NST, slot);
-        chunk<FMT, SWIDE, U, 3, true>(c, cur, nxt, t, op, acc);
+            issue<FMT, MS, SWIDE>(c, t + NST, slot);
+        chunk<FMT, MS, SWIDE, U, 3, true>(c, cur, nxt, t, op, acc);
     } else {
-        chunk<FMT, SWIDE, U, 3, false>(c, cur, nxt, t, op, acc);
+        chunk<FMT, MS, SWIDE, U, 3, false>(c, cur, nxt, t, op, acc);
     }
     slot = nslot;
 }
 
 // SWIDE: scales 16 bytes at a time.  EPI: an epilogue beyond the output's type.
-template <int FMT, bool GATED, bool SWIDE, bool EPI>
+template <int FMT, int MS, bool GATED, bool SWIDE, bool EPI>
 __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a)
 {
-    using G = Geo<FMT>;
-    constexpr int NST = G::NST;
+    using G = Geo<FMT, MS>;
+    constexpr int NST = G::NST, BM = G::BM, GROUP_M = 16 / MS;
     constexpr int COLS = GATED ? BN / 2 : BN;  // output columns of a tile
     __shared__ __align__(16) uint8_t ring[G::LDS];
     const int M = a.M, N = a.N, K = a.K, nb = K >> 5;
@@ -360,7 +361,7 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
     // (an odd number of steps gets one of zeros)
     const int plane_steps = (nb + 1) >> 1, ns = (plane_steps * a.planes + 1) & ~1;
 
-    Ctx<FMT, SWIDE> c;
+    Ctx<FMT, MS, SWIDE> c;
     c.ring = ring;
     c.sring = ring + NST * G::STAGE;
     c.wave = wave;
@@ -406,43 +407,43 @@ __global__ __launch_bounds__(THREADS, 2) void qgemm_tile_kernel(const TileArgs a
 
     {
         if (SWIDE)
-            issue_scales<FMT, SWIDE>(c);
+            issue_scales<FMT, MS, SWIDE>(c);
 #pragma unroll
         for (int t = 0; t < NST; ++t)
-            issue<FMT, SWIDE>(c, t, t);
+            issue<FMT, MS, SWIDE>(c, t, t);
         // stage 0: the younger ones may be in flight (ns >= 4 > NST)
         __builtin_amdgcn_s_waitcnt(dma_vmcnt((NST - 1) * (G::LOADS + (SWIDE ? 0 : 2))));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
-        Ops<FMT> op;
+        Ops<FMT, MS> op;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-            read_weights<FMT, SWIDE, 0>(c, c.ring, 0, j, op);
-            scale_value<FMT, SWIDE, 0>(lane, j, op);
+            read_weights<FMT, MS, SWIDE, 0>(c, c.ring, 0, j, op);
+            scale_value<FMT, MS, SWIDE, 0>(lane, j, op);
         }
 #pragma unroll
         for (int i = 0; i < MS; ++i)
-            op.a[i] = read_x<FMT>(c.ring, lane, 0, i);
+            op.a[i] = read_x(c.ring, lane, 0, i);
 #pragma unroll
         for (int w = 0; w < 8; ++w)
-            weight_word<FMT>(op, w / 4, 0, w % 4, op.b);
+            weight_word<FMT, MS>(op, w / 4, 0, w % 4, op.b);
         int slot = 0, t = 0;
         if (!SWIDE && (ns & 2)) {  // (then ns is 6 at least: the tail follows)
-            step<FMT, SWIDE, 0, false>(c, 0, slot, op, acc);
-            step<FMT, SWIDE, 1, false>(c, 1, slot, op, acc);
+            step<FMT, MS, SWIDE, 0, false>(c, 0, slot, op, acc);
+            step<FMT, MS, SWIDE, 1, false>(c, 1, slot, op, acc);
             t = 2;
         }
 #pragma unroll 1
         for (; t + 4 < ns; t += 4) {
-            step<FMT, SWIDE, 0, false>(c, t, slot, op, acc);
-            step<FMT, SWIDE, 1, false>(c, t + 1, slot, op, acc);
-            step<FMT, SWIDE, 2, false>(c, t + 2, slot, op, acc);
-            step<FMT, SWIDE, 3, false>(c, t + 3, slot, op, acc);
+            step<FMT, MS, SWIDE, 0, false>(c, t, slot, op, acc);
+            step<FMT, MS, SWIDE, 1, false>(c, t + 1, slot, op, acc);
+            step<FMT, MS, SWIDE, 2, false>(c, t + 2, slot, op, acc);
+            step<FMT, MS, SWIDE, 3, false>(c, t + 3, slot, op, acc);
         }
-        step<FMT, SWIDE, 0, true>(c, t, slot, op, acc);
-        step<FMT, SWIDE, 1, true>(c, t + 1, slot, op, acc);
-        step<FMT, SWIDE, 2, true>(c, t + 2, slot, op, acc);
-        step<FMT, SWIDE, 3, true>(c, t + 3, slot, op, acc);
+        step<FMT, MS, SWIDE, 0, true>(c, t, slot, op, acc);
+        step<FMT, MS, SWIDE, 1, true>(c, t + 1, slot, op, acc);
+        step<FMT, MS, SWIDE, 2, true>(c, t + 2, slot, op, acc);
+        step<FMT, MS, SWIDE, 3, true>(c, t + 3, slot, op, acc);
     }
     __syncthreads();  // the ring is free: the 32 x 32 tiles turn through patches of it
 
@@ -475,10 +476,10 @@ __global__ __launch_bounds__(256) void split3_kernel(const float *__restrict__ X
 
 }  // namespace
 
-int64_t tile_tiles(int64_t M, int64_t N, bool gated)
+static int64_t tile_tiles(int rows, int64_t M, int64_t N, bool gated)
 {
     const int cols = gated ? BN / 2 : BN;
-    return (M + BM - 1) / BM * ((N + cols - 1) / cols);
+    return (M + rows - 1) / rows * ((N + cols - 1) / cols);
 }
 
 // scales in 16-byte chunks: whole groups in a row, 16-byte aligned
@@ -491,17 +492,39 @@ static bool scales_wide(int fmt, int64_t K, const void *scales0, const void *sca
 // (four steps at least: the loop's last round)
 bool tile_takes(int64_t K) { return K >= 224 && K < ((int64_t)1 << 22); }
 
-// A 64-k step of a tile takes 0.64 us while few CUs work and 0.88 when most do (what
-// a CU gets of the caches' bandwidth and the clock), two on a CU 0.9 each; q4 and
-// int8, with twice the matrix instructions, 1.45 to 1.87.
-double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus)
+// us of tiles of 128 and 64 rows: fixed; of a 64-k step where a tile has its CU to
+// itself (latency, and rising with the share of the CUs that work), and per tile of a
+// CU that several share.  Products with MXFP4 weights, gated pairs of MXFP4, and of q4
+// and int8 (twice the matrix instructions).  Measured, 64 / 128 rows: product 6144 x
+// 1536 at 512 rows 14.6 / 21.2, at 768 22.3 / 21.8, 1536 x 6144 at 2048 46.0 / 67.9,
+// fp32 there 262 / 397; pairs 6144 x 1536 at 256 rows 17.1 / 25.8, at 2048 78.5 / 70.9,
+// q4 at 256 rows 32.5 / 44.6, at 512 54.4 / 47.4.
+struct TileRate {
+    double fixed, alone, rise, shared;
+};
+constexpr TileRate TILE_RATES[3][2] = {{{5.2, 0.63, 0.08, 0.88}, {4.5, 0.38, 0.06, 0.49}},
+                                       {{10.0, 0.62, 0.16, 0.86}, {7.0, 0.36, 0.09, 0.50}},
+                                       {{10.0, 1.42, 0.30, 1.82}, {7.0, 0.96, 0.10, 1.14}}};
+
+double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus, int *rows)
 {
-    const bool mx = fmt == QL_FMT_MXFP4;
-    const double r = (double)tile_tiles(M, N, gated) / cus, up = std::ceil(r);
-    const double step = r <= 1.0 ? (mx ? 0.64 : 1.45) + (mx ? 0.24 : 0.4) * std::min(1.0, r / 0.75)
-                                 : (mx ? 0.9 : 1.87) * (r + 0.4 * (up - r));
-    return 5.2 + (double)((K + 63) / 64) * (xf32 ? 3 : 1) * step +
-           (xf32 ? 2.0 + 10.0 * (double)M * (double)K / 5e6 : 0.0);
+    const double steps = (double)((K + 63) / 64) * (xf32 ? 3 : 1);
+    double best = 1e30;
+    for (int h = 0; h < 2; ++h) {
+        const TileRate &t = TILE_RATES[!gated ? 0 : fmt == QL_FMT_MXFP4 ? 1 : 2][h];
+        const int tile = h ? 64 : 128;
+        const int64_t tiles = tile_tiles(tile, M, N, gated);
+        if (tiles > MAX_WORKGROUPS)
+            continue;
+        const double r = (double)tiles / cus, up = std::ceil(r);
+        const double us = t.fixed + steps * (r <= 1.0 ? t.alone + t.rise * r
+                                                      : t.shared * (r + 0.4 * (up - r)));
+        if (us < best) {
+            best = us;
+            *rows = tile;
+        }
+    }
+    return best + (xf32 ? 2.0 + 10.0 * (double)M * (double)K / 5e6 : 0.0);
 }
 
 hipError_t launch_split3(const float *X, int64_t count, uint16_t *planes, hipStream_t stream)
@@ -515,13 +538,18 @@ hipError_t launch_split3(const float *X, int64_t count, uint16_t *planes, hipStr
 hipError_t launch_qgemm_tile(int fmt, const TileArgs &a, hipStream_t stream)
 {
     const bool gated = a.codes[1] != nullptr;
-    const dim3 grid((unsigned)tile_tiles(a.M, a.N, gated)), block(THREADS);
+    const dim3 grid((unsigned)tile_tiles(a.rows, a.M, a.N, gated)), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
     const bool swide = scales_wide(fmt, a.K, a.scales[0], a.scales[1]);
     auto with = [&](auto fmtc, auto gatedc, auto epic) {
         constexpr int F = decltype(fmtc)::value;
         constexpr bool GD = decltype(gatedc)::value, E = decltype(epic)::value;
-        swide ? go(qgemm_tile_kernel<F, GD, true, E>) : go(qgemm_tile_kernel<F, GD, false, E>);
+        if (a.rows == 64)
+            swide ? go(qgemm_tile_kernel<F, 2, GD, true, E>)
+                  : go(qgemm_tile_kernel<F, 2, GD, false, E>);
+        else
+            swide ? go(qgemm_tile_kernel<F, 4, GD, true, E>)
+                  : go(qgemm_tile_kernel<F, 4, GD, false, E>);
     };
     using Mx = std::integral_constant<int, QL_FMT_MXFP4>;
     if (!gated && !strip_plain(a.ep))

@@ -1256,7 +1256,7 @@ GroupPath choose_path(const ql_linear_ep *const *ls, int n, int forced, KgPlan &
     return tall && all_wide ? GroupPath::WIDE : GroupPath::TILED;
 }
 
-constexpr int64_t PLANES_BYTES = (int64_t)64 << 20;
+constexpr int64_t PLANES_BYTES = (int64_t)120 << 20;  // (fits the static scratch)
 
 // rows of fp32 activations that launch_mx splits into planes at a time: all, or whole
 // tiles' rows that PLANES_BYTES hold
@@ -1298,12 +1298,11 @@ int launch_mx(const ql_linear_ep *const *ls, int n, WsSource &wsrc, hipStream_t 
             t.M = (int)l.M;
             t.N = (int)l.N;
             t.K = (int)l.K;
+            t.rows = shape;
             if (xf32) {
                 t.planes = 3;
                 bytes = std::max(bytes, (size_t)(plane_rows(l.M, l.K) * l.K * 6));
             }
-            if (tile_tiles(l.M, l.N, false) > MAX_WORKGROUPS)
-                return QL_ERR_UNSUPPORTED;
             continue;
         }
         RowsGroup &g = kernel == ROWS_KGM ? kgm : any;

@@ -169,16 +169,16 @@ __device__ inline void strip_gated(const GateArgs &t, int M, int N, int m0, int 
         load_dh(m0 + rl);
 #pragma unroll 1
     for (int i = 0; i < MS; ++i) {
-        static_assert(MS == 4, "row blocks");
+        static_assert(MS == 2 || MS == 4, "row blocks");
         const int mb = m0 + 32 * i + rl;
         if (i == 0)
             put(std::integral_constant<int, 0>{});
-        else if (i == 1)
+        else if (MS == 2 || i == 1)
             put(std::integral_constant<int, 1>{});
         else if (i == 2)
-            put(std::integral_constant<int, 2>{});
+            put(std::integral_constant<int, MS - 2>{});
         else
-            put(std::integral_constant<int, 3>{});
+            put(std::integral_constant<int, MS - 1>{});
         auto pair = [&](int u, float(&g)[4], float(&v)[4]) {
             const float *const p = patch + (8 * u + rl) * 64 + 4 * (lane & 7);
 #pragma unroll

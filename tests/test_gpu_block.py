@@ -298,16 +298,16 @@ def test_mx_groups_of_many_rows(gpu):
     K = 2048
     codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((520, K)).astype(np.float32) * 0.05)
     c, s = dev(torch, codes), dev(torch, scales)
-    big = rng.standard_normal((6000, K)).astype(np.float32)
+    big = rng.standard_normal((10500, K)).astype(np.float32)
     tall, few = big[:300], big[:1]
-    resid = dev(torch, rng.standard_normal((6000, 520)).astype(np.float32))
-    copy = torch.empty((6000, 520), dtype=torch.bfloat16, device="cuda")
-    rows = [0, 127, 128, 4999, 5375, 5376, 5377, 5503, 5504, 5999]
+    resid = dev(torch, rng.standard_normal((10500, 520)).astype(np.float32))
+    copy = torch.empty((10500, 520), dtype=torch.bfloat16, device="cuda")
+    rows = [0, 127, 128, 4999, 10239, 10240, 10241, 10303, 10304, 10499]
     bigd, talld = dev(torch, big), dev(torch, tall)
     f = lambda X, N, Y, r=None, y=None: (ql.FMT_MXFP4, X, c[:N], s[:N], N, Y, None, ql.ACT_NONE,
                                          r, None, y)
     new = lambda M, N, dt=torch.float32: torch.empty((M, N), dtype=dt, device="cuda")
-    ents = [f(bigd, 520, new(6000, 520), resid, copy), f(dev(torch, few), 100, new(1, 100)),
+    ents = [f(bigd, 520, new(10500, 520), resid, copy), f(dev(torch, few), 100, new(1, 100)),
             f(talld, 520, new(300, 520)), f(talld, 516, new(300, 516, torch.bfloat16)),
             f(dev(torch, few).to(torch.bfloat16), 520, new(1, 520)),
             f(dev(torch, tall).to(torch.bfloat16), 520, new(300, 520))]
