@@ -93,6 +93,11 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
                                      : launch_qgemm_rows(g.fmt, false, r, stream));
 }
 
+// gemm_dx's costs by planes (MXFP4; q4, int8) and rows of a tile (128, 64).  Measured,
+// us of dX in 128 / 64 rows, N = 2752, K = 1024: MXFP4 107 rows 20.2 / 18.1, 400 rows 26.0
+// / 24.8; q4 107 rows 25.2 / 23.6, 400 rows 32.2 / 35.0.
+constexpr GemmCost DX_COST[2][2] = {{{0.55, 0.55}, {0.45, 0.40}}, {{1.0, 1.0}, {0.87, 0.87}}};
+
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 }  // namespace
@@ -229,11 +234,13 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         return QL_ERR_ALIGN;
     const int cus = current_cus();
     const bool want_x = d->dX && M > 0;
-    // workspace: both weights in bf16 (q4, int8: two planes each), then the larger of the products' partial
-    // sums (the products run one after the other)
+    // workspace: both weights in bf16 (q4, int8: two planes each) where dX is not formed
+    // from the compressed ones, then the larger of the products' partial sums (the
+    // products run one after the other)
     constexpr size_t PART_BYTES = (size_t)256 << 20;
-    auto parts = [&](int64_t R, int64_t S, int64_t C, int problems, GemmCost cost) {
-        const int p = gemm_parts(gemm_tiles(R, S) * problems, R * problems, S, C, cost, cus);
+    auto parts = [&](int rows, int64_t R, int64_t S, int64_t C, int problems, GemmCost cost,
+                     double *us = nullptr) {
+        const int p = gemm_parts(gemm_tiles(rows, R, S) * problems, R * problems, S, C, cost, cus, us);
         const size_t one = (size_t)problems * R * S * 4;
         return (int)std::max<int64_t>(1, std::min<int64_t>(p, (int64_t)(PART_BYTES / one)));
     };
@@ -242,16 +249,25 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
     // a bf16 copy (us of dX at N = 4096, mxfp4 / q4: 128 rows of K = 1536 21.9 / 27.8
     // against 28.8 / 36.0, 1024 rows of K = 2048 61.6 / 89.2 against 58.2 / 90.6)
     const bool direct = M <= 512 && dx_takes(K, g->gate_scales, g->up_scales);
-    const int px = !want_x  ? 1
-                   : direct ? parts(M, K, 2 * N, 1, planes == 1 ? GemmCost{0.64, 0.45} : GemmCost{1.2, 1.2})
-                            : parts(M, K, 2 * planes * N, 1, GemmCost{0.5, 0.43});
-    const int pw = d->dWg ? parts(N, K, M, 2, GemmCost{0.5, 0.43}) : 1;
+    int px = 1, xrows = 128;
+    if (want_x && direct) {
+        // tiles of 128 or 64 rows
+        double us[2];
+        const int p128 = parts(128, M, K, 2 * N, 1, DX_COST[planes - 1][0], &us[0]);
+        const int p64 = parts(64, M, K, 2 * N, 1, DX_COST[planes - 1][1], &us[1]);
+        const bool small = us[1] < us[0];
+        xrows = small ? 64 : 128;
+        px = small ? p64 : p128;
+    } else if (want_x) {
+        px = parts(128, M, K, 2 * planes * N, 1, GemmCost{0.5, 0.43});
+    }
+    const int pw = d->dWg ? parts(128, N, K, M, 2, GemmCost{0.5, 0.43}) : 1;
     const size_t plane = want_x && !direct ? round256((size_t)N * K * 2) : 0;
     const size_t wbytes = 2 * planes * plane;
     const size_t part_bytes = std::max(px > 1 ? (size_t)px * M * K * 4 : 0,
                                        pw > 1 ? (size_t)pw * 2 * N * K * 4 : 0);
-    if ((want_x && gemm_tiles(M, K) * px > MAX_WORKGROUPS) ||
-        (d->dWg && gemm_tiles(N, K) * 2 * pw > MAX_WORKGROUPS))
+    if ((want_x && gemm_tiles(xrows, M, K) * px > MAX_WORKGROUPS) ||
+        (d->dWg && gemm_tiles(128, N, K) * 2 * pw > MAX_WORKGROUPS))
         return QL_ERR_UNSUPPORTED;
     uint8_t *ws = nullptr;
     bool own = false;
@@ -282,7 +298,7 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         const DxArgs a{{d->dG, d->dU},
                        {(const uint8_t *)g->gate_codes, (const uint8_t *)g->up_codes},
                        {g->gate_scales, g->up_scales},
-                       (int)M, (int)N, (int)K, px, part, d->dX, d->dxdt == QL_DT_BF16};
+                       (int)M, (int)N, (int)K, px, part, d->dX, d->dxdt == QL_DT_BF16, xrows};
         s = status(launch_gemm_dx(g->fmt, a, stream));
         void *const out[1] = {d->dX};
         if (s == QL_OK && px > 1)

@@ -24,6 +24,11 @@
 //
 // Few tiles: the reduction is cut into parts whose fp32 sums another launch
 // adds in order (split_sum_kernel).
+//
+// Bound: the matrix cores at the power limit's clock while two workgroups share a CU,
+// then the tail.  2048 rows, N = 4096, K = 1536 (51.5 Gflop each): dX 56 us in 5 parts
+// (480 workgroups) and 15 us for their sum, dW 59 us (384 workgroups on 512 places, a
+// quarter of them idle).
 #include <algorithm>
 
 #include "dma.h"
@@ -314,15 +319,19 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const uint16_t *dG, co
 
 }  // namespace
 
-int64_t gemm_tiles(int64_t R, int64_t S) { return (R + BM - 1) / BM * ((S + BN - 1) / BN); }
+int64_t gemm_tiles(int rows, int64_t R, int64_t S)
+{
+    return (R + rows - 1) / rows * ((S + BN - 1) / BN);
+}
 
-int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, int cus)
+int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, int cus,
+               double *best_us)
 {
     // a part more costs a sum's round trip through memory at 5 TB/s, and the first
     // one the sum's launch
     const int64_t steps = (C + BC - 1) / BC;
     int best = 1;
-    double us = 0.0;
+    double us = 0.0;  // (of the best so far)
     for (int p = 1; p <= 32 && p * 8 <= std::max<int64_t>(8, steps); ++p) {
         const int64_t rounds = (tiles * p + cus - 1) / cus;
         const double stage = rounds == 1 ? cost.alone_us : rounds * cost.shared_us;
@@ -333,12 +342,14 @@ int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, in
             us = t;
         }
     }
+    if (best_us)
+        *best_us = us;
     return best;
 }
 
 hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream)
 {
-    const int64_t wgs = gemm_tiles(a.R, a.S) * problems * a.parts;
+    const int64_t wgs = gemm_tiles(BM, a.R, a.S) * problems * a.parts;
     const dim3 grid((unsigned)wgs), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
     if (wgs <= current_cus())

@@ -11,17 +11,21 @@
 // rows of one column each).  Matrix instruction v_mfma_f32_32x32x16_bf16 as in
 // gemm_bf16.hip.
 //
-// Tile: 4 wavefronts compute 128 x 256, each a strip of 64 columns.  A stage is 32
-// weight rows: dG's 128 x 32 and the codes move directly to LDS (as do scale
+// Tile: 4 wavefronts compute 128 x 256, or 64 x 256 where tiles are few, each a strip of
+// 64 columns.  A stage is 32 weight rows: dG's 128 x 32 and the codes move directly to LDS (as do scale
 // dwords), and each thread converts one scale block of 32 codes, which it loaded
 // itself, a share behind every MFMA of a stage's first 16-n chunk, into the other
 // of two weight tiles; the barrier before the second chunk hands it over.  As codes
 // the weights are 4 KB of a stage's 12 instead of 16 of 24: what bounds these
-// products is the traffic into LDS (about 42 KB per us and CU).  One workgroup per
-// CU, with as many stages in flight as LDS holds.
+// products is the traffic into LDS (about 42 KB per us and CU).  MXFP4 two workgroups
+// per CU, q4 and int8 one, with as many stages in flight as LDS holds.
 //
 // Few tiles: the reduction is cut into parts whose fp32 sums another launch
 // adds in order (split_sum_kernel).
+//
+// Bound: the latency of a stage (0.45 to 1.0 us by format and tile, a quarter of it on
+// the matrix cores) while a CU has one workgroup, and the sum's launch: q4, 107 rows, N
+// = 2752, K = 1024 (1.2 Gflop): 23.6 us with the sum's 4.6.
 #include <algorithm>
 
 #include "dma.h"
@@ -39,19 +43,22 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-constexpr int BM = 128, BN = 256, BC = 32;
-constexpr int MS = 4, NS = 2;  // MFMA tiles of a wavefront
-constexpr int GROUP_M = 4;
+constexpr int BN = 256, BC = 32;
+constexpr int NS = 2;  // MFMA tiles of a wavefront across
 
 template <int FMT>
+constexpr int WGS = FMT == QL_FMT_MXFP4 ? 2 : 1;  // workgroups per CU
+
+// MS: blocks of 32 rows of the tile.
+template <int FMT, int MS>
 struct Geo {
+    static constexpr int BM = 32 * MS;
     static constexpr int PLANES = FMT == QL_FMT_MXFP4 ? 1 : 2;
     static constexpr int CODES = FMT == QL_FMT_INT8 ? 32 : 16;  // bytes of a block's codes
     static constexpr int ABYTES = BM * BC * 2, CBYTES = THREADS * CODES, SBYTES = THREADS * 4;
     static constexpr int STAGE = ABYTES + CBYTES + SBYTES;
     static constexpr int BTILE = BC * BN * 2;  // a plane of a converted stage
-    static constexpr int WGS = PLANES == 1 ? 2 : 1;  // workgroups per CU
-    static constexpr int NST = (160 * 1024 / WGS - 2 * PLANES * BTILE) / STAGE;
+    static constexpr int NST = (160 * 1024 / WGS<FMT> - 2 * PLANES * BTILE) / STAGE;
     static constexpr int LDS = NST * STAGE + 2 * PLANES * BTILE;
     static constexpr int ALOADS = ABYTES / 16 / THREADS, CLOADS = CODES / 16;
     static constexpr int LOADS = ALOADS + CLOADS + 1;
@@ -119,7 +126,7 @@ struct Ctx {
 // A thread's block of codes of one stage and its scale (a row past the last: zeros).
 template <int FMT>
 struct Raw {
-    uint32_t c[Geo<FMT>::CODES / 4];
+    uint32_t c[(FMT == QL_FMT_INT8 ? 32 : 16) / 4];
     float s;
 };
 
@@ -129,15 +136,15 @@ __device__ inline void start_segment(const DxArgs &a, Ctx &c, int m0, int k0)
     c.A = reinterpret_cast<const uint8_t *>(a.d[c.seg] + (int64_t)m0 * a.N + c.c0);
     // (blocks past K repeat the row's last one: those columns are not stored)
     const int b = min(k0 / 32 + c.blk, a.K / 32 - 1);
-    c.codes = a.codes[c.seg] + (int64_t)b * Geo<FMT>::CODES;
+    c.codes = a.codes[c.seg] + (int64_t)b * (FMT == QL_FMT_INT8 ? 32 : 16);
     c.scales = static_cast<const uint8_t *>(a.scales[c.seg]) +
                (FMT == QL_FMT_MXFP4 ? b & ~3 : 2 * (b & ~1));
 }
 
-template <int FMT>
+template <int FMT, int MS>
 __device__ inline void issue(const DxArgs &a, Ctx &c, int m0, int k0, int slot)
 {
-    using G = Geo<FMT>;
+    using G = Geo<FMT, MS>;
     const uint32_t base = dma_lds(c.ring + slot * G::STAGE);
     if (c.c0 + BC <= a.N) {
 #pragma unroll
@@ -168,10 +175,10 @@ __device__ inline void issue(const DxArgs &a, Ctx &c, int m0, int k0, int slot)
 // step s of the whole reduction: first weight row in its projection
 __device__ inline int first_row(int s, int seg_steps) { return (s >= seg_steps ? s - seg_steps : s) * BC; }
 
-template <int FMT>
+template <int FMT, int MS>
 __device__ inline void read_raw(const Ctx &c, const uint8_t *st, int b, int n0, int N, Raw<FMT> &r)
 {
-    using G = Geo<FMT>;
+    using G = Geo<FMT, MS>;
     const int tid = c.wave * 64 + c.lane;
     const bool in = n0 + c.row < N;
 #pragma unroll
@@ -196,11 +203,11 @@ __device__ inline uint32_t w_at(const Ctx &c, int w)
     return (uint32_t)(c.row * (BN * 2) + (chunk ^ bswz(c.row, chunk)) * 16);
 }
 
-template <int FMT>
-__global__ __launch_bounds__(THREADS, Geo<FMT>::WGS) void gemm_dx_kernel(const DxArgs a)
+template <int FMT, int MS>
+__global__ __launch_bounds__(THREADS, WGS<FMT>) void gemm_dx_kernel(const DxArgs a)
 {
-    using G = Geo<FMT>;
-    constexpr int NST = G::NST, P = G::PLANES, KK = MS * NS * P;
+    using G = Geo<FMT, MS>;
+    constexpr int NST = G::NST, P = G::PLANES, KK = MS * NS * P, BM = G::BM, GROUP_M = 16 / MS;
     __shared__ __align__(16) uint8_t lds[G::LDS];
     const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.K + BN - 1) / BN;
     // each XCD takes a contiguous range of the tiles, in groups of 4 row tiles
@@ -249,13 +256,13 @@ __global__ __launch_bounds__(THREADS, Geo<FMT>::WGS) void gemm_dx_kernel(const D
         start_segment<FMT>(a, c, m0, k0);
 #pragma unroll 1
         for (int t = 0; t < NST && t < ns; ++t)
-            issue<FMT>(a, c, m0, k0, t);
+            issue<FMT, MS>(a, c, m0, k0, t);
 
         // stage 0 converted, its first chunk's fragments and stage 1's codes in
         // registers
         Raw<FMT> raw;
         dma_wait<G::LOADS, NST - 1>(min(ns, NST) - 1);
-        read_raw<FMT>(c, c.ring, blk, first_row(s0, seg_steps), a.N, raw);
+        read_raw<FMT, MS>(c, c.ring, blk, first_row(s0, seg_steps), a.N, raw);
         uint32_t wat[4], aat[2], bat[NS];
 #pragma unroll
         for (int w = 0; w < 4; ++w)
@@ -282,7 +289,7 @@ __global__ __launch_bounds__(THREADS, Geo<FMT>::WGS) void gemm_dx_kernel(const D
         }
         if (ns > 1) {
             dma_wait<G::LOADS, NST - 2>(min(ns, NST) - 2);
-            read_raw<FMT>(c, c.ring + G::STAGE, blk, first_row(s0 + 1, seg_steps), a.N, raw);
+            read_raw<FMT, MS>(c, c.ring + G::STAGE, blk, first_row(s0 + 1, seg_steps), a.N, raw);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -346,13 +353,13 @@ __global__ __launch_bounds__(THREADS, Geo<FMT>::WGS) void gemm_dx_kernel(const D
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (t + NST < ns)
-                issue<FMT>(a, c, m0, k0, slot);
+                issue<FMT, MS>(a, c, m0, k0, slot);
             // stage t + 2 has landed where only those younger are in flight
             if (t + NST < ns)
                 __builtin_amdgcn_s_waitcnt(dma_vmcnt((NST - 2) * G::LOADS));
             else if (t + 2 < ns)
                 dma_wait<G::LOADS, NST - 2>(ns - 3 - t);
-            read_raw<FMT>(c, c.ring + slot2 * G::STAGE, blk, first_row(s0 + t + 2, seg_steps), a.N,
+            read_raw<FMT, MS>(c, c.ring + slot2 * G::STAGE, blk, first_row(s0 + t + 2, seg_steps), a.N,
                           raw);
             // chunk 1; behind its MFMAs stage t + 1's first fragments
             bf16x8 a0[MS], b0[P][NS];
@@ -404,13 +411,18 @@ bool dx_takes(int64_t K, const void *scales0, const void *scales1)
 
 hipError_t launch_gemm_dx(int fmt, const DxArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(gemm_tiles(a.M, a.K) * a.parts)), block(THREADS);
+    const dim3 grid((unsigned)(gemm_tiles(a.rows, a.M, a.K) * a.parts)), block(THREADS);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+    auto with = [&](auto fmtc) {
+        constexpr int F = decltype(fmtc)::value;
+        a.rows == 64 ? go(gemm_dx_kernel<F, 2>) : go(gemm_dx_kernel<F, 4>);
+    };
     if (fmt == QL_FMT_MXFP4)
-        hipLaunchKernelGGL(gemm_dx_kernel<QL_FMT_MXFP4>, grid, block, 0, stream, a);
+        with(std::integral_constant<int, QL_FMT_MXFP4>{});
     else if (fmt == QL_FMT_Q4)
-        hipLaunchKernelGGL(gemm_dx_kernel<QL_FMT_Q4>, grid, block, 0, stream, a);
+        with(std::integral_constant<int, QL_FMT_Q4>{});
     else
-        hipLaunchKernelGGL(gemm_dx_kernel<QL_FMT_INT8>, grid, block, 0, stream, a);
+        with(std::integral_constant<int, QL_FMT_INT8>{});
     return hipGetLastError();
 }
 

@@ -368,14 +368,15 @@ struct GemmArgs {
     void *out[2];
     int outbf16;
 };
-int64_t gemm_tiles(int64_t R, int64_t S);
+int64_t gemm_tiles(int rows, int64_t R, int64_t S);  // tiles of `rows` rows
 // parts of the reduction C estimated to be fastest, for `tiles` tiles and R * S
 // outputs in all; us that a stage of 32 takes a workgroup alone on its CU, and each
 // workgroup's share where a CU has several
 struct GemmCost {
     double alone_us, shared_us;
 };
-int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, int cus);
+int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, int cus,
+               double *us = nullptr);
 hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream);
 // dX of a gated pair from the compressed weights (gemm_dx.hip): d = {dG, dU} bf16
 // [M][N], N % 8 == 0, K % 128 == 0, scales 4-byte aligned (dx_takes); parts > 1:
@@ -389,6 +390,7 @@ struct DxArgs {
     float *part;
     void *out;
     int outbf16;
+    int rows;  // of a tile: 128 or 64
 };
 bool dx_takes(int64_t K, const void *scales0, const void *scales1);
 hipError_t launch_gemm_dx(int fmt, const DxArgs &a, hipStream_t stream);

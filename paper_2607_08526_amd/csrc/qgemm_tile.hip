@@ -33,6 +33,13 @@
 // otherwise each by itself with its step (a memory request each: as many as the
 // codes).  Steps that K leaves unfilled, and those that fill up the loop's rounds,
 // come from a page of zeros.
+//
+// Bound: the matrix cores at the clock that the power limit leaves (0.44 to 0.48 of
+// all cycles busy), and at the end of a tile, where every CU is there at once, the
+// VALU of the activation and the stores.  2048 rows x 8192 x 2048 with GELU, bf16
+// output: 65 to 67 us, 1.03 to 1.06 PFLOP/s (a library product of 8192^3 bf16 1.5);
+// gated pair 2048 x 5504 x 2048 with SiLU: 80 to 84 us, 1.10 to 1.16 PFLOP/s, 688
+// tiles on 512 places.
 #include <algorithm>
 #include <cmath>
 
@@ -497,7 +504,7 @@ bool tile_takes(int64_t K) { return K >= 224 && K < ((int64_t)1 << 22); }
 // CU that several share.  Products with MXFP4 weights, gated pairs of MXFP4, and of q4
 // and int8 (twice the matrix instructions).  Measured, 64 / 128 rows: product 6144 x
 // 1536 at 512 rows 14.6 / 21.2, at 768 22.3 / 21.8, 1536 x 6144 at 2048 46.0 / 67.9,
-// fp32 there 262 / 397; pairs 6144 x 1536 at 256 rows 17.1 / 25.8, at 2048 78.5 / 70.9,
+// fp32 at 1536 140 / 206; pairs 6144 x 1536 at 256 rows 17.1 / 25.8, at 2048 78.5 / 70.9,
 // q4 at 256 rows 32.5 / 44.6, at 512 54.4 / 47.4.
 struct TileRate {
     double fixed, alone, rise, shared;
