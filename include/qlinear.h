@@ -101,8 +101,11 @@
  *     stream or replays of other graphs captured on it.  A call under
  *     capture that needs more than its stream's buffer allocates for itself
  *     from the pool (allocation and free nodes in the graph) instead.  A
- *     destroyed stream's handle value, if reused, inherits its buffer.  No
- *     other forward path uses device memory beyond its arguments.
+ *     destroyed stream's handle value, if reused, inherits its buffer.  fp32
+ *     activations of large MXFP4 products (QL_FMT_MXFP4) take up to 120 MiB
+ *     for three bf16 planes of a slice of their rows (768 K bytes where 128
+ *     rows are more than that).  No other forward path uses device memory
+ *     beyond its arguments.
  *     Allocation failure returns QL_ERR_HIP.
  */
 #ifndef QLINEAR_H

@@ -102,7 +102,8 @@ typedef struct {
 
 /* No output may alias an input or another output.  N % 8 == 0 and K % 32 == 0;
  * M == 0 writes zeros to dW and db and nothing else.  Workspace (per stream, as
- * in qlinear.h): for dX the weights in bf16 (4 N K bytes; q4, int8: 8), and fp32
+ * in qlinear.h): for dX above 512 rows, or where K % 128 != 0 or a scale tensor is
+ * not 4-byte aligned, the weights in bf16 (4 N K bytes; q4, int8: 8), and fp32
  * partial sums where few tiles make the products split their reductions (at most
  * 256 MiB).
  * Sizes: M, N, K < 2^22 and M, N times K < 2^40 (QL_ERR_UNSUPPORTED otherwise).
