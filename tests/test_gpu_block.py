@@ -175,7 +175,7 @@ SHAPES = [(1, 1, 32), (1, 200, 96), (3, 33, 64), (8, 2000, 128), (16, 1000, 160)
           (520, 2052, 128), (1100, 2064, 640), (1100, 4100, 256), (1100, 4099, 384),
           (1100, 4100, 512), (1030, 4100, 1152), (1030, 4102, 1536), (130, 1000, 416),
           (300, 2050, 1056), (1100, 4100, 224), (1100, 4100, 288), (1030, 4100, 1056),
-          (1030, 4098, 864)]
+          (1030, 4098, 864), (1900, 4092, 512), (1900, 4090, 544)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -226,7 +226,8 @@ def test_mx_extreme_activations(gpu):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 100, 64), (40, 258, 96), (40, 260, 128), (200, 264, 512),
-                                   (700, 512, 256), (1100, 4100, 256), (1100, 4098, 512)])
+                                   (700, 512, 256), (1100, 4100, 256), (1100, 4098, 512),
+                                   (1900, 4092, 512), (1900, 4090, 544)])
 @pytest.mark.parametrize("mx", [False, True])
 def test_mx_epilogue(gpu, M, N, K, mx):
     """Bias, GELU, residual, steering, bf16 outputs and copies."""
@@ -379,7 +380,8 @@ GATED = [(1, 8, 32), (1, 1000, 96), (5, 17, 64), (16, 130, 1056), (33, 64, 160),
          (65, 500, 128), (129, 264, 512), (260, 128, 1536), (700, 640, 384), (9, 40, 4096),
          (20, 1000, 128), (130, 1032, 384), (260, 2048, 256), (1100, 2056, 256), (1100, 2050, 384),
          (1100, 2056, 512), (1030, 2056, 1152), (130, 1032, 416), (1100, 2056, 224),
-         (1100, 2056, 288), (1030, 2056, 1056)]
+         (1100, 2056, 288), (1030, 2056, 1056), (1900, 2042, 1536), (1900, 2040, 1568),
+         (7, 72, 2080), (400, 2048, 1024), (260, 136, 16384)]
 
 
 def gated_case(torch, fmt, M, N, K, seed, bias):
@@ -834,3 +836,104 @@ def test_captured_without_workspace(gpu):
         torch.cuda.synchronize()
         for a, b in zip(got[:5], want[:5]):
             assert torch.equal(a, b)
+
+
+def test_two_graphs_on_one_stream(gpu):
+    """Two graphs captured on a stream share its workspace; replayed one after the
+    other, with a larger call on the stream between, each gives its own results."""
+    torch, ql = gpu
+    cases = []
+    for fmt, M, seed in (("q4", 40, 1), ("mxfp4", 130, 2)):
+        rng, Xb, _, pair, _, _, _ = gated_case(torch, fmt, M, 1024, 384, seed, False)
+        dH = dev(torch, rng.standard_normal((M, 1024)).astype(np.float32))
+        cases.append((fmts(ql)[fmt], Xb, *pair, dH))
+    call = lambda c: ql.gated_backward(*c, weight_grads=True)
+    want = [call(c) for c in cases]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for c in cases:
+            call(c)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for c in cases:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            outs.append(call(c))
+    _, Xb, _, pair, _, _, _ = gated_case(torch, "int8", 700, 2048, 1024, 3, False)
+    big = (ql.FMT_INT8, Xb, *pair, torch.randn((700, 2048), device="cuda"))
+    big_want = call(big)
+    for i in range(3):
+        for k in (0, 1):
+            for t in outs[k][:5]:
+                t.zero_()
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                graphs[k].replay()
+                got = call(big)
+            torch.cuda.synchronize()
+            for a, b in zip((*outs[k][:5], *got[:5]), (*want[k][:5], *big_want[:5])):
+                assert torch.equal(a, b), (i, k)
+
+
+def test_calls_at_once(gpu):
+    """Threads with a stream each, calling at once: the same bits as alone."""
+    import threading
+    torch, ql = gpu
+    cases = [block(torch, ql, seed=9, fmt=f, M=(1, 100 + 60 * i))
+             for i, f in enumerate((ql.FMT_MXFP4, ql.FMT_Q4, ql.FMT_INT8))]
+    want = [run_block(torch, ql, c) for c in cases]
+    torch.cuda.synchronize()
+    fails = []
+
+    def work(k):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got = run_block(torch, ql, cases[k])
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[k])):
+                    fails.append(k)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not fails
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 264, 96), (40, 264, 1056), (300, 2056, 1056),
+                                   (600, 4104, 288), (1100, 4104, 1056), (1100, 4104, 512)])
+def test_infinities_stay_in_their_rows(gpu, M, N, K):
+    """An infinity, a NaN and the largest bf16 in some rows leave every other row as it
+    was; a bf16 infinity times a weight is an infinity of the product's sign, or a NaN
+    for a weight of zero."""
+    torch, ql = gpu
+    rng = np.random.default_rng(M)
+    codes, scales, Wv = R.weight("mxfp4", rng.standard_normal((N, K)).astype(np.float32) * 0.05)
+    w = dev(torch, codes), dev(torch, scales)
+    q4 = tuple(dev(torch, t) for t in
+               R.weight("q4", rng.standard_normal((N, K)).astype(np.float32) * 0.05)[:2])
+    Xb, _ = bf16(torch, rng.standard_normal((M, K)))
+    bad = Xb.clone()
+    rows = [0, M // 2, M - 1]
+    bad[rows[0], K - 1] = float("inf")
+    bad[rows[1], 5] = float("nan")
+    bad[rows[2], 0] = torch.finfo(torch.bfloat16).max
+    rest = torch.ones(M, dtype=torch.bool, device="cuda")
+    rest[rows] = False
+    dH = torch.randn((M, N), device="cuda")
+    for f in (lambda X: ql.forward(ql.FMT_MXFP4, X, *w, N),
+              lambda X: ql.forward(ql.FMT_MXFP4, X.float(), *w, N),
+              lambda X: ql.forward_mx(*ql.quantize_act_mx(X), *w, N),
+              lambda X: ql.gated_forward(ql.FMT_MXFP4, X, w, w),
+              lambda X: ql.gated_forward(ql.FMT_Q4, X, q4, q4),
+              lambda X: ql.gated_backward(ql.FMT_MXFP4, X, w, w, dH).X,
+              lambda X: ql.gated_backward(ql.FMT_Q4, X, q4, q4, dH).X):
+        assert torch.equal(f(Xb)[rest], f(bad)[rest])
+    Y = host(ql.forward(ql.FMT_MXFP4, bad, *w, N))
+    with np.errstate(invalid="ignore"):
+        want = np.inf * Wv[:, K - 1]
+    np.testing.assert_array_equal(Y[rows[0]], want)
+    assert np.isnan(Y[rows[1]]).all()
