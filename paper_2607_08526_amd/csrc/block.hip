@@ -244,6 +244,17 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         const size_t one = (size_t)problems * R * S * 4;
         return (int)std::max<int64_t>(1, std::min<int64_t>(p, (int64_t)(PART_BYTES / one)));
     };
+    // tiles of 128 or 64 rows of the bf16 products (us, 2048 rows: dW of 2048 x 1024
+    // 38.4 / 27.0, of 4096 x 1536 56.7 / 59.5, of 5504 x 2048 100 / 112; dX of 1024 x 1024
+    // 32.1 / 29.5)
+    auto gemm_plan = [&](int64_t R, int64_t S, int64_t C, int problems, int &rows, int &p) {
+        double us[2];
+        p = parts(128, R, S, C, problems, GemmCost{0.47, 0.43}, &us[0]);
+        const int p64 = parts(64, R, S, C, problems, GemmCost{0.31, 0.28}, &us[1]);
+        rows = us[1] < us[0] ? 64 : 128;
+        if (rows == 64)
+            p = p64;
+    };
     const int planes = g->fmt == QL_FMT_MXFP4 ? 1 : 2;
     // dX straight from the compressed weights up to a few hundred rows, beyond from
     // a bf16 copy (us of dX at N = 4096, mxfp4 / q4: 128 rows of K = 1536 21.9 / 27.8
@@ -259,15 +270,17 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         xrows = small ? 64 : 128;
         px = small ? p64 : p128;
     } else if (want_x) {
-        px = parts(128, M, K, 2 * planes * N, 1, GemmCost{0.5, 0.43});
+        gemm_plan(M, K, 2 * planes * N, 1, xrows, px);
     }
-    const int pw = d->dWg ? parts(128, N, K, M, 2, GemmCost{0.5, 0.43}) : 1;
+    int pw = 1, wrows = 128;
+    if (d->dWg)
+        gemm_plan(N, K, M, 2, wrows, pw);
     const size_t plane = want_x && !direct ? round256((size_t)N * K * 2) : 0;
     const size_t wbytes = 2 * planes * plane;
     const size_t part_bytes = std::max(px > 1 ? (size_t)px * M * K * 4 : 0,
                                        pw > 1 ? (size_t)pw * 2 * N * K * 4 : 0);
     if ((want_x && gemm_tiles(xrows, M, K) * px > MAX_WORKGROUPS) ||
-        (d->dWg && gemm_tiles(128, N, K) * 2 * pw > MAX_WORKGROUPS))
+        (d->dWg && gemm_tiles(wrows, N, K) * 2 * pw > MAX_WORKGROUPS))
         return QL_ERR_UNSUPPORTED;
     uint8_t *ws = nullptr;
     bool own = false;
@@ -318,6 +331,7 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         a.C = (int)N;
         a.segs = 2 * planes;
         a.parts = px;
+        a.rows = xrows;
         a.part = part;
         a.out[0] = d->dX;
         a.outbf16 = d->dxdt == QL_DT_BF16;
@@ -344,6 +358,7 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         a.C = (int)M;
         a.segs = 1;
         a.parts = pw;
+        a.rows = wrows;
         a.part = part;
         a.out[0] = d->dWg;
         a.out[1] = d->dWu;

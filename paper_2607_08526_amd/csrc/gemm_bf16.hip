@@ -15,8 +15,9 @@
 // receive 4 rows of one column each), so neither needs a transposed copy.
 //
 // Tile: 4 wavefronts compute 128 x 256, each a strip of 64 columns (4 x 2 MFMA
-// tiles).  Direct-to-LDS loads fill a ring of stages of 32 c: three (72 KB, two
-// workgroups per CU), or six where there is no more than a workgroup for each CU.
+// tiles), or 64 x 256 where tiles are few (twice the wavefronts).  Direct-to-LDS loads
+// fill a ring of stages of 32 c: three (64 rows: four; two workgroups per CU), or six
+// where there is no more than a workgroup for each CU.
 // The barrier of a stage sits before its last 16-c chunk; behind every MFMA goes a
 // share of the next chunk's LDS reads.  Chunks of 16 bytes are XOR-swizzled
 // against bank conflicts.  Reductions that do not divide into whole stages end in
@@ -47,20 +48,28 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
-constexpr int BM = 128, BN = 256, BC = 32;
-constexpr int MS = 4, NS = 2;  // MFMA tiles of a wavefront
-constexpr int ABYTES = BM * BC * 2, BBYTES = BN * BC * 2, STAGE = ABYTES + BBYTES;
-constexpr int ALOADS = ABYTES / 16 / THREADS, BLOADS = BBYTES / 16 / THREADS;
-constexpr int LOADS = ALOADS + BLOADS;
-constexpr int GROUP_M = 4;
+constexpr int BN = 256, BC = 32;
+constexpr int NS = 2;  // MFMA tiles of a wavefront across
+constexpr int BBYTES = BN * BC * 2, BLOADS = BBYTES / 16 / THREADS;
+
+// MS: blocks of 32 rows of the tile.
+template <int MS>
+struct Geo {
+    static constexpr int BM = 32 * MS, ABYTES = BM * BC * 2, STAGE = ABYTES + BBYTES;
+    static constexpr int ALOADS = ABYTES / 16 / THREADS, LOADS = ALOADS + BLOADS;
+};
 
 __device__ __align__(16) const uint32_t zeros[4] = {0, 0, 0, 0};
 
 // swizzles of 16-byte chunks: rows of 4 chunks (reduction along the row; a cycle
 // of a 16-byte read serves rows 0-3, 12-15, 20-27, or the others of 32), and rows
-// of 16 or 32 (reduction over rows)
+// of 8, 16 or 32 (reduction over rows)
 __device__ inline int swz4(int row) { return ((row >> 2) & 3) ^ ((row >> 4) & 1) * 3; }
-__device__ inline int swzt(int row) { return (row & 3) << 2; }
+template <int LINES>
+__device__ inline int swzt(int row)
+{
+    return (row & 3) << (LINES == 64 ? 1 : 2);
+}
 
 // Where the chunk in slot i of an operand's stage comes from: its byte offset
 // in the matrix, from the tile's corner at (first line, first reduction index).
@@ -71,7 +80,7 @@ __device__ inline uint32_t chunk_at(int i, int lines, int64_t ld, int &c)
 {
     if constexpr (TR) {
         constexpr int CH = LINES / 8;
-        const int row = i / CH, lc = (i % CH) ^ swzt(row);
+        const int row = i / CH, lc = (i % CH) ^ swzt<LINES>(row);
         c = row;
         return (uint32_t)((row * ld + min(lc * 8, lines - 8)) * 2);
     } else {
@@ -90,7 +99,7 @@ __device__ inline bf16x8 fragment(const uint8_t *st, int line, int q, int lane)
         const int row = 16 * q + 8 * g + ((lane & 15) >> 2);
         const int unit = line / 4 + 4 * ((lane >> 4) & 1) + (lane & 3);  // of 4 lines, 8 bytes
         auto at = [&](int r) {
-            return st + r * (LINES * 2) + ((unit >> 1) ^ swzt(r)) * 16 + (unit & 1) * 8;
+            return st + r * (LINES * 2) + ((unit >> 1) ^ swzt<LINES>(r)) * 16 + (unit & 1) * 8;
         };
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (__attribute__((address_space(3))) s16x4 *)at(row));
@@ -107,18 +116,19 @@ __device__ inline bf16x8 fragment(const uint8_t *st, int line, int q, int lane)
 
 // What a lane needs of a tile, fixed for the whole reduction, and how far the
 // loads have come.
+template <int MS>
 struct Ctx {
     uint8_t *ring;
-    uint32_t aoff[ALOADS], boff[BLOADS];
-    int ac[ALOADS], bc[BLOADS];  // each chunk's first reduction index in its stage
+    uint32_t aoff[Geo<MS>::ALOADS], boff[BLOADS];
+    int ac[Geo<MS>::ALOADS], bc[BLOADS];  // each chunk's first reduction index in its stage
     const uint8_t *A, *B;        // of the next stage
     int64_t astep, bstep;        // from one stage to the next
     int seg, c0;                 // of the next stage
     int wave, lane;
 };
 
-template <bool TRA>
-__device__ inline void start_segment(const GemmArgs &a, Ctx &c, int prob, int m0, int n0)
+template <bool TRA, int MS>
+__device__ inline void start_segment(const GemmArgs &a, Ctx<MS> &c, int prob, int m0, int n0)
 {
     const bool many = a.segs > 1;
     c.A = reinterpret_cast<const uint8_t *>(a.A[many ? c.seg : prob] +
@@ -126,9 +136,10 @@ __device__ inline void start_segment(const GemmArgs &a, Ctx &c, int prob, int m0
     c.B = reinterpret_cast<const uint8_t *>(a.B[many ? c.seg : 0] + c.c0 * a.ldb + n0);
 }
 
-template <bool TRA>
-__device__ inline void issue(const GemmArgs &a, Ctx &c, int prob, int m0, int n0, int slot)
+template <bool TRA, int MS>
+__device__ inline void issue(const GemmArgs &a, Ctx<MS> &c, int prob, int m0, int n0, int slot)
 {
+    constexpr int ALOADS = Geo<MS>::ALOADS, ABYTES = Geo<MS>::ABYTES, STAGE = Geo<MS>::STAGE;
     const uint32_t base = dma_lds(c.ring + slot * STAGE) + c.wave * 1024;
     if (c.c0 + BC <= a.C) {
 #pragma unroll
@@ -153,16 +164,17 @@ __device__ inline void issue(const GemmArgs &a, Ctx &c, int prob, int m0, int n0
     if (c.c0 >= a.C && c.seg + 1 < a.segs) {
         ++c.seg;
         c.c0 = 0;
-        start_segment<TRA>(a, c, prob, m0, n0);
+        start_segment<TRA, MS>(a, c, prob, m0, n0);
     }
 }
 
 // The MFMAs of a 16-c chunk, and behind each, in a group that the compiler keeps
 // together, a share of the operands of chunk QN of stage nxt.
-template <bool TRA, int QN>
-__device__ inline void chunk(const Ctx &c, const uint8_t *nxt, bf16x8 (&av)[MS], bf16x8 (&bv)[NS],
+template <bool TRA, int MS, int QN>
+__device__ inline void chunk(const Ctx<MS> &c, const uint8_t *nxt, bf16x8 (&av)[MS], bf16x8 (&bv)[NS],
                              f32x16 (&acc)[MS][NS])
 {
+    constexpr int BM = Geo<MS>::BM, ABYTES = Geo<MS>::ABYTES;
     bf16x8 an[MS], bn[NS];
 #pragma unroll
     for (int k = 0; k < MS * NS; ++k) {
@@ -187,15 +199,18 @@ __device__ inline void chunk(const Ctx &c, const uint8_t *nxt, bf16x8 (&av)[MS],
         bv[j] = bn[j];
 }
 
-template <bool TRA, int NST>
-__global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(const GemmArgs a)
+template <bool TRA, int MS, int NST>
+__global__ __launch_bounds__(THREADS, NST > 4 ? 1 : 2) void gemm_bf16_kernel(const GemmArgs a)
 {
+    using G = Geo<MS>;
+    constexpr int BM = G::BM, ALOADS = G::ALOADS, LOADS = G::LOADS, ABYTES = G::ABYTES;
+    constexpr int STAGE = G::STAGE, GROUP_M = 16 / MS;
     __shared__ __align__(16) uint8_t ring[NST * STAGE];
     const int tiles_m = (a.R + BM - 1) / BM, tiles_n = (a.S + BN - 1) / BN;
     // each XCD takes a contiguous range of the tiles, in groups of 4 row tiles
     // walked row tile fastest; the parts of a tile are adjacent
-    const int p = (int)blockIdx.x, G = (int)gridDim.x;
-    const int gq = G >> 3, gr = G & 7, xcd = p & 7, idx = p >> 3;
+    const int p = (int)blockIdx.x, grid = (int)gridDim.x;
+    const int gq = grid >> 3, gr = grid & 7, xcd = p & 7, idx = p >> 3;
     const int local = xcd < gr ? xcd * (gq + 1) + idx : gr * (gq + 1) + (xcd - gr) * gq + idx;
     const int part = local % a.parts, pt = local / a.parts;
     const int prob = pt / (tiles_m * tiles_n), tile = pt - prob * (tiles_m * tiles_n);
@@ -219,7 +234,7 @@ __global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(con
                 acc[i][j][r] = 0.f;
 
     if (ns > 0) {
-        Ctx c;
+        Ctx<MS> c;
         c.ring = ring;
         c.wave = wave;
         c.lane = lane;
@@ -233,10 +248,10 @@ __global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(con
         c.bstep = BC * a.ldb * 2;
         c.seg = s0 / seg_steps;
         c.c0 = (s0 - c.seg * seg_steps) * BC;
-        start_segment<TRA>(a, c, prob, m0, n0);
+        start_segment<TRA, MS>(a, c, prob, m0, n0);
 #pragma unroll 1
         for (int t = 0; t < NST && t < ns; ++t)
-            issue<TRA>(a, c, prob, m0, n0, t);
+            issue<TRA, MS>(a, c, prob, m0, n0, t);
         dma_wait<LOADS, NST - 1>(min(ns, NST) - 1);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");  // (no read of the stage before the barrier)
@@ -251,7 +266,7 @@ __global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(con
         for (int t = 0; t < ns; ++t) {
             uint8_t *const cur = ring + slot * STAGE;
             const int nslot = slot + 1 == NST ? 0 : slot + 1;
-            chunk<TRA, 1>(c, cur, av, bv, acc);
+            chunk<TRA, MS, 1>(c, cur, av, bv, acc);
             // all of the stage is in registers; the next one has landed where only
             // those younger than it are in flight (loads land in order); behind the
             // barrier the stage's slot is refilled while its last chunk runs and
@@ -265,8 +280,8 @@ __global__ __launch_bounds__(THREADS, NST > 3 ? 1 : 2) void gemm_bf16_kernel(con
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (t + NST < ns)
-                issue<TRA>(a, c, prob, m0, n0, slot);
-            chunk<TRA, 0>(c, ring + nslot * STAGE, av, bv, acc);
+                issue<TRA, MS>(a, c, prob, m0, n0, slot);
+            chunk<TRA, MS, 0>(c, ring + nslot * STAGE, av, bv, acc);
             slot = nslot;
         }
     }
@@ -349,13 +364,18 @@ int gemm_parts(int64_t tiles, int64_t R, int64_t S, int64_t C, GemmCost cost, in
 
 hipError_t launch_gemm_bf16(bool tra, const GemmArgs &a, int problems, hipStream_t stream)
 {
-    const int64_t wgs = gemm_tiles(BM, a.R, a.S) * problems * a.parts;
+    const int64_t wgs = gemm_tiles(a.rows, a.R, a.S) * problems * a.parts;
     const dim3 grid((unsigned)wgs), block(THREADS);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-    if (wgs <= current_cus())
-        tra ? go(gemm_bf16_kernel<true, 6>) : go(gemm_bf16_kernel<false, 6>);
-    else
-        tra ? go(gemm_bf16_kernel<true, 3>) : go(gemm_bf16_kernel<false, 3>);
+    const bool alone = wgs <= current_cus();
+    auto with = [&](auto trac) {
+        constexpr bool T = decltype(trac)::value;
+        if (a.rows == 64)
+            alone ? go(gemm_bf16_kernel<T, 2, 6>) : go(gemm_bf16_kernel<T, 2, 4>);
+        else
+            alone ? go(gemm_bf16_kernel<T, 4, 6>) : go(gemm_bf16_kernel<T, 4, 3>);
+    };
+    tra ? with(std::true_type{}) : with(std::false_type{});
     return hipGetLastError();
 }
 

@@ -367,6 +367,7 @@ struct GemmArgs {
     float *part;
     void *out[2];
     int outbf16;
+    int rows;  // of a tile: 128 or 64
 };
 int64_t gemm_tiles(int rows, int64_t R, int64_t S);  // tiles of `rows` rows
 // parts of the reduction C estimated to be fastest, for `tiles` tiles and R * S
