@@ -100,7 +100,8 @@ typedef struct {
     float *dbg, *dbu;            /* fp32 [N], each may be NULL */
 } ql_gated_grad;
 
-/* No output may alias an input or another output.  N % 8 == 0 and K % 32 == 0;
+/* No output may alias an input or another output (the same address:
+ * QL_ERR_INVALID).  N % 8 == 0 and K % 32 == 0;
  * M == 0 writes zeros to dW and db and nothing else.  Workspace (per stream, as
  * in qlinear.h): for dX above 512 rows, or where K % 128 != 0 or a scale tensor is
  * not 4-byte aligned, the weights in bf16 (4 N K bytes; q4, int8: 8), and fp32
@@ -125,7 +126,8 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
  * `period` rows).  freqs: device fp64 [rot/2], radians per position, where a
  * longer context's scaling enters; angles are formed in fp64 (positions up to
  * 2^31 in size).  x, o: rows of ldx, ldo elements, fp32 or bf16 (dt, both), x ==
- * o with ldx == ldo for in place, otherwise no overlap; aligned to an element.
+ * o with ldx == ldo for in place, otherwise no element of both (QL_ERR_INVALID; other
+ * columns of the same rows may be); aligned to an element.
  * rot even, 2 <= rot <= dh; heads * dh <= ldx, ldo < 2^31; rows < 2^24.
  * Asynchronous; rows == 0 is a no-op. */
 int qlinear_rotary(const void *x, int64_t ldx, void *o, int64_t ldo, int dt, int64_t rows,

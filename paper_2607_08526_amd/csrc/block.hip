@@ -22,6 +22,24 @@ bool fmt_ok(int f) { return f == QL_FMT_MXFP4 || f == QL_FMT_Q4 || f == QL_FMT_I
 // a * b >= limit, for a, b >= 0
 bool product_reaches(int64_t a, int64_t b, int64_t limit) { return b > 0 && a >= (limit + b - 1) / b; }
 
+// whether rows of w elements (of `size` bytes) at strides ldx and ldo share any, the
+// same rows in the same place (in place) left out
+bool rows_overlap(const void *x, int64_t ldx, const void *o, int64_t ldo, int64_t rows, int64_t w,
+                  uintptr_t size)
+{
+    const uintptr_t a = (uintptr_t)x, b = (uintptr_t)o;
+    if (a == b)
+        return rows > 1 && ldx != ldo;
+    if (a >= b + (uintptr_t)((rows - 1) * ldo + w) * size ||
+        b >= a + (uintptr_t)((rows - 1) * ldx + w) * size)
+        return false;
+    // columns of one buffer: apart in every row, or not
+    if (rows == 1 || ldx != ldo)
+        return true;
+    const int64_t apart = (int64_t)((a > b ? a - b : b - a) / size) % ldx;
+    return apart < w || ldx - apart < w;
+}
+
 int status(hipError_t e) { return e == hipSuccess ? QL_OK : QL_ERR_HIP; }
 
 int check_gated(const ql_gated *g)
@@ -232,6 +250,11 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         !aligned(d->dU, 16) || !aligned(d->dX, 16) || !aligned(d->dWg, 16) ||
         !aligned(d->dWu, 16) || !aligned(d->dbg, 4) || !aligned(d->dbu, 4))
         return QL_ERR_ALIGN;
+    const void *const outs[] = {d->dG, d->dU, d->dX, d->dWg, d->dWu, d->dbg, d->dbu};
+    for (int i = 0; i < 7 && M > 0; ++i)
+        for (int k = 0; k <= i; ++k)
+            if (outs[i] && (k < i ? outs[i] == outs[k] : outs[i] == d->dH || outs[i] == g->X))
+                return QL_ERR_INVALID;
     const int cus = current_cus();
     const bool want_x = d->dX && M > 0;
     // workspace: both weights in bf16 (q4, int8: two planes each) where dX is not formed
@@ -389,11 +412,13 @@ int qlinear_rotary(const void *x, int64_t ldx, void *o, int64_t ldo, int dt, int
         return QL_ERR_SHAPE;
     if (rows == 0)
         return QL_OK;
-    if (!x || !o || !freqs || (x == o && ldx != ldo))
-        return QL_ERR_INVALID;
     const uintptr_t size = dt == QL_DT_BF16 ? 2 : 4;
+    if (!x || !o || !freqs)
+        return QL_ERR_INVALID;
     if (!aligned(x, size) || !aligned(o, size) || !aligned(freqs, 8) || !aligned(positions, 8))
         return QL_ERR_ALIGN;
+    if (rows_overlap(x, ldx, o, ldo, rows, heads * dh, size))
+        return QL_ERR_INVALID;
     RotaryArgs a{};
     a.x = x;
     a.ldx = ldx;

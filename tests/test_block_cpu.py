@@ -150,6 +150,13 @@ def test_gated_backward_errors(lib):
     for bad in (dict(dhdt=2), dict(dxdt=2), dict(dwdt=2), dict(dWg=None), dict(dWu=None),
                 dict(dH=None), dict(dG=None), dict(dU=None), dict(fmt=F16), dict(act=9)):
         assert f(**bad) == INVALID, bad
+    # outputs that are an input, or each other
+    p = lambda i: 0x100000 * i
+    apart = dict(X=p(1), dH=p(2), dG=p(3), dU=p(4), dX=p(5), dWg=p(6), dWu=p(7), dbg=p(8),
+                 dbu=p(9))
+    for name, other in (("dG", "dH"), ("dU", "X"), ("dX", "X"), ("dU", "dG"), ("dWg", "dX"),
+                        ("dWu", "dWg"), ("dbu", "dbg")):
+        assert f(**(apart | {name: apart[other]})) == INVALID, (name, other)
     for bad in (dict(N=12), dict(K=40), dict(M=-1)):
         assert f(**bad) == SHAPE, bad
     for bad in (dict(M=1 << 22), dict(N=1 << 22), dict(M=1 << 21, N=1 << 21)):
@@ -167,6 +174,10 @@ def test_rotary_errors(lib):
     assert f(rows=0, x=None) == OK
     for bad in (dict(dt=2), dict(x=None), dict(o=None), dict(fr=None), dict(o=A16, ldo=300)):
         assert f(**bad) == INVALID, bad
+    # elements of both x and o: the next element, the next row, half a row on
+    for o, ldo in ((A16 + 2, 256), (A16 + 512, 256), (A16 + 256, 256), (A16 + 2046, 300)):
+        assert f(x=A16, ldx=256, o=o, ldo=ldo) == INVALID, (o, ldo)
+    assert f(x=A16 + 512, o=A16, ldx=512, ldo=512, heads=5) == INVALID
     for bad in (dict(rows=-1), dict(heads=0), dict(dh=0), dict(rot=0), dict(rot=7), dict(rot=66),
                 dict(ldx=255), dict(ldo=255), dict(pos=None), dict(rot=-2)):
         assert f(**bad) == SHAPE, bad

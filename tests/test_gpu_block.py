@@ -569,6 +569,16 @@ def test_rotary_overlapping_rows(gpu):
     ql.rotary(x, H, freqs, out=out)
     assert torch.equal(out[:, :128], want) and (out[:, 128:] == 3).all()
     tail = flat[rows * 128:].clone()
+    both = torch.cat((flat[:rows * 128].view(rows, 128), torch.empty((rows, 130), device="cuda")),
+                     dim=1)
+    ql.rotary(both[:, :128], H, freqs, out=both[:, 130:])  # into other columns of the rows
+    assert torch.equal(both[:, 130:], want)
+    with pytest.raises(ql.QLinearError):
+        ql.rotary(both[:, :128], H, freqs, out=both[:, 127:255])
+    one = flat[:256].view(1, 256).clone()
+    row = ql.rotary(one[:, :128].clone(), H, freqs, start=5)
+    ql.rotary(one, H, freqs, start=5, out=one[:, :128])  # one row in place, by another length
+    assert torch.equal(one[:, :128], row)
     ql.rotary(x, H, freqs)
     assert torch.equal(flat[:rows * 128].view(rows, 128), want)
     assert torch.equal(flat[rows * 128:], tail)
