@@ -501,24 +501,28 @@ bool tile_takes(int64_t K) { return K >= 224 && K < ((int64_t)1 << 22); }
 
 // us of tiles of 128 and 64 rows: fixed; of a 64-k step where a tile has its CU to
 // itself (latency, and rising with the share of the CUs that work), and per tile of a
-// CU that several share.  Products with MXFP4 weights, gated pairs of MXFP4, and of q4
-// and int8 (twice the matrix instructions).  Measured, 64 / 128 rows: product 6144 x
+// CU that several share.  Products with MXFP4 weights, gated pairs of MXFP4, of q4 and
+// int8 (twice the matrix instructions), and of these where scales come one by one (whose
+// 128-row tiles do not fit the registers).  Measured, 64 / 128 rows: product 6144 x
 // 1536 at 512 rows 14.6 / 21.2, at 768 22.3 / 21.8, 1536 x 6144 at 2048 46.0 / 67.9,
 // fp32 at 1536 140 / 206; pairs 6144 x 1536 at 256 rows 17.1 / 25.8, at 2048 78.5 / 70.9,
-// q4 at 256 rows 32.5 / 44.6, at 512 54.4 / 47.4.
+// q4 at 256 rows 32.5 / 44.6, at 512 54.4 / 47.4; scales one by one, int8 2048 x 1056 at
+// 1748 rows 46.6 / 65.6, q4 4096 x 1504 at 1100 91.4 / 104, at 2048 122 / 109.
 struct TileRate {
     double fixed, alone, rise, shared;
 };
-constexpr TileRate TILE_RATES[3][2] = {{{5.2, 0.63, 0.08, 0.88}, {4.5, 0.38, 0.06, 0.49}},
+constexpr TileRate TILE_RATES[4][2] = {{{5.2, 0.63, 0.08, 0.88}, {4.5, 0.38, 0.06, 0.49}},
                                        {{10.0, 0.62, 0.16, 0.86}, {7.0, 0.36, 0.09, 0.50}},
-                                       {{10.0, 1.42, 0.30, 1.82}, {7.0, 0.96, 0.10, 1.14}}};
+                                       {{10.0, 1.42, 0.30, 1.82}, {7.0, 0.96, 0.10, 1.14}},
+                                       {{10.0, 2.30, 0.40, 2.20}, {7.0, 1.05, 0.15, 1.25}}};
 
 double tile_us(int fmt, bool xf32, bool gated, int64_t M, int64_t N, int64_t K, int cus, int *rows)
 {
     const double steps = (double)((K + 63) / 64) * (xf32 ? 3 : 1);
+    const int kind = !gated ? 0 : fmt == QL_FMT_MXFP4 ? 1 : K % 256 == 0 ? 2 : 3;
     double best = 1e30;
     for (int h = 0; h < 2; ++h) {
-        const TileRate &t = TILE_RATES[!gated ? 0 : fmt == QL_FMT_MXFP4 ? 1 : 2][h];
+        const TileRate &t = TILE_RATES[kind][h];
         const int tile = h ? 64 : 128;
         const int64_t tiles = tile_tiles(tile, M, N, gated);
         if (tiles > MAX_WORKGROUPS)

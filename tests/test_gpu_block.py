@@ -382,7 +382,7 @@ GATED = [(1, 8, 32), (1, 1000, 96), (5, 17, 64), (16, 130, 1056), (33, 64, 160),
          (1100, 2056, 512), (1030, 2056, 1152), (130, 1032, 416), (1100, 2056, 224),
          (1100, 2056, 288), (1030, 2056, 1056), (1900, 2042, 1536), (1900, 2040, 1568),
          (7, 72, 2080), (400, 2048, 1024), (260, 136, 16384), (70, 320, 12320),
-         (320, 72, 25632)]
+         (320, 72, 25632), (512, 16380, 544)]
 
 
 def gated_case(torch, fmt, M, N, K, seed, bias):
