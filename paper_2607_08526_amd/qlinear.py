@@ -719,7 +719,8 @@ def rotary_frequencies(rot, base=10000.0, scaling=None, factor=1.0, context=None
     factor); "ntk" (the base raised so that the slowest frequency is divided by
     factor and the fastest kept); "yarn" (frequencies that turn more than 32 times
     within `context`, the length trained on, kept, those that turn less than once
-    divided by factor, a ramp over j between; mscale 0.1 ln(factor) + 1)."""
+    divided by factor, a ramp over j between, also where it ends past the last pair;
+    mscale 0.1 ln(factor) + 1)."""
     if rot < 2 or rot % 2:
         raise ValueError(f"rot = {rot} is not a positive even number")
     if not factor >= 1.0 or not base > 1.0:
@@ -737,7 +738,7 @@ def rotary_frequencies(rot, base=10000.0, scaling=None, factor=1.0, context=None
             raise ValueError("yarn scaling needs the context trained on")
         # the pair index whose frequency turns r times within the context
         index = lambda r: rot * math.log(context / (2 * math.pi * r)) / (2 * math.log(base))
-        lo, hi = max(0, math.floor(index(32))), min(rot // 2 - 1, math.ceil(index(1)))
+        lo, hi = max(0, math.floor(index(32))), min(rot - 1, math.ceil(index(1)))
         ramp = ((torch.arange(rot // 2, dtype=torch.float64) - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
         freqs = freqs * (1 - ramp) + freqs / factor * ramp
         mscale = 0.1 * math.log(factor) + 1.0
