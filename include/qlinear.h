@@ -95,10 +95,12 @@
  *     grows when a call outside graph capture needs more (the old buffer
  *     goes back to the pool in stream order), so steady-state calls
  *     allocate nothing.  Consequences: calls on one stream share it, which
- *     their stream order makes safe; a graph captured on a stream keeps
- *     that stream's buffer (it is then never released before the process
- *     ends), so replays of the graph must not overlap calls on the capture
- *     stream or replays of other graphs captured on it.  A call under
+ *     their stream order makes safe (from several threads too: a call that
+ *     uses it enqueues all its work before the next one); a graph captured
+ *     on a stream keeps that stream's buffer (it is then never released
+ *     before the process ends), so replays of the graph must not overlap
+ *     calls on the capture stream or replays of other graphs captured on
+ *     it.  A call under
  *     capture that needs more than its stream's buffer allocates for itself
  *     from the pool (allocation and free nodes in the graph) instead.  A
  *     destroyed stream's handle value, if reused, inherits its buffer.  fp32

@@ -307,7 +307,8 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         return QL_ERR_UNSUPPORTED;
     uint8_t *ws = nullptr;
     bool own = false;
-    if (wbytes + part_bytes && !stream_workspace(wbytes + part_bytes, stream, &ws, &own))
+    std::unique_lock<std::mutex> turn;
+    if (wbytes + part_bytes && !stream_workspace(wbytes + part_bytes, stream, &ws, &own, &turn))
         return QL_ERR_HIP;
     float *const part = reinterpret_cast<float *>(ws + wbytes);
 

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "qlinear.h"
 
 namespace qlk {
@@ -404,9 +406,10 @@ constexpr int64_t MAX_WORKGROUPS = ((int64_t)1 << 24) - 1;
 
 // What the entry points share (qlinear.hip): the current device's CUs, its
 // workspace for a stream (own: the caller frees it on the stream after its
-// launches), an epilogue's checks and its form for the kernels.
+// launches; turn: held until then), an epilogue's checks and its form for the kernels.
 int current_cus();
-bool stream_workspace(size_t bytes, hipStream_t stream, uint8_t **p, bool *own);
+bool stream_workspace(size_t bytes, hipStream_t stream, uint8_t **p, bool *own,
+                      std::unique_lock<std::mutex> *turn);
 int epilogue_status(const ql_epilogue &ep, const void *Y);
 Epilogue kernel_epilogue(const ql_epilogue *ep);
 

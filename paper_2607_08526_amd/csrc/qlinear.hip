@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <atomic>
 #include <functional>
+#include <list>
 #include <mutex>
 #include <new>
 #include <queue>
@@ -133,9 +134,14 @@ size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 // stays allocated for the life of the process (replays still use it).  A
 // call under capture that needs more than the stream's buffer takes a
 // stream-ordered allocation for itself (freed after its launch) instead.
+// Stream order protects the buffer only while a call's launches stand together
+// in it, so the call holds the buffer's lock until they are enqueued: another
+// thread's launches on the stream between them would overwrite what they hand
+// over, and its growth would free the buffer under the later ones.
 struct Workspace {
     uint8_t *ptr;
     bool own_alloc;  // allocated for this call: free after the launch
+    std::unique_lock<std::mutex> turn;
 };
 
 bool take_workspace(size_t bytes, hipStream_t stream, Workspace &w)
@@ -143,12 +149,13 @@ bool take_workspace(size_t bytes, hipStream_t stream, Workspace &w)
     struct Entry {
         int dev;
         hipStream_t stream;
-        void *ptr;
-        size_t bytes;
-        bool captured;  // a graph holds this buffer
+        void *ptr = nullptr;
+        size_t bytes = 0;
+        bool captured = false;  // a graph holds this buffer
+        std::mutex turn;
     };
-    static std::mutex mu;
-    static std::vector<Entry> cache;
+    static std::mutex mu;  // of the list; an entry stays where it is
+    static std::list<Entry> cache;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess)
         return false;
@@ -159,25 +166,29 @@ bool take_workspace(size_t bytes, hipStream_t stream, Workspace &w)
     hipMemPool_t pool = workspace_pool();
     if (!pool)
         return false;
-    std::lock_guard<std::mutex> g(mu);
     Entry *e = nullptr;
-    for (Entry &c : cache)
-        if (c.dev == dev && c.stream == stream)
-            e = &c;
-    if (!e) {
-        cache.push_back(Entry{dev, stream, nullptr, 0, false});
-        e = &cache.back();
+    {
+        std::lock_guard<std::mutex> g(mu);
+        for (Entry &c : cache)
+            if (c.dev == dev && c.stream == stream)
+                e = &c;
+        if (!e) {
+            e = &cache.emplace_back();
+            e->dev = dev;
+            e->stream = stream;
+        }
     }
+    std::unique_lock<std::mutex> turn(e->turn);
     if (e->bytes >= bytes) {
         e->captured |= capturing;
-        w = Workspace{(uint8_t *)e->ptr, false};
+        w = Workspace{(uint8_t *)e->ptr, false, std::move(turn)};
         return true;
     }
     void *p = nullptr;
     if (capturing) {
         if (hipMallocFromPoolAsync(&p, bytes, pool, stream) != hipSuccess)
             return false;
-        w = Workspace{(uint8_t *)p, true};
+        w = Workspace{(uint8_t *)p, true, {}};
         return true;
     }
     const size_t grow = ((std::max(bytes, e->bytes + e->bytes / 2)) + ((size_t)1 << 21) - 1) &
@@ -188,8 +199,10 @@ bool take_workspace(size_t bytes, hipStream_t stream, Workspace &w)
         (void)hipFreeAsync(p, stream);  // already failing; nothing to report
         return false;
     }
-    *e = Entry{dev, stream, p, grow, false};
-    w = Workspace{(uint8_t *)p, false};
+    e->ptr = p;
+    e->bytes = grow;
+    e->captured = false;
+    w = Workspace{(uint8_t *)p, false, std::move(turn)};
     return true;
 }
 
@@ -211,7 +224,7 @@ bool get_workspace(WsSource &wsrc, size_t bytes, hipStream_t stream, Workspace &
     if (wsrc.fixed) {
         if (bytes > wsrc.cap)
             return false;
-        w = Workspace{wsrc.fixed, false};
+        w = Workspace{wsrc.fixed, false, {}};
         return true;
     }
     return take_workspace(bytes, stream, w);
@@ -1668,13 +1681,15 @@ namespace qlk {
 
 int current_cus() { return device_cus(); }
 
-bool stream_workspace(size_t bytes, hipStream_t stream, uint8_t **p, bool *own)
+bool stream_workspace(size_t bytes, hipStream_t stream, uint8_t **p, bool *own,
+                      std::unique_lock<std::mutex> *turn)
 {
     Workspace w{};
     if (!take_workspace(bytes, stream, w))
         return false;
     *p = w.ptr;
     *own = w.own_alloc;
+    *turn = std::move(w.turn);
     return true;
 }
 
