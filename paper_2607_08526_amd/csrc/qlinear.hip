@@ -1771,6 +1771,15 @@ int qlinear_block_forward_ep(const ql_linear_ep *lin, int n_lin, hipStream_t str
     const int st = classify(lin, n_lin, c);
     if (st != QL_OK)
         return st;
+    // with several classes, each is looked at before the first one is enqueued
+    if (std::count(c.cnt, c.cnt + Classes::N, 0) < Classes::N - 1) {
+        WsSource dry{nullptr, 0, true, 0};
+        for (int k = 0; k < Classes::N; ++k) {
+            const int s = launch_group(c.cls[k], c.cnt[k], dry, stream);
+            if (s != QL_OK)
+                return s;
+        }
+    }
     for (int k = 0; k < Classes::N; ++k) {
         WsSource src = pool_source();
         const int s = launch_group(c.cls[k], c.cnt[k], src, stream);
