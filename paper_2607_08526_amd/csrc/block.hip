@@ -250,11 +250,15 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
         !aligned(d->dU, 16) || !aligned(d->dX, 16) || !aligned(d->dWg, 16) ||
         !aligned(d->dWu, 16) || !aligned(d->dbg, 4) || !aligned(d->dbu, 4))
         return QL_ERR_ALIGN;
-    const void *const outs[] = {d->dG, d->dU, d->dX, d->dWg, d->dWu, d->dbg, d->dbu};
-    for (int i = 0; i < 7 && M > 0; ++i)
-        for (int k = 0; k <= i; ++k)
-            if (outs[i] && (k < i ? outs[i] == outs[k] : outs[i] == d->dH || outs[i] == g->X))
-                return QL_ERR_INVALID;
+    // (M == 0: what it writes of them and reads)
+    const void *const outs[] = {d->dWg, d->dWu, d->dbg, d->dbu, d->dG, d->dU, d->dX};
+    const void *const ins[] = {g->gate_codes, g->gate_scales, g->up_codes, g->up_scales,
+                               g->gate_bias, g->up_bias, d->dH, g->X};
+    for (int i = 0; i < (M > 0 ? 7 : 4); ++i) {
+        if (outs[i] && (std::find(outs, outs + i, outs[i]) != outs + i ||
+                        std::find(ins, ins + (M > 0 ? 8 : 6), outs[i]) != ins + (M > 0 ? 8 : 6)))
+            return QL_ERR_INVALID;
+    }
     const int cus = current_cus();
     const bool want_x = d->dX && M > 0;
     // workspace: both weights in bf16 (q4, int8: two planes each) where dX is not formed
