@@ -269,7 +269,9 @@ def _on_device(*tensors):
 
 def _on_current_device(*tensors):
     """_on_device, and the device that the call's stream belongs to."""
-    dev = _device() if _device is not None and torch.cuda.is_initialized() else None
+    dev = None
+    if torch.cuda.is_initialized():
+        dev = _device() if _device is not None else torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             _on_device(*tensors)
