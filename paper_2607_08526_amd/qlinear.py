@@ -222,6 +222,20 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+def _new(like, shape, dtype, stream):
+    """An output on like's device that a call on `stream` (None: the current one)
+    writes.  Its memory comes from the allocator's blocks of that stream: one of the
+    current stream's may still be in use there by work of a tensor that is gone.  The
+    current stream is noted as a user too, so the block is not given out again before
+    the work that stream holds when the output goes."""
+    if stream is None or not like.is_cuda:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream(like.device))
+    return t
+
+
 # Argument checks of the binding.  The library receives bare pointers and
 # sizes, so a tensor of the wrong dtype, shape or layout would be read or
 # written out of bounds; these checks run before the library is called.
@@ -363,8 +377,10 @@ def quantize(fmt, W, codes=None, scales=None, stream=None):
     N, K = W.shape
     if K % BLOCK:
         raise ValueError(f"K = {K} is not a multiple of {BLOCK}")
-    codes = empty_codes(fmt, N, K, W.device) if codes is None else codes
-    scales = empty_scales(N, K, W.device, fmt) if scales is None else scales
+    if codes is None:
+        codes = _new(W, (N, K) if fmt == FMT_INT8 else (N, K // 2), torch.uint8, stream)
+    if scales is None:
+        scales = _new(W, (N, K // BLOCK), torch.uint8 if fmt == FMT_MXFP4 else torch.int16, stream)
     _require_weights(fmt, codes, scales, N, K)
     _on_device(W, codes, scales)
     _check(load().qlinear_quantize(fmt, _ptr(W), N, K, _ptr(codes), _ptr(scales),
@@ -387,7 +403,7 @@ def forward(fmt, X, codes, scales, N, Y=None, stream=None):
     M, K = _require_x(X)
     _require_weights(fmt, codes, scales, N, K)
     if Y is None:
-        Y = torch.empty((M, N), dtype=torch.float32, device=X.device)
+        Y = _new(X, (M, N), torch.float32, stream)
     _require_y(Y, M, N)
     _on_device(X, codes, scales, Y)
     _check(load().qlinear_forward(fmt, _ptr(X), _xdt(X), M, K, _ptr(codes), _ptr(scales), N,
@@ -429,7 +445,7 @@ def forward_ep(fmt, X, codes, scales, N, Y=None, bias=None, act=ACT_NONE, residu
     M, K = _require_x(X)
     _require_weights(fmt, codes, scales, N, K)
     if Y is None:
-        Y = X.new_empty((M, N), dtype=ydtype)
+        Y = _new(X, (M, N), ydtype, stream)
     _require_y(Y, M, N, (torch.float32, torch.bfloat16))
     _require_ep(bias, residual, M, N)
     _require_steer(steer, N)
@@ -520,9 +536,9 @@ def quantize_act(X, qx=None, sx=None, stream=None):
     returns (qx int8 [M][K], sx fp16 bits as int16 [M]).  Asynchronous."""
     M, K = _require_x(X)
     if qx is None:
-        qx = torch.empty((M, K), dtype=torch.int8, device=X.device)
+        qx = _new(X, (M, K), torch.int8, stream)
     if sx is None:
-        sx = torch.empty(M, dtype=torch.int16, device=X.device)
+        sx = _new(X, (M,), torch.int16, stream)
     _require(qx, "qx", (torch.int8,), (M, K))
     _require(sx, "sx", _TWO_BYTE, (M,))
     _on_device(X, qx, sx)
@@ -541,7 +557,7 @@ def forward_w8a8(qx, sx, codes, scales, N, Y=None, bias=None, act=ACT_NONE, resi
     _require(sx, "sx", _TWO_BYTE, (M,))
     _require_weights(FMT_INT8, codes, scales, N, K)
     if Y is None:
-        Y = qx.new_empty((M, N), dtype=ydtype)
+        Y = _new(qx, (M, N), ydtype, stream)
     _require_y(Y, M, N, (torch.float32, torch.bfloat16))
     _require_ep(bias, residual, M, N)
     _require_steer(steer, N)
@@ -575,7 +591,7 @@ def attention(q, k, v, B, T, H, dh=64, scale=None, O=None, odtype=torch.float32,
         if t.shape[0] != B * T:
             raise ValueError(f"{name} has {t.shape[0]} rows, expected B * T = {B * T}")
     if O is None:
-        O = torch.empty((B * T, H * dh), dtype=odtype, device=q.device)
+        O = _new(q, (B * T, H * dh), odtype, stream)
     _require(O, "O", (torch.float32, torch.bfloat16), min_cols=H * dh)
     if O.shape[0] != B * T:
         raise ValueError(f"O has {O.shape[0]} rows, expected B * T = {B * T}")
@@ -597,7 +613,7 @@ def dequantize(fmt, codes, scales, dtype=torch.float32, out=None, stream=None):
     N, K = codes.shape[0], codes.shape[1] * (1 if fmt == FMT_INT8 else 2)
     _require_weights(fmt, codes, scales, N, K)
     if out is None:
-        out = codes.new_empty((N, K), dtype=dtype)
+        out = _new(codes, (N, K), dtype, stream)
     _require(out, "out", (torch.float32, torch.bfloat16), (N, K))
     _on_current_device(codes, scales, out)
     _check(load().qlinear_dequantize(fmt, _ptr(codes), _ptr(scales), N, K, _ptr(out), _ydt(out),
@@ -613,11 +629,11 @@ def quantize_act_mx(X, qx=None, sx=None, stream=None):
     if K % BLOCK or K == 0:
         raise ValueError(f"K = {K} is not a positive multiple of {BLOCK}")
     if qx is None:
-        qx = X.new_empty((M, K // 2), dtype=torch.uint8)
+        qx = _new(X, (M, K // 2), torch.uint8, stream)
     else:
         _require(qx, "qx", (torch.uint8,), (M, K // 2))
     if sx is None:
-        sx = X.new_empty((M, K // BLOCK), dtype=torch.uint8)
+        sx = _new(X, (M, K // BLOCK), torch.uint8, stream)
     else:
         _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
     _on_current_device(X, qx, sx)
@@ -636,7 +652,7 @@ def forward_mx(qx, sx, codes, scales, N, Y=None, bias=None, act=ACT_NONE, residu
     _require_weights(FMT_MXFP4, codes, scales, N, K)
     _require(sx, "sx", (torch.uint8,), (M, K // BLOCK))
     if Y is None:
-        Y = qx.new_empty((M, N), dtype=ydtype)
+        Y = _new(qx, (M, N), ydtype, stream)
     _require_y(Y, M, N, (torch.float32, torch.bfloat16))
     _require_ep(bias, residual, M, N)
     _require_steer(steer, N)
@@ -676,7 +692,7 @@ def gated_forward(fmt, X, gate, up, H=None, bias=None, act=ACT_SILU, hdtype=torc
     forward_ep on H.  Asynchronous."""
     g, M, K, N, tensors = _gated(fmt, X, gate, up, bias, act)
     if H is None:
-        H = X.new_empty((M, N), dtype=hdtype)
+        H = _new(X, (M, N), hdtype, stream)
     _require(H, "H", (torch.float32, torch.bfloat16), (M, N))
     _on_current_device(H, *tensors)
     _check(load().qlinear_gated_forward(ctypes.byref(g), _ptr(H), _ydt(H), _stream(stream)))
@@ -702,7 +718,7 @@ def gated_backward(fmt, X, gate, up, dH, bias=None, act=ACT_SILU, x_grad=True,
     if N % 8:
         raise ValueError(f"N = {N} is not a multiple of 8")
     _on_current_device(dH, *tensors)
-    new = lambda shape, dt: X.new_empty(shape, dtype=dt)
+    new = lambda shape, dt: _new(X, shape, dt, stream)
     both = new((2, M, N), torch.bfloat16)
     dX = new((M, K), dtype) if x_grad else None
     dW = new((2, N, K), dtype) if weight_grads else (None, None)

@@ -55,3 +55,42 @@ def test_threads_on_one_stream(gpu):
     for t in threads:
         t.join()
     assert not fails
+
+
+def test_outputs_of_another_stream(gpu):
+    """Outputs that a call on another stream makes do not take memory that the
+    current stream's queue may still use: a block freed there stays away from them,
+    and they have the values of a call on the current stream."""
+    torch, ql = gpu
+    rng, Xb, _, pair, _, _, db = gated_case(torch, "q4", 64, 256, 128, 5, True)
+    dH = dev(torch, rng.standard_normal((64, 256)).astype(np.float32))
+    W = dev(torch, rng.standard_normal((256, 128)).astype(np.float32))
+    mx = ql.quantize(ql.FMT_MXFP4, W)
+    q = ql.quantize_act_mx(Xb)
+    q8 = ql.quantize_act(Xb)
+    w8 = ql.quantize(ql.FMT_INT8, W)
+    calls = [lambda s: ql.gated_forward(ql.FMT_Q4, Xb, *pair, bias=db, stream=s),
+             lambda s: ql.gated_backward(ql.FMT_Q4, Xb, *pair, dH, bias=db, weight_grads=True,
+                                         bias_grads=True, stream=s),
+             lambda s: ql.forward_mx(*q, *mx, 256, stream=s),
+             lambda s: ql.quantize_act_mx(Xb, stream=s),
+             lambda s: ql.dequantize(ql.FMT_MXFP4, *mx, stream=s),
+             lambda s: ql.quantize(ql.FMT_MXFP4, W, stream=s),
+             lambda s: ql.forward(ql.FMT_MXFP4, Xb, *mx, 256, stream=s),
+             lambda s: ql.forward_ep(ql.FMT_Q4, Xb, *pair[0], 256, stream=s),
+             lambda s: ql.quantize_act(Xb, stream=s),
+             lambda s: ql.forward_w8a8(*q8, *w8, 256, stream=s),
+             lambda s: ql.attention(Xb[:, :64], Xb[:, :64], Xb[:, 64:], 1, 64, 1, stream=s)]
+    side = torch.cuda.Stream()
+    for i, call in enumerate(calls):
+        tensors = lambda r: [r] if isinstance(r, torch.Tensor) else list(r)
+        want = [t.clone() for t in tensors(call(None))]  # its own outputs are free again
+        torch.cuda.synchronize()
+        gone = [torch.empty_like(t) for t in want]
+        freed = {t.data_ptr() for t in gone}
+        del gone
+        got = tensors(call(side))
+        side.synchronize()
+        for a, b in zip(got, want):
+            assert a.data_ptr() not in freed, i
+            assert torch.equal(a, b), i
