@@ -212,6 +212,9 @@ _device = getattr(torch._C, "_cuda_getDevice", None)
 
 def _stream(stream=None):
     if stream is not None:
+        dev = getattr(stream, "device_index", None)
+        if dev is not None and dev != torch.cuda.current_device():
+            raise ValueError(f"the stream is of cuda:{dev}, not of the current device")
         return stream.cuda_stream
     if _raw_stream is None or _device is None or not torch.cuda.is_initialized():
         return torch.cuda.current_stream().cuda_stream

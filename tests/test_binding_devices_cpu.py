@@ -30,3 +30,14 @@ def test_tensors_on_the_current_device(device0):
         ql._on_current_device(DeviceTensor(0), DeviceTensor(1))
     with pytest.raises(ValueError, match="device"):
         ql._on_current_device(torch.zeros(1))
+
+
+def test_stream_of_the_current_device(device0):
+    class Stream:
+        cuda_stream = 7
+        device_index = 0
+
+    assert ql._stream(Stream()) == 7
+    Stream.device_index = 1
+    with pytest.raises(ValueError, match="stream"):
+        ql._stream(Stream())
