@@ -124,8 +124,8 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
  * turns by -t: the gradient of x from that of the output.  Row r's position is
  * positions[r], or start + r % period when positions is NULL (sequences of
  * `period` rows).  freqs: device fp64 [rot/2], radians per position, where a
- * longer context's scaling enters; angles are formed in fp64 (positions up to
- * 2^31 in size).  x, o: rows of ldx, ldo elements, fp32 or bf16 (dt, both), x ==
+ * longer context's scaling enters; the angle is the exact product, reduced before it
+ * is rounded (positions up to 2^31 in size).  x, o: rows of ldx, ldo elements, fp32 or bf16 (dt, both), x ==
  * o with ldx == ldo for in place, otherwise no element of both (QL_ERR_INVALID; other
  * columns of the same rows may be); aligned to an element.
  * rot even, 2 <= rot <= dh; heads * dh <= ldx, ldo < 2^31; rows < 2^24.

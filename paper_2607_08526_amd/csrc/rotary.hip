@@ -9,7 +9,11 @@
 //
 // Angles: positions of long contexts leave an fp32 angle no fractional digits
 // (2^20 radians: 2^-4), so the angle is formed in fp64, in turns, and reduced
-// to [-1/2, 1/2) there; sine and cosine of the reduced angle are fp32.
+// to [-1/2, 1/2] there.  Plain fp64 products are off by up to 2^-24 of a turn near position
+// 2^31, more than what follows, so frequencies in turns have two terms and whole turns
+// are taken off the unrounded product: positions to 2^31 are as exact as 0.  The reduced
+// angle is rounded to fp32 (2^-26 of a turn at most) for its sine and cosine in fp32,
+// whose own steps are as large.
 //
 // Bound: HBM (every channel read and written once).  A workgroup takes a few rows
 // at a time and computes their angles once, in LDS, for all heads; a thread turns
@@ -58,11 +62,22 @@ __device__ inline int64_t position(const RotaryArgs &a, int64_t row)
     return a.positions ? a.positions[row] : a.start + row % a.period;
 }
 
-// mscale times cosine and sine of the angle at a position
-__device__ inline mx_f32x2 angle(const RotaryArgs &a, int64_t pos, double freq)
+// a frequency in turns per position, as a sum
+struct Turns {
+    double hi, lo;
+};
+__device__ inline Turns in_turns(double freq)
 {
-    const double t = (double)pos * (freq * 0.15915494309189533577);  // turns
-    const float f = (float)(t - __builtin_rint(t));
+    constexpr double HI = 0x1.45f306dc9c883p-3, LO = -0x1.6b01ec5417056p-57;  // 1 / (2 pi)
+    const double h = freq * HI;
+    return Turns{h, __builtin_fma(freq, HI, -h) + freq * LO};
+}
+
+// mscale times cosine and sine of the angle at a position
+__device__ inline mx_f32x2 angle(const RotaryArgs &a, int64_t pos, Turns freq)
+{
+    const double p = (double)pos, whole = __builtin_rint(p * freq.hi);
+    const float f = (float)(__builtin_fma(p, freq.hi, -whole) + p * freq.lo);
     float s, c;
     sincospif(2.0f * f, &s, &c);
     return mx_f32x2{c * a.mscale, (a.adjoint ? -s : s) * a.mscale};
@@ -107,13 +122,13 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(const RotaryArgs a)
     const int ai = threadIdx.x;
     const bool mine2 = ai + THREADS < R * half;
     int am[2], aj[2];
-    double fr[2];
+    Turns fr[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int i = ai + k * THREADS;
         am[k] = i / half;
         aj[k] = i - am[k] * half;
-        fr[k] = i < R * half ? a.freqs[aj[k]] : 0.0;
+        fr[k] = in_turns(i < R * half ? a.freqs[aj[k]] : 0.0);
     }
     const T *const x = static_cast<const T *>(a.x);
     T *const o = static_cast<T *>(a.o);
@@ -207,7 +222,7 @@ __global__ __launch_bounds__(THREADS) void rotary_pairs_kernel(const RotaryArgs 
             o[a.rot + u - half] = x[a.rot + u - half];
             continue;
         }
-        const mx_f32x2 t = angle(a, position(a, row), a.freqs[u]);
+        const mx_f32x2 t = angle(a, position(a, row), in_turns(a.freqs[u]));
         const int ca = a.interleaved ? 2 * u : u, cb = a.interleaved ? 2 * u + 1 : u + half;
         const float f = E::get(x[ca]), s = E::get(x[cb]);
         o[ca] = E::put(f * t[0] - s * t[1]);

@@ -94,3 +94,51 @@ def test_outputs_of_another_stream(gpu):
         for a, b in zip(got, want):
             assert a.data_ptr() not in freed, i
             assert torch.equal(a, b), i
+
+
+def exact_turn(freqs, positions):
+    """cos and sin [position][frequency] of the exact product of both: 60 digits down
+    to less than a turn."""
+    import math
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    pi2 = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+    out = np.empty((2, len(positions), len(freqs)))
+    for i, p in enumerate(positions):
+        for j, f in enumerate(freqs):
+            turns = Decimal(int(p)) * Decimal(float(f)) / pi2
+            t = float((turns - turns.to_integral_value()) * pi2)
+            out[:, i, j] = math.cos(t), math.sin(t)
+    return out
+
+
+@pytest.mark.parametrize("rot", [64, 20])  # whole vectors, and pair by pair
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_far_positions(gpu, rot, interleaved):
+    """Positions at both ends of the range: angles as exact there as near zero.  Of
+    (1, 0) the turned pair is cosine and sine themselves.  Rounding the reduced angle
+    (at most half a turn) to fp32 is off by 2^-26 of a turn, below 2^-23; sine and
+    cosine of it by two steps of values up to 1, 2^-23."""
+    torch, ql = gpu
+    rng = np.random.default_rng(rot)
+    far = 1 << 31
+    pos = np.concatenate([[0, 1, -1, far, far - 1, -far, 1 - far, (1 << 30) + 7],
+                          rng.integers(far - (1 << 20), far, 8), rng.integers(-far, far, 8)])
+    freqs = rng.uniform(0.5, 1.0, rot // 2)  # (radians per position)
+    freqs[-3:] = [1.0, 2.0 * np.pi, 1e-5]
+    x = torch.zeros((len(pos), 64), device="cuda")
+    a = np.arange(0, rot, 2) if interleaved else np.arange(rot // 2)
+    b = a + (1 if interleaved else rot // 2)
+    x[:, a] = 1.0
+    c, s = exact_turn(freqs, pos)
+    for adjoint in (False, True):
+        y = host(ql.rotary(x, 1, dev(torch, freqs), positions=dev(torch, pos),
+                           interleaved=interleaved, adjoint=adjoint, out=torch.empty_like(x)))
+        check(y[:, a], c, 2.0 ** -22, "cosine")
+        check(y[:, b], -s if adjoint else s, 2.0 ** -22, "sine")
+    # rows that count from a start
+    y = host(ql.rotary(x[:4], 1, dev(torch, freqs), start=far - 2, T=3, interleaved=interleaved,
+                       out=torch.empty_like(x[:4])))
+    c, s = exact_turn(freqs, [far - 2, far - 1, far, far - 2])
+    check(y[:, a], c, 2.0 ** -22, "cosine")
+    check(y[:, b], s, 2.0 ** -22, "sine")
