@@ -58,9 +58,11 @@ int qlinear_mx_forward(const uint8_t *qx, const uint8_t *sx, int64_t M, int64_t 
  * (the second half is a linear layer on H).  Weights: QL_FMT_MXFP4, QL_FMT_Q4 or
  * QL_FMT_INT8, both of one format, [N][K]; X bf16 [M][K]; act QL_ACT_NONE,
  * QL_ACT_GELU (exact form) or QL_ACT_SILU.  G and U stay in fp32; MXFP4 weights
- * enter exactly, q4 and int8 weights c * s as the sum of two bf16 (off by at
- * most 2^-18 of each weight).  Alignment: X and codes 16 bytes, fp16 scales 2,
- * biases 4. */
+ * enter exactly, q4 and int8 weights c * s exactly or as the sum of two bf16 (off by
+ * at most 2^-22 of each q4 weight, 2^-16 of each int8 weight).  An infinite
+ * activation gives an infinity of the product's sign, NaN for a weight of zero;
+ * finite ones of q4 and int8 pairs: up to 7e34 in size (as in qlinear.h).
+ * Alignment: X and codes 16 bytes, fp16 scales 2, biases 4. */
 typedef struct {
     int fmt;                     /* ql_fmt */
     const uint16_t *X;           /* bf16 [M][K] */

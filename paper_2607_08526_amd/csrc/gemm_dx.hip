@@ -5,7 +5,7 @@
 //
 // The reduction runs over weight rows, so a matrix operand's 8 consecutive
 // reduction indices lie in 8 rows: weights are converted to bf16 (MXFP4 exactly;
-// q4 / int8 as the sum of two bf16, off by at most 2^-18) into an LDS tile as they
+// q4 / int8 as the sum of two bf16, mx.h) into an LDS tile as they
 // are stored, [32 n][256 k], and read with the transposing LDS read
 // (ds_read_b64_tr_b16: 16 lanes that address 4 rows x 4 runs of 4 columns receive 4
 // rows of one column each).  Matrix instruction v_mfma_f32_32x32x16_bf16 as in
@@ -192,7 +192,7 @@ __device__ inline void read_raw(const Ctx &c, const uint8_t *st, int b, int n0, 
     if constexpr (FMT == QL_FMT_MXFP4)
         r.s = mx_scale(d >> (8 * (b & 3)) & 255u);
     else
-        r.s = (float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * (b & 1))));
+        r.s = plane_scale((float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * (b & 1)))));
     r.s = in ? r.s : 1.0f;
 }
 

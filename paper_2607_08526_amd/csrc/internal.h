@@ -256,8 +256,8 @@ hipError_t launch_qgemm_stream(int fmt, const StreamPlan &p, const LayerGroup &g
 
 // MXFP4 (mxquant.hip): quantization of rows * K fp32 or bf16 values, to an
 // error status (weights, fp32) or NaN scales (status nullptr: activations),
-// and code * scale of n (<= 2) tensors of a quantized format as fp32 or bf16 (lo,
-// if any: the bf16 rest of a bf16 value).
+// and code * scale of n (<= 2) tensors of a quantized format as fp32 or bf16 (q4 and
+// int8 with lo: as the two bf16 of a product, mx.h).
 hipError_t launch_mx_quantize(const void *X, bool bf16, int64_t rows, int64_t K, uint8_t *codes,
                               uint8_t *scales, int *status, hipStream_t stream);
 struct DequantJob {

@@ -53,8 +53,8 @@ __device__ inline uint32_t mx_bf16x2(uint32_t word, float scale, int w)
     return __builtin_bit_cast(uint32_t, v);
 }
 
-// fp32 weights c * s of 8 q4 codes (one word) or int8 codes (two words): exact
-// (the code has at most 8 significant bits and the scale 11)
+// fp32 weights c * s of 8 q4 codes (one word) or int8 codes (two words): exact for a
+// scale as stored (the code has at most 8 significant bits and the scale 11)
 __device__ inline void q4_f32x8(uint32_t word, float s, float (&v)[8])
 {
 #pragma unroll
@@ -68,8 +68,26 @@ __device__ inline void int8_f32x8(uint32_t w0, uint32_t w1, float s, float (&v)[
         v[e] = (float)((int32_t)((e < 4 ? w0 : w1) << (24 - 8 * (e & 3))) >> 24) * s;
 }
 
+// A q4 / int8 weight v = c * s as two bf16: hi the leading 8 bits, lo the rest
+// rounded to nearest.  Both have v's sign and neither is zero where v is not, so an
+// infinite activation meets two infinities of one sign (hi rounded to nearest leaves lo 0
+// or of the other sign: NaN).  For that s is taken one fp32 step larger: c times the
+// step is more than half a step of c * s, whose 18 bits (q4: 14) end above it, so v
+// always has bits behind hi.  Off by at most 2^-16 of c * s for int8, 2^-22 for q4.
+__device__ inline float plane_scale(float s) { return __uint_as_float(__float_as_uint(s) | 1u); }
+__device__ inline uint32_t plane_hi(float v0, float v1)
+{
+    return __builtin_amdgcn_perm(__float_as_uint(v1), __float_as_uint(v0), 0x07060302u);
+}
+__device__ inline uint32_t plane_lo(float v0, float v1)
+{
+    return mx_pack_bf16(v0 - __uint_as_float(__float_as_uint(v0) & 0xFFFF0000u),
+                        v1 - __uint_as_float(__float_as_uint(v1) & 0xFFFF0000u));
+}
+
 // word w (two k, w known at compile time) of a run of codes as bf16 planes: raw
-// holds 8 codes a word (int8: 4); MXFP4 has one plane, hi
+// holds 8 codes a word (int8: 4), s is its scale (q4, int8: its plane_scale); MXFP4 has
+// one plane, hi
 template <int FMT>
 __device__ inline void decode_word(const uint32_t *raw, int w, float s, uint32_t &hi, uint32_t &lo)
 {
@@ -87,20 +105,18 @@ __device__ inline void decode_word(const uint32_t *raw, int w, float s, uint32_t
         }
         v0 *= s;
         v1 *= s;
-        hi = mx_pack_bf16(v0, v1);
-        lo = mx_pack_bf16(v0 - __uint_as_float(hi << 16), v1 - __uint_as_float(hi & 0xFFFF0000u));
+        hi = plane_hi(v0, v1);
+        lo = plane_lo(v0, v1);
     }
 }
 
-// v as hi + lo, bf16 each and packed: |v - hi - lo| <= 2^-18 |v|
+// the planes of 8 weights c * plane_scale(s)
 __device__ inline void split2(const float (&v)[8], mx_u32x4 &hi, mx_u32x4 &lo)
 {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        const uint32_t h = mx_pack_bf16(v[2 * w], v[2 * w + 1]);
-        hi[w] = h;
-        lo[w] = mx_pack_bf16(v[2 * w] - __uint_as_float(h << 16),
-                             v[2 * w + 1] - __uint_as_float(h & 0xFFFF0000u));
+        hi[w] = plane_hi(v[2 * w], v[2 * w + 1]);
+        lo[w] = plane_lo(v[2 * w], v[2 * w + 1]);
     }
 }
 

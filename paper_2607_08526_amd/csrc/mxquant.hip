@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const void *__restrict
 }
 
 // 8 values of one block per thread: code * scale, exact in fp32 (a bf16 output
-// of q4 / int8 is rounded once, and lo, if any, receives what that leaves)
+// of q4 / int8 is rounded once; with lo, W and lo receive the two bf16 of a product)
 struct DequantArgs {
     DequantJob j[2];
 };
@@ -119,7 +119,9 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const DequantArgs a, in
             for (int e = 0; e < 8; ++e)
                 v[e] = p[e >> 1][e & 1] * s;
         } else {
-            const float s = (float)static_cast<const _Float16 *>(scales)[g >> 2];
+            float s = (float)static_cast<const _Float16 *>(scales)[g >> 2];
+            if (lo)
+                s = plane_scale(s);
             if constexpr (FMT == QL_FMT_Q4) {
                 q4_f32x8(reinterpret_cast<const uint32_t *>(codes)[g], s, v);
             } else {
@@ -129,10 +131,15 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const DequantArgs a, in
         }
         if constexpr (BF16) {
             mx_u32x4 h, l;
-            split2(v, h, l);
-            static_cast<mx_u32x4 *>(W)[g] = h;
-            if (lo)
+            if (FMT != QL_FMT_MXFP4 && lo) {
+                split2(v, h, l);
                 static_cast<mx_u32x4 *>(lo)[g] = l;
+            } else {
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    h[w] = mx_pack_bf16(v[2 * w], v[2 * w + 1]);
+            }
+            static_cast<mx_u32x4 *>(W)[g] = h;
         } else {
             f32x4_t *const o = static_cast<f32x4_t *>(W) + 2 * g;
             o[0] = f32x4_t{v[0], v[1], v[2], v[3]};

@@ -13,7 +13,8 @@
 //
 // Operand planes keep products as exact as their formats: MXFP4 values are
 // exact in bf16; a q4 / int8 weight c * s enters as two bf16 planes (off by at
-// most 2^-18 of itself); an fp32 activation as three (2^-27).  MXFP4
+// most 2^-22 / 2^-16 of itself: mx.h); an fp32 activation as three (exact but for
+// what lies below fp32's smallest normal).  MXFP4
 // activations meet MXFP4 weights in one v_mfma_scale_f32_16x16x128_f8f6f4 per
 // step, which takes codes and scale bytes as they are.
 //
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(THREADS) void qgemm_rows_kernel(const RowsGroup arg
             for (int j = 0; j < 2; ++j)
                 sc[j] = FMT == QL_FMT_MXFP4
                             ? mx_scale(wn[j].s)
-                            : (float)__builtin_bit_cast(_Float16, (uint16_t)wn[j].s);
+                            : plane_scale((float)__builtin_bit_cast(_Float16, (uint16_t)wn[j].s));
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 u32x4 xp[MT][XP];

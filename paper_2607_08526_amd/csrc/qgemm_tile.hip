@@ -5,7 +5,7 @@
 //
 // Weights become bf16 in registers: MXFP4 values are exact there (one
 // instruction turns two codes and the block's scale into two bf16), a q4 / int8
-// weight enters as the sum of two bf16 (off by at most 2^-18 of itself).  fp32
+// weight enters as the sum of two bf16 (off by at most 2^-22 / 2^-16 of itself: mx.h).  fp32
 // activations come as three bf16 planes (launch_split3), one after the other
 // along the reduction.
 //
@@ -230,7 +230,7 @@ __device__ inline void scale_value(int lane, int j, Ops<FMT, MS> &op)
     if constexpr (FMT == QL_FMT_MXFP4)
         op.sc[j] = mx_scale(d >> ((SWIDE ? 16 * (U & 1) : 0) + 8 * g) & 255u);
     else
-        op.sc[j] = (float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * g)));
+        op.sc[j] = plane_scale((float)__builtin_bit_cast(_Float16, (uint16_t)(d >> (16 * g))));
 }
 
 // word w (two k) of fragment j, chunk q

@@ -142,3 +142,88 @@ def test_rotary_far_positions(gpu, rot, interleaved):
     c, s = exact_turn(freqs, [far - 2, far - 1, far, far - 2])
     check(y[:, a], c, 2.0 ** -22, "cosine")
     check(y[:, b], s, 2.0 ** -22, "sine")
+
+
+# ---- the values that q4 and int8 weights have in the products ----------------------
+
+PLANES = {"q4": 2.0 ** -22, "int8": 2.0 ** -16, "mxfp4": 0.0}  # of a weight, at most
+
+
+def every_weight(torch, fmt):
+    """(codes, scales, 64-bit values) [1024][256]: every code with every fp16 mantissa,
+    exponents in turn (MXFP4: every code with scale bytes 97 to 160)."""
+    rng = np.random.default_rng(0)
+    N, K = 1024, 256
+    if fmt == "mxfp4":
+        c = np.tile(np.arange(16), (N, K // 16)).astype(np.uint8)
+        s = (97 + np.arange(N * (K // 32)) % 64).reshape(N, K // 32).astype(np.uint8)
+        return dev(torch, R.pack4(c)), dev(torch, s), R.mx_decode(c, s)
+    s = np.repeat(np.arange(1024, 2048) * 2.0 ** (np.arange(N) % 12 - 18.0), K // 32)
+    s = s.reshape(N, K // 32).astype(np.float16)
+    lo, hi = (-8, 8) if fmt == "q4" else (-128, 128)
+    c = np.tile(np.arange(lo, hi), (N, K // (hi - lo))).astype(np.int8)
+    c = c[:, rng.permutation(K)]
+    packed = R.pack4(c.view(np.uint8) & 15) if fmt == "q4" else c.view(np.uint8)
+    return dev(torch, packed), dev(torch, s.view(np.int16)), R.int_decode(c, s)
+
+
+@pytest.mark.parametrize("fmt", ["q4", "int8", "mxfp4"])
+@pytest.mark.parametrize("M", [1, 8, 16, 40, 256, 700, 2048, 6144])
+@pytest.mark.parametrize("narrow", [False, True])
+def test_every_weight_forward(gpu, fmt, M, narrow):
+    """Rows of the identity (and rows with an infinity in its place) against weights of
+    every code and mantissa, U = 1: H is the weight as the kernel has it, plus zeros;
+    an infinity of its sign, NaN for a zero.  narrow: K = 224, where scales of a row
+    come one by one (and short reductions)."""
+    torch, ql = gpu
+    codes, scales, W = every_weight(torch, fmt)
+    K = 224 if narrow else 256
+    if narrow:
+        codes = codes[:, :codes.shape[1] * 7 // 8].contiguous()
+        scales = scales[:, :7].contiguous()
+        W = W[:, :K]
+    zero = (torch.zeros_like(codes), torch.zeros_like(scales) + (127 if fmt == "mxfp4" else 0))
+    bias = (torch.zeros(1024, device="cuda"), torch.ones(1024, device="cuda"))
+    rng = np.random.default_rng(M)
+    k = torch.from_numpy(rng.permutation(np.arange(max(M, K)) % K)[:M]).cuda()
+    want = W.T[k.cpu().numpy()]
+    X = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    rows = torch.arange(M, device="cuda")
+    X[rows, k] = 1.0
+    # (one product, its planes and zeros: no sum rounds but the planes' own, 2^-24; the
+    # bias and the product with 1 keep it)
+    H = ql.gated_forward(fmts(ql)[fmt], X, (codes, scales), zero, bias=bias, act=ql.ACT_NONE,
+                         hdtype=torch.float32)
+    check(H, want, (PLANES[fmt] + R.F32) * np.abs(want), "weights")
+    # an infinity: both projections see it, the up projection's zeros give NaN; so the
+    # weights in both, and H = G U = infinity squared, or NaN
+    X[rows, k] = float("inf")
+    H = host(ql.gated_forward(fmts(ql)[fmt], X, (codes, scales), (codes, scales),
+                              act=ql.ACT_NONE, hdtype=torch.float32))
+    want = np.where(W == 0, np.nan, np.inf)
+    np.testing.assert_array_equal(H, want.T[k.cpu().numpy()])
+
+
+@pytest.mark.parametrize("fmt", ["q4", "int8", "mxfp4"])
+@pytest.mark.parametrize("M", [8, 107, 500, 1024])
+def test_every_weight_backward(gpu, fmt, M):
+    """dX of rows of the identity (and of infinities), G = U = 1: twice the weight as
+    the kernel has it, an infinity of its sign, NaN for a zero."""
+    torch, ql = gpu
+    codes, scales, W = every_weight(torch, fmt)
+    N, K = W.shape
+    one = torch.ones(N, device="cuda")
+    n = torch.from_numpy(np.random.default_rng(M).permutation(N)[:M]).cuda()
+    rows = torch.arange(M, device="cuda")
+    X = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    dH = torch.zeros((M, N), device="cuda")
+    pair = (codes, scales), (codes, scales)
+    call = lambda: ql.gated_backward(fmts(ql)[fmt], X, *pair, dH, bias=(one, one), act=ql.ACT_NONE,
+                                     dtype=torch.float32)
+    want = 2 * W[n.cpu().numpy()]
+    dH[rows, n] = 1.0
+    check(call().X, want, (PLANES[fmt] + 2 * R.F32) * np.abs(want), "weights")
+    dH[rows, n] = float("inf")
+    # (0 * inf: the other weights of the reduction meet zeros, not infinities)
+    with np.errstate(invalid="ignore"):
+        np.testing.assert_array_equal(host(call().X), np.inf * want)
