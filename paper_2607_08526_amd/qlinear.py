@@ -712,8 +712,10 @@ def gated_backward(fmt, X, gate, up, dH, bias=None, act=ACT_SILU, x_grad=True,
                    weight_grads=False, bias_grads=False, dtype=torch.bfloat16, stream=None):
     """The backward pass of gated_forward (its arguments) from dH [M][N], fp32 or
     bf16: GatedGrads, X's and the weights' of `dtype` (fp32 or bf16), the biases'
-    fp32.  The gradients of weights are those of their values (adapters on frozen
-    weights take `gate` and `up` instead).  N % 8 == 0.  Asynchronous."""
+    fp32.  `gate` and `up` are rounded to bf16, and the other gradients are formed
+    from them so, with fp32 sums, whatever dH's dtype and `dtype` are.  The gradients
+    of weights are those of their values (adapters on frozen weights take `gate` and
+    `up` instead).  N % 8 == 0.  Asynchronous."""
     g, M, K, N, tensors = _gated(fmt, X, gate, up, bias, act)
     _require(dH, "dH", (torch.float32, torch.bfloat16), (M, N))
     if dtype not in (torch.float32, torch.bfloat16):
