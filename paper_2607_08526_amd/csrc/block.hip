@@ -116,9 +116,58 @@ int launch_gated(const ql_gated &g, const GateArgs &t, hipStream_t stream)
 // / 24.8; q4 107 rows 25.2 / 23.6, 400 rows 32.2 / 35.0.
 constexpr GemmCost DX_COST[2][2] = {{{0.55, 0.55}, {0.45, 0.40}}, {{1.0, 1.0}, {0.87, 0.87}}};
 
+// gemm_bf16's by rows of a tile (128, 64), fitted to 78 products in 1 to 8 parts of both
+// (the choice takes 1.015 times the best one's time on average, 1.05 at the ninth decile).
+// Measured, us in 128 / 64 rows: dW 2048 rows of 2048 x 1024 38.5 / 29.5, of 4096 x 1536
+// 54.4 / 64.2, of 5504 x 2048 96 / 113; dX 2048 rows of 1024 x 1024 33.0 / 31.0; and in 2 /
+// 5 parts of 128 rows dX 2048 rows of 4096 x 1536 81.9 / 72.2.
+constexpr GemmCost BF16_COST[2] = {{0.48, 0.38}, {0.34, 0.25}};
+
+// the rows of a tile and the parts estimated to be fastest for outputs R x S of a
+// reduction of C; cost: of tiles of 128 and 64 rows
+void gemm_plan(int64_t R, int64_t S, int64_t C, int problems, const GemmCost *cost, int cus,
+               int &rows, int &parts)
+{
+    constexpr int64_t PART_BYTES = (int64_t)256 << 20;  // of partial sums
+    double best = 0.0;
+    for (int h = 0; h < 2; ++h) {
+        const int tile = h ? 64 : 128;
+        double us;
+        const int64_t p = gemm_parts(gemm_tiles(tile, R, S) * problems, R * problems, S, C,
+                                     cost[h], cus, &us);
+        if (h == 0 || us < best) {
+            best = us;
+            rows = tile;
+            parts = (int)std::max<int64_t>(1, std::min(p, PART_BYTES / (problems * R * S * 4)));
+        }
+    }
+}
+
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 }  // namespace
+
+namespace qlk {
+
+GradPlan grad_plan(int fmt, int64_t M, int64_t N, int64_t K, const void *scales0,
+                   const void *scales1, bool dx, bool dw, int cus)
+{
+    GradPlan g{false, 1, 128, 1, 128};
+    const int planes = fmt == QL_FMT_MXFP4 ? 1 : 2;
+    // dX straight from the compressed weights up to a few hundred rows, beyond from
+    // a bf16 copy (us of dX at N = 4096, mxfp4 / q4: 128 rows of K = 1536 21.9 / 27.8
+    // against 28.8 / 36.0, 1024 rows of K = 2048 61.6 / 89.2 against 58.2 / 90.6)
+    g.direct = M <= 512 && dx_takes(K, scales0, scales1);
+    if (dx && g.direct)
+        gemm_plan(M, K, 2 * N, 1, DX_COST[planes - 1], cus, g.xrows, g.xparts);
+    else if (dx)
+        gemm_plan(M, K, 2 * planes * N, 1, BF16_COST, cus, g.xrows, g.xparts);
+    if (dw)
+        gemm_plan(N, K, M, 2, BF16_COST, cus, g.wrows, g.wparts);
+    return g;
+}
+
+}  // namespace qlk
 
 extern "C" {
 
@@ -264,44 +313,11 @@ int qlinear_gated_backward(const ql_gated *g, const ql_gated_grad *d, hipStream_
     // workspace: both weights in bf16 (q4, int8: two planes each) where dX is not formed
     // from the compressed ones, then the larger of the products' partial sums (the
     // products run one after the other)
-    constexpr size_t PART_BYTES = (size_t)256 << 20;
-    auto parts = [&](int rows, int64_t R, int64_t S, int64_t C, int problems, GemmCost cost,
-                     double *us = nullptr) {
-        const int p = gemm_parts(gemm_tiles(rows, R, S) * problems, R * problems, S, C, cost, cus, us);
-        const size_t one = (size_t)problems * R * S * 4;
-        return (int)std::max<int64_t>(1, std::min<int64_t>(p, (int64_t)(PART_BYTES / one)));
-    };
-    // tiles of 128 or 64 rows of the bf16 products (us, 2048 rows: dW of 2048 x 1024
-    // 38.4 / 27.0, of 4096 x 1536 56.7 / 59.5, of 5504 x 2048 100 / 112; dX of 1024 x 1024
-    // 32.1 / 29.5)
-    auto gemm_plan = [&](int64_t R, int64_t S, int64_t C, int problems, int &rows, int &p) {
-        double us[2];
-        p = parts(128, R, S, C, problems, GemmCost{0.47, 0.43}, &us[0]);
-        const int p64 = parts(64, R, S, C, problems, GemmCost{0.31, 0.28}, &us[1]);
-        rows = us[1] < us[0] ? 64 : 128;
-        if (rows == 64)
-            p = p64;
-    };
     const int planes = g->fmt == QL_FMT_MXFP4 ? 1 : 2;
-    // dX straight from the compressed weights up to a few hundred rows, beyond from
-    // a bf16 copy (us of dX at N = 4096, mxfp4 / q4: 128 rows of K = 1536 21.9 / 27.8
-    // against 28.8 / 36.0, 1024 rows of K = 2048 61.6 / 89.2 against 58.2 / 90.6)
-    const bool direct = M <= 512 && dx_takes(K, g->gate_scales, g->up_scales);
-    int px = 1, xrows = 128;
-    if (want_x && direct) {
-        // tiles of 128 or 64 rows
-        double us[2];
-        const int p128 = parts(128, M, K, 2 * N, 1, DX_COST[planes - 1][0], &us[0]);
-        const int p64 = parts(64, M, K, 2 * N, 1, DX_COST[planes - 1][1], &us[1]);
-        const bool small = us[1] < us[0];
-        xrows = small ? 64 : 128;
-        px = small ? p64 : p128;
-    } else if (want_x) {
-        gemm_plan(M, K, 2 * planes * N, 1, xrows, px);
-    }
-    int pw = 1, wrows = 128;
-    if (d->dWg)
-        gemm_plan(N, K, M, 2, wrows, pw);
+    const GradPlan plan = grad_plan(g->fmt, M, N, K, g->gate_scales, g->up_scales, want_x,
+                                    d->dWg != nullptr, cus);
+    const bool direct = plan.direct;
+    const int px = plan.xparts, xrows = plan.xrows, pw = plan.wparts, wrows = plan.wrows;
     const size_t plane = want_x && !direct ? round256((size_t)N * K * 2) : 0;
     const size_t wbytes = 2 * planes * plane;
     const size_t part_bytes = std::max(px > 1 ? (size_t)px * M * K * 4 : 0,

@@ -355,6 +355,7 @@ struct Mx4Args {
 bool mx4_takes(const Mx4Args &a);
 int64_t mx4_tiles(const Mx4Args &a, int rows);
 bool mx4_wins(const Mx4Args &a, int cus);
+int mx4_rows(const Mx4Args &a, int cus);  // of a tile: 128 or 64
 hipError_t launch_qgemm_mx4(const Mx4Args &a, hipStream_t stream);
 
 // bf16 products of the backward pass (gemm_bf16.hip): out[R][S] of a problem,
@@ -397,6 +398,14 @@ struct DxArgs {
 };
 bool dx_takes(int64_t K, const void *scales0, const void *scales1);
 hipError_t launch_gemm_dx(int fmt, const DxArgs &a, hipStream_t stream);
+// How a gated pair's backward pass forms dX (direct: gemm_dx, otherwise gemm_bf16) and
+// dW: rows of a tile and parts of the reduction (block.hip)
+struct GradPlan {
+    bool direct;
+    int xparts, xrows, wparts, wrows;
+};
+GradPlan grad_plan(int fmt, int64_t M, int64_t N, int64_t K, const void *scales0,
+                   const void *scales1, bool dx, bool dw, int cus);
 // dbg, dbu (each may be nullptr): column sums of dG, dU [M][N], N % 8 == 0
 hipError_t launch_column_sums(const uint16_t *dG, const uint16_t *dU, float *dbg, float *dbu, int M,
                               int N, hipStream_t stream);

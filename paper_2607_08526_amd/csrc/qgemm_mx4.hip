@@ -265,7 +265,7 @@ static double mx4_us(const Mx4Args &a, int rows, int cus)
            epi * rows / 128 * std::max(1.0, std::min(r, 2.0));
 }
 
-static int mx4_rows(const Mx4Args &a, int cus)
+int mx4_rows(const Mx4Args &a, int cus)
 {
     return mx4_us(a, 64, cus) < mx4_us(a, 128, cus) ? 64 : 128;
 }
