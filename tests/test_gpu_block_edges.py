@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 import block_ref as R
-from test_gpu_block import acts, bf16, check, dev, fmts, gated_case, host
+from test_gpu_block import check, dev, fmts, gated_case, host
 
 pytestmark = pytest.mark.gpu
 
