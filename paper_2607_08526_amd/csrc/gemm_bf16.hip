@@ -26,10 +26,12 @@
 // Few tiles: the reduction is cut into parts whose fp32 sums another launch
 // adds in order (split_sum_kernel).
 //
-// Bound: the matrix cores at the power limit's clock while two workgroups share a CU,
-// then the tail.  2048 rows, N = 4096, K = 1536 (51.5 Gflop each): dX 56 us in 5 parts
-// (480 workgroups) and 15 us for their sum, dW 59 us (384 workgroups on 512 places, a
-// quarter of them idle).
+// Bound: the issue of matrix instructions.  While a CU holds a workgroup its matrix cores
+// are busy 0.56 (dX) and 0.51 (dW) of the cycles, its LDS 0.24; wavefronts wait 0.45 of
+// theirs for an instruction's unit, 0.22 for data or a barrier.  Then the clock (1.75 GHz of
+// 2.4 in a run of 32768 rows, where the cores are busy 0.61 to 0.64) and the tail.  2048
+// rows, N = 4096, K = 1536 (51.5 Gflop each): dX 53.5 us in 5 parts (480 workgroups) and
+// 14.7 us for their sum, dW 59.6 us (384 workgroups on 512 places, a quarter of them idle).
 #include <algorithm>
 
 #include "dma.h"
@@ -303,7 +305,8 @@ __global__ __launch_bounds__(THREADS, NST > 4 ? 1 : 2) void gemm_bf16_kernel(con
 
 // Column sums of bf16 matrices [M][N] (bias gradients), in a fixed order: a
 // workgroup owns 64 columns of one, its threads rows t / 8, t / 8 + 32, ... of 8
-// columns each, added up in LDS.
+// columns each, added up in LDS.  Bound: the latency of M / 32 dependent rows a thread, on
+// half of the CUs: 2048 x 4096 of both 23 us (33.6 MB, 6.6 us of a copy).
 __global__ __launch_bounds__(256) void column_sums_kernel(const uint16_t *dG, const uint16_t *dU,
                                                           float *dbg, float *dbu, int M, int N)
 {

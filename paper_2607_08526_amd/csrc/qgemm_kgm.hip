@@ -27,7 +27,9 @@
 // Bound: latency of a launch, a first stage and the sums (about 5 us) at few rows,
 // then the decoding beside the MFMAs.  6144 x 1536: one row 5.4 us, 128 rows 9.0, 256
 // rows 12.4; fp32 1000 x 1056 at 77 rows 8.9 us; a q4 pair of 2752 x 1024 at 107 rows
-// with both gradients 13.0 us.
+// with both gradients 12.6 us.  A launch holds all shapes of its rows, with the registers
+// and LDS of the largest; pairs of more than 32 rows spill (MXFP4 4 registers, int8 22,
+// q4 28: the 64-row shapes at 128 registers, 16 wavefronts).
 #include <algorithm>
 #include <cmath>
 

@@ -34,12 +34,16 @@
 // codes).  Steps that K leaves unfilled, and those that fill up the loop's rounds,
 // come from a page of zeros.
 //
-// Bound: the matrix cores at the clock that the power limit leaves (0.44 to 0.48 of
-// all cycles busy), and at the end of a tile, where every CU is there at once, the
-// VALU of the activation and the stores.  2048 rows x 8192 x 2048 with GELU, bf16
-// output: 65 to 67 us, 1.03 to 1.06 PFLOP/s (a library product of 8192^3 bf16 1.5);
-// gated pair 2048 x 5504 x 2048 with SiLU: 80 to 84 us, 1.10 to 1.16 PFLOP/s, 688
-// tiles on 512 places.
+// Bound: the issue of matrix and vector instructions.  While a CU holds a workgroup its
+// matrix cores are busy 0.53 (products) to 0.62 (pairs) of the cycles; wavefronts wait
+// 0.45 of theirs for an instruction's unit, 0.11 to 0.23 for data or a barrier.  Then the
+// clock (1.6 GHz of 2.4 in a run of 32768 rows), and at the end of a tile, where every CU
+// is there at once, the VALU of the activation and the stores.  2048 rows x 8192 x 2048
+// with GELU, bf16 output: 65 to 67 us, 1.03 to 1.06 PFLOP/s (a library product of 8192^3
+// bf16 1.5); gated pair 2048 x 5504 x 2048 with SiLU: 80 to 84 us, 1.10 to 1.16 PFLOP/s,
+// 688 tiles on 512 places; of q4 174 and of int8 170 us (two planes: twice the matrix
+// instructions).  The 128-row tiles of int8 spill 28 registers (67 with scales one by
+// one), of q4 47 with scales one by one.
 #include <algorithm>
 #include <cmath>
 
