@@ -100,9 +100,9 @@
  *     on a stream keeps that stream's buffer (it is then never released
  *     before the process ends), so replays of the graph must not overlap
  *     calls on the capture stream or replays of other graphs captured on
- *     it.  A call under
- *     capture that needs more than its stream's buffer allocates for itself
- *     from the pool (allocation and free nodes in the graph) instead.  A
+ *     it.  A call under capture that needs more than its stream's buffer
+ *     allocates for itself from the pool (allocation and free nodes in the
+ *     graph) instead, and so does every call on hipStreamPerThread.  A
  *     destroyed stream's handle value, if reused, inherits its buffer.  fp32
  *     activations of large MXFP4 products (QL_FMT_MXFP4) take up to 120 MiB
  *     for three bf16 planes of a slice of their rows (768 K bytes where 128

@@ -132,7 +132,8 @@ size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 // stream order, when a call outside graph capture needs more; the old one is
 // returned to the pool unless a graph was captured with it, in which case it
 // stays allocated for the life of the process (replays still use it).  A
-// call under capture that needs more than the stream's buffer takes a
+// call under capture that needs more than the stream's buffer, or any call on
+// hipStreamPerThread (one handle for a stream of each thread), takes a
 // stream-ordered allocation for itself (freed after its launch) instead.
 // Stream order protects the buffer only while a call's launches stand together
 // in it, so the call holds the buffer's lock until they are enqueued: another
@@ -166,6 +167,15 @@ bool take_workspace(size_t bytes, hipStream_t stream, Workspace &w)
     hipMemPool_t pool = workspace_pool();
     if (!pool)
         return false;
+    auto for_itself = [&] {
+        void *p = nullptr;
+        if (hipMallocFromPoolAsync(&p, bytes, pool, stream) != hipSuccess)
+            return false;
+        w = Workspace{(uint8_t *)p, true, {}};
+        return true;
+    };
+    if (stream == hipStreamPerThread)
+        return for_itself();
     Entry *e = nullptr;
     {
         std::lock_guard<std::mutex> g(mu);
@@ -184,13 +194,9 @@ bool take_workspace(size_t bytes, hipStream_t stream, Workspace &w)
         w = Workspace{(uint8_t *)e->ptr, false, std::move(turn)};
         return true;
     }
+    if (capturing)
+        return for_itself();
     void *p = nullptr;
-    if (capturing) {
-        if (hipMallocFromPoolAsync(&p, bytes, pool, stream) != hipSuccess)
-            return false;
-        w = Workspace{(uint8_t *)p, true, {}};
-        return true;
-    }
     const size_t grow = ((std::max(bytes, e->bytes + e->bytes / 2)) + ((size_t)1 << 21) - 1) &
                         ~(((size_t)1 << 21) - 1);
     if (hipMallocFromPoolAsync(&p, grow, pool, stream) != hipSuccess)

@@ -1,5 +1,6 @@
 """The operators of include/qlinear_block.h where calls meet each other or the
 ends of their ranges: threads on one stream, infinite activations, far positions."""
+import ctypes
 import threading
 
 import numpy as np
@@ -227,3 +228,46 @@ def test_every_weight_backward(gpu, fmt, M):
     # (0 * inf: the other weights of the reduction meet zeros, not infinities)
     with np.errstate(invalid="ignore"):
         np.testing.assert_array_equal(host(call().X), np.inf * want)
+
+
+def test_stream_per_thread(gpu):
+    """hipStreamPerThread is one handle for a stream of each thread: calls of several
+    threads on it do not share a workspace."""
+    torch, ql = gpu
+
+    class PerThread:
+        cuda_stream = 2  # hipStreamPerThread
+
+    calls = []
+    for fmt, M, N, K, seed in (("q4", 40, 1024, 384, 1), ("int8", 700, 1024, 256, 2),
+                               ("mxfp4", 600, 2048, 512, 3)):
+        rng, Xb, _, pair, _, _, _ = gated_case(torch, fmt, M, N, K, seed, False)
+        dH = dev(torch, rng.standard_normal((M, N)).astype(np.float32))
+        both = torch.empty((2, M, N), dtype=torch.bfloat16, device="cuda")
+        dX = torch.empty((M, K), dtype=torch.bfloat16, device="cuda")
+        g, _, _, _, keep = ql._gated(fmts(ql)[fmt], Xb, *pair, None, ql.ACT_SILU)
+        d = ql._GatedGrad(dH.data_ptr(), ql.DT_F32, both[0].data_ptr(), both[1].data_ptr(),
+                          dX.data_ptr(), ql.DT_BF16, None, None, 0, None, None)
+        calls.append((g, d, dX, (keep, dH, both),
+                      ql.gated_backward(fmts(ql)[fmt], Xb, *pair, dH).X))
+    torch.cuda.synchronize()
+    fails = []
+    lib = ql.load()
+
+    def work(k):
+        g, d, dX, _, want = calls[k]
+        torch.cuda.set_device(0)
+        for _ in range(40):
+            if lib.qlinear_gated_backward(ctypes.byref(g), ctypes.byref(d),
+                                          ql._stream(PerThread())) != 0:
+                fails.append((k, "status"))
+            torch.cuda.synchronize()
+            if not torch.equal(dX, want):
+                fails.append(k)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not fails
