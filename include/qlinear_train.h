@@ -1,0 +1,90 @@
+/*
+ * qlinear_train.h — the normalisation and the masked attention of a transformer
+ * block, each with its backward pass (qlinear.h's conventions apply to every function
+ * here; the linears are there, the gated feed-forward and rotary positions in
+ * qlinear_block.h).
+ */
+#ifndef QLINEAR_TRAIN_H
+#define QLINEAR_TRAIN_H
+
+#include "qlinear.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- normalisation ----------------------------------------------------------
+ *
+ * A block's root-mean-square normalisation with the residual's addition: by row,
+ *
+ *     v = x + res                       one fp32 rounding (res NULL: v = x)
+ *     h = v                             the new residual stream, in res's dtype
+ *     y = v weight / sqrt(mean(v^2) + eps)
+ *
+ * x, res, h and y: rows of ldx, ldr, ldh, ldy >= N elements, fp32 or bf16 (h as res:
+ * rdt, also where res is NULL), aligned to an element.  weight fp32 [N] or NULL (ones).
+ * y is formed from v before its rounding to h's dtype, as the fp32 nearest to the
+ * exact value (a few fp64 roundings off a tie), for bf16 rounded again.  qx int8
+ * [M][N], sx fp16 [M]: the int8 activations of qlinear_forward_w8a8, as
+ * qlinear_quantize_act gives them for the fp32 y (N % 32 == 0, qx 16-byte aligned).
+ * h, y, and qx with sx may each be NULL, not all.  h or y may be x or res in place
+ * (same address, dtype and ld); no output shares elements with another argument
+ * otherwise (QL_ERR_INVALID; other columns of the same rows may be).  eps >= 0.
+ * N <= 16384, M < 2^24 (QL_ERR_UNSUPPORTED).  Asynchronous; M == 0 is a no-op. */
+typedef struct {
+    const void *x;
+    int64_t ldx;
+    int xdt;                     /* ql_dtype */
+    const void *res;
+    int64_t ldr;
+    int rdt;                     /* of res and h */
+    const float *weight;
+    double eps;
+    int64_t M, N;
+    void *h;
+    int64_t ldh;
+    void *y;
+    int64_t ldy;
+    int ydt;
+    int8_t *qx;
+    uint16_t *sx;
+} ql_norm;
+
+int qlinear_rms_norm(const ql_norm *n, hipStream_t stream);
+
+/* Its backward pass from dy, the gradient of y, and h, the normalised values (the v
+ * above, or their rounding that was kept):
+ *
+ *     dx = dres + r (g - u mean(g u)),  dw = sum over rows of dy u,
+ *          r = 1 / sqrt(mean(h^2) + eps),  u = h r,  g = dy weight
+ *
+ * dx, the gradient of x and of res alike; dres: the one that arrives at h from further
+ * on (NULL: 0), of dx's dtype.  dw fp32 [N] or NULL.  dx may be dy, h or dres in place
+ * (same address, dtype and ld); other conventions as above.  Sums of a row in
+ * fp64, of dw in fp32 in one fixed order.  Workspace with dw (per stream, as in
+ * qlinear.h): at most 8 N bytes per CU.  M == 0 writes zeros to dw and nothing else. */
+typedef struct {
+    const void *dy;
+    int64_t lddy;
+    int dydt;                    /* ql_dtype */
+    const void *h;
+    int64_t ldh;
+    int hdt;
+    const void *dres;
+    int64_t lddres;
+    const float *weight;
+    double eps;
+    int64_t M, N;
+    void *dx;
+    int64_t lddx;
+    int dxdt;                    /* of dx and dres */
+    float *dw;
+} ql_norm_grad;
+
+int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* QLINEAR_TRAIN_H */

@@ -17,7 +17,7 @@ SOURCES = ["qlinear.hip", "quantize.hip", "qgemm.hip", "qgemm_wide.hip", "qgemm_
            "qgemm_w8a8.hip", "steer.hip", "attention.hip", "qgemm_mid.hip",
            "qgemm_kg.hip", "block.hip", "mxquant.hip", "rotary.hip", "qgemm_rows.hip",
            "gemm_bf16.hip", "qgemm_tile.hip",
-           "qgemm_mx4.hip", "gemm_dx.hip", "qgemm_kgm.hip"]
+           "qgemm_mx4.hip", "gemm_dx.hip", "qgemm_kgm.hip", "norm.hip", "train.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -286,6 +286,39 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(RotaryArgs a, int cus, hipStream_t stream);
 
+// Root-mean-square normalisation (norm.hip): v = x + res (res may be nullptr), h = v
+// (its dtype is res's), y = v rstd weight, and act_quant's qx, sx of y; each output may
+// be nullptr.  N <= NORM_MAX_N, M <= MAX_WORKGROUPS; N % 32 == 0 with qx.
+constexpr int NORM_MAX_N = 16384;
+struct NormArgs {
+    const void *x, *res;
+    int64_t ldx, ldr, M;
+    int N;
+    int xbf16, hbf16, ybf16;
+    const float *weight;  // [N] or nullptr
+    double eps, inv_n;    // inv_n: 1 / N
+    void *h, *y;
+    int64_t ldh, ldy;
+    int8_t *qx;    // [M][N], 8-byte aligned
+    uint16_t *sx;  // [M]
+};
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream);
+// Its backward pass: dx = dres (or nullptr: 0) + the gradient of h from dy, and dw
+// (with part: fp32 [parts][N], parts of norm_grad_parts).
+struct NormGradArgs {
+    const void *dy, *h, *dres;
+    int64_t lddy, ldh, ldres, M;
+    int N;
+    int ybf16, hbf16, dbf16;
+    const float *weight;
+    double eps, inv_n;
+    void *dx;  // dres's dtype
+    int64_t lddx;
+    float *part, *dw;
+};
+int norm_grad_parts(int64_t M, int N, int cus);
+hipError_t launch_norm_grad(const NormGradArgs &a, int parts, hipStream_t stream);
+
 // The outputs of a gated pair (gated.h): H, or with dG the gradients of both
 // projections.
 struct GateArgs {

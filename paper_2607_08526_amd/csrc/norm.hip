@@ -1,0 +1,437 @@
+// Root-mean-square normalisation with the residual's addition, and its backward pass.
+//
+//   v = x + r (one fp32 rounding),  rstd = 1 / sqrt(mean v^2 + eps),  y = v rstd w
+//   dv = dres + rstd (g - u mean(g u)),  dw = sum over rows of dy u,
+//        with g = dy w and u = v rstd
+//
+// The squares are summed and the scalars of a row formed in fp64: a square of an
+// fp32 value is exact there and neither overflows nor underflows, so rows of any
+// size are right.  y is the product in fp64 rounded once to fp32 and then, for bf16
+// outputs, to bf16; the int8 outputs are act_quant's of that fp32 y (codes.h), so
+// they do not depend on an order of roundings.  fp64 costs nothing here: seven such
+// instructions per value against 10 to 14 bytes of HBM.
+//
+// Bound: HBM; at few rows the latency of one load and of the row's reduction.  A
+// row's values stay in registers between the sum and the output (W wavefronts of
+// R groups of 8 columns per lane), so each is read once.
+#include "codes.h"
+#include "internal.h"
+
+namespace qlk {
+namespace {
+
+// groups of 8 values at any element address (the hardware takes unaligned vectors)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
+
+__device__ inline uint32_t bf16_bits(float f)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+
+// values 8 g .. 8 g + 7 of a row (n of them; those past the row's end are 0)
+template <bool BF16>
+__device__ inline void load8(const void *p, int64_t e, int n, float (&v)[8])
+{
+    if constexpr (BF16) {
+        const uint16_t *q = static_cast<const uint16_t *>(p) + e;
+        if (n >= 8) {
+            const u32x4 a = *reinterpret_cast<const u32x4_at2 *>(q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = __uint_as_float(a[j] << 16);
+                v[2 * j + 1] = __uint_as_float(a[j] & 0xFFFF0000u);
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = j < n ? __uint_as_float((uint32_t)q[j] << 16) : 0.0f;
+    } else {
+        const float *q = static_cast<const float *>(p) + e;
+        if (n >= 8) {
+            const f32x4 a = *reinterpret_cast<const f32x4_at4 *>(q);
+            const f32x4 b = *reinterpret_cast<const f32x4_at4 *>(q + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = a[j];
+                v[4 + j] = b[j];
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = j < n ? q[j] : 0.0f;
+    }
+}
+
+__device__ inline void store8(void *p, bool bf16, int64_t e, int n, const float (&v)[8])
+{
+    if (bf16) {
+        uint16_t *q = static_cast<uint16_t *>(p) + e;
+        if (n >= 8) {
+            u32x4 a;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                a[j] = bf16_bits(v[2 * j]) | bf16_bits(v[2 * j + 1]) << 16;
+            *reinterpret_cast<u32x4_at2 *>(q) = a;
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n)
+                q[j] = (uint16_t)bf16_bits(v[j]);
+    } else {
+        float *q = static_cast<float *>(p) + e;
+        if (n >= 8) {
+            *reinterpret_cast<f32x4_at4 *>(q) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4_at4 *>(q + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n)
+                q[j] = v[j];
+    }
+}
+
+__device__ inline double wave_sum(double s)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1)
+        s += __shfl_xor(s, o);
+    return s;
+}
+
+// 1 / sqrt(x) for x >= 0: the hardware's estimate (2^-26 or better) and two Newton steps;
+// 0, infinities and NaN as the estimate has them
+__device__ inline double inverse_sqrt(double x)
+{
+    double r = __builtin_amdgcn_rsq(x);
+    if (x > 0.0 && x < __builtin_inf()) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            r = __builtin_fma(0.5 * r, __builtin_fma(-x * r, r, 1.0), r);
+    }
+    return r;
+}
+
+// rows per workgroup and threads of it, for W wavefronts a row
+template <int W>
+constexpr int ROWS = W >= 4 ? 1 : 4 / W;
+template <int W>
+constexpr int THREADS = 64 * W * ROWS<W>;
+
+template <bool XB, bool HB, int W, int R>
+__global__ __launch_bounds__(THREADS<W>) void norm_kernel(const NormArgs a)
+{
+    constexpr int T = 64 * W;
+    __shared__ double ssum[W];
+    __shared__ uint32_t smax[W];
+    const int t = (int)threadIdx.x % T, wave = t >> 6;
+    const int64_t m = (int64_t)blockIdx.x * ROWS<W> + (int)threadIdx.x / T;
+    if (W < 4 && m >= a.M)
+        return;  // (a wavefront of its own: no barrier below)
+    const int N = a.N;
+    float v[R][8];
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int c = 8 * (t + i * T), n = N - c;
+        float r[8];
+        load8<XB>(a.x, m * a.ldx + c, n, v[i]);
+        if (a.res) {
+            load8<HB>(a.res, m * a.ldr + c, n, r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[i][j] += r[j];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int c = 8 * (t + i * T);
+        if (a.h)
+            store8(a.h, HB, m * a.ldh + c, N - c, v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            s = __builtin_fma((double)v[i][j], (double)v[i][j], s);
+    }
+    s = wave_sum(s);
+    if constexpr (W > 1) {
+        if ((t & 63) == 0)
+            ssum[wave] = s;
+        __syncthreads();
+        s = 0.0;
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            s += ssum[w];
+    }
+    const double rstd = inverse_sqrt(__builtin_fma(s, a.inv_n, a.eps));
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int c = 8 * (t + i * T), n = N - c;
+        float w[8];
+        if (a.weight)
+            load8<false>(a.weight, c, n, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double u = (double)v[i][j] * rstd;
+            v[i][j] = (float)(a.weight ? u * (double)w[j] : u);
+        }
+        if (a.y)
+            store8(a.y, a.ybf16, m * a.ldy + c, n, v[i]);
+    }
+    if (!a.qx)
+        return;
+
+    // act_quant's scale and codes of the row (|y| bit patterns compare like the
+    // values; columns past the row's end are 0, or NaN where rstd is infinite: out)
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b = __float_as_uint(v[i][j]) & 0x7FFFFFFFu;
+            if (8 * (t + i * T) < N)
+                amax = b > amax ? b : amax;
+        }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t b = (uint32_t)__shfl_xor((int)amax, o);
+        amax = b > amax ? b : amax;
+    }
+    if constexpr (W > 1) {
+        if ((t & 63) == 0)
+            smax[wave] = amax;
+        __syncthreads();
+        amax = smax[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w)
+            amax = smax[w] > amax ? smax[w] : amax;
+    }
+    uint32_t sbits = 0x7C00;
+    if (amax < 0x7F800000u)
+        sbits = scale_bits<127>(__uint_as_float(amax));
+    const bool zero = sbits == 0x7C00 || sbits == 0;
+    if (t == 0)
+        a.sx[m] = (uint16_t)(sbits == 0x7C00 ? 0x7E00 : sbits);
+    const float sc = zero ? 1.0f : f16_value(sbits);
+    const float inv = inverse(sc), half_s = 0.5f * sc;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int c = 8 * (t + i * T);
+        if (c >= N)  // N % 32 == 0
+            continue;
+        uint32_t q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            q[j] = zero ? 0u : (uint32_t)nearest_code(v[i][j], sc, inv, half_s, 127) & 0xFFu;
+        *reinterpret_cast<uint2 *>(a.qx + m * N + c) =
+            make_uint2(q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24,
+                       q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24);
+    }
+}
+
+// Each workgroup takes every gridDim.x-th row (ROWS of them at a time) and adds up
+// its rows' dy u by columns; those sums go to part[workgroup][N], added in that order
+// by norm_dw_kernel, so that dw has one order of additions.
+template <bool YB, bool HB, bool DB, int W, int R>
+__global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArgs a)
+{
+    constexpr int T = 64 * W;
+    __shared__ double sums[2][W][2];
+    __shared__ float shared_dw[W < 4 ? THREADS<W> : 1][8];
+    const int t = (int)threadIdx.x % T, wave = t >> 6;
+    const int N = a.N;
+    float dw[R][8];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            dw[i][j] = 0.0f;
+    int turn = 0;
+    for (int64_t m = (int64_t)blockIdx.x * ROWS<W> + (int)threadIdx.x / T; m < a.M;
+         m += (int64_t)gridDim.x * ROWS<W>, turn ^= 1) {
+        float v[R][8], dy[R][8], w[R][8];
+        double s = 0.0, p = 0.0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int c = 8 * (t + i * T), n = N - c;
+            load8<HB>(a.h, m * a.ldh + c, n, v[i]);
+            load8<YB>(a.dy, m * a.lddy + c, n, dy[i]);
+            if (a.weight)
+                load8<false>(a.weight, c, n, w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const double x = v[i][j], g = a.weight ? (double)dy[i][j] * (double)w[i][j]
+                                                       : (double)dy[i][j];
+                s = __builtin_fma(x, x, s);
+                p = __builtin_fma(x, g, p);
+            }
+        s = wave_sum(s);
+        p = wave_sum(p);
+        if constexpr (W > 1) {
+            // (two turns' places: a wavefront that is a row ahead writes the other)
+            if ((t & 63) == 0) {
+                sums[turn][wave][0] = s;
+                sums[turn][wave][1] = p;
+            }
+            __syncthreads();
+            s = p = 0.0;
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                s += sums[turn][k][0];
+                p += sums[turn][k][1];
+            }
+        }
+        const double rstd = inverse_sqrt(__builtin_fma(s, a.inv_n, a.eps));
+        const double mean = p * rstd * a.inv_n;  // of g u
+        const float r32 = (float)rstd, k32 = (float)(mean * rstd);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int c = 8 * (t + i * T), n = N - c;
+            float d[8], out[8];
+            if (a.dres)
+                load8<DB>(a.dres, m * a.ldres + c, n, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float u = v[i][j] * r32, g = a.weight ? dy[i][j] * w[i][j] : dy[i][j];
+                const float o = __builtin_fmaf(g, r32, -u * k32);
+                out[j] = a.dres ? d[j] + o : o;
+                dw[i][j] = __builtin_fmaf(dy[i][j], u, dw[i][j]);
+            }
+            store8(a.dx, DB, m * a.lddx + c, n, out);
+        }
+    }
+    if (!a.part)
+        return;
+    if constexpr (W < 4) {  // the rows that ran beside each other
+        static_assert(R == 1 && W == 1, "");
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            shared_dw[threadIdx.x][j] = dw[0][j];
+        __syncthreads();
+        if (threadIdx.x >= T)
+            return;
+        for (int k = 1; k < ROWS<W>; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                dw[0][j] += shared_dw[k * T + t][j];
+    }
+    float *const part = a.part + (int64_t)blockIdx.x * N;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int c = 8 * (t + i * T);
+        store8(part, false, c, N - c, dw[i]);
+    }
+}
+
+// dw[c] = the sum of part[0 .. parts)[c]: 64 columns a workgroup, every 16th part a
+// wavefront
+__global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, int parts, int N,
+                                                       float *dw)
+{
+    __shared__ float sums[16][64];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const int c = (int)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (c < N) {
+#pragma unroll 8
+        for (int p = wave; p < parts; p += 16)
+            s += part[(int64_t)p * N + c];
+    }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave || c >= N)
+        return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w)
+        s += sums[w][lane];
+    dw[c] = s;
+}
+
+template <bool XB, bool HB>
+void forward(const NormArgs &a, hipStream_t s)
+{
+#define QL_GO(W, R)                                                                          \
+    hipLaunchKernelGGL((norm_kernel<XB, HB, W, R>),                                          \
+                       dim3((unsigned)((a.M + ROWS<W> - 1) / ROWS<W>)), dim3(THREADS<W>), 0, s, a)
+    if (a.N <= 512)
+        QL_GO(1, 1);
+    else if (a.N <= 2048)
+        QL_GO(4, 1);
+    else if (a.N <= 4096)
+        QL_GO(4, 2);
+    else if (a.N <= 8192)
+        QL_GO(8, 2);
+    else
+        QL_GO(16, 2);
+#undef QL_GO
+}
+
+template <bool YB, bool HB, bool DB>
+void backward(const NormGradArgs &a, int parts, hipStream_t s)
+{
+#define QL_GO(W, R)                                                                         \
+    hipLaunchKernelGGL((norm_grad_kernel<YB, HB, DB, W, R>), dim3((unsigned)parts),         \
+                       dim3(THREADS<W>), 0, s, a)
+    if (a.N <= 512)
+        QL_GO(1, 1);
+    else if (a.N <= 2048)
+        QL_GO(4, 1);
+    else if (a.N <= 4096)
+        QL_GO(4, 2);
+    else if (a.N <= 8192)
+        QL_GO(8, 2);
+    else
+        QL_GO(8, 4);
+#undef QL_GO
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream)
+{
+    if (a.xbf16)
+        a.hbf16 ? forward<true, true>(a, stream) : forward<true, false>(a, stream);
+    else
+        a.hbf16 ? forward<false, true>(a, stream) : forward<false, false>(a, stream);
+    return hipGetLastError();
+}
+
+// Workgroups of the backward pass, and partial sums of dw: up to two per CU.
+int norm_grad_parts(int64_t M, int N, int cus)
+{
+    const int64_t rows = N <= 512 ? 4 : 1, groups = (M + rows - 1) / rows;
+    const int64_t most = 2 * (int64_t)cus;
+    return (int)(groups < most ? groups : most);
+}
+
+hipError_t launch_norm_grad(const NormGradArgs &a, int parts, hipStream_t stream)
+{
+    const int form = (a.ybf16 ? 4 : 0) | (a.hbf16 ? 2 : 0) | (a.dbf16 ? 1 : 0);
+    switch (parts ? form : -1) {
+    case -1: break;  // no rows: dw is 0
+    case 0: backward<false, false, false>(a, parts, stream); break;
+    case 1: backward<false, false, true>(a, parts, stream); break;
+    case 2: backward<false, true, false>(a, parts, stream); break;
+    case 3: backward<false, true, true>(a, parts, stream); break;
+    case 4: backward<true, false, false>(a, parts, stream); break;
+    case 5: backward<true, false, true>(a, parts, stream); break;
+    case 6: backward<true, true, false>(a, parts, stream); break;
+    default: backward<true, true, true>(a, parts, stream); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.dw)
+        return e;
+    hipLaunchKernelGGL(norm_dw_kernel, dim3((unsigned)((a.N + 63) / 64)), dim3(1024), 0, stream,
+                       a.part, parts, a.N, a.dw);
+    return hipGetLastError();
+}
+
+}  // namespace qlk

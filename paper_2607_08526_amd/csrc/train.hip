@@ -1,0 +1,175 @@
+// C-ABI entry points of include/qlinear_train.h: argument checks, choice of kernel and
+// launches.  Every check happens before anything is enqueued; no entry point throws or
+// aborts.
+#include <algorithm>
+
+#include "internal.h"
+#include "qlinear_train.h"
+
+using namespace qlk;
+
+namespace {
+
+constexpr int64_t I31 = (int64_t)1 << 31;
+
+bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+bool dt_ok(int dt) { return dt == QL_DT_F32 || dt == QL_DT_BF16; }
+
+uintptr_t element(int dt) { return dt == QL_DT_BF16 ? 2 : 4; }
+
+int status(hipError_t e) { return e == hipSuccess ? QL_OK : QL_ERR_HIP; }
+
+// rows of w bytes at a stride of ld bytes
+struct Rows {
+    const void *p;
+    int64_t ld, w, rows;
+};
+
+Rows rows_of(const void *p, int64_t ld, int dt, int64_t rows, int64_t w)
+{
+    const int64_t size = (int64_t)element(dt);
+    return {p, ld * size, w * size, rows};
+}
+
+// the same elements, one by one
+bool same_rows(const Rows &a, const Rows &b)
+{
+    return a.p == b.p && a.w == b.w && a.rows == b.rows && (a.rows == 1 || a.ld == b.ld);
+}
+
+// whether any byte is of both (rows at unlike strides whose ranges meet: taken as so)
+bool share_bytes(const Rows &a, const Rows &b)
+{
+    if (!a.p || !b.p || !a.rows || !b.rows)
+        return false;
+    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+    const Rows &lo = pa <= pb ? a : b, &hi = pa <= pb ? b : a;
+    const uintptr_t diff = pa <= pb ? pb - pa : pa - pb;
+    if (diff >= (uintptr_t)((lo.rows - 1) * lo.ld + lo.w))
+        return false;
+    if ((lo.rows == 1 && hi.rows == 1) || lo.ld != hi.ld)
+        return true;
+    // columns of one buffer: apart in every row, or not
+    const int64_t apart = (int64_t)(diff % (uintptr_t)lo.ld);
+    return apart < lo.w || apart + hi.w > lo.ld;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qlinear_rms_norm(const ql_norm *n, hipStream_t stream)
+{
+    if (!n || !dt_ok(n->xdt) || ((n->res || n->h) && !dt_ok(n->rdt)) || (n->y && !dt_ok(n->ydt)) ||
+        !n->qx != !n->sx || !(n->eps >= 0.0) || n->eps > 3e38)
+        return QL_ERR_INVALID;
+    const int64_t M = n->M, N = n->N;
+    if (M < 0 || N <= 0 || n->ldx < N || (n->res && n->ldr < N) || (n->h && n->ldh < N) ||
+        (n->y && n->ldy < N) || (n->qx && N % QL_BLOCK))
+        return QL_ERR_SHAPE;
+    if (N > NORM_MAX_N || M > MAX_WORKGROUPS || n->ldx >= I31 || n->ldr >= I31 || n->ldh >= I31 ||
+        n->ldy >= I31)
+        return QL_ERR_UNSUPPORTED;
+    if (M == 0)
+        return QL_OK;
+    if (!n->x || (!n->h && !n->y && !n->qx))
+        return QL_ERR_INVALID;
+    if (!aligned(n->x, element(n->xdt)) || (n->res && !aligned(n->res, element(n->rdt))) ||
+        (n->h && !aligned(n->h, element(n->rdt))) || (n->y && !aligned(n->y, element(n->ydt))) ||
+        !aligned(n->weight, 4) || !aligned(n->qx, 16) || !aligned(n->sx, 2))
+        return QL_ERR_ALIGN;
+    const Rows ins[] = {rows_of(n->x, n->ldx, n->xdt, M, N), rows_of(n->res, n->ldr, n->rdt, M, N),
+                        {n->weight, 4 * N, 4 * N, 1}};
+    const Rows outs[] = {rows_of(n->h, n->ldh, n->rdt, M, N), rows_of(n->y, n->ldy, n->ydt, M, N),
+                         {n->qx, N, N, M}, {n->sx, 2 * M, 2 * M, 1}};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 3; ++j)
+            if (share_bytes(outs[i], ins[j]) && !(i < 2 && j < 2 && same_rows(outs[i], ins[j])))
+                return QL_ERR_INVALID;
+        for (int j = 0; j < i; ++j)
+            if (share_bytes(outs[i], outs[j]))
+                return QL_ERR_INVALID;
+    }
+    NormArgs a{};
+    a.x = n->x;
+    a.res = n->res;
+    a.ldx = n->ldx;
+    a.ldr = n->ldr;
+    a.M = M;
+    a.N = (int)N;
+    a.xbf16 = n->xdt == QL_DT_BF16;
+    a.hbf16 = n->rdt == QL_DT_BF16;
+    a.ybf16 = n->ydt == QL_DT_BF16;
+    a.weight = n->weight;
+    a.eps = n->eps;
+    a.inv_n = 1.0 / (double)N;
+    a.h = n->h;
+    a.y = n->y;
+    a.ldh = n->ldh;
+    a.ldy = n->ldy;
+    a.qx = n->qx;
+    a.sx = n->sx;
+    return status(launch_norm(a, stream));
+}
+
+int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream)
+{
+    if (!g || !dt_ok(g->dydt) || !dt_ok(g->hdt) || !dt_ok(g->dxdt) || !(g->eps >= 0.0) ||
+        g->eps > 3e38)
+        return QL_ERR_INVALID;
+    const int64_t M = g->M, N = g->N;
+    if (M < 0 || N <= 0 || g->lddy < N || g->ldh < N || (g->dres && g->lddres < N) || g->lddx < N)
+        return QL_ERR_SHAPE;
+    if (N > NORM_MAX_N || M > MAX_WORKGROUPS || g->lddy >= I31 || g->ldh >= I31 ||
+        g->lddres >= I31 || g->lddx >= I31)
+        return QL_ERR_UNSUPPORTED;
+    if (M > 0 && (!g->dy || !g->h || !g->dx))
+        return QL_ERR_INVALID;
+    if (!aligned(g->dy, element(g->dydt)) || !aligned(g->h, element(g->hdt)) ||
+        !aligned(g->dres, element(g->dxdt)) || !aligned(g->dx, element(g->dxdt)) ||
+        !aligned(g->weight, 4) || !aligned(g->dw, 4))
+        return QL_ERR_ALIGN;
+    const Rows ins[] = {rows_of(g->dy, g->lddy, g->dydt, M, N), rows_of(g->h, g->ldh, g->hdt, M, N),
+                        rows_of(g->dres, g->lddres, g->dxdt, M, N), {g->weight, 4 * N, 4 * N, 1}};
+    const Rows outs[] = {rows_of(g->dx, g->lddx, g->dxdt, M, N), {g->dw, 4 * N, 4 * N, 1}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 4; ++j)
+            if (share_bytes(outs[i], ins[j]) && !(i == 0 && j < 3 && same_rows(outs[i], ins[j])))
+                return QL_ERR_INVALID;
+    if (share_bytes(outs[0], outs[1]))
+        return QL_ERR_INVALID;
+    if (M == 0 && !g->dw)
+        return QL_OK;
+    NormGradArgs a{};
+    a.dy = g->dy;
+    a.h = g->h;
+    a.dres = g->dres;
+    a.lddy = g->lddy;
+    a.ldh = g->ldh;
+    a.ldres = g->lddres;
+    a.M = M;
+    a.N = (int)N;
+    a.ybf16 = g->dydt == QL_DT_BF16;
+    a.hbf16 = g->hdt == QL_DT_BF16;
+    a.dbf16 = g->dxdt == QL_DT_BF16;
+    a.weight = g->weight;
+    a.eps = g->eps;
+    a.inv_n = 1.0 / (double)N;
+    a.dx = g->dx;
+    a.lddx = g->lddx;
+    a.dw = g->dw;
+    const int parts = norm_grad_parts(M, a.N, current_cus());
+    uint8_t *ws = nullptr;
+    bool own = false;
+    std::unique_lock<std::mutex> turn;
+    if (g->dw && parts && !stream_workspace((size_t)parts * N * 4, stream, &ws, &own, &turn))
+        return QL_ERR_HIP;
+    a.part = reinterpret_cast<float *>(ws);
+    const int s = status(launch_norm_grad(a, parts, stream));
+    if (own && hipFreeAsync(ws, stream) != hipSuccess)
+        return QL_ERR_HIP;
+    return s;
+}
+
+}  // extern "C"

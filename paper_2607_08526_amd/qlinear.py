@@ -1,4 +1,5 @@
-"""Python binding of libqlinear.so (include/qlinear.h, include/qlinear_block.h).
+"""Python binding of libqlinear.so (include/qlinear.h, include/qlinear_block.h,
+include/qlinear_train.h).
 
 Argument marshalling only: every step of quantization and of the forward
 product runs in the library's HIP kernels.  PyTorch provides device memory
@@ -40,6 +41,8 @@ EXPORTS = [
     # include/qlinear_block.h
     "qlinear_mx_scales_bytes", "qlinear_dequantize", "qlinear_mx_quantize_act",
     "qlinear_mx_forward", "qlinear_gated_forward", "qlinear_gated_backward", "qlinear_rotary",
+    # include/qlinear_train.h
+    "qlinear_rms_norm", "qlinear_rms_norm_backward",
 ]
 
 PATH_AUTO, PATH_GEMV, PATH_STREAM, PATH_SKINNY, PATH_TILED, PATH_WIDE, PATH_MID = range(7)
@@ -112,6 +115,49 @@ class _GatedGrad(ctypes.Structure):
         ("dwdt", ctypes.c_int),
         ("dbg", ctypes.c_void_p),
         ("dbu", ctypes.c_void_p),
+    ]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("ldx", ctypes.c_int64),
+        ("xdt", ctypes.c_int),
+        ("res", ctypes.c_void_p),
+        ("ldr", ctypes.c_int64),
+        ("rdt", ctypes.c_int),
+        ("weight", ctypes.c_void_p),
+        ("eps", ctypes.c_double),
+        ("M", ctypes.c_int64),
+        ("N", ctypes.c_int64),
+        ("h", ctypes.c_void_p),
+        ("ldh", ctypes.c_int64),
+        ("y", ctypes.c_void_p),
+        ("ldy", ctypes.c_int64),
+        ("ydt", ctypes.c_int),
+        ("qx", ctypes.c_void_p),
+        ("sx", ctypes.c_void_p),
+    ]
+
+
+class _NormGrad(ctypes.Structure):
+    _fields_ = [
+        ("dy", ctypes.c_void_p),
+        ("lddy", ctypes.c_int64),
+        ("dydt", ctypes.c_int),
+        ("h", ctypes.c_void_p),
+        ("ldh", ctypes.c_int64),
+        ("hdt", ctypes.c_int),
+        ("dres", ctypes.c_void_p),
+        ("lddres", ctypes.c_int64),
+        ("weight", ctypes.c_void_p),
+        ("eps", ctypes.c_double),
+        ("M", ctypes.c_int64),
+        ("N", ctypes.c_int64),
+        ("dx", ctypes.c_void_p),
+        ("lddx", ctypes.c_int64),
+        ("dxdt", ctypes.c_int),
+        ("dw", ctypes.c_void_p),
     ]
 
 
@@ -188,6 +234,10 @@ def load():
     lib.qlinear_rotary.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, i64, vp, vp, i64, i64,
                                    ctypes.c_float, ci, ci, vp]
     lib.qlinear_rotary.restype = ci
+    lib.qlinear_rms_norm.argtypes = [ctypes.POINTER(_Norm), vp]
+    lib.qlinear_rms_norm.restype = ci
+    lib.qlinear_rms_norm_backward.argtypes = [ctypes.POINTER(_NormGrad), vp]
+    lib.qlinear_rms_norm_backward.restype = ci
     lib.qlinear_block_forward.restype = ci
     lib.qlinear_force_path.argtypes = [ci]
     lib.qlinear_force_path.restype = ci
@@ -800,6 +850,103 @@ def rotary(x, heads, freqs, dh=64, positions=None, start=0, T=None, interleaved=
                                  _ptr(freqs), _ptr(positions), start, T or max(rows, 1),
                                  float(mscale), interleaved, adjoint, _stream(stream)))
     return out
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _require_rows(t, name, M, N, dtypes=_FLOATS):
+    """A row view [M][N] with unit column stride; returns its row stride (of a single
+    row, which may be anything: its length)."""
+    _require(t, name, dtypes, min_cols=N)
+    if t.shape != (M, N):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(M, N)}")
+    return t.stride(0) if M > 1 else N
+
+
+def _norm(x, weight, eps, residual, h, y, ydtype, int8, stream):
+    """The call behind rms_norm and rms_norm_int8; int8: None or the (qx, sx) given."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor [M][N]")
+    M, N = x.shape
+    ldx = _require_rows(x, "x", M, N)
+    if weight is not None:
+        _require(weight, "weight", (torch.float32,), (N,))
+    if not 0.0 <= eps < math.inf:
+        raise ValueError(f"eps = {eps} is not a finite number of at least 0")
+    ldr = _require_rows(residual, "residual", M, N) if residual is not None else 0
+    if h is None and residual is not None:
+        h = _new(x, (M, N), residual.dtype, stream)
+    ldh = 0
+    if h is not None:
+        ldh = _require_rows(h, "h", M, N, _FLOATS if residual is None else (residual.dtype,))
+    qx = sx = None
+    if int8 is None:
+        if y is None:
+            y = _new(x, (M, N), ydtype, stream)
+        ldy = _require_rows(y, "y", M, N)
+    else:
+        if N % BLOCK:
+            raise ValueError(f"N = {N} is not a multiple of {BLOCK}")
+        qx, sx = int8
+        if qx is None:
+            qx = _new(x, (M, N), torch.int8, stream)
+        if sx is None:
+            sx = _new(x, (M,), torch.int16, stream)
+        _require(qx, "qx", (torch.int8,), (M, N))
+        _require(sx, "sx", _TWO_BYTE, (M,))
+        ldy = 0
+    _on_current_device(x, weight, residual, h, y, qx, sx)
+    n = _Norm(_ptr(x), ldx, _ydt(x), _ptr(residual), ldr, _ydt(h) if h is not None else DT_F32,
+              _ptr(weight), eps, M, N, _ptr(h), ldh, _ptr(y), ldy,
+              _ydt(y) if y is not None else DT_F32, _ptr(qx), _ptr(sx))
+    _check(load().qlinear_rms_norm(ctypes.byref(n), _stream(stream)))
+    return (y, h) if int8 is None else (qx, sx, h)
+
+
+def rms_norm(x, weight=None, eps=1e-6, residual=None, h=None, y=None, ydtype=torch.bfloat16,
+             stream=None):
+    """(y, h): h = x + residual, y = weight * h / sqrt(mean(h^2) + eps) by row.  x,
+    residual, h and y: fp32 or bf16 row views [M][N] with unit column stride (y of
+    ydtype where it is made here, h of residual's dtype; None without residual unless it
+    is given); weight fp32 [N] or None.  y is formed from the fp32 sum, before its
+    rounding to h's dtype.  h or y may be x or residual itself.  N <= 16384.
+    Asynchronous."""
+    return _norm(x, weight, eps, residual, h, y, ydtype, None, stream)
+
+
+def rms_norm_int8(x, weight=None, eps=1e-6, residual=None, h=None, qx=None, sx=None, stream=None):
+    """(qx, sx, h): rms_norm with its output as the activations of forward_w8a8, the
+    codes and scales that quantize_act gives for the fp32 y.  N % 32 == 0.
+    Asynchronous."""
+    return _norm(x, weight, eps, residual, h, None, None, (qx, sx), stream)
+
+
+def rms_norm_backward(dy, h, weight=None, eps=1e-6, dres=None, dx=None, dtype=torch.float32,
+                      weight_grad=True, stream=None):
+    """(dx, dw): the backward pass of rms_norm from dy, the gradient of y, and h as it
+    was kept.  dx, the gradient of x and of residual alike: with dres, the gradient that
+    arrives at h from further on, added (of dx's dtype; dtype where dx is made here);
+    dx may be dy, h or dres itself.  dw fp32 [N], None without weight_grad.
+    Asynchronous."""
+    if not isinstance(h, torch.Tensor) or h.dim() != 2:
+        raise ValueError("h must be a 2-D tensor [M][N]")
+    M, N = h.shape
+    ldh, lddy = _require_rows(h, "h", M, N), _require_rows(dy, "dy", M, N)
+    if weight is not None:
+        _require(weight, "weight", (torch.float32,), (N,))
+    if not 0.0 <= eps < math.inf:
+        raise ValueError(f"eps = {eps} is not a finite number of at least 0")
+    if dx is None:
+        dx = _new(h, (M, N), dtype, stream)
+    lddx = _require_rows(dx, "dx", M, N)
+    lddres = _require_rows(dres, "dres", M, N, (dx.dtype,)) if dres is not None else 0
+    dw = _new(h, (N,), torch.float32, stream) if weight_grad else None
+    _on_current_device(dy, h, weight, dres, dx, dw)
+    g = _NormGrad(_ptr(dy), lddy, _ydt(dy), _ptr(h), ldh, _ydt(h), _ptr(dres), lddres,
+                  _ptr(weight), eps, M, N, _ptr(dx), lddx, _ydt(dx), _ptr(dw))
+    _check(load().qlinear_rms_norm_backward(ctypes.byref(g), _stream(stream)))
+    return dx, dw
 
 
 class forced_path:
