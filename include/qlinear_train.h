@@ -83,6 +83,56 @@ typedef struct {
 
 int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream);
 
+/* ---- masked attention --------------------------------------------------------
+ *
+ * Softmax attention of B sequences, of up to Tq queries and Tk keys: for query i of a
+ * sequence with n queries and m keys, and each of the H query heads (dh channels, 64
+ * or 128; head h at column h * dh of its row), which share Hk key heads (H % Hk == 0;
+ * query head h reads key head h / (H / Hk)),
+ *
+ *     O_i = sum_j P_ij V_j,  P_ij = exp(s_ij - lse_i),  s_ij = scale * <Q_i, K_j>,
+ *     lse_i = log sum_j exp(s_ij)
+ *
+ * over the keys j < m, with causal only those up to i + m - n (the last query sees
+ * every key).  A query that sees no key has O = 0 and lse = -infinity.
+ *
+ * Where a sequence's rows lie, for queries (q, O, lse: q_rows rows) and keys (k, v:
+ * k_rows rows) each: Tq (Tk) rows from b * Tq on; or with offsets (device, [B + 1], not
+ * decreasing) those from offsets[b] up to offsets[b + 1], Tq (Tk) of them at most.  With
+ * lens (device, [B]) the first lens[b] of these rows are the sequence's and the others
+ * padding: never read, written as zeros (lse: -infinity).  Rows of no sequence stay as
+ * they are.  Offsets and lens are read on the device; values that lie outside of a
+ * tensor or a sequence's place are cut to it.  Sequences that share query rows (for the
+ * backward pass: key rows) give what the last writer leaves.
+ *
+ * q, k, v: bf16, 16-byte aligned, rows of ldq, ldk, ldv elements (% 8 == 0, < 2^24).  O:
+ * fp32 (16-byte aligned) or bf16 (8-byte), rows of ldo (% 4 == 0).  scale >= 0, finite.
+ * The probabilities enter the product with V rounded to bf16, sums are fp32.  A value
+ * that is not finite in a row which only the causal mask hides may reach queries of
+ * the same tile (0 * infinity).  Sizes: B * H * Tq, B * Hk * Tk < 2^31, B * Hk *
+ * ceil(Tq * H / Hk / 32) < 2^24 (QL_ERR_UNSUPPORTED). */
+typedef struct {
+    const uint16_t *q;
+    int64_t ldq;
+    const uint16_t *k;
+    int64_t ldk;
+    const uint16_t *v;
+    int64_t ldv;
+    int64_t q_rows, k_rows;
+    const int64_t *q_offsets, *k_offsets;  /* device, or NULL */
+    const int64_t *q_lens, *k_lens;        /* device, or NULL */
+    int64_t B, Tq, Tk, H, Hk, dh;
+    int causal;
+    float scale;
+} ql_attn;
+
+/* O, and with lse (fp32 [H][q_rows], or NULL) what the backward pass takes.  O and lse
+ * share no elements with an input (QL_ERR_INVALID).  Workspace (per stream, as in
+ * qlinear.h) where few queries leave CUs idle: fp32 partial results of parts of the
+ * keys, at most 40 MiB.  Asynchronous; B == 0 or Tq == 0 is a no-op. */
+int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, float *lse,
+                              hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,148 @@
+// What the masked attention's forward (attn_forward.hip) and backward kernels
+// (attn_backward.hip) share: where a sequence's rows lie, tiles of rows in LDS, and the
+// operands of the matrix instructions.
+#pragma once
+
+#include "dma.h"
+#include "internal.h"
+
+namespace qlk {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// two fp32 values rounded to nearest even bf16, packed
+__device__ inline uint32_t pack_bf16(float lo, float hi)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
+}
+
+// One side (queries or keys) of sequence b: its first row, its live rows, and the rows
+// of its place (those past the live ones are padding).
+struct SeqRows {
+    int64_t first;
+    int len, cap;
+};
+
+// Offsets and lengths are the caller's device data: whatever they hold, the rows stay
+// inside the tensor and no sequence has more than T.
+__device__ inline SeqRows seq_rows(const int64_t *off, const int64_t *lens, int64_t rows, int T,
+                                   int b)
+{
+    SeqRows s;
+    s.first = (int64_t)b * T;
+    s.cap = T;
+    if (off) {
+        const int64_t lo = off[b] < 0 ? 0 : off[b] > rows ? rows : off[b];
+        const int64_t hi = off[b + 1] < lo ? lo : off[b + 1] > rows ? rows : off[b + 1];
+        s.first = lo;
+        s.cap = hi - lo < T ? (int)(hi - lo) : T;
+    }
+    s.len = s.cap;
+    if (lens)
+        s.len = lens[b] < 0 ? 0 : lens[b] > s.cap ? s.cap : (int)lens[b];
+    return s;
+}
+
+// LDS tiles hold rows of D channels as they come, in chunks of 16 bytes; chunk c of
+// row r is kept at place c ^ swz(r), so that both ways in which a tile is read spread
+// over the banks (64 of 4 bytes): 16 rows' equal chunks (rows of an operand), and four
+// consecutive rows' four neighbouring chunks (transposed).  D = 64: a row is half the
+// banks, so rows of one parity need eight places, rows r and r + 2 unlike halves of them;
+// D = 128: 16 rows need 16 places, four consecutive ones unlike quarters.
+template <int D>
+__device__ inline int swz(int r)
+{
+    if constexpr (D == 64)
+        return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
+    else
+        return (r & 3) << 2 | ((r >> 2) & 3);
+}
+
+// Operand of 32 rows of a tile, 8 channels from 16 s + 8 hf on a lane (row l32 of them)
+template <int D>
+__device__ inline bf16x8 row_operand(const uint8_t *tile, int row, int s, int hf)
+{
+    return __builtin_bit_cast(
+        bf16x8, *reinterpret_cast<const u32x4 *>(tile + row * (2 * D) +
+                                                 ((2 * s + hf) ^ swz<D>(row)) * 16));
+}
+
+// Operand of 32 channels from 32 t on, transposed: lane l has channel 32 t + l % 32 of
+// the 8 rows {16 c + 4 h + i, 16 c + 8 + 4 h + i : i < 4}, h = l / 32 (the order in
+// which the accumulators of a 32 x 32 product hold their rows), by the transposing LDS
+// read: within each group of 16 lanes, result lane 4 q + p receives element p of the 8
+// bytes that source lanes q, 4 + q, 8 + q and 12 + q address.
+template <int D>
+__device__ inline bf16x8 transposed_operand(const uint8_t *tile, int c, int t, int lane)
+{
+    const int row0 = 16 * c + 4 * (lane >> 5) + ((lane & 15) >> 2);
+    const int unit = 8 * t + 4 * ((lane >> 4) & 1) + (lane & 3);  // of 8 bytes
+    u32x2 v[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int row = row0 + 8 * u;
+        const uint32_t off = row * (2 * D) + (((unit >> 1) ^ swz<D>(row)) * 16) + (unit & 1) * 8;
+        v[u] = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                       (__attribute__((address_space(3))) s16x4 *)(tile + off)));
+    }
+    return __builtin_bit_cast(bf16x8, u32x4{v[0][0], v[0][1], v[1][0], v[1][1]});
+}
+
+__device__ inline f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Loads of a tile of ROWS rows by T threads: slot i = j T + t of 16 bytes for thread t's
+// load j is row i / (D / 8), place i % (D / 8).
+template <int D, int ROWS, int T>
+struct TileLoad {
+    static constexpr int CH = D / 8, N = ROWS * CH / T;
+    static_assert(N >= 1 && ROWS * CH % T == 0, "");
+    uint32_t full[N];
+
+    // offsets from the tile's first row (ld: elements of a row, fewer than 2^24)
+    __device__ inline void init(int64_t ld, int tid)
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            full[j] = offset(j, ROWS, ld, tid);
+    }
+    __device__ static inline uint32_t offset(int j, int rows, int64_t ld, int tid)
+    {
+        const int i = j * T + tid, r = i / CH, lc = (i % CH) ^ swz<D>(r);
+        return (uint32_t)(min(r, rows - 1) * (int)ld + 8 * lc) * 2u;
+    }
+    // rows: those there are (>= 1); the tile's others repeat the last of them
+    __device__ inline void issue(const uint8_t *first, int rows, int64_t ld, const uint8_t *lds,
+                                 int tid) const
+    {
+        const uint32_t at = dma_lds(lds) + (tid & ~63) * 16;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            dma_load16(first, rows >= ROWS ? full[j] : offset(j, rows, ld, tid), at + j * T * 16);
+    }
+};
+
+template <bool B>
+struct Flag {
+    static constexpr bool value = B;
+};
+
+// Workgroup p runs on XCD p % 8: each XCD takes a contiguous range of the grid's work,
+// so that the tiles which several workgroups read come into one L2.
+__device__ inline int xcd_order(int p, int grid)
+{
+    const int q = grid >> 3, r = grid & 7, xcd = p & 7, i = p >> 3;
+    return xcd < r ? xcd * (q + 1) + i : r * (q + 1) + (xcd - r) * q + i;
+}
+
+}  // namespace qlk

@@ -1,0 +1,437 @@
+// Masked attention: sequences of unlike lengths, causal masks, query heads that share
+// key heads, few queries over long caches, and the logarithms of the row sums that the
+// backward pass starts from.  For query i of a head with n queries and m keys
+//
+//   O_i = sum_j p_ij V_j / l_i,  p_ij = exp(s_ij - max),  s_ij = scale <Q_i, K_j>,
+//   l_i = sum_j p_ij,  lse_i = max + log l_i,  j < m, and with causal j <= i + m - n
+//
+// in one pass over the keys with a running maximum and sum (online softmax).  The
+// products and their layout are those of attention.hip: S^T = K Q^T (a lane holds
+// scores of one query), then O^T += V^T P^T with P^T straight from the score
+// registers; a lane's query never changes, so its maximum, sum, mask and rescaling
+// are its own.  Tiles of keys come in by direct-to-LDS loads, two buffers each for K
+// and V, one tile apart; the scores of tile j + 1 are formed between the maximum of
+// tile j and its value product.
+//
+// Rows of a tile are (query, head of the group) pairs, i = t G + g for the G query
+// heads of a key head: each K and V tile is read once for all of them, and one token's
+// G heads fill G rows.  KG groups of wavefronts share out a tile's keys (KG = 4: one
+// wavefront of 32 rows each, for one token; merged through LDS at the end); beyond that
+// `splits` workgroups take parts of the keys and attn_join_kernel adds them up.
+#include "attn.h"
+
+namespace qlk {
+namespace {
+
+constexpr int THREADS = 256;
+// The running maximum may trail the true one by 2^LAZY in the exponent (as in
+// attention.hip): the quotient O / l is the same for any.
+constexpr float LAZY = 8.0f;
+constexpr float LN2 = 0.693147180559945309f;
+
+template <int D, int KG, int BK>
+__global__ __launch_bounds__(THREADS)
+__attribute__((amdgpu_waves_per_eu(D == 128 && KG == 4 ? 1 : 2, 2)))
+void seq_attn_kernel(const SeqAttnOut a)
+{
+    constexpr int GT = THREADS / KG, GW = GT / 64;  // threads, wavefronts of a key group
+    constexpr int BQ = 32 * GW;                     // rows of the workgroup
+    constexpr int TILE = BK * D * 2;                // bytes
+    constexpr int SUB = BK / 32, DT = D / 32, DS = D / 16;
+    __shared__ __align__(16) uint8_t lds[KG * 4 * TILE];
+    const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / GT);
+    const int tid = (int)threadIdx.x - kg * GT, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, hf = lane >> 5;
+    uint8_t *const mine = lds + kg * 4 * TILE;
+    auto kbuf = [&](int i) { return mine + i * TILE; };
+    auto vbuf = [&](int i) { return mine + (2 + i) * TILE; };
+
+    const SeqAttn &s = a.s;
+    const int G = s.H / s.Hk;
+    const int nq = (s.T * G + BQ - 1) / BQ;
+    int L = xcd_order((int)blockIdx.x, (int)gridDim.x);
+    const int part = L % a.splits;
+    L /= a.splits;
+    const int unit = L / nq, b = unit / s.Hk, hk = unit - b * s.Hk;
+    // causal: the longest first, the last tiles of the grid are short
+    const int qblk = s.causal ? nq - 1 - (L - unit * nq) : L - unit * nq;
+    const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
+    const SeqRows K = seq_rows(s.k_off, s.k_len, s.krows, s.KT, b);
+    const int row0 = qblk * BQ;
+    if (row0 >= Q.cap * G)
+        return;
+    const int row = row0 + wave * 32 + l32, t = row / G, g = row - t * G;
+    const int head = hk * G + g;
+    const bool live = t < Q.len;
+
+    // the last key of this lane's query, of any query of the workgroup, and of the
+    // wavefront's first: tiles up to that one need no mask
+    auto last_of = [&](int q) {
+        return s.causal ? min(K.len - 1, q + K.len - Q.len) : K.len - 1;
+    };
+    const int tmax = min((row0 + BQ - 1) / G, Q.len - 1);
+    const int keys = Q.len > row0 / G ? max(0, last_of(tmax) + 1) : 0;
+    const int tiles = (keys + BK - 1) / BK;
+    const int kt0 = (int)((int64_t)tiles * part / a.splits);
+    const int kt1 = (int)((int64_t)tiles * (part + 1) / a.splits);
+    const int lim = live ? min(last_of(t), kt1 * BK - 1) : -1;
+    const int free_keys = last_of((row0 + wave * 32) / G) + 1;
+
+    bf16x8 qb[DS];
+#pragma unroll
+    for (int i = 0; i < DS; ++i) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (live)
+            v = *reinterpret_cast<const u32x4 *>(s.q + (Q.first + t) * s.ldq + head * D + 16 * i +
+                                                 8 * hf);
+        qb[i] = __builtin_bit_cast(bf16x8, v);
+    }
+
+    const uint8_t *const kbase =
+        reinterpret_cast<const uint8_t *>(s.k + K.first * s.ldk + hk * D);
+    const uint8_t *const vbase =
+        reinterpret_cast<const uint8_t *>(s.v + K.first * s.ldv + hk * D);
+    TileLoad<D, BK, GT> kload, vload;
+    kload.init(s.ldk, tid);
+    vload.init(s.ldv, tid);
+    auto fetch_k = [&](int kt, uint8_t *buf) {
+        kload.issue(kbase + (int64_t)kt * BK * s.ldk * 2, K.len - kt * BK, s.ldk, buf, tid);
+    };
+    auto fetch_v = [&](int kt, uint8_t *buf) {
+        vload.issue(vbase + (int64_t)kt * BK * s.ldv * 2, K.len - kt * BK, s.ldv, buf, tid);
+    };
+
+    auto scores = [&](const uint8_t *ks, f32x16 (&sc)[SUB]) {
+        const f32x16 zero = {};
+#pragma unroll
+        for (int i = 0; i < DS; ++i)
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub)
+                sc[sub] = mfma(row_operand<D>(ks, 32 * sub + l32, i, hf), qb[i],
+                               i == 0 ? zero : sc[sub]);
+    };
+
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            oacc[d][r] = 0.0f;
+    float mrun = -INFINITY, lrun = 0.0f;
+    const float c = s.c;
+    // score r of subtile sub is key kt BK + 32 sub + 8 (r / 4) + 4 hf + r % 4
+    auto tile_max = [&](auto maskc, int kt, const f32x16 (&sc)[SUB]) {
+        constexpr bool MASK = decltype(maskc)::value;
+        const int left = lim - kt * BK - 4 * hf;
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                mx[r & 3] = fmaxf(mx[r & 3],
+                                  !MASK || 32 * sub + 8 * (r >> 2) + (r & 3) <= left ? sc[sub][r]
+                                                                                     : -INFINITY);
+        float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        mt = fmaxf(mt, __shfl_xor(mt, 32));
+        const bool up = mt > -INFINITY && (mrun == -INFINITY || (mt - mrun) * c > LAZY);
+        if (__ballot(up) != 0) {
+            const float mnew = fmaxf(mrun, mt);
+            const float alpha =
+                mrun == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mrun - mnew) * c);
+            mrun = mnew;
+            lrun *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    oacc[d][r] *= alpha;
+        }
+    };
+    auto tile_pv = [&](auto maskc, int kt, const f32x16 (&sc)[SUB], const uint8_t *vt) {
+        constexpr bool MASK = decltype(maskc)::value;
+        const int left = lim - kt * BK - 4 * hf;
+        const float mc = mrun == -INFINITY ? 0.0f : mrun * c;
+        float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        bf16x8 pb[SUB][2];
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+            for (int ch = 0; ch < 2; ++ch) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r0 = 8 * ch + 2 * e, k0 = 32 * sub + 8 * (r0 >> 2) + (r0 & 3);
+                    float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][r0], c, -mc));
+                    float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][r0 + 1], c, -mc));
+                    if (MASK) {
+                        p0 = k0 <= left ? p0 : 0.0f;
+                        p1 = k0 + 1 <= left ? p1 : 0.0f;
+                    }
+                    ls[e] += p0 + p1;
+                    w[e] = pack_bf16(p0, p1);
+                }
+                pb[sub][ch] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+            }
+        lrun += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+#pragma unroll
+        for (int kc = 0; kc < 2 * SUB; ++kc)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                oacc[d] = mfma(transposed_operand<D>(vt, kc, d, lane), pb[kc >> 1][kc & 1],
+                               oacc[d]);
+    };
+
+    // this group's tiles: kt0 + KG j + kg, j < n; one past kt1 is loaded as the last
+    // tile again (every key of it lies past lim)
+    const int n = (kt1 - kt0 + KG - 1) / KG;
+    auto tile_at = [&](int j) { return kt0 + KG * j + kg; };
+    auto load_at = [&](int j) { return min(tile_at(j), kt1 - 1); };
+    auto body = [&](int j, const f32x16 (&cur)[SUB], auto next, const uint8_t *vt) {
+        const int kt = tile_at(j);
+        if (kt >= kt1 || (kt + 1) * BK > free_keys) {
+            tile_max(Flag<true>{}, kt, cur);
+            next();
+            tile_pv(Flag<true>{}, kt, cur, vt);
+        } else {
+            tile_max(Flag<false>{}, kt, cur);
+            next();
+            tile_pv(Flag<false>{}, kt, cur, vt);
+        }
+    };
+    // At the start of a step every load issued so far has landed (K of tile j + 1, V of
+    // tile j) and every wavefront has finished the step before it: K's buffer of tile j
+    // (read then) takes tile j + 2, V's of tile j - 1 tile j + 1.
+    auto step = [&](auto oddc, int j, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB]) {
+        constexpr int P = decltype(oddc)::value ? 1 : 0;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (j + 2 < n)
+            fetch_k(load_at(j + 2), kbuf(P));
+        fetch_v(load_at(j + 1), vbuf(P ^ 1));
+        body(j, cur, [&] { scores(kbuf(P ^ 1), nxt); }, vbuf(P));
+    };
+    auto last = [&](auto oddc, int j, const f32x16 (&cur)[SUB]) {
+        constexpr int P = decltype(oddc)::value ? 1 : 0;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        body(j, cur, [] {}, vbuf(P));
+    };
+    if (n > 0) {
+        fetch_k(load_at(0), kbuf(0));
+        fetch_v(load_at(0), vbuf(0));
+        if (n > 1)
+            fetch_k(load_at(1), kbuf(1));
+        f32x16 sa[SUB], sb[SUB];
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        scores(kbuf(0), sa);
+        int j = 0;
+        for (; j + 2 < n; j += 2) {
+            step(Flag<false>{}, j, sa, sb);
+            step(Flag<true>{}, j + 1, sb, sa);
+        }
+        if (j + 1 < n) {
+            step(Flag<false>{}, j, sa, sb);
+            last(Flag<true>{}, j + 1, sb);
+        } else {
+            last(Flag<false>{}, j, sa);
+        }
+    }
+    lrun += __shfl_xor(lrun, 32);
+
+    if constexpr (KG > 1) {
+        // the other groups' states through LDS (over the buffers, which every wavefront
+        // has finished with), [value][lane] per wavefront; group 0 adds them in order
+        constexpr int VALUES = 2 + 16 * DT;
+        static_assert((KG - 1) * GW * VALUES * 64 * 4 <= KG * 4 * TILE, "");
+        __syncthreads();
+        if (kg > 0) {
+            float *const x =
+                reinterpret_cast<float *>(lds) + ((kg - 1) * GW + wave) * VALUES * 64 + lane;
+            x[0] = mrun;
+            x[64] = lrun;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    x[(2 + 16 * d + r) * 64] = oacc[d][r];
+        }
+        __syncthreads();
+        if (kg > 0)
+            return;
+#pragma unroll
+        for (int k = 1; k < KG; ++k) {
+            const float *const x =
+                reinterpret_cast<const float *>(lds) + ((k - 1) * GW + wave) * VALUES * 64 + lane;
+            const float m1 = x[0], m = fmaxf(mrun, m1);
+            const float a0 = mrun == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mrun - m) * c);
+            const float a1 = m1 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m1 - m) * c);
+            mrun = m;
+            lrun = a0 * lrun + a1 * x[64];
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    oacc[d][r] = a0 * oacc[d][r] + a1 * x[(2 + 16 * d + r) * 64];
+        }
+    }
+
+    // channel 32 d + 8 e + 4 hf + r % 4 of the lane's row
+    if (t >= Q.cap)
+        return;
+    if (a.splits > 1) {
+        const int64_t at = ((int64_t)part * s.B * s.Hk + unit) * s.T * G + row;
+        float *const o = a.part + at * D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<f32x4_t *>(o + 32 * d + 8 * e + 4 * hf) =
+                    f32x4_t{oacc[d][4 * e], oacc[d][4 * e + 1], oacc[d][4 * e + 2],
+                            oacc[d][4 * e + 3]};
+        if (hf == 0)
+            *reinterpret_cast<f32x2_t *>(a.part +
+                                         (int64_t)a.splits * s.B * s.Hk * s.T * G * D + at * 2) =
+                f32x2_t{mrun, lrun};
+        return;
+    }
+    // no key: zeros (also of a padding row)
+    const bool none = lim < 0;
+    const float inv = 1.0f / lrun;
+    const int64_t orow = (Q.first + t) * a.ldo + head * D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int ch = 32 * d + 8 * e + 4 * hf;
+            f32x4_t v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = none ? 0.0f : oacc[d][4 * e + i] * inv;
+            if (a.obf16)
+                *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.o) + orow + ch) =
+                    u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            else
+                *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.o) + orow + ch) = v;
+        }
+    if (a.lse && hf == 0)
+        a.lse[head * s.qrows + Q.first + t] =
+            none ? -INFINITY : (mrun * c + __builtin_amdgcn_logf(lrun)) * LN2;
+}
+
+// The parts of a split, joined in order: a wavefront per (query, head).
+template <int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(const SeqAttnOut a)
+{
+    constexpr int V = D / 64;
+    const SeqAttn &s = a.s;
+    const int G = s.H / s.Hk, lane = (int)threadIdx.x & 63;
+    const int64_t rows = (int64_t)s.B * s.Hk * s.T * G;
+    const int64_t at = (int64_t)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
+    if (at >= rows)
+        return;
+    const int unit = (int)(at / (s.T * G)), row = (int)(at - (int64_t)unit * s.T * G);
+    const int b = unit / s.Hk, t = row / G, head = (unit - b * s.Hk) * G + row - t * G;
+    const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
+    if (t >= Q.cap)
+        return;
+    const SeqRows K = seq_rows(s.k_off, s.k_len, s.krows, s.KT, b);
+    const bool none = t >= Q.len || K.len == 0 || (s.causal && t + K.len - Q.len < 0);
+    const f32x2_t *const ml = reinterpret_cast<const f32x2_t *>(a.part + a.splits * rows * D);
+    float m = -INFINITY, l = 0.0f, o[V] = {};
+    for (int p = 0; p < a.splits; ++p)
+        m = fmaxf(m, ml[p * rows + at][0]);
+#pragma unroll 4
+    for (int p = 0; p < a.splits; ++p) {
+        const f32x2_t x = ml[p * rows + at];
+        const float w = x[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((x[0] - m) * s.c);
+        const float *const po = a.part + (p * rows + at) * D + lane * V;
+        l += w * x[1];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            o[i] += w * po[i];
+    }
+    const float inv = 1.0f / l;
+    const int64_t out = (Q.first + t) * a.ldo + head * D + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float v = none ? 0.0f : o[i] * inv;
+        if (a.obf16)
+            static_cast<uint16_t *>(a.o)[out + i] = __builtin_bit_cast(uint16_t, (__bf16)v);
+        else
+            static_cast<float *>(a.o)[out + i] = v;
+    }
+    if (a.lse && lane == 0)
+        a.lse[head * s.qrows + Q.first + t] =
+            none ? -INFINITY : (m * s.c + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+int tile_rows(int groups) { return 128 / groups; }
+
+}  // namespace
+
+SeqAttnPlan seq_attn_plan(const SeqAttn &s, int cus)
+{
+    const int64_t units = (int64_t)s.B * s.Hk, rows = (int64_t)s.T * (s.H / s.Hk);
+    const int64_t tiles = ((int64_t)s.KT + 63) / 64;
+    auto wgs = [&](int groups) {
+        return (rows + tile_rows(groups) - 1) / tile_rows(groups) * units;
+    };
+    SeqAttnPlan p{1, 1};
+    if (rows <= 32)
+        p.groups = 4;
+    else if (wgs(2) <= cus ? tiles >= 2 : wgs(2) <= 2 * (int64_t)cus && tiles >= 8)
+        p.groups = 2;
+    const int64_t w = wgs(p.groups), most = tiles / (2 * p.groups);
+    if (w < cus && most > 1) {
+        const int64_t want = (cus + w - 1) / w;
+        p.splits = (int)(want < most ? want : most);
+    }
+    return p;
+}
+
+int64_t seq_attn_workgroups(const SeqAttn &s, const SeqAttnPlan &p)
+{
+    const int64_t rows = (int64_t)s.T * (s.H / s.Hk);
+    return (rows + tile_rows(p.groups) - 1) / tile_rows(p.groups) * s.B * s.Hk * p.splits;
+}
+
+size_t seq_attn_bytes(const SeqAttn &s, const SeqAttnPlan &p)
+{
+    return p.splits < 2 ? 0 : (size_t)p.splits * s.B * s.H * s.T * (s.dh + 2) * 4;
+}
+
+hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)seq_attn_workgroups(a.s, p)), block(THREADS);
+#define QL_GO(D, KG, BK) \
+    hipLaunchKernelGGL((seq_attn_kernel<D, KG, BK>), grid, block, 0, stream, a)
+    if (a.s.dh == 64) {
+        if (p.groups == 1)
+            QL_GO(64, 1, 64);
+        else if (p.groups == 2)
+            QL_GO(64, 2, 64);
+        else
+            QL_GO(64, 4, 32);
+    } else {
+        if (p.groups == 1)
+            QL_GO(128, 1, 32);
+        else if (p.groups == 2)
+            QL_GO(128, 2, 32);
+        else
+            QL_GO(128, 4, 32);
+    }
+#undef QL_GO
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits < 2)
+        return e;
+    const dim3 joins((unsigned)(((int64_t)a.s.B * a.s.H * a.s.T + 3) / 4));
+    if (a.s.dh == 64)
+        hipLaunchKernelGGL(attn_join_kernel<64>, joins, dim3(256), 0, stream, a);
+    else
+        hipLaunchKernelGGL(attn_join_kernel<128>, joins, dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace qlk

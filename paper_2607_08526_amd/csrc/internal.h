@@ -319,6 +319,38 @@ struct NormGradArgs {
 int norm_grad_parts(int64_t M, int N, int cus);
 hipError_t launch_norm_grad(const NormGradArgs &a, int parts, hipStream_t stream);
 
+// Masked attention (attn_forward.hip, attn_backward.hip): B sequences of up to T queries
+// and KT keys, H query heads of dh channels (64 or 128) that share Hk key heads; q, k,
+// v bf16 with rows of fewer than 2^24 elements.  A sequence's rows: T (KT) from b T (b
+// KT) on, or those between its offset and the next; of them the first lens[b] are live.
+struct SeqAttn {
+    const uint16_t *q, *k, *v;
+    int64_t ldq, ldk, ldv;
+    int64_t qrows, krows;  // of the tensors
+    const int64_t *q_off, *k_off, *q_len, *k_len;  // each may be nullptr
+    int B, T, KT, H, Hk, dh;
+    int causal;
+    float c;  // scale * log2(e)
+};
+struct SeqAttnOut {
+    SeqAttn s;
+    void *o;
+    int64_t ldo;
+    int obf16;
+    float *lse;   // [H][qrows] or nullptr
+    float *part;  // of a split: [splits][B Hk][T H / Hk][dh], then [..][2]
+    int splits;
+};
+// How the forward pass cuts its work: wavefronts of one tile of queries that share out
+// the keys (1, 2 or 4), and the parts of the keys that are joined by a second launch.
+struct SeqAttnPlan {
+    int groups, splits;
+};
+SeqAttnPlan seq_attn_plan(const SeqAttn &s, int cus);
+size_t seq_attn_bytes(const SeqAttn &s, const SeqAttnPlan &p);  // workspace
+int64_t seq_attn_workgroups(const SeqAttn &s, const SeqAttnPlan &p);
+hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_t stream);
+
 // The outputs of a gated pair (gated.h): H, or with dG the gradients of both
 // projections.
 struct GateArgs {

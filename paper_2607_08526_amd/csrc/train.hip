@@ -55,6 +55,85 @@ bool share_bytes(const Rows &a, const Rows &b)
     return apart < lo.w || apart + hi.w > lo.ld;
 }
 
+int check_attn(const ql_attn *a)
+{
+    if (!a || !(a->scale >= 0.0f) || a->scale > 3e38f)
+        return QL_ERR_INVALID;
+    if (a->B < 0 || a->Tq < 0 || a->Tk < 0 || a->H <= 0 || a->Hk <= 0 || a->H % a->Hk ||
+        a->q_rows < 0 || a->k_rows < 0)
+        return QL_ERR_SHAPE;
+    if ((a->dh != 64 && a->dh != 128) || a->B >= I31 || a->Tq >= I31 || a->Tk >= I31 ||
+        a->H >= 1 << 16 || a->q_rows >= I31 || a->k_rows >= I31 || a->ldq >= 1 << 24 ||
+        a->ldk >= 1 << 24 || a->ldv >= 1 << 24)
+        return QL_ERR_UNSUPPORTED;
+    const int64_t rows = a->Tq * (a->H / a->Hk);  // of a key head's queries
+    // (each factor is below 2^31 and 2^16: no product overflows)
+    if (a->B * a->H >= I31 || (a->Tq && a->B * a->H >= (I31 + a->Tq - 1) / a->Tq) ||
+        (a->Tk && a->B * a->Hk >= (I31 + a->Tk - 1) / a->Tk) ||
+        a->B * a->Hk * ((rows + 31) / 32) > MAX_WORKGROUPS)
+        return QL_ERR_UNSUPPORTED;
+    if (a->ldq < a->H * a->dh || a->ldk < a->Hk * a->dh || a->ldv < a->Hk * a->dh ||
+        (!a->q_offsets && a->q_rows < a->B * a->Tq) || (!a->k_offsets && a->k_rows < a->B * a->Tk))
+        return QL_ERR_SHAPE;
+    if (a->B == 0 || a->Tq == 0)
+        return QL_OK;
+    const bool keys = a->Tk > 0 && a->k_rows > 0;
+    if ((a->q_rows > 0 && !a->q) || (keys && (!a->k || !a->v)))
+        return QL_ERR_INVALID;
+    if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || a->ldq % 8 ||
+        a->ldk % 8 || a->ldv % 8 || !aligned(a->q_offsets, 8) || !aligned(a->k_offsets, 8) ||
+        !aligned(a->q_lens, 8) || !aligned(a->k_lens, 8))
+        return QL_ERR_ALIGN;
+    return QL_OK;
+}
+
+SeqAttn seq_attn(const ql_attn &a)
+{
+    SeqAttn s{};
+    s.q = a.q;
+    s.k = a.k;
+    s.v = a.v;
+    s.ldq = a.ldq;
+    s.ldk = a.ldk;
+    s.ldv = a.ldv;
+    s.qrows = a.q_rows;
+    s.krows = a.k_rows;
+    s.q_off = a.q_offsets;
+    s.k_off = a.k_offsets;
+    s.q_len = a.q_lens;
+    s.k_len = a.k_lens;
+    s.B = (int)a.B;
+    s.T = (int)a.Tq;
+    s.KT = (int)a.Tk;
+    s.H = (int)a.H;
+    s.Hk = (int)a.Hk;
+    s.dh = (int)a.dh;
+    s.causal = a.causal != 0;
+    s.c = a.scale * 1.44269504088896340736f;
+    return s;
+}
+
+// the inputs' rows, for the checks of outputs against them
+struct AttnRows {
+    Rows r[7];
+};
+AttnRows attn_inputs(const ql_attn &a)
+{
+    return {{rows_of(a.q, a.ldq, QL_DT_BF16, a.q_rows, a.H * a.dh),
+             rows_of(a.k, a.ldk, QL_DT_BF16, a.k_rows, a.Hk * a.dh),
+             rows_of(a.v, a.ldv, QL_DT_BF16, a.k_rows, a.Hk * a.dh),
+             {a.q_offsets, 8 * (a.B + 1), 8 * (a.B + 1), 1},
+             {a.k_offsets, 8 * (a.B + 1), 8 * (a.B + 1), 1},
+             {a.q_lens, 8 * a.B, 8 * a.B, 1},
+             {a.k_lens, 8 * a.B, 8 * a.B, 1}}};
+}
+
+bool meets_inputs(const Rows &out, const ql_attn &a)
+{
+    const AttnRows in = attn_inputs(a);
+    return std::any_of(in.r, in.r + 7, [&](const Rows &r) { return share_bytes(out, r); });
+}
+
 }  // namespace
 
 extern "C" {
@@ -167,6 +246,51 @@ int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream)
         return QL_ERR_HIP;
     a.part = reinterpret_cast<float *>(ws);
     const int s = status(launch_norm_grad(a, parts, stream));
+    if (own && hipFreeAsync(ws, stream) != hipSuccess)
+        return QL_ERR_HIP;
+    return s;
+}
+
+int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, float *lse,
+                              hipStream_t stream)
+{
+    if (!dt_ok(odt))
+        return QL_ERR_INVALID;
+    const int st = check_attn(a);
+    if (st != QL_OK)
+        return st;
+    if (ldo < a->H * a->dh)
+        return QL_ERR_SHAPE;
+    if (ldo >= I31)
+        return QL_ERR_UNSUPPORTED;
+    if (a->B == 0 || a->Tq == 0 || a->q_rows == 0)
+        return QL_OK;
+    if (!o)
+        return QL_ERR_INVALID;
+    if (!aligned(o, odt == QL_DT_BF16 ? 8 : 16) || ldo % 4 || !aligned(lse, 4))
+        return QL_ERR_ALIGN;
+    const Rows out = rows_of(o, ldo, odt, a->q_rows, a->H * a->dh);
+    const Rows sums = {lse, 4 * a->q_rows, 4 * a->q_rows, a->H};
+    if (meets_inputs(out, *a) || meets_inputs(sums, *a) || share_bytes(out, sums))
+        return QL_ERR_INVALID;
+    SeqAttnOut t{};
+    t.s = seq_attn(*a);
+    t.o = o;
+    t.ldo = ldo;
+    t.obf16 = odt == QL_DT_BF16;
+    t.lse = lse;
+    const SeqAttnPlan plan = seq_attn_plan(t.s, current_cus());
+    if (seq_attn_workgroups(t.s, plan) > MAX_WORKGROUPS)
+        return QL_ERR_UNSUPPORTED;
+    t.splits = plan.splits;
+    uint8_t *ws = nullptr;
+    bool own = false;
+    std::unique_lock<std::mutex> turn;
+    const size_t bytes = seq_attn_bytes(t.s, plan);
+    if (bytes && !stream_workspace(bytes, stream, &ws, &own, &turn))
+        return QL_ERR_HIP;
+    t.part = reinterpret_cast<float *>(ws);
+    const int s = status(launch_seq_attn(t, plan, stream));
     if (own && hipFreeAsync(ws, stream) != hipSuccess)
         return QL_ERR_HIP;
     return s;

@@ -42,7 +42,7 @@ EXPORTS = [
     "qlinear_mx_scales_bytes", "qlinear_dequantize", "qlinear_mx_quantize_act",
     "qlinear_mx_forward", "qlinear_gated_forward", "qlinear_gated_backward", "qlinear_rotary",
     # include/qlinear_train.h
-    "qlinear_rms_norm", "qlinear_rms_norm_backward",
+    "qlinear_rms_norm", "qlinear_rms_norm_backward", "qlinear_attention_forward",
 ]
 
 PATH_AUTO, PATH_GEMV, PATH_STREAM, PATH_SKINNY, PATH_TILED, PATH_WIDE, PATH_MID = range(7)
@@ -161,6 +161,31 @@ class _NormGrad(ctypes.Structure):
     ]
 
 
+class _Attn(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p),
+        ("ldq", ctypes.c_int64),
+        ("k", ctypes.c_void_p),
+        ("ldk", ctypes.c_int64),
+        ("v", ctypes.c_void_p),
+        ("ldv", ctypes.c_int64),
+        ("q_rows", ctypes.c_int64),
+        ("k_rows", ctypes.c_int64),
+        ("q_offsets", ctypes.c_void_p),
+        ("k_offsets", ctypes.c_void_p),
+        ("q_lens", ctypes.c_void_p),
+        ("k_lens", ctypes.c_void_p),
+        ("B", ctypes.c_int64),
+        ("Tq", ctypes.c_int64),
+        ("Tk", ctypes.c_int64),
+        ("H", ctypes.c_int64),
+        ("Hk", ctypes.c_int64),
+        ("dh", ctypes.c_int64),
+        ("causal", ctypes.c_int),
+        ("scale", ctypes.c_float),
+    ]
+
+
 _LIB = None
 
 
@@ -238,6 +263,8 @@ def load():
     lib.qlinear_rms_norm.restype = ci
     lib.qlinear_rms_norm_backward.argtypes = [ctypes.POINTER(_NormGrad), vp]
     lib.qlinear_rms_norm_backward.restype = ci
+    lib.qlinear_attention_forward.argtypes = [ctypes.POINTER(_Attn), vp, i64, ci, vp, vp]
+    lib.qlinear_attention_forward.restype = ci
     lib.qlinear_block_forward.restype = ci
     lib.qlinear_force_path.argtypes = [ci]
     lib.qlinear_force_path.restype = ci
@@ -947,6 +974,79 @@ def rms_norm_backward(dy, h, weight=None, eps=1e-6, dres=None, dx=None, dtype=to
                   _ptr(weight), eps, M, N, _ptr(dx), lddx, _ydt(dx), _ptr(dw))
     _check(load().qlinear_rms_norm_backward(ctypes.byref(g), _stream(stream)))
     return dx, dw
+
+
+def _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets, k_offsets, q_lens, k_lens):
+    """(_Attn, its tensors) of a masked attention's checked arguments."""
+    Hk, kT = H if kv_heads is None else kv_heads, T if kT is None else kT
+    if H < 1 or Hk < 1 or H % Hk:
+        raise ValueError(f"{H} query heads do not share {Hk} key heads")
+    if B < 0 or T < 0 or kT < 0:
+        raise ValueError(f"B = {B}, T = {T} or kT = {kT} is negative")
+    ld = []
+    for name, t, heads in (("q", q, H), ("k", k, Hk), ("v", v, Hk)):
+        _require(t, name, _BF16_BITS, min_cols=heads * dh)
+        # (a single row's stride may be anything: its length serves, in whole eights)
+        ld.append(t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8)
+    if v.shape[0] != k.shape[0]:
+        raise ValueError(f"v has {v.shape[0]} rows, k {k.shape[0]}")
+    for name, t, n in (("q_offsets", q_offsets, B + 1), ("k_offsets", k_offsets, B + 1),
+                       ("q_lens", q_lens, B), ("k_lens", k_lens, B)):
+        if t is not None:
+            _require(t, name, (torch.int64,), (n,))
+    if q_offsets is None and q.shape[0] < B * T:
+        raise ValueError(f"q has {q.shape[0]} rows, expected at least B * T = {B * T}")
+    if k_offsets is None and k.shape[0] < B * kT:
+        raise ValueError(f"k has {k.shape[0]} rows, expected at least B * kT = {B * kT}")
+    scale = 1.0 / float(dh) ** 0.5 if scale is None else float(scale)
+    a = _Attn(_ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], q.shape[0], k.shape[0],
+              _ptr(q_offsets), _ptr(k_offsets), _ptr(q_lens), _ptr(k_lens), B, T, kT, H, Hk, dh,
+              causal, scale)
+    return a, (q, k, v, q_offsets, k_offsets, q_lens, k_lens)
+
+
+def _attn_new(like, shape, dtype, stream, value):
+    """An output of the masked attention; with value (rows that belong to no sequence
+    stay as they are) filled with it."""
+    t = _new(like, shape, dtype, stream)
+    if value is not None:
+        with torch.cuda.stream(stream):
+            t.fill_(value)
+    return t
+
+
+def attention_forward(q, k, v, B, T, H, kv_heads=None, dh=64, kT=None, causal=False, scale=None,
+                      q_offsets=None, k_offsets=None, q_lens=None, k_lens=None, O=None,
+                      odtype=torch.bfloat16, lse=None, with_lse=True, stream=None):
+    """(O, lse): masked softmax attention of B sequences of up to T queries and kT
+    keys (None: T).  q, k, v: bf16 (or int16 bit patterns) row views with unit column
+    stride; H query heads of dh (64 or 128) channels share kv_heads key heads (None:
+    H).  causal: query i of n sees the keys up to i + m - n of m.  A sequence's rows: T
+    (kT) from b * T on, or with offsets (int64 [B + 1] on the device) those between its
+    offset and the next, at most T (kT); with lens (int64 [B] on the device) only the
+    first of them are live, the others padding (never read; O zero, lse -inf).  A query
+    that sees no key gives zeros and -inf too.  Rows of no sequence are not written (in
+    outputs made here: zeros and -inf).  O: row view [rows of q][>= H * dh], bf16 or
+    fp32 (odtype where it is made here); lse: fp32 [H][rows of q], the logarithms of the
+    row sums that attention_backward takes (None without with_lse).  Asynchronous."""
+    a, tensors = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets, k_offsets,
+                       q_lens, k_lens)
+    rows = q.shape[0]
+    loose = q_offsets is not None or rows != B * T  # rows that may be of no sequence
+    if O is None:
+        O = _attn_new(q, (rows, H * dh), odtype, stream, 0.0 if loose else None)
+    _require(O, "O", _FLOATS, min_cols=H * dh)
+    if O.shape[0] != rows:
+        raise ValueError(f"O has {O.shape[0]} rows, expected {rows}")
+    if lse is None and with_lse:
+        lse = _attn_new(q, (H, rows), torch.float32, stream, -math.inf if loose else None)
+    if lse is not None:
+        _require(lse, "lse", (torch.float32,), (H, rows))
+    _on_current_device(O, lse, *tensors)
+    ldo = O.stride(0) if rows > 1 else -(-O.shape[1] // 4) * 4
+    _check(load().qlinear_attention_forward(ctypes.byref(a), _ptr(O), ldo, _ydt(O), _ptr(lse),
+                                            _stream(stream)))
+    return O, lse
 
 
 class forced_path:

@@ -41,7 +41,7 @@ def test_structures(tmp_path):
         pytest.skip("no host C compiler or HIP headers")
     src = ['#include <stdio.h>', '#include <stddef.h>', '#include "qlinear_train.h"',
            'int main(void) {']
-    pairs = [("ql_norm", ql._Norm), ("ql_norm_grad", ql._NormGrad)]
+    pairs = [("ql_norm", ql._Norm), ("ql_norm_grad", ql._NormGrad), ("ql_attn", ql._Attn)]
     for name, cls in pairs:
         src.append(f'printf("%zu\\n", sizeof({name}));')
         src += [f'printf("%zu\\n", offsetof({name}, {f}));' for f, _ in cls._fields_]
@@ -159,3 +159,76 @@ def test_binding_refuses_norm():
         ql.rms_norm_backward(x[:, :63], x)
     with pytest.raises(ValueError, match="device"):
         ql.rms_norm_backward(x, x)
+
+
+def attn(**kw):
+    a = dict(q=A, ldq=256, k=B, ldk=128, v=C, ldv=128, q_rows=20, k_rows=40, q_offsets=None,
+             k_offsets=None, q_lens=None, k_lens=None, B=2, Tq=10, Tk=20, H=4, Hk=2, dh=64,
+             causal=0, scale=0.125)
+    a.update(kw)
+    return ql._Attn(**a)
+
+
+def attend(lib, o=D, ldo=256, odt=BF16, lse=E, **kw):
+    return lib.qlinear_attention_forward(ctypes.byref(attn(**kw)), o, ldo, odt, lse, None)
+
+
+# what both directions refuse: fields and the status
+ATTN_ERRORS = [
+    (dict(B=-1), SHAPE), (dict(Tq=-1), SHAPE), (dict(Tk=-1), SHAPE), (dict(H=0), SHAPE),
+    (dict(Hk=0), SHAPE), (dict(H=3), SHAPE), (dict(q_rows=19), SHAPE), (dict(k_rows=39), SHAPE),
+    (dict(q_rows=-1, q_offsets=F), SHAPE), (dict(ldq=248), SHAPE), (dict(ldk=120), SHAPE),
+    (dict(ldv=64), SHAPE),
+    (dict(dh=32), UNSUPPORTED), (dict(dh=96), UNSUPPORTED), (dict(ldq=1 << 24), UNSUPPORTED),
+    (dict(ldk=1 << 24), UNSUPPORTED), (dict(ldv=1 << 24), UNSUPPORTED),
+    (dict(B=1 << 31), UNSUPPORTED), (dict(Tq=1 << 31), UNSUPPORTED),
+    (dict(Tk=1 << 31), UNSUPPORTED), (dict(H=1 << 16, Hk=1 << 16), UNSUPPORTED),
+    (dict(B=1 << 15, Tq=1 << 15), UNSUPPORTED), (dict(B=1 << 15, Tk=1 << 15), UNSUPPORTED),
+    (dict(B=1 << 30, Tq=1, Tk=0, H=1, Hk=1), UNSUPPORTED),
+    (dict(q_rows=1 << 31), UNSUPPORTED), (dict(k_rows=1 << 31), UNSUPPORTED),
+    (dict(q=None), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID),
+    (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(scale=float("inf")), INVALID),
+    (dict(q=A + 8), ALIGN), (dict(k=B + 2), ALIGN), (dict(v=C + 4), ALIGN),
+    (dict(ldq=260), ALIGN), (dict(ldk=132), ALIGN), (dict(ldv=129), ALIGN),
+    (dict(q_offsets=F + 4), ALIGN), (dict(k_offsets=F + 1), ALIGN), (dict(q_lens=F + 4), ALIGN),
+    (dict(k_lens=F + 4), ALIGN),
+]
+
+
+def test_attention_forward_errors(lib):
+    for kw, status in ATTN_ERRORS:
+        assert attend(lib, **kw) == status, kw
+    assert lib.qlinear_attention_forward(None, D, 256, BF16, E, None) == INVALID
+    assert attend(lib, B=0) == OK and attend(lib, Tq=0) == OK
+    assert attend(lib, odt=2) == INVALID and attend(lib, o=None) == INVALID
+    assert attend(lib, ldo=252) == SHAPE and attend(lib, ldo=258) == ALIGN
+    assert attend(lib, ldo=1 << 31) == UNSUPPORTED
+    assert attend(lib, o=D + 4) == ALIGN and attend(lib, o=D + 8, odt=F32) == ALIGN
+    assert attend(lib, lse=E + 2) == ALIGN
+    # outputs on inputs or each other
+    for o in (A, B, C, A + 64 * 8, F):
+        assert attend(lib, o=o, q_lens=F) == INVALID
+    for lse in (A + 4, B + 4, D + 4, F):
+        assert attend(lib, lse=lse, k_offsets=F) == INVALID
+
+
+def test_binding_refuses_attention():
+    q = torch.zeros((20, 256), dtype=torch.bfloat16)
+    k = v = torch.zeros((40, 128), dtype=torch.bfloat16)
+    call = lambda q=q, k=k, v=v, B=2, T=10, H=4, Hk=2, kT=20, **kw: ql.attention_forward(
+        q, k, v, B, T, H, kv_heads=Hk, kT=kT, **kw)
+    i64 = lambda n: torch.zeros(n, dtype=torch.int64)
+    with pytest.raises(ValueError, match="device"):
+        call()
+    for kw, match in ((dict(Hk=3), "share"), (dict(H=0), "share"), (dict(T=11), "rows"),
+                      (dict(kT=21), "rows"), (dict(B=-1), "negative"), (dict(v=v[1:]), "rows"),
+                      (dict(q=q[:, :255]), "256 columns"), (dict(q=q.t()), "stride"),
+                      (dict(q_offsets=i64(2)), "shape"), (dict(k_lens=i64(3)), "shape"),
+                      (dict(O=q[:3]), "rows"), (dict(lse=torch.zeros((4, 19))), "shape")):
+        with pytest.raises(ValueError, match=match):
+            call(**kw)
+    for kw in (dict(q=q.float()), dict(k=k.half()), dict(q_lens=torch.zeros(2, dtype=torch.int32)),
+               dict(O=q.half()), dict(lse=torch.zeros((4, 20), dtype=torch.bfloat16))):
+        with pytest.raises(TypeError, match="dtype"):
+            call(**kw)
