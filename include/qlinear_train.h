@@ -133,6 +133,35 @@ typedef struct {
 int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, float *lse,
                               hipStream_t stream);
 
+/* The backward pass, from O and lse of qlinear_attention_forward on the same inputs and
+ * dO, the gradient of O:
+ *
+ *     dV_j = sum_i P_ij dO_i,  dS_ij = P_ij (<dO_i, V_j> - <dO_i, O_i>),
+ *     dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i
+ *
+ * (K_j and V_j: summed over the query heads that share them.)  The probabilities are
+ * formed again from lse; P and dS enter the products rounded to bf16, sums are fp32 in
+ * one fixed order.  dO: bf16, 16-byte aligned, rows of lddo (% 8 == 0, < 2^24).  dq, dk,
+ * dv: dtype dt, aligned and strided as O; dk and dv both or neither.  Rows as above:
+ * padding rows of q (k, v) get zeros in dq (dk, dv), those of no sequence stay.  No output
+ * shares elements with an input or another output (QL_ERR_INVALID; other columns of the
+ * same rows may be: the gradients may be those of a fused QKV output).  Workspace (per
+ * stream, as in qlinear.h): 8 H q_rows bytes, and fp32 partial sums where few rows leave
+ * CUs idle, at most 80 MiB.  Asynchronous. */
+typedef struct {
+    const void *o;
+    int64_t ldo;
+    int odt;                     /* ql_dtype */
+    const float *lse;
+    const uint16_t *dO;
+    int64_t lddo;
+    void *dq, *dk, *dv;
+    int64_t lddq, lddk, lddv;
+    int dt;                      /* of dq, dk and dv */
+} ql_attn_grad;
+
+int qlinear_attention_backward(const ql_attn *a, const ql_attn_grad *g, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,7 @@ SOURCES = ["qlinear.hip", "quantize.hip", "qgemm.hip", "qgemm_wide.hip", "qgemm_
            "qgemm_kg.hip", "block.hip", "mxquant.hip", "rotary.hip", "qgemm_rows.hip",
            "gemm_bf16.hip", "qgemm_tile.hip",
            "qgemm_mx4.hip", "gemm_dx.hip", "qgemm_kgm.hip", "norm.hip", "train.hip",
-           "attn_forward.hip"]
+           "attn_forward.hip", "attn_backward.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -42,7 +42,8 @@ SOURCE_FLAGS = {"qgemm.hip": VGPR_FORM, "qgemm_skinny.hip": VGPR_FORM,
                 "qgemm_kg.hip": VGPR_FORM, "qgemm_rows.hip": VGPR_FORM,
                 "gemm_bf16.hip": VGPR_FORM, "qgemm_tile.hip": VGPR_FORM,
                 "qgemm_mx4.hip": VGPR_FORM, "gemm_dx.hip": VGPR_FORM,
-                "qgemm_kgm.hip": VGPR_FORM, "attn_forward.hip": VGPR_FORM}
+                "qgemm_kgm.hip": VGPR_FORM, "attn_forward.hip": VGPR_FORM,
+                "attn_backward.hip": VGPR_FORM}
 
 
 def _compile(src):

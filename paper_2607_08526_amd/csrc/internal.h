@@ -351,6 +351,33 @@ size_t seq_attn_bytes(const SeqAttn &s, const SeqAttnPlan &p);  // workspace
 int64_t seq_attn_workgroups(const SeqAttn &s, const SeqAttnPlan &p);
 hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_t stream);
 
+// Its backward pass: dq, dk and dv (both or neither) of one dtype.  sums: workspace of
+// 2 H qrows floats, lse * log2(e) (infinity where a query sees no key) and sum dO O.
+// parts of the reductions over keys (dq) and over queries (dk, dv): partial sums in part,
+// [parts][B Hk][T H / Hk][dh], for dk and dv [parts][B Hk][KT][dh] each.
+struct SeqAttnGrad {
+    SeqAttn s;
+    const void *o;
+    int64_t ldo;
+    int obf16;
+    const float *lse;
+    const uint16_t *dO;
+    int64_t lddo;
+    void *dq, *dk, *dv;
+    int64_t lddq, lddk, lddv;
+    int bf16;
+    float scale;
+    float *sums, *part;
+    int qparts, kparts;
+};
+struct SeqAttnGradPlan {
+    int qparts, kparts;
+};
+SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys, int cus);
+size_t seq_attn_grad_bytes(const SeqAttn &s, const SeqAttnGradPlan &p);
+int64_t seq_attn_grad_workgroups(const SeqAttn &s, const SeqAttnGradPlan &p);
+hipError_t launch_seq_attn_grad(const SeqAttnGrad &a, hipStream_t stream);
+
 // The outputs of a gated pair (gated.h): H, or with dG the gradients of both
 // projections.
 struct GateArgs {

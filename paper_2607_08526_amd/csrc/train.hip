@@ -55,7 +55,8 @@ bool share_bytes(const Rows &a, const Rows &b)
     return apart < lo.w || apart + hi.w > lo.ld;
 }
 
-int check_attn(const ql_attn *a)
+// (backward: there is work for the keys without queries too)
+int check_attn(const ql_attn *a, bool backward)
 {
     if (!a || !(a->scale >= 0.0f) || a->scale > 3e38f)
         return QL_ERR_INVALID;
@@ -75,10 +76,10 @@ int check_attn(const ql_attn *a)
     if (a->ldq < a->H * a->dh || a->ldk < a->Hk * a->dh || a->ldv < a->Hk * a->dh ||
         (!a->q_offsets && a->q_rows < a->B * a->Tq) || (!a->k_offsets && a->k_rows < a->B * a->Tk))
         return QL_ERR_SHAPE;
-    if (a->B == 0 || a->Tq == 0)
+    if (a->B == 0 || (a->Tq == 0 && !backward))
         return QL_OK;
     const bool keys = a->Tk > 0 && a->k_rows > 0;
-    if ((a->q_rows > 0 && !a->q) || (keys && (!a->k || !a->v)))
+    if ((a->Tq > 0 && a->q_rows > 0 && !a->q) || (keys && (!a->k || !a->v)))
         return QL_ERR_INVALID;
     if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || a->ldq % 8 ||
         a->ldk % 8 || a->ldv % 8 || !aligned(a->q_offsets, 8) || !aligned(a->k_offsets, 8) ||
@@ -256,7 +257,7 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
 {
     if (!dt_ok(odt))
         return QL_ERR_INVALID;
-    const int st = check_attn(a);
+    const int st = check_attn(a, false);
     if (st != QL_OK)
         return st;
     if (ldo < a->H * a->dh)
@@ -291,6 +292,81 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
         return QL_ERR_HIP;
     t.part = reinterpret_cast<float *>(ws);
     const int s = status(launch_seq_attn(t, plan, stream));
+    if (own && hipFreeAsync(ws, stream) != hipSuccess)
+        return QL_ERR_HIP;
+    return s;
+}
+
+int qlinear_attention_backward(const ql_attn *a, const ql_attn_grad *g, hipStream_t stream)
+{
+    const int st = check_attn(a, true);
+    if (st != QL_OK)
+        return st;
+    if (!g || !dt_ok(g->odt) || !dt_ok(g->dt) || !g->dk != !g->dv)
+        return QL_ERR_INVALID;
+    const int64_t wide = a->H * a->dh, narrow = a->Hk * a->dh;
+    if (g->ldo < wide || g->lddo < wide || g->lddq < wide ||
+        (g->dk && (g->lddk < narrow || g->lddv < narrow)))
+        return QL_ERR_SHAPE;
+    if (g->ldo >= I31 || g->lddo >= 1 << 24 || g->lddq >= I31 || g->lddk >= I31 || g->lddv >= I31)
+        return QL_ERR_UNSUPPORTED;
+    if (a->B == 0)
+        return QL_OK;
+    const bool queries = a->Tq > 0 && a->q_rows > 0;
+    if (queries && (!g->o || !g->lse || !g->dO || !g->dq))
+        return QL_ERR_INVALID;
+    const uintptr_t grads = g->dt == QL_DT_BF16 ? 8 : 16;
+    if (!aligned(g->o, g->odt == QL_DT_BF16 ? 8 : 16) || g->ldo % 4 || !aligned(g->lse, 4) ||
+        !aligned(g->dO, 16) || g->lddo % 8 || !aligned(g->dq, grads) || !aligned(g->dk, grads) ||
+        !aligned(g->dv, grads) || g->lddq % 4 || (g->dk && (g->lddk % 4 || g->lddv % 4)))
+        return QL_ERR_ALIGN;
+    const Rows more[] = {rows_of(g->o, g->ldo, g->odt, a->q_rows, wide),
+                         rows_of(g->dO, g->lddo, QL_DT_BF16, a->q_rows, wide),
+                         {g->lse, 4 * a->q_rows, 4 * a->q_rows, a->H}};
+    const Rows outs[] = {rows_of(g->dq, g->lddq, g->dt, a->q_rows, wide),
+                         rows_of(g->dk, g->lddk, g->dt, a->k_rows, narrow),
+                         rows_of(g->dv, g->lddv, g->dt, a->k_rows, narrow)};
+    for (int i = 0; i < 3; ++i) {
+        if (meets_inputs(outs[i], *a))
+            return QL_ERR_INVALID;
+        for (const Rows &r : more)
+            if (share_bytes(outs[i], r))
+                return QL_ERR_INVALID;
+        for (int j = 0; j < i; ++j)
+            if (share_bytes(outs[i], outs[j]))
+                return QL_ERR_INVALID;
+    }
+    SeqAttnGrad t{};
+    t.s = seq_attn(*a);
+    if (!queries)
+        t.s.T = 0;
+    t.o = g->o;
+    t.ldo = g->ldo;
+    t.obf16 = g->odt == QL_DT_BF16;
+    t.lse = g->lse;
+    t.dO = g->dO;
+    t.lddo = g->lddo;
+    t.dq = g->dq;
+    t.dk = g->dk;
+    t.dv = g->dv;
+    t.lddq = g->lddq;
+    t.lddk = g->lddk;
+    t.lddv = g->lddv;
+    t.bf16 = g->dt == QL_DT_BF16;
+    t.scale = a->scale;
+    const SeqAttnGradPlan plan = seq_attn_grad_plan(t.s, t.dk != nullptr, current_cus());
+    if (seq_attn_grad_workgroups(t.s, plan) > MAX_WORKGROUPS)
+        return QL_ERR_UNSUPPORTED;
+    t.qparts = plan.qparts;
+    t.kparts = plan.kparts;
+    uint8_t *ws = nullptr;
+    bool own = false;
+    std::unique_lock<std::mutex> turn;
+    const size_t bytes = seq_attn_grad_bytes(t.s, plan);
+    if (bytes && !stream_workspace(bytes, stream, &ws, &own, &turn))
+        return QL_ERR_HIP;
+    t.sums = reinterpret_cast<float *>(ws);
+    const int s = status(launch_seq_attn_grad(t, stream));
     if (own && hipFreeAsync(ws, stream) != hipSuccess)
         return QL_ERR_HIP;
     return s;

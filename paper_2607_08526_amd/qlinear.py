@@ -43,6 +43,7 @@ EXPORTS = [
     "qlinear_mx_forward", "qlinear_gated_forward", "qlinear_gated_backward", "qlinear_rotary",
     # include/qlinear_train.h
     "qlinear_rms_norm", "qlinear_rms_norm_backward", "qlinear_attention_forward",
+    "qlinear_attention_backward",
 ]
 
 PATH_AUTO, PATH_GEMV, PATH_STREAM, PATH_SKINNY, PATH_TILED, PATH_WIDE, PATH_MID = range(7)
@@ -186,6 +187,24 @@ class _Attn(ctypes.Structure):
     ]
 
 
+class _AttnGrad(ctypes.Structure):
+    _fields_ = [
+        ("o", ctypes.c_void_p),
+        ("ldo", ctypes.c_int64),
+        ("odt", ctypes.c_int),
+        ("lse", ctypes.c_void_p),
+        ("dO", ctypes.c_void_p),
+        ("lddo", ctypes.c_int64),
+        ("dq", ctypes.c_void_p),
+        ("dk", ctypes.c_void_p),
+        ("dv", ctypes.c_void_p),
+        ("lddq", ctypes.c_int64),
+        ("lddk", ctypes.c_int64),
+        ("lddv", ctypes.c_int64),
+        ("dt", ctypes.c_int),
+    ]
+
+
 _LIB = None
 
 
@@ -265,6 +284,9 @@ def load():
     lib.qlinear_rms_norm_backward.restype = ci
     lib.qlinear_attention_forward.argtypes = [ctypes.POINTER(_Attn), vp, i64, ci, vp, vp]
     lib.qlinear_attention_forward.restype = ci
+    lib.qlinear_attention_backward.argtypes = [ctypes.POINTER(_Attn), ctypes.POINTER(_AttnGrad),
+                                               vp]
+    lib.qlinear_attention_backward.restype = ci
     lib.qlinear_block_forward.restype = ci
     lib.qlinear_force_path.argtypes = [ci]
     lib.qlinear_force_path.restype = ci
@@ -1047,6 +1069,56 @@ def attention_forward(q, k, v, B, T, H, kv_heads=None, dh=64, kT=None, causal=Fa
     _check(load().qlinear_attention_forward(ctypes.byref(a), _ptr(O), ldo, _ydt(O), _ptr(lse),
                                             _stream(stream)))
     return O, lse
+
+
+# Gradients of a masked attention's inputs.
+AttentionGrads = collections.namedtuple("AttentionGrads", "q k v")
+
+
+def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=None, causal=False,
+                       scale=None, q_offsets=None, k_offsets=None, q_lens=None, k_lens=None,
+                       dq=None, dk=None, dv=None, kv_grads=True, dtype=torch.bfloat16,
+                       stream=None):
+    """The backward pass of attention_forward (its arguments, and the O and lse it
+    returned) from dO, the gradient of O (bf16): AttentionGrads, k's and v's None without
+    kv_grads.  dq [rows of q][>= H * dh], dk and dv [rows of k][>= kv_heads * dh]: row views
+    of one dtype (fp32 or bf16; dtype where they are made here), e.g. the columns of a
+    fused QKV output's gradient.  Padding rows get zeros, rows of no sequence are not
+    written (zeros in outputs made here).  Asynchronous."""
+    a, tensors = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets, k_offsets,
+                       q_lens, k_lens)
+    qrows, krows, wide, narrow = q.shape[0], k.shape[0], H * dh, a.Hk * dh
+    _require(O, "O", _FLOATS, min_cols=wide)
+    _require(dO, "dO", _BF16_BITS, min_cols=wide)
+    _require(lse, "lse", (torch.float32,), (H, qrows))
+    if O.shape[0] != qrows or dO.shape[0] != qrows:
+        raise ValueError(f"O has {O.shape[0]} rows, dO {dO.shape[0]}, expected {qrows}")
+    if not kv_grads and (dk is not None or dv is not None):
+        raise ValueError("dk and dv are given, but not asked for")
+    if dtype not in _FLOATS:
+        raise TypeError(f"gradients are float32 or bfloat16, not {dtype}")
+    given = [t for t in (dq, dk, dv) if t is not None]
+    dtype = given[0].dtype if given else dtype
+    zero = [0.0 if off is not None or rows != B * n else None  # rows that may be of no sequence
+            for off, rows, n in ((q_offsets, qrows, T), (k_offsets, krows, a.Tk))]
+    if dq is None:
+        dq = _attn_new(q, (qrows, wide), dtype, stream, zero[0])
+    if kv_grads:
+        dk = _attn_new(q, (krows, narrow), dtype, stream, zero[1]) if dk is None else dk
+        dv = _attn_new(q, (krows, narrow), dtype, stream, zero[1]) if dv is None else dv
+    for name, t, rows, cols in (("dq", dq, qrows, wide), ("dk", dk, krows, narrow),
+                                ("dv", dv, krows, narrow)):
+        if t is not None:
+            _require(t, name, _FLOATS if name == "dq" else (dq.dtype,), min_cols=cols)
+            if t.shape[0] != rows:
+                raise ValueError(f"{name} has {t.shape[0]} rows, expected {rows}")
+    _on_current_device(O, lse, dO, dq, dk, dv, *tensors)
+    ld = lambda t, n: t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // n) * n
+    g = _AttnGrad(_ptr(O), ld(O, 4), _ydt(O), _ptr(lse), _ptr(dO), ld(dO, 8), _ptr(dq), _ptr(dk),
+                  _ptr(dv), ld(dq, 4), ld(dk, 4) if kv_grads else 0, ld(dv, 4) if kv_grads else 0,
+                  _ydt(dq))
+    _check(load().qlinear_attention_backward(ctypes.byref(a), ctypes.byref(g), _stream(stream)))
+    return AttentionGrads(dq, dk, dv)
 
 
 class forced_path:

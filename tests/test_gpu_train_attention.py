@@ -209,3 +209,158 @@ def test_forward_as_attention(gpu):
                          odtype=torch.bfloat16)
     bound = c.want()["O"][1]
     assert (np.abs(host(O) - host(plain)) <= 2 * bound).all()
+
+
+def check_backward(torch, ql, c, dtype=None, odtype=None):
+    dtype, odtype = dtype or torch.bfloat16, odtype or torch.bfloat16
+    O, lse = ql.attention_forward(c.q, c.k, c.v, *c.shape, odtype=odtype, **c.how)
+    g = ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, dtype=dtype, **c.how)
+    want = c.want(odtype == torch.bfloat16, True, dtype == torch.bfloat16)
+    for name, t in (("dv", g.v), ("dk", g.k), ("dq", g.q)):
+        assert t.dtype == dtype
+        of, got = compare(t, want, name)
+        assert (got[~of] == 0).all()
+    return O, lse, g
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [s for s in FORWARD if s["B"] * s["T"] * s["H"] < 9000],
+                         ids=lambda s: "-".join(map(str, s.values())))
+def test_backward(gpu, shape, causal, dh):
+    torch, ql = gpu
+    check_backward(torch, ql, Case(torch, **shape, causal=causal, dh=dh, size=2.0, pad=8))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("rows", ["padded", "packed", "both"])
+@pytest.mark.parametrize("shape", LENGTHS, ids=lambda s: "-".join(map(str, s.values())))
+def test_backward_lengths(gpu, shape, rows, causal, dh):
+    torch, ql = gpu
+    check_backward(torch, ql, Case(torch, **shape, rows=rows, causal=causal, dh=dh))
+
+
+def test_backward_types_and_scales(gpu):
+    torch, ql = gpu
+    check_backward(torch, ql, Case(torch, 2, 150, 3), torch.float32)
+    check_backward(torch, ql, Case(torch, 2, 150, 4, Hk=2, dh=128), torch.float32, torch.float32)
+    check_backward(torch, ql, Case(torch, 2, 90, 2, scale=0.0, causal=True))
+    for dh in (64, 128):
+        check_backward(torch, ql, Case(torch, 1, 200, 2, dh=dh, size=30.0, causal=True))
+    # parts of the reductions: keys for a few queries, queries (of several heads) for few keys
+    check_backward(torch, ql, Case(torch, 1, 5, 2, kT=3000))
+    check_backward(torch, ql, Case(torch, 1, 700, 8, Hk=1, dh=128, causal=True), torch.float32)
+
+
+def test_backward_against_differences(gpu):
+    """Central differences of the 64-bit forward's <O, dO> along random directions of
+    q, k and v, with steps of 1e-4; their own error, 1e-8 / 6 of a third derivative, is
+    below a thousandth of the bound's sum (scores move by |direction| sqrt(dh) * 1e-4)."""
+    torch, ql = gpu
+    c = Case(torch, 1, 48, 2, Hk=1, kT=60, causal=True)
+    _, _, g = check_backward(torch, ql, c, torch.float32)
+    want = c.want(True, True, False)
+    args = lambda x: (*x, c.seqs, 2, 1, 64, c.scale, True, True)
+    base = [host(t) for t in (c.q, c.k, c.v)]
+    dO = host(c.dO)
+    rng = np.random.default_rng(5)
+    for i, (name, got) in enumerate((("dq", g.q), ("dk", g.k), ("dv", g.v))):
+        for _ in range(3):
+            d = rng.standard_normal(base[i].shape)
+            value = []
+            for t in (1e-4, -1e-4):
+                x = list(base)
+                x[i] = base[i] + t * d
+                value.append((R.attention(*args(x))["O"][0] * dO).sum())
+            diff = (value[0] - value[1]) / 2e-4
+            bound = (want[name][1] * np.abs(d)).sum()
+            assert abs((host(got) * d).sum() - diff) <= 1.001 * bound
+
+
+def test_backward_keeps_other_rows(gpu):
+    """Gradients as the columns of a fused QKV gradient: rows of no sequence and the
+    columns behind keep what they held; only dq on request."""
+    torch, ql = gpu
+    c = Case(torch, 3, 90, 4, Hk=2, rows="packed", lens=[90, 11, 4], causal=True)
+    rows = c.q.shape[0]
+    O, lse = ql.attention_forward(c.q, c.k, c.v, *c.shape, **c.how)
+    for dtype in (torch.bfloat16, torch.float32):
+        d = torch.full((rows, 512 + 8), 7.0, device="cuda", dtype=dtype)
+        dq, dk, dv = d[:, :256], d[:, 256:384], d[:, 384:512]
+        g = ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, dq=dq, dk=dk, dv=dv,
+                                  **c.how)
+        assert g.q is dq and g.k is dk and g.v is dv
+        want = c.want(True, True, dtype == torch.bfloat16)
+        for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+            of, got = compare(t, want, name)
+            assert (got[~of] == 7).all()
+        assert (d[:, 512:] == 7).all()
+        only = ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, kv_grads=False,
+                                     dtype=dtype, **c.how)
+        live = torch.from_numpy(~np.isnan(want["dq"][0])).cuda()
+        assert only.k is None and only.v is None and torch.equal(only.q[live], dq[live])
+    for bad in ([0, 10 ** 12, -5, 2], [rows, 0, rows, rows]):
+        how = c.how | dict(q_offsets=i64(torch, bad), k_offsets=i64(torch, bad))
+        ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, **how)
+    torch.cuda.synchronize()
+
+
+def test_backward_equals_itself(gpu):
+    """Bit for bit the same again (no sum's order depends on anything but the sizes)."""
+    torch, ql = gpu
+    for c in (Case(torch, 2, 300, 8, Hk=2, causal=True), Case(torch, 1, 700, 4, Hk=1, dh=128)):
+        O, lse, g = check_backward(torch, ql, c)
+        for _ in range(4):
+            again = ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, **c.how)
+            assert all(torch.equal(a, b) for a, b in zip(g, again))
+
+
+def test_no_rows(gpu):
+    """No sequences, no queries, no keys: zeros where there are rows, and no fault."""
+    torch, ql = gpu
+    q, none = torch.randn((6, 128), device="cuda").to(torch.bfloat16), None
+    none = q[:0]
+    O, lse = ql.attention_forward(q, none, none, 2, 3, 2, kT=0)
+    assert (O == 0).all() and (lse == -math.inf).all()
+    g = ql.attention_backward(q, none, none, O, lse, q, 2, 3, 2, kT=0)
+    assert (g.q == 0).all() and g.k.shape == (0, 128)
+    O, lse = ql.attention_forward(none, q, q, 2, 0, 2, kT=3)
+    assert O.shape == (0, 128) and lse.shape == (2, 0)
+    g = ql.attention_backward(none, q, q, O, lse, none, 2, 0, 2, kT=3)
+    assert (g.k == 0).all() and (g.v == 0).all()
+    O, lse = ql.attention_forward(q, q, q, 0, 3, 2)
+    assert (O == 0).all() and (lse == -math.inf).all()
+
+
+def test_graph(gpu):
+    """Forward and backward captured, replayed on other inputs and lengths between eager
+    calls (split reductions and their joins among them)."""
+    torch, ql = gpu
+    for c in (Case(torch, 2, 130, 4, Hk=2, rows="padded", lens=[130, 60], causal=True),
+              Case(torch, 1, 2, 4, Hk=1, dh=128, kT=2000)):
+        def step():
+            O, lse = ql.attention_forward(c.q, c.k, c.v, *c.shape, **c.how)
+            return (O, lse, *ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, **c.how))
+
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            step()
+        torch.cuda.current_stream().wait_stream(stream)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            got = step()
+        for k in range(4):
+            for t in (c.q, c.k, c.v, c.dO):
+                t.normal_()
+            if c.how["k_lens"] is not None:
+                for name in ("q_lens", "k_lens"):
+                    c.how[name].copy_(i64(torch, [130 - 40 * k, 7 + k]))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            copies = [t.clone() for t in got]
+            for a, b in zip(copies, step()):
+                assert torch.equal(a, b)
+            torch.cuda.synchronize()
