@@ -146,7 +146,7 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
  * padding rows of q (k, v) get zeros in dq (dk, dv), those of no sequence stay.  No output
  * shares elements with an input or another output (QL_ERR_INVALID; other columns of the
  * same rows may be: the gradients may be those of a fused QKV output).  Workspace (per
- * stream, as in qlinear.h): 8 H q_rows bytes, and fp32 partial sums where few rows leave
+ * stream, as in qlinear.h): 16 H q_rows bytes, and fp32 partial sums where few rows leave
  * CUs idle, at most 80 MiB.  Asynchronous. */
 typedef struct {
     const void *o;

@@ -126,9 +126,15 @@ struct TileLoad {
                                  int tid) const
     {
         const uint32_t at = dma_lds(lds) + (tid & ~63) * 16;
+        if (rows >= ROWS) {
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            dma_load16(first, rows >= ROWS ? full[j] : offset(j, rows, ld, tid), at + j * T * 16);
+            for (int j = 0; j < N; ++j)
+                dma_load16(first, full[j], at + j * T * 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                dma_load16(first, offset(j, rows, ld, tid), at + j * T * 16);
+        }
     }
 };
 
@@ -136,6 +142,35 @@ template <bool B>
 struct Flag {
     static constexpr bool value = B;
 };
+template <int I>
+struct Index {
+    static constexpr int value = I;
+};
+
+// f(Index<0>), f(Index<1>), ..., f(Index<N - 1>)
+template <int N, int I = 0, typename F>
+__device__ inline void each(F &&f)
+{
+    if constexpr (I < N) {
+        f(Index<I>{});
+        each<N, I + 1>(f);
+    }
+}
+
+// x of lanes l and l ^ 32, in this order for both
+__device__ inline void both_halves(float x, float &lo, float &hi)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    lo = __uint_as_float(r[0]);
+    hi = __uint_as_float(r[1]);
+}
+
+// Accumulators that stay in the accumulation registers
+__device__ inline void in_agprs(f32x16 &v) { asm volatile("" : "+a"(v)); }
+
+// The order of instructions stays as written across this point.
+__device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Workgroup p runs on XCD p % 8: each XCD takes a contiguous range of the grid's work,
 // so that the tiles which several workgroups read come into one L2.

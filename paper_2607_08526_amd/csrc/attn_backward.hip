@@ -9,12 +9,14 @@
 // for the second), the second keeps keys and streams queries (dK, dV).  Both form P and
 // dP: 7 products of dh flops per pair instead of 5.
 //
-// A wavefront keeps NS x 32 rows of two tensors in registers as right operands (Q, dO; or
-// K, V); tiles of BT rows of the other two (K, V; or Q, dO) come into LDS by direct loads,
-// two buffers.  For 32 of them at a time, S and dP are formed with the streamed rows as
-// left operand: a lane then holds 16 streamed rows of one kept row, just what the right
-// operand of the second products (transposed left operand: dQ^T += K^T dS^T, dV^T += dO^T
-// P, dK^T += Q^T dS) wants of P and dS, which are rounded to bf16 for it.
+// A wavefront keeps 32 rows of two tensors in registers as right operands (Q, dO; or K,
+// V); tiles of 32 rows of the other two (K, V; or Q, dO) come into LDS by direct loads, a
+// ring of BUFS of them.  S and dP of a tile are formed with the streamed rows as left
+// operand: a lane then holds 16 streamed rows of one kept row, just what the right operand
+// of the second products (transposed left operand: dQ^T += K^T dS^T, dV^T += dO^T P, dK^T
+// += Q^T dS) wants of P and dS, which are rounded to bf16 for it.  Matrix and vector units
+// run beside each other within a wavefront: P and dS of tile j are formed between the
+// matrix instructions of tile j + 1's S and dP; tile j's second products follow.
 #include "attn.h"
 
 namespace qlk {
@@ -23,18 +25,24 @@ namespace {
 constexpr int THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
 
-// kept rows of a workgroup
-template <int NS>
-constexpr int KEEP = 128 * NS;
+constexpr int KEEP = 128;  // kept rows of a workgroup
+constexpr int BT = 32;     // streamed rows of a tile
+// Where the queries of a workgroup see at most so many tiles of keys, d_i is formed as sum
+// P_ij dP_ij in a pass of its own: the rounding of a bf16 O, harmless in a sum over many
+// keys, is not when a few make up the row (dq off by 0.0030 of its norm at 3 keys against
+// 0.0024, of which the output's rounding is 0.0017).
+constexpr int FEW_TILES = 4;
 
-template <int D, bool KEYS, int NS, int BT>
+template <int D, bool KEYS, int BUFS>
 __global__ __launch_bounds__(THREADS)
+__attribute__((amdgpu_waves_per_eu(D == 128 && KEYS ? 1 : 2, 2)))
 void seq_attn_grad_kernel(const SeqAttnGrad a)
 {
     constexpr int TILE = BT * D * 2;  // bytes of a tile
-    constexpr int SUB = BT / 32, DT = D / 32, DS = D / 16;
-    constexpr int BUF = 2 * TILE + (KEYS ? 512 : 0);  // (two arrays of 64 sums)
-    __shared__ __align__(16) uint8_t lds[2 * BUF];
+    constexpr int DT = D / 32, DS = D / 16;
+    constexpr int BUF = 2 * TILE + (KEYS ? 1024 : 0);  // (the sums of 64 rows)
+    __shared__ __align__(16) uint8_t lds[BUFS * BUF + (KEYS ? 16 : 0)];
+    uint8_t *const zeros = lds + BUFS * BUF;
     const int tid = (int)threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, hf = lane >> 5;
@@ -42,7 +50,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const SeqAttn &s = a.s;
     const int G = s.H / s.Hk, parts = KEYS ? a.kparts : a.qparts;
     const int rows = KEYS ? s.KT : s.T * G;  // kept, of a (sequence, key head)
-    const int nb = (rows + KEEP<NS> - 1) / KEEP<NS>;
+    const int nb = (rows + KEEP - 1) / KEEP;
     int L = xcd_order((int)blockIdx.x, (int)gridDim.x);
     const int part = L % parts;
     L /= parts;
@@ -51,23 +59,18 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const int blk = s.causal && !KEYS ? nb - 1 - (L - unit * nb) : L - unit * nb;
     const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
     const SeqRows K = seq_rows(s.k_off, s.k_len, s.krows, s.KT, b);
-    const int row0 = blk * KEEP<NS>;
+    const int row0 = blk * KEEP;
     if (row0 >= (KEYS ? K.cap : Q.cap * G))
         return;
     const int shift = K.len - Q.len;  // causal: query t sees the keys up to t + shift
     const float c = s.c;
 
-    // the kept rows of this lane: a row's operands, and the streamed rows lo to hi that
-    // meet it; of the wavefront: the streamed rows that meet all its live rows
-    bf16x8 x1[NS][DS], x2[NS][DS];
-    int lo[NS], hi[NS];
-    float lse2[NS], delta[NS];  // of a kept query
-    const int wrow = row0 + wave * 32 * NS;
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-        const int row = wrow + 32 * n + l32;
-        const int t = KEYS ? row : row / G, head = KEYS ? hk : hk * G + row - t * G;
-        const bool live = t < (KEYS ? K.len : Q.len);
+    // the kept row of this lane: its operands, and the streamed rows lo to hi that meet it
+    const int wrow = row0 + wave * 32, row = wrow + l32;
+    const int t = KEYS ? row : row / G, head = KEYS ? hk : hk * G + row - t * G;
+    const bool live = t < (KEYS ? K.len : Q.len);
+    bf16x8 x1[DS], x2[DS];
+    {
         const uint16_t *p1 = KEYS ? s.k + (K.first + t) * s.ldk : s.q + (Q.first + t) * s.ldq;
         const uint16_t *p2 = KEYS ? s.v + (K.first + t) * s.ldv : a.dO + (Q.first + t) * a.lddo;
 #pragma unroll
@@ -77,65 +80,57 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
                 v1 = *reinterpret_cast<const u32x4 *>(p1 + head * D + 16 * i + 8 * hf);
                 v2 = *reinterpret_cast<const u32x4 *>(p2 + head * D + 16 * i + 8 * hf);
             }
-            x1[n][i] = __builtin_bit_cast(bf16x8, v1);
-            x2[n][i] = __builtin_bit_cast(bf16x8, v2);
-        }
-        if (KEYS) {
-            lo[n] = s.causal ? t - shift : 0;
-            hi[n] = live ? Q.len - 1 : -1;
-        } else {
-            lo[n] = 0;
-            hi[n] = live ? (s.causal ? min(K.len - 1, t + shift) : K.len - 1) : -1;
-            // d = sum dO O, and lse in powers of two
-            float d = 0.0f;
-            lse2[n] = INFINITY;
-            if (live) {
-                const int64_t at = (Q.first + t) * a.ldo + head * D + 8 * hf;
-#pragma unroll
-                for (int i = 0; i < DS; ++i) {
-                    float o[8];
-                    if (a.obf16) {
-                        const uint16_t *p = static_cast<const uint16_t *>(a.o) + at + 16 * i;
-                        const u32x2 w[2] = {*reinterpret_cast<const u32x2 *>(p),
-                                            *reinterpret_cast<const u32x2 *>(p + 4)};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            o[2 * j] = __uint_as_float(w[j >> 1][j & 1] << 16);
-                            o[2 * j + 1] = __uint_as_float(w[j >> 1][j & 1] & 0xFFFF0000u);
-                        }
-                    } else {
-                        const float *p = static_cast<const float *>(a.o) + at + 16 * i;
-                        const f32x4_t w[2] = {*reinterpret_cast<const f32x4_t *>(p),
-                                              *reinterpret_cast<const f32x4_t *>(p + 4)};
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            o[j] = w[j >> 2][j & 3];
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        d = __builtin_fmaf((float)x2[n][i][j], o[j], d);
-                }
-            }
-            d += __shfl_xor(d, 32);
-            delta[n] = d;
-            if (live) {
-                const int64_t at = head * s.qrows + Q.first + t;
-                const float l = a.lse[at];
-                lse2[n] = l == -INFINITY ? INFINITY : l * LOG2E;
-                if (part == 0 && hf == 0) {
-                    a.sums[at] = lse2[n];
-                    a.sums[s.H * s.qrows + at] = d;
-                }
-            }
+            x1[i] = __builtin_bit_cast(bf16x8, v1);
+            x2[i] = __builtin_bit_cast(bf16x8, v2);
         }
     }
+    const int lo = KEYS && s.causal ? t - shift : 0;
+    const int hi = !live ? -1 : KEYS ? Q.len - 1 : s.causal ? min(K.len - 1, t + shift) : K.len - 1;
+    // of a kept query: lse in powers of two, and d = sum dO O
+    float lse2 = INFINITY, delta = 0.0f;
+    if (!KEYS && live) {
+        const int64_t at = (Q.first + t) * a.ldo + head * D + 8 * hf;
+#pragma unroll
+        for (int i = 0; i < DS; ++i) {
+            float o[8];
+            if (a.obf16) {
+                const uint16_t *p = static_cast<const uint16_t *>(a.o) + at + 16 * i;
+                const u32x2 w[2] = {*reinterpret_cast<const u32x2 *>(p),
+                                    *reinterpret_cast<const u32x2 *>(p + 4)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    o[2 * j] = __uint_as_float(w[j >> 1][j & 1] << 16);
+                    o[2 * j + 1] = __uint_as_float(w[j >> 1][j & 1] & 0xFFFF0000u);
+                }
+            } else {
+                const float *p = static_cast<const float *>(a.o) + at + 16 * i;
+                const f32x4_t w[2] = {*reinterpret_cast<const f32x4_t *>(p),
+                                      *reinterpret_cast<const f32x4_t *>(p + 4)};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    o[j] = w[j >> 2][j & 3];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                delta = __builtin_fmaf((float)x2[i][j], o[j], delta);
+        }
+        const float l = a.lse[head * s.qrows + Q.first + t];
+        lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
+    }
+    auto halves = [](float x) {
+        float l, h;
+        both_halves(x, l, h);
+        return l + h;
+    };
+    if (!KEYS)
+        delta = halves(delta);
     // tiles [first, first + tiles) of streamed rows, for keys of each head in turn
     int first = 0, tiles;
     if (KEYS) {
         first = s.causal ? max(0, row0 - shift) / BT : 0;
         tiles = row0 < K.len ? max(0, (Q.len + BT - 1) / BT - first) : 0;
     } else {
-        const int tmax = min((row0 + KEEP<NS> - 1) / G, Q.len - 1);
+        const int tmax = min((row0 + KEEP - 1) / G, Q.len - 1);
         const int keys = Q.len > row0 / G
                              ? max(0, (s.causal ? min(K.len - 1, tmax + shift) : K.len - 1) + 1)
                              : 0;
@@ -144,7 +139,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const int64_t all = (int64_t)tiles * (KEYS ? G : 1);
     const int j0 = (int)(all * part / parts), j1 = (int)(all * (part + 1) / parts);
     // streamed rows that need no mask
-    const int free_lo = KEYS && s.causal ? wrow + 32 * NS - 1 - shift : 0;
+    const int free_lo = KEYS && s.causal ? wrow + 31 - shift : 0;
     const int free_hi = KEYS ? Q.len - 1
                              : (s.causal ? min(K.len - 1, wrow / G + shift) : K.len - 1);
 
@@ -152,168 +147,291 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     TileLoad<D, BT, THREADS> load1, load2;
     load1.init(ld1, tid);
     load2.init(ld2, tid);
-    auto tile_of = [&](int j, int &head) {
+    constexpr int LOADS = 2 * TileLoad<D, BT, THREADS>::N + (KEYS ? 1 : 0);  // a tile's
+    // the first streamed row of tile j, and its head
+    auto start_of = [&](int j, int &h) {
         const int g = KEYS ? j / tiles : 0;
-        head = KEYS ? hk * G + g : hk;
-        return first + j - g * tiles;
+        h = KEYS ? hk * G + g : hk;
+        return (first + j - g * tiles) * BT;
     };
-    auto fetch = [&](int j, uint8_t *buf) {
-        int head;
-        const int r0 = tile_of(j, head) * BT, left = (KEYS ? Q.len : K.len) - r0;
+    auto buffer = [&](int j) { return lds + j % BUFS * BUF; };
+    auto fetch = [&](int j) {
+        int h;
+        const int r0 = start_of(j, h), left = (KEYS ? Q.len : K.len) - r0;
         const int64_t at = (KEYS ? Q.first : K.first) + r0;
-        const uint16_t *p1 = (KEYS ? s.q : s.k) + at * ld1 + head * D;
-        const uint16_t *p2 = (KEYS ? a.dO : s.v) + at * ld2 + head * D;
+        const uint16_t *p1 = (KEYS ? s.q : s.k) + at * ld1 + h * D;
+        const uint16_t *p2 = (KEYS ? a.dO : s.v) + at * ld2 + h * D;
+        uint8_t *const buf = buffer(j);
         load1.issue(reinterpret_cast<const uint8_t *>(p1), left, ld1, buf, tid);
         load2.issue(reinterpret_cast<const uint8_t *>(p2), left, ld2, buf + TILE, tid);
-        if (KEYS && wave < 2) {
-            const float *sums = a.sums + (int64_t)wave * s.H * s.qrows + head * s.qrows + at;
-            dma_load4_at(sums + min(lane, left - 1), dma_lds(buf + 2 * TILE + wave * 256));
-        }
+        if (KEYS)  // (every wavefront the same: all have as many loads in flight)
+            dma_load16_at(a.sums + (h * s.qrows + at + min(lane, left - 1)) * 4,
+                          dma_lds(buf + 2 * TILE));
     };
 
-    f32x16 acc1[NS][DT], acc2[KEYS ? NS : 1][KEYS ? DT : 1];
+    f32x16 acc1[DT], acc2[KEYS ? DT : 1];
 #pragma unroll
-    for (int n = 0; n < NS; ++n)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int r = 0; r < 16; ++r) {
+            acc1[d][r] = 0.0f;
+            if (KEYS)
+                acc2[d][r] = 0.0f;
+        }
+
+    // What a tile's products leave: its scores and dP, then P and dS as operands.
+    struct Raw {
+        f32x16 s, dp;
+    };
+    struct Cooked {
+        bf16x8 p[KEYS ? 2 : 1], ds[2];
+    };
+    // Values 2 I and 2 I + 1 of a lane: streamed rows r0 + 8 (r / 4) + 4 hf + r % 4, r = 2 I
+    // and 2 I + 1; from, to: lo and hi less r0 + 4 hf.
+    auto cook = [&](auto maskc, auto ic, int from, int to, const Raw &x, Cooked &y) {
+        constexpr bool MASK = decltype(maskc)::value;
+        constexpr int I = decltype(ic)::value;
+        float p[2], ds[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int r = 2 * I + k, at = 8 * (r >> 2) + (r & 3);
+            p[k] = __builtin_amdgcn_exp2f(KEYS ? x.s[r] * c : __builtin_fmaf(x.s[r], c, -lse2));
+            if (MASK)
+                p[k] = at <= to && (!KEYS || at >= from) ? p[k] : 0.0f;
+            ds[k] = p[k] * (KEYS ? x.dp[r] : x.dp[r] - delta);
+        }
+        auto put = [](bf16x8 &v, int i, uint32_t w) {
+            u32x4 u = __builtin_bit_cast(u32x4, v);
+            u[i] = w;
+            v = __builtin_bit_cast(bf16x8, u);
+        };
+        if constexpr (KEYS)
+            put(y.p[I / 4], I % 4, pack_bf16(p[0], p[1]));
+        put(y.ds[I / 4], I % 4, pack_bf16(ds[0], ds[1]));
+    };
+    // D = 128 (one code for every tile, or the accumulators' registers run out): the mask
+    // is what a tile's scores start from, 0 or -infinity.
+    constexpr bool BIAS = D == 128 || KEYS;
+    auto bias = [&](int j, Raw &x) {
+        int h;
+        const int r0 = start_of(j, h), from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
+        if (r0 >= free_lo && r0 + BT - 1 <= free_hi) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                x.s[r] = 0.0f;
+        } else {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                acc1[n][d][r] = 0.0f;
-                if (KEYS)
-                    acc2[n][d][r] = 0.0f;
-            }
-
-    auto block = [&](auto maskc, const uint8_t *buf, int sub, int r0) {
-        constexpr bool MASK = decltype(maskc)::value;
-        const uint8_t *t1 = buf, *t2 = buf + TILE;
-        f32x16 sc[NS], dp[NS];
-        const f32x16 zero = {};
-#pragma unroll
-        for (int i = 0; i < DS; ++i) {
-            const bf16x8 w = row_operand<D>(t1, 32 * sub + l32, i, hf);
-#pragma unroll
-            for (int n = 0; n < NS; ++n)
-                sc[n] = mfma(w, x1[n][i], i == 0 ? zero : sc[n]);
-        }
-#pragma unroll
-        for (int i = 0; i < DS; ++i) {
-            const bf16x8 w = row_operand<D>(t2, 32 * sub + l32, i, hf);
-#pragma unroll
-            for (int n = 0; n < NS; ++n)
-                dp[n] = mfma(w, x2[n][i], i == 0 ? zero : dp[n]);
-        }
-        f32x4_t ls[4], dl[4];  // of streamed queries 8 e + 4 hf + 0 .. 3
-        if (KEYS) {
-            const float *const f = reinterpret_cast<const float *>(buf + 2 * TILE) + 32 * sub + 4 * hf;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                ls[e] = *reinterpret_cast<const f32x4_t *>(f + 8 * e);
-                dl[e] = *reinterpret_cast<const f32x4_t *>(f + 64 + 8 * e);
+                const int at = 8 * (r >> 2) + (r & 3);
+                x.s[r] = at <= to && (!KEYS || at >= from) ? 0.0f : -INFINITY;
             }
         }
-        bf16x8 pb[NS][2], sb[NS][2];
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            const int from = lo[n] - r0 - 32 * sub - 4 * hf, to = hi[n] - r0 - 32 * sub - 4 * hf;
-#pragma unroll
-            for (int ch = 0; ch < 2; ++ch) {
-                uint32_t pw[4], sw[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p[2], ds[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int r = 8 * ch + 2 * e + k, x = 8 * (r >> 2) + (r & 3);
-                        p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(
-                            sc[n][r], c, -(KEYS ? ls[r >> 2][r & 3] : lse2[n])));
-                        ds[k] = p[k] * (dp[n][r] - (KEYS ? dl[r >> 2][r & 3] : delta[n]));
-                        if (MASK) {
-                            const bool in = x <= to && (!KEYS || x >= from);
-                            p[k] = in ? p[k] : 0.0f;
-                            ds[k] = in ? ds[k] : 0.0f;
-                        }
-                    }
-                    pw[e] = pack_bf16(p[0], p[1]);
-                    sw[e] = pack_bf16(ds[0], ds[1]);
-                }
-                pb[n][ch] = __builtin_bit_cast(bf16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
-                sb[n][ch] = __builtin_bit_cast(bf16x8, u32x4{sw[0], sw[1], sw[2], sw[3]});
-            }
+    };
+    // The matrix instructions of a step: S and dP of the tile in next (for kept keys they
+    // start with -lse / scale and -d of the streamed queries, three bf16 each that add up
+    // to 24 bits: as products with ones, where reading them from LDS in the accumulators'
+    // layout, 16 values a lane, would take as long as reading the tiles' rows), then the
+    // second products of the tile in prev.
+    constexpr int SUMS = KEYS ? 2 : 0, FIRST = SUMS + 2 * DS, SECOND = (KEYS ? 4 : 2) * DT;
+    const uint32_t one = hf == 0 ? 0x3F80u : 0u, ones = one | one << 16;
+    const bf16x8 ones_lse = __builtin_bit_cast(bf16x8, u32x4{ones, one, 0u, 0u});
+    const bf16x8 ones_d = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, ones, one});
+    auto operand = [&](auto ic, const uint8_t *next, const uint8_t *prev) {
+        constexpr int I = decltype(ic)::value;
+        if constexpr (I < SUMS) {
+            return __builtin_bit_cast(
+                bf16x8, *reinterpret_cast<const u32x4 *>(hf ? zeros : next + 2 * TILE + l32 * 16));
+        } else if constexpr (I < FIRST) {
+            return row_operand<D>(next + (I % 2) * TILE, l32, (I - SUMS) / 2, hf);
+        } else {
+            constexpr int k = I - FIRST, which = KEYS ? k % 2 : 0, m = KEYS ? k / 2 : k;
+            return transposed_operand<D>(prev + which * TILE, m / DT, m % DT, lane);
         }
-#pragma unroll
-        for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const bf16x8 w1 = transposed_operand<D>(t1, 2 * sub + ch, d, lane);
-#pragma unroll
-                for (int n = 0; n < NS; ++n)
-                    acc1[n][d] = mfma(w1, sb[n][ch], acc1[n][d]);
-                if constexpr (KEYS) {
-                    const bf16x8 w2 = transposed_operand<D>(t2, 2 * sub + ch, d, lane);
-#pragma unroll
-                    for (int n = 0; n < NS; ++n)
-                        acc2[n][d] = mfma(w2, pb[n][ch], acc2[n][d]);
-                }
+    };
+    auto multiply = [&](auto ic, bf16x8 w, Raw &x, const Cooked &y) {
+        constexpr int I = decltype(ic)::value;
+        if constexpr (I < FIRST) {
+            const f32x16 zero = {};
+            constexpr int i = (I - SUMS) / 2;
+            if constexpr (I % 2 == 0)
+                x.s = mfma(w, I < SUMS ? ones_lse : x1[I < SUMS ? 0 : i],
+                           I == 0 && !BIAS ? zero : x.s);
+            else
+                x.dp = mfma(w, I < SUMS ? ones_d : x2[I < SUMS ? 0 : i], I == 1 ? zero : x.dp);
+        } else {
+            constexpr int k = I - FIRST, m = KEYS ? k / 2 : k;
+            if constexpr (KEYS && k % 2)
+                acc2[m % DT] = mfma(w, y.p[KEYS ? m / DT : 0], acc2[KEYS ? m % DT : 0]);
+            else
+                acc1[m % DT] = mfma(w, y.ds[m / DT], acc1[m % DT]);
+        }
+    };
+    // The first products of tile j + 1 with the PAIRS steps of cook for tile j between them,
+    // then the second products of tile j; operands are read AHEAD of their instruction.
+    constexpr int AHEAD = 3, PAIRS = 8;
+    auto run = [&](auto maskc, int j, int r0, const Raw &cur, Raw &nxt, Cooked &now) {
+        const uint8_t *const next = buffer(j + 1), *const buf = buffer(j);
+        const int from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
+        constexpr int N = FIRST + SECOND;
+        bf16x8 w[AHEAD + 1];
+        each<AHEAD>([&](auto ic) { w[decltype(ic)::value] = operand(ic, next, buf); });
+        each<N>([&](auto ic) {
+            constexpr int I = decltype(ic)::value;
+            if constexpr (I + AHEAD < N)
+                w[(I + AHEAD) % (AHEAD + 1)] = operand(Index<I + AHEAD>{}, next, buf);
+            multiply(ic, w[I % (AHEAD + 1)], nxt, now);
+            if constexpr (I < FIRST) {
+                constexpr int P0 = PAIRS * I / FIRST, P1 = PAIRS * (I + 1) / FIRST;
+                each<P1 - P0>([&](auto pc) {
+                    cook(maskc, Index<P0 + decltype(pc)::value>{}, from, to, cur, now);
+                });
+                keep_order();
             }
+        });
+    };
+    auto first_products = [&](int j, Raw &x) {
+        const uint8_t *const buf = buffer(j);
+        if (BIAS)
+            bias(j, x);
+        Cooked none;
+        each<FIRST>([&](auto ic) { multiply(ic, operand(ic, buf, buf), x, none); });
+    };
+    auto second_products = [&](int j, const Cooked &y) {
+        const uint8_t *const buf = buffer(j);
+        Raw none;
+        each<SECOND>([&](auto ic) {
+            constexpr int I = FIRST + decltype(ic)::value;
+            multiply(Index<I>{}, operand(Index<I>{}, buf, buf), none, y);
+        });
     };
 
-    // At the start of a step its tile's loads (the last issued) have landed and every
-    // wavefront has finished the step before it, whose buffer takes the next tile.
-    if (j0 < j1)
-        fetch(j0, lds);
-    for (int j = j0; j < j1; ++j) {
-        const uint8_t *const buf = lds + ((j - j0) & 1) * BUF;
+    if constexpr (!KEYS) {
+        if (tiles > 0 && tiles <= FEW_TILES) {
+            float d = 0.0f;
+            for (int j = 0; j < tiles; ++j) {
+                fetch(j);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                Raw x;
+                first_products(j, x);
+                const int to = hi - j * BT - 4 * hf;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[r], c, -lse2));
+                    if (8 * (r >> 2) + (r & 3) <= to)
+                        d = __builtin_fmaf(p, x.dp[r], d);
+                }
+                __syncthreads();
+            }
+            delta = halves(d);
+        }
+        if (live && part == 0 && hf == 0) {
+            // -lse / scale and -d as three bf16 each (a query that sees no key: so low that
+            // its probabilities are 0)
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float x = i ? -delta : lse2 == INFINITY ? -1e38f : -lse2 / c;
+                uint32_t part3[3];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    part3[k] = pack_bf16(x, 0.0f);
+                    x -= __uint_as_float(part3[k] << 16);
+                }
+                w[2 * i] = part3[0] | part3[1] << 16;
+                w[2 * i + 1] = part3[2];
+            }
+            *reinterpret_cast<u32x4 *>(a.sums + (head * s.qrows + Q.first + t) * 4) =
+                u32x4{w[0], w[1], w[2], w[3]};
+        }
+    }
+
+    // At the start of step j the loads of tile j + 1 have landed (of those issued, up to tile
+    // j + BUFS - 2, later ones may be in flight) and every wavefront has finished step j -
+    // 1, so the buffer of tile j - 1 takes tile j + BUFS - 1.
+    static_assert(BUFS == 3 || BUFS == 4, "");
+    auto begin = [&](int j) {
+        if (BUFS == 4 && j + 2 < j1)
+            __builtin_amdgcn_s_waitcnt(dma_vmcnt(LOADS));
+        else
+            __builtin_amdgcn_s_waitcnt(dma_vmcnt(0));
+        asm volatile("" ::: "memory");
+        __syncthreads();
+        if (j + BUFS - 1 < j1)
+            fetch(j + BUFS - 1);
+    };
+    Cooked y;
+    auto step = [&](int j, const Raw &cur, Raw &nxt) {
+        begin(j);
+        int h;
+        const int r0 = start_of(j, h);
+        if (BIAS)
+            bias(j + 1, nxt);
+        if (BIAS || (r0 >= free_lo && r0 + BT - 1 <= free_hi))
+            run(Flag<false>{}, j, r0, cur, nxt, y);
+        else
+            run(Flag<true>{}, j, r0, cur, nxt, y);
+    };
+    auto last = [&](const Raw &cur) {
+        const int j = j1 - 1;
+        int h;
+        const int r0 = start_of(j, h) + 4 * hf;
+        each<PAIRS>([&](auto ic) { cook(Flag<!BIAS>{}, ic, lo - r0, hi - r0, cur, y); });
+        second_products(j, y);
+    };
+    if (j0 < j1) {
+        Raw xa, xb;
+        if (KEYS && tid == 0)
+            *reinterpret_cast<u32x4 *>(zeros) = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < BUFS - 1; ++i)
+            if (j0 + i < j1)
+                fetch(j0 + i);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (j + 1 < j1)
-            fetch(j + 1, lds + ((j - j0 + 1) & 1) * BUF);
-        int head;
-        const int r0 = tile_of(j, head) * BT;
-#pragma unroll 1
-        for (int sub = 0; sub < SUB; ++sub) {
-            const int from = r0 + 32 * sub;
-            if (from >= free_lo && from + 31 <= free_hi)
-                block(Flag<false>{}, buf, sub, r0);
-            else
-                block(Flag<true>{}, buf, sub, r0);
+        first_products(j0, xa);
+        int j = j0;
+        for (; j + 2 < j1; j += 2) {
+            step(j, xa, xb);
+            step(j + 1, xb, xa);
+        }
+        if (j + 1 < j1) {
+            step(j, xa, xb);
+            last(xb);
+        } else {
+            last(xa);
         }
     }
 
     // channel 32 d + 8 e + 4 hf + r % 4 of the lane's row; padding rows: zeros
+    if (t >= (KEYS ? K.cap : Q.cap))
+        return;
+    auto store = [&](const f32x16 (&acc)[DT], void *out, int64_t ld, float *to, float f) {
+        const int64_t at = ((KEYS ? K.first : Q.first) + t) * ld + head * D;
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
-        const int row = wrow + 32 * n + l32;
-        const int t = KEYS ? row : row / G, head = KEYS ? hk : hk * G + row - t * G;
-        if (t >= (KEYS ? K.cap : Q.cap))
-            continue;
-        const bool live = t < (KEYS ? K.len : Q.len);
-        auto store = [&](const f32x16 (&acc)[DT], void *out, int64_t ld, float *to, float f) {
-            const int64_t at = ((KEYS ? K.first : Q.first) + t) * ld + head * D;
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+            for (int e = 0; e < 4; ++e) {
+                const int ch = 32 * d + 8 * e + 4 * hf;
+                f32x4_t v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int ch = 32 * d + 8 * e + 4 * hf;
-                    f32x4_t v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        v[i] = live ? acc[d][4 * e + i] * f : 0.0f;
-                    if (parts > 1)
-                        *reinterpret_cast<f32x4_t *>(
-                            to + (((int64_t)part * s.B * s.Hk + unit) * rows + row) * D + ch) = v;
-                    else if (a.bf16)
-                        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(out) + at + ch) =
-                            u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                    else
-                        *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + at + ch) = v;
-                }
-        };
-        if constexpr (KEYS) {
-            store(acc1[n], a.dk, a.lddk, a.part, a.scale);
-            store(acc2[n], a.dv, a.lddv, a.part + (int64_t)parts * s.B * s.Hk * rows * D, 1.0f);
-        } else {
-            store(acc1[n], a.dq, a.lddq, a.part, a.scale);
-        }
+                for (int i = 0; i < 4; ++i)
+                    v[i] = live ? acc[d][4 * e + i] * f : 0.0f;
+                if (parts > 1)
+                    *reinterpret_cast<f32x4_t *>(
+                        to + (((int64_t)part * s.B * s.Hk + unit) * rows + row) * D + ch) = v;
+                else if (a.bf16)
+                    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(out) + at + ch) =
+                        u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                else
+                    *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + at + ch) = v;
+            }
+    };
+    if constexpr (KEYS) {
+        store(acc1, a.dk, a.lddk, a.part, a.scale);
+        store(acc2, a.dv, a.lddv, a.part + (int64_t)parts * s.B * s.Hk * rows * D, 1.0f);
+    } else {
+        store(acc1, a.dq, a.lddq, a.part, a.scale);
     }
 }
 
@@ -353,7 +471,7 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
 int64_t blocks(const SeqAttn &s, bool keys)
 {
     const int64_t rows = keys ? s.KT : (int64_t)s.T * (s.H / s.Hk);
-    return (rows + KEEP<1> - 1) / KEEP<1> * s.B * s.Hk;
+    return (rows + KEEP - 1) / KEEP * s.B * s.Hk;
 }
 
 template <int D, bool KEYS>
@@ -362,7 +480,7 @@ hipError_t go(const SeqAttnGrad &a, hipStream_t stream)
     const int parts = KEYS ? a.kparts : a.qparts;
     const unsigned grid = (unsigned)(blocks(a.s, KEYS) * parts);
     if (grid)
-        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, 1, D == 64 ? 64 : 32>), dim3(grid),
+        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, 4>), dim3(grid),
                            dim3(THREADS), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts < 2 || !grid)
@@ -382,14 +500,13 @@ SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys, int cus)
     auto parts = [&](int64_t wgs, int64_t tiles) {
         if (wgs == 0 || wgs >= cus)
             return 1;
-        const int64_t want = (cus + wgs - 1) / wgs, most = tiles / 4;
+        const int64_t want = (cus + wgs - 1) / wgs, most = tiles / 8;
         return (int)(most < 2 ? 1 : want < most ? want : most);
     };
-    const int64_t bt = s.dh == 64 ? 64 : 32;
     SeqAttnGradPlan p{1, 1};
-    p.qparts = parts(blocks(s, false), (s.KT + bt - 1) / bt);
+    p.qparts = parts(blocks(s, false), (s.KT + BT - 1) / BT);
     if (keys)
-        p.kparts = parts(blocks(s, true), (s.T + bt - 1) / bt * (s.H / s.Hk));
+        p.kparts = parts(blocks(s, true), (s.T + BT - 1) / BT * (s.H / s.Hk));
     return p;
 }
 
@@ -401,7 +518,7 @@ int64_t seq_attn_grad_workgroups(const SeqAttn &s, const SeqAttnGradPlan &p)
 
 size_t seq_attn_grad_bytes(const SeqAttn &s, const SeqAttnGradPlan &p)
 {
-    const size_t sums = ((size_t)2 * s.H * s.qrows * 4 + 255) & ~(size_t)255;
+    const size_t sums = (size_t)16 * s.H * s.qrows;
     size_t q = 0, k = 0;
     if (p.qparts > 1)
         q = (size_t)p.qparts * s.B * s.H * s.T * s.dh * 4;
@@ -413,7 +530,7 @@ size_t seq_attn_grad_bytes(const SeqAttn &s, const SeqAttnGradPlan &p)
 hipError_t launch_seq_attn_grad(const SeqAttnGrad &g, hipStream_t stream)
 {
     SeqAttnGrad a = g;
-    a.part = a.sums + (((size_t)2 * a.s.H * a.s.qrows * 4 + 255) & ~(size_t)255) / 4;
+    a.part = a.sums + (size_t)4 * a.s.H * a.s.qrows;
     const hipError_t e = a.s.dh == 64 ? go<64, false>(a, stream) : go<128, false>(a, stream);
     if (e != hipSuccess || !a.dk)
         return e;

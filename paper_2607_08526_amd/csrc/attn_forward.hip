@@ -102,16 +102,6 @@ void seq_attn_kernel(const SeqAttnOut a)
         vload.issue(vbase + (int64_t)kt * BK * s.ldv * 2, K.len - kt * BK, s.ldv, buf, tid);
     };
 
-    auto scores = [&](const uint8_t *ks, f32x16 (&sc)[SUB]) {
-        const f32x16 zero = {};
-#pragma unroll
-        for (int i = 0; i < DS; ++i)
-#pragma unroll
-            for (int sub = 0; sub < SUB; ++sub)
-                sc[sub] = mfma(row_operand<D>(ks, 32 * sub + l32, i, hf), qb[i],
-                               i == 0 ? zero : sc[sub]);
-    };
-
     f32x16 oacc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -120,27 +110,57 @@ void seq_attn_kernel(const SeqAttnOut a)
             oacc[d][r] = 0.0f;
     float mrun = -INFINITY, lrun = 0.0f;
     const float c = s.c;
-    // score r of subtile sub is key kt BK + 32 sub + 8 (r / 4) + 4 hf + r % 4
-    auto tile_max = [&](auto maskc, int kt, const f32x16 (&sc)[SUB]) {
+    // Softmax of a tile's scores in PARTS parts, to be placed between matrix instructions:
+    // its maximum, the factor that brings the sums so far to it, then the probabilities as
+    // operands, two at a time.  Score r of subtile sub is key kt BK + 32 sub + 8 (r / 4) + 4
+    // hf + r % 4.
+    // D = 128 (one code for every tile, or the registers run out): the mask is what a
+    // tile's scores start from, 0 or -infinity.
+    constexpr bool BIAS = D == 128;
+    constexpr int MAXES = 4 * SUB, PAIRS = 8 * SUB, PARTS = MAXES + 1 + PAIRS;
+    float mx[2], ls[2], mc, alpha;
+    auto softmax = [&](auto maskc, auto ic, int left, const f32x16 (&sc)[SUB],
+                       bf16x8 (&pb)[SUB][2]) {
         constexpr bool MASK = decltype(maskc)::value;
-        const int left = lim - kt * BK - 4 * hf;
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        constexpr int I = decltype(ic)::value;
+        auto in = [&](int sub, int r) { return 32 * sub + 8 * (r >> 2) + (r & 3) <= left; };
+        if constexpr (I < MAXES) {
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                mx[r & 3] = fmaxf(mx[r & 3],
-                                  !MASK || 32 * sub + 8 * (r >> 2) + (r & 3) <= left ? sc[sub][r]
-                                                                                     : -INFINITY);
-        float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        mt = fmaxf(mt, __shfl_xor(mt, 32));
-        const bool up = mt > -INFINITY && (mrun == -INFINITY || (mt - mrun) * c > LAZY);
-        if (__ballot(up) != 0) {
-            const float mnew = fmaxf(mrun, mt);
-            const float alpha =
-                mrun == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mrun - mnew) * c);
+            for (int e = 0; e < 4; ++e) {
+                const int sub = I / 4, r = 4 * (I % 4) + e;
+                const float x = !MASK || in(sub, r) ? sc[sub][r] : -INFINITY;
+                mx[e & 1] = I == 0 && e < 2 ? x : fmaxf(mx[e & 1], x);
+            }
+        } else if constexpr (I == MAXES) {
+            float lo, hi;
+            both_halves(fmaxf(mx[0], mx[1]), lo, hi);
+            const float mt = fmaxf(lo, hi);
+            // the maximum moves only where the scores exceed it by more than LAZY (no score
+            // at all: it stays at -inf; c > 0, so that the factor from there is 0)
+            const bool up = mt > mrun && !((mt - mrun) * c <= LAZY);
+            const float mnew = up ? mt : mrun;
+            alpha = up ? __builtin_amdgcn_exp2f((mrun - mnew) * c) : 1.0f;
             mrun = mnew;
-            lrun *= alpha;
+            mc = BIAS && mrun == -INFINITY ? 0.0f : mrun * c;
+        } else {
+            constexpr int p = I - MAXES - 1, sub = p / 8, r = 2 * (p % 8);
+            float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][r], c, -mc));
+            float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][r + 1], c, -mc));
+            if (MASK) {
+                p0 = in(sub, r) ? p0 : 0.0f;
+                p1 = in(sub, r + 1) ? p1 : 0.0f;
+            }
+            ls[0] = p == 0 ? p0 : ls[0] + p0;
+            ls[1] = p == 0 ? p1 : ls[1] + p1;
+            u32x4 w = __builtin_bit_cast(u32x4, pb[sub][r / 8]);
+            w[r / 2 % 4] = pack_bf16(p0, p1);
+            pb[sub][r / 8] = __builtin_bit_cast(bf16x8, w);
+            if constexpr (I == PARTS - 1)
+                lrun = __builtin_fmaf(lrun, alpha, ls[0] + ls[1]);
+        }
+    };
+    auto rescale = [&] {
+        if (__ballot(alpha != 1.0f) != 0) {
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -148,38 +168,79 @@ void seq_attn_kernel(const SeqAttnOut a)
                     oacc[d][r] *= alpha;
         }
     };
-    auto tile_pv = [&](auto maskc, int kt, const f32x16 (&sc)[SUB], const uint8_t *vt) {
-        constexpr bool MASK = decltype(maskc)::value;
+    auto bias = [&](int kt, f32x16 (&sc)[SUB]) {
         const int left = lim - kt * BK - 4 * hf;
-        const float mc = mrun == -INFINITY ? 0.0f : mrun * c;
-        float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        bf16x8 pb[SUB][2];
+        if (BIAS && kt < kt1 && (kt + 1) * BK <= free_keys) {
 #pragma unroll
-        for (int sub = 0; sub < SUB; ++sub)
+            for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
-            for (int ch = 0; ch < 2; ++ch) {
-                uint32_t w[4];
+                for (int r = 0; r < 16; ++r)
+                    sc[sub][r] = 0.0f;
+        } else if (BIAS) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r0 = 8 * ch + 2 * e, k0 = 32 * sub + 8 * (r0 >> 2) + (r0 & 3);
-                    float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][r0], c, -mc));
-                    float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][r0 + 1], c, -mc));
-                    if (MASK) {
-                        p0 = k0 <= left ? p0 : 0.0f;
-                        p1 = k0 + 1 <= left ? p1 : 0.0f;
-                    }
-                    ls[e] += p0 + p1;
-                    w[e] = pack_bf16(p0, p1);
-                }
-                pb[sub][ch] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
-            }
-        lrun += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+            for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
-        for (int kc = 0; kc < 2 * SUB; ++kc)
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-                oacc[d] = mfma(transposed_operand<D>(vt, kc, d, lane), pb[kc >> 1][kc & 1],
-                               oacc[d]);
+                for (int r = 0; r < 16; ++r)
+                    sc[sub][r] = 32 * sub + 8 * (r >> 2) + (r & 3) <= left ? 0.0f : -INFINITY;
+        }
+    };
+    // The matrix instructions of a step, one by one: the scores of a tile (K in ks), then
+    // the value product with the probabilities pb (V in vt).
+    constexpr int SCORES = SUB * DS, PRODUCTS = 2 * SUB * DT;
+    auto operand = [&](auto ic, const uint8_t *ks, const uint8_t *vt) {
+        constexpr int I = decltype(ic)::value;
+        if constexpr (I < SCORES)
+            return row_operand<D>(ks, 32 * (I % SUB) + l32, I / SUB, hf);
+        else
+            return transposed_operand<D>(vt, (I - SCORES) / DT, (I - SCORES) % DT, lane);
+    };
+    auto multiply = [&](auto ic, bf16x8 w, f32x16 (&sc)[SUB], const bf16x8 (&pb)[SUB][2]) {
+        constexpr int I = decltype(ic)::value;
+        if constexpr (I < SCORES) {
+            constexpr int sub = I % SUB, i = I / SUB;
+            const f32x16 zero = {};
+            sc[sub] = mfma(w, qb[i], i == 0 && !BIAS ? zero : sc[sub]);
+        } else {
+            constexpr int kc = (I - SCORES) / DT, d = (I - SCORES) % DT;
+            oacc[d] = mfma(w, pb[kc / 2][kc % 2], oacc[d]);
+        }
+    };
+    // Matrix instructions FROM .. TO - 1 with the parts of a softmax spread between them,
+    // operands read AHEAD of them.
+    constexpr int AHEAD = 3;
+    auto run = [&](auto fromc, auto toc, auto maskc, int kt, const f32x16 (&cur)[SUB],
+                   f32x16 (&nxt)[SUB], const bf16x8 (&pold)[SUB][2], bf16x8 (&pnew)[SUB][2],
+                   const uint8_t *ks, const uint8_t *vt) {
+        constexpr int FROM = decltype(fromc)::value, N = decltype(toc)::value - FROM;
+        const int left = lim - kt * BK - 4 * hf;
+        bf16x8 w[AHEAD + 1];
+        each<AHEAD>([&](auto ic) {
+            constexpr int I = decltype(ic)::value;
+            if constexpr (I < N)
+                w[I] = operand(Index<FROM + I>{}, ks, vt);
+        });
+        each<N>([&](auto ic) {
+            constexpr int I = decltype(ic)::value;
+            if constexpr (I + AHEAD < N)
+                w[(I + AHEAD) % (AHEAD + 1)] = operand(Index<FROM + I + AHEAD>{}, ks, vt);
+            multiply(Index<FROM + I>{}, w[I % (AHEAD + 1)], nxt, pold);
+            constexpr int P0 = PARTS * I / N, P1 = PARTS * (I + 1) / N;
+            each<P1 - P0>([&](auto pc) {
+                softmax(maskc, Index<P0 + decltype(pc)::value>{}, left, cur, pnew);
+            });
+            keep_order();
+        });
+    };
+    auto scores = [&](const uint8_t *ks, f32x16 (&sc)[SUB]) {
+        const bf16x8 none[SUB][2] = {};
+        each<SCORES>([&](auto ic) { multiply(ic, operand(ic, ks, ks), sc, none); });
+    };
+    auto product = [&](const uint8_t *vt, const bf16x8 (&pb)[SUB][2]) {
+        f32x16 none[SUB];
+        each<PRODUCTS>([&](auto ic) {
+            constexpr int I = SCORES + decltype(ic)::value;
+            multiply(Index<I>{}, operand(Index<I>{}, vt, vt), none, pb);
+        });
     };
 
     // this group's tiles: kt0 + KG j + kg, j < n; one past kt1 is loaded as the last
@@ -187,35 +248,47 @@ void seq_attn_kernel(const SeqAttnOut a)
     const int n = (kt1 - kt0 + KG - 1) / KG;
     auto tile_at = [&](int j) { return kt0 + KG * j + kg; };
     auto load_at = [&](int j) { return min(tile_at(j), kt1 - 1); };
-    auto body = [&](int j, const f32x16 (&cur)[SUB], auto next, const uint8_t *vt) {
-        const int kt = tile_at(j);
-        if (kt >= kt1 || (kt + 1) * BK > free_keys) {
-            tile_max(Flag<true>{}, kt, cur);
-            next();
-            tile_pv(Flag<true>{}, kt, cur, vt);
-        } else {
-            tile_max(Flag<false>{}, kt, cur);
-            next();
-            tile_pv(Flag<false>{}, kt, cur, vt);
-        }
+    // Step j: the softmax of tile j on the vector units, and beside it, independent of it,
+    // the scores of tile j + 1 and the value product of tile j - 1 on the matrix cores.  At
+    // its start every load issued so far has landed (K of tile j + 1, V of tile j - 1)
+    // and every wavefront has finished the step before it: K's buffer of tile j takes tile
+    // j + 2, V's of tile j - 2 takes tile j.
+    auto step = [&](auto oddc, auto maskc, int j, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB],
+                    const bf16x8 (&pold)[SUB][2], bf16x8 (&pnew)[SUB][2]) {
+        constexpr int P = decltype(oddc)::value ? 1 : 0;
+        bias(tile_at(j + 1), nxt);
+        run(Index<0>{}, Index<SCORES + PRODUCTS>{}, maskc, tile_at(j), cur, nxt, pold, pnew,
+            kbuf(P ^ 1), vbuf(P ^ 1));
+        rescale();
     };
-    // At the start of a step every load issued so far has landed (K of tile j + 1, V of
-    // tile j) and every wavefront has finished the step before it: K's buffer of tile j
-    // (read then) takes tile j + 2, V's of tile j - 1 tile j + 1.
-    auto step = [&](auto oddc, int j, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB]) {
+    auto begin = [&](auto oddc, int j) {
         constexpr int P = decltype(oddc)::value ? 1 : 0;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (j + 2 < n)
             fetch_k(load_at(j + 2), kbuf(P));
-        fetch_v(load_at(j + 1), vbuf(P ^ 1));
-        body(j, cur, [&] { scores(kbuf(P ^ 1), nxt); }, vbuf(P));
+        fetch_v(load_at(j), vbuf(P));
     };
-    auto last = [&](auto oddc, int j, const f32x16 (&cur)[SUB]) {
+    auto middle = [&](auto oddc, int j, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB],
+                      const bf16x8 (&pold)[SUB][2], bf16x8 (&pnew)[SUB][2]) {
+        begin(oddc, j);
+        const int kt = tile_at(j);
+        if (!BIAS && (kt >= kt1 || (kt + 1) * BK > free_keys))
+            step(oddc, Flag<true>{}, j, cur, nxt, pold, pnew);
+        else
+            step(oddc, Flag<false>{}, j, cur, nxt, pold, pnew);
+    };
+    auto last = [&](auto oddc, int j, const f32x16 (&cur)[SUB], const bf16x8 (&pold)[SUB][2],
+                    bf16x8 (&pnew)[SUB][2]) {
         constexpr int P = decltype(oddc)::value ? 1 : 0;
+        f32x16 none[SUB];
+        begin(oddc, j);
+        run(Index<SCORES>{}, Index<SCORES + PRODUCTS>{}, Flag<!BIAS>{}, tile_at(j), cur, none, pold,
+            pnew, vbuf(P ^ 1), vbuf(P ^ 1));
+        rescale();
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        body(j, cur, [] {}, vbuf(P));
+        product(vbuf(P), pnew);
     };
     if (n > 0) {
         fetch_k(load_at(0), kbuf(0));
@@ -223,22 +296,42 @@ void seq_attn_kernel(const SeqAttnOut a)
         if (n > 1)
             fetch_k(load_at(1), kbuf(1));
         f32x16 sa[SUB], sb[SUB];
+        bf16x8 pa[SUB][2], pz[SUB][2];
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+        bias(tile_at(0), sa);
         scores(kbuf(0), sa);
-        int j = 0;
-        for (; j + 2 < n; j += 2) {
-            step(Flag<false>{}, j, sa, sb);
-            step(Flag<true>{}, j + 1, sb, sa);
-        }
-        if (j + 1 < n) {
-            step(Flag<false>{}, j, sa, sb);
-            last(Flag<true>{}, j + 1, sb);
+        if (n > 1) {
+            // step 0: no value product yet
+            if (n > 2) {
+                __syncthreads();
+                fetch_k(load_at(2), kbuf(0));
+            }
+            bias(tile_at(1), sb);
+            run(Index<0>{}, Index<SCORES>{}, Flag<!BIAS>{}, tile_at(0), sa, sb, pz, pa, kbuf(1),
+                kbuf(1));
+            int j = 1;
+            for (; j + 2 < n; j += 2) {
+                middle(Flag<true>{}, j, sb, sa, pa, pz);
+                middle(Flag<false>{}, j + 1, sa, sb, pz, pa);
+            }
+            if (j + 1 < n) {
+                middle(Flag<true>{}, j, sb, sa, pa, pz);
+                last(Flag<false>{}, j + 1, sa, pz, pa);
+            } else {
+                last(Flag<true>{}, j, sb, pa, pz);
+            }
         } else {
-            last(Flag<false>{}, j, sa);
+            const int left = lim - tile_at(0) * BK - 4 * hf;
+            each<PARTS>([&](auto ic) { softmax(Flag<!BIAS>{}, ic, left, sa, pa); });
+            product(vbuf(0), pa);
         }
     }
-    lrun += __shfl_xor(lrun, 32);
+    {
+        float lo, hi;
+        both_halves(lrun, lo, hi);
+        lrun = lo + hi;
+    }
 
     if constexpr (KG > 1) {
         // the other groups' states through LDS (over the buffers, which every wavefront

@@ -330,7 +330,7 @@ struct SeqAttn {
     const int64_t *q_off, *k_off, *q_len, *k_len;  // each may be nullptr
     int B, T, KT, H, Hk, dh;
     int causal;
-    float c;  // scale * log2(e)
+    float c;  // scale * log2(e), > 0
 };
 struct SeqAttnOut {
     SeqAttn s;
@@ -352,7 +352,7 @@ int64_t seq_attn_workgroups(const SeqAttn &s, const SeqAttnPlan &p);
 hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_t stream);
 
 // Its backward pass: dq, dk and dv (both or neither) of one dtype.  sums: workspace of
-// 2 H qrows floats, lse * log2(e) (infinity where a query sees no key) and sum dO O.
+// 16 bytes a query and head, -lse / scale and -sum dO O as three bf16 each.
 // parts of the reductions over keys (dq) and over queries (dk, dv): partial sums in part,
 // [parts][B Hk][T H / Hk][dh], for dk and dv [parts][B Hk][KT][dh] each.
 struct SeqAttnGrad {

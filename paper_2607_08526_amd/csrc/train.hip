@@ -110,7 +110,8 @@ SeqAttn seq_attn(const ql_attn &a)
     s.Hk = (int)a.Hk;
     s.dh = (int)a.dh;
     s.causal = a.causal != 0;
-    s.c = a.scale * 1.44269504088896340736f;
+    // (scale 0: so small that every power of it is 1; quotients by it stay finite)
+    s.c = std::max(a.scale * 1.44269504088896340736f, 1e-30f);
     return s;
 }
 
