@@ -148,25 +148,40 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     load1.init(ld1, tid);
     load2.init(ld2, tid);
     constexpr int LOADS = 2 * TileLoad<D, BT, THREADS>::N + (KEYS ? 1 : 0);  // a tile's
-    // the first streamed row of tile j, and its head
-    auto start_of = [&](int j, int &h) {
+    // The tile that is loaded next: tile ft of head fh, its rows' first bytes and number,
+    // and its buffer.  (Counted on from tile to tile: scalar instructions take their turn
+    // with the others of a wavefront, and a division and four products a tile took 0.3 of
+    // the time of a step.)
+    int ft, fh, fleft, fbuf = 0;
+    const uint8_t *f1, *f2;
+    const float *fsums;
+    auto aim = [&](int j) {
         const int g = KEYS ? j / tiles : 0;
-        h = KEYS ? hk * G + g : hk;
-        return (first + j - g * tiles) * BT;
+        ft = j - g * tiles;
+        fh = KEYS ? hk * G + g : hk;
+        const int64_t at = (KEYS ? Q.first : K.first) + (first + ft) * BT;
+        fleft = (KEYS ? Q.len : K.len) - (first + ft) * BT;
+        f1 = reinterpret_cast<const uint8_t *>((KEYS ? s.q : s.k) + at * ld1 + fh * D);
+        f2 = reinterpret_cast<const uint8_t *>((KEYS ? a.dO : s.v) + at * ld2 + fh * D);
+        fsums = a.sums + (fh * s.qrows + at) * 4;
     };
-    auto buffer = [&](int j) { return lds + j % BUFS * BUF; };
-    auto fetch = [&](int j) {
-        int h;
-        const int r0 = start_of(j, h), left = (KEYS ? Q.len : K.len) - r0;
-        const int64_t at = (KEYS ? Q.first : K.first) + r0;
-        const uint16_t *p1 = (KEYS ? s.q : s.k) + at * ld1 + h * D;
-        const uint16_t *p2 = (KEYS ? a.dO : s.v) + at * ld2 + h * D;
-        uint8_t *const buf = buffer(j);
-        load1.issue(reinterpret_cast<const uint8_t *>(p1), left, ld1, buf, tid);
-        load2.issue(reinterpret_cast<const uint8_t *>(p2), left, ld2, buf + TILE, tid);
+    auto following = [](int buf) { return buf == (BUFS - 1) * BUF ? 0 : buf + BUF; };
+    auto fetch = [&] {
+        const uint8_t *const buf = lds + fbuf;
+        load1.issue(f1, fleft, ld1, buf, tid);
+        load2.issue(f2, fleft, ld2, buf + TILE, tid);
         if (KEYS)  // (every wavefront the same: all have as many loads in flight)
-            dma_load16_at(a.sums + (h * s.qrows + at + min(lane, left - 1)) * 4,
-                          dma_lds(buf + 2 * TILE));
+            dma_load16(fsums, min(lane, fleft - 1) * 16, dma_lds(buf + 2 * TILE));
+        fbuf = following(fbuf);
+        ++ft;
+        if (KEYS && ft == tiles) {
+            aim((fh - hk * G + 1) * tiles);
+        } else {
+            f1 += BT * 2 * ld1;
+            f2 += BT * 2 * ld2;
+            fsums += BT * 4;
+            fleft -= BT;
+        }
     };
 
     f32x16 acc1[DT], acc2[KEYS ? DT : 1];
@@ -212,9 +227,8 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     // D = 128 (one code for every tile, or the accumulators' registers run out): the mask
     // is what a tile's scores start from, 0 or -infinity.
     constexpr bool BIAS = D == 128 || KEYS;
-    auto bias = [&](int j, Raw &x) {
-        int h;
-        const int r0 = start_of(j, h), from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
+    auto bias = [&](int r0, Raw &x) {
+        const int from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
         if (r0 >= free_lo && r0 + BT - 1 <= free_hi) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
@@ -269,8 +283,8 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     // The first products of tile j + 1 with the PAIRS steps of cook for tile j between them,
     // then the second products of tile j; operands are read AHEAD of their instruction.
     constexpr int AHEAD = 3, PAIRS = 8;
-    auto run = [&](auto maskc, int j, int r0, const Raw &cur, Raw &nxt, Cooked &now) {
-        const uint8_t *const next = buffer(j + 1), *const buf = buffer(j);
+    auto run = [&](auto maskc, const uint8_t *buf, const uint8_t *next, int r0, const Raw &cur,
+                   Raw &nxt, Cooked &now) {
         const int from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
         constexpr int N = FIRST + SECOND;
         bf16x8 w[AHEAD + 1];
@@ -289,15 +303,13 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             }
         });
     };
-    auto first_products = [&](int j, Raw &x) {
-        const uint8_t *const buf = buffer(j);
+    auto first_products = [&](const uint8_t *buf, int r0, Raw &x) {
         if (BIAS)
-            bias(j, x);
+            bias(r0, x);
         Cooked none;
         each<FIRST>([&](auto ic) { multiply(ic, operand(ic, buf, buf), x, none); });
     };
-    auto second_products = [&](int j, const Cooked &y) {
-        const uint8_t *const buf = buffer(j);
+    auto second_products = [&](const uint8_t *buf, const Cooked &y) {
         Raw none;
         each<SECOND>([&](auto ic) {
             constexpr int I = FIRST + decltype(ic)::value;
@@ -308,13 +320,15 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     if constexpr (!KEYS) {
         if (tiles > 0 && tiles <= FEW_TILES) {
             float d = 0.0f;
-            for (int j = 0; j < tiles; ++j) {
-                fetch(j);
+            aim(0);
+            for (int r0 = 0; r0 < tiles * BT; r0 += BT) {
+                fbuf = 0;
+                fetch();
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 Raw x;
-                first_products(j, x);
-                const int to = hi - j * BT - 4 * hf;
+                first_products(lds, r0, x);
+                const int to = hi - r0 - 4 * hf;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[r], c, -lse2));
@@ -350,7 +364,9 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     // j + BUFS - 2, later ones may be in flight) and every wavefront has finished step j -
     // 1, so the buffer of tile j - 1 takes tile j + BUFS - 1.
     static_assert(BUFS == 3 || BUFS == 4, "");
-    auto begin = [&](int j) {
+    Cooked y;
+    int r0 = 0, cbuf = 0;  // of tile j
+    auto step = [&](int j, const Raw &cur, Raw &nxt) {
         if (BUFS == 4 && j + 2 < j1)
             __builtin_amdgcn_s_waitcnt(dma_vmcnt(LOADS));
         else
@@ -358,38 +374,38 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         asm volatile("" ::: "memory");
         __syncthreads();
         if (j + BUFS - 1 < j1)
-            fetch(j + BUFS - 1);
-    };
-    Cooked y;
-    auto step = [&](int j, const Raw &cur, Raw &nxt) {
-        begin(j);
-        int h;
-        const int r0 = start_of(j, h);
+            fetch();
+        const int nbuf = following(cbuf);
+        // (the last tile of a head: the next one's first follows)
+        const int next = KEYS && r0 + BT >= Q.len ? first * BT : r0 + BT;
         if (BIAS)
-            bias(j + 1, nxt);
+            bias(next, nxt);
         if (BIAS || (r0 >= free_lo && r0 + BT - 1 <= free_hi))
-            run(Flag<false>{}, j, r0, cur, nxt, y);
+            run(Flag<false>{}, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
         else
-            run(Flag<true>{}, j, r0, cur, nxt, y);
+            run(Flag<true>{}, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
+        cbuf = nbuf;
+        r0 = next;
     };
     auto last = [&](const Raw &cur) {
-        const int j = j1 - 1;
-        int h;
-        const int r0 = start_of(j, h) + 4 * hf;
-        each<PAIRS>([&](auto ic) { cook(Flag<!BIAS>{}, ic, lo - r0, hi - r0, cur, y); });
-        second_products(j, y);
+        const int at = r0 + 4 * hf;
+        each<PAIRS>([&](auto ic) { cook(Flag<!BIAS>{}, ic, lo - at, hi - at, cur, y); });
+        second_products(lds + cbuf, y);
     };
     if (j0 < j1) {
         Raw xa, xb;
         if (KEYS && tid == 0)
             *reinterpret_cast<u32x4 *>(zeros) = u32x4{0u, 0u, 0u, 0u};
+        aim(j0);
+        r0 = (first + ft) * BT;
+        fbuf = 0;
 #pragma unroll
         for (int i = 0; i < BUFS - 1; ++i)
             if (j0 + i < j1)
-                fetch(j0 + i);
+                fetch();
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        first_products(j0, xa);
+        first_products(lds, r0, xa);
         int j = j0;
         for (; j + 2 < j1; j += 2) {
             step(j, xa, xb);

@@ -95,12 +95,32 @@ void seq_attn_kernel(const SeqAttnOut a)
     TileLoad<D, BK, GT> kload, vload;
     kload.init(s.ldk, tid);
     vload.init(s.ldv, tid);
-    auto fetch_k = [&](int kt, uint8_t *buf) {
-        kload.issue(kbase + (int64_t)kt * BK * s.ldk * 2, K.len - kt * BK, s.ldk, buf, tid);
+    // K and V of this group's next tiles (counted on: scalar instructions take their turn
+    // with the others of a wavefront).  This group's tiles: kt0 + KG j + kg, j < n; one past
+    // kt1 is loaded as the last tile again (every key of it lies past lim).
+    const int n = (kt1 - kt0 + KG - 1) / KG;
+    auto tile_at = [&](int j) { return kt0 + KG * j + kg; };
+    struct Next {
+        const uint8_t *p;
+        int left;
+    } nextk, nextv;
+    {
+        const int kt = max(0, min(kt0 + kg, kt1 - 1));
+        nextk = {kbase + (int64_t)kt * BK * s.ldk * 2, K.len - kt * BK};
+        nextv = {vbase + (int64_t)kt * BK * s.ldv * 2, K.len - kt * BK};
+    }
+    // (keys from the next tile's first to kt1's: no more than those of the tile itself)
+    const int beyond = K.len - kt1 * BK;
+    auto fetch = [&](const TileLoad<D, BK, GT> &load, Next &x, int64_t ld, uint8_t *buf) {
+        load.issue(x.p, x.left, ld, buf, tid);
+        const int tiles_on = KG == 1 || x.left - beyond > KG * BK
+                                 ? KG
+                                 : (x.left - beyond + BK - 1) / BK - 1;
+        x.p += tiles_on * (BK * 2 * ld);
+        x.left -= tiles_on * BK;
     };
-    auto fetch_v = [&](int kt, uint8_t *buf) {
-        vload.issue(vbase + (int64_t)kt * BK * s.ldv * 2, K.len - kt * BK, s.ldv, buf, tid);
-    };
+    auto fetch_k = [&](uint8_t *buf) { fetch(kload, nextk, s.ldk, buf); };
+    auto fetch_v = [&](uint8_t *buf) { fetch(vload, nextv, s.ldv, buf); };
 
     f32x16 oacc[DT];
 #pragma unroll
@@ -243,11 +263,6 @@ void seq_attn_kernel(const SeqAttnOut a)
         });
     };
 
-    // this group's tiles: kt0 + KG j + kg, j < n; one past kt1 is loaded as the last
-    // tile again (every key of it lies past lim)
-    const int n = (kt1 - kt0 + KG - 1) / KG;
-    auto tile_at = [&](int j) { return kt0 + KG * j + kg; };
-    auto load_at = [&](int j) { return min(tile_at(j), kt1 - 1); };
     // Step j: the softmax of tile j on the vector units, and beside it, independent of it,
     // the scores of tile j + 1 and the value product of tile j - 1 on the matrix cores.  At
     // its start every load issued so far has landed (K of tile j + 1, V of tile j - 1)
@@ -266,8 +281,8 @@ void seq_attn_kernel(const SeqAttnOut a)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (j + 2 < n)
-            fetch_k(load_at(j + 2), kbuf(P));
-        fetch_v(load_at(j), vbuf(P));
+            fetch_k(kbuf(P));
+        fetch_v(vbuf(P));
     };
     auto middle = [&](auto oddc, int j, const f32x16 (&cur)[SUB], f32x16 (&nxt)[SUB],
                       const bf16x8 (&pold)[SUB][2], bf16x8 (&pnew)[SUB][2]) {
@@ -291,10 +306,10 @@ void seq_attn_kernel(const SeqAttnOut a)
         product(vbuf(P), pnew);
     };
     if (n > 0) {
-        fetch_k(load_at(0), kbuf(0));
-        fetch_v(load_at(0), vbuf(0));
+        fetch_k(kbuf(0));
+        fetch_v(vbuf(0));
         if (n > 1)
-            fetch_k(load_at(1), kbuf(1));
+            fetch_k(kbuf(1));
         f32x16 sa[SUB], sb[SUB];
         bf16x8 pa[SUB][2], pz[SUB][2];
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -305,7 +320,7 @@ void seq_attn_kernel(const SeqAttnOut a)
             // step 0: no value product yet
             if (n > 2) {
                 __syncthreads();
-                fetch_k(load_at(2), kbuf(0));
+                fetch_k(kbuf(0));
             }
             bias(tile_at(1), sb);
             run(Index<0>{}, Index<SCORES>{}, Flag<!BIAS>{}, tile_at(0), sa, sb, pz, pa, kbuf(1),

@@ -902,15 +902,29 @@ def rotary(x, heads, freqs, dh=64, positions=None, start=0, T=None, interleaved=
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
+_FLOAT_DT = {torch.float32: DT_F32, torch.bfloat16: DT_BF16}
 
 
-def _require_rows(t, name, M, N, dtypes=_FLOATS):
-    """A row view [M][N] with unit column stride; returns its row stride (of a single
-    row, which may be anything: its length)."""
-    _require(t, name, dtypes, min_cols=N)
-    if t.shape != (M, N):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(M, N)}")
-    return t.stride(0) if M > 1 else N
+def _require_rows(t, name, rows, cols, dtypes=_FLOATS, exact=True, whole=1):
+    """A row view of `rows` rows (None: any) and cols columns (or, not exact, at least so
+    many) with unit column stride; returns its row stride (of a single row, which may be
+    anything: its length in whole `whole`s)."""
+    # the plain case in as few steps as it takes
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.dim() == 2:
+        (m, n), (ld, unit) = t.shape, t.stride()
+        if unit == 1 and (n == cols or (n > cols and not exact)) and \
+                (m == rows or rows is None):
+            if m > 1:
+                if ld >= cols:
+                    return ld
+            else:
+                return -(-n // whole) * whole
+    _require(t, name, dtypes, min_cols=cols)
+    if exact and t.shape[1] != cols:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name} has {t.shape[0]} rows, expected shape {(rows, cols)}")
+    raise ValueError(f"{name} must be a 2-D row view with unit column stride")
 
 
 def _norm(x, weight, eps, residual, h, y, ydtype, int8, stream):
@@ -923,12 +937,16 @@ def _norm(x, weight, eps, residual, h, y, ydtype, int8, stream):
         _require(weight, "weight", (torch.float32,), (N,))
     if not 0.0 <= eps < math.inf:
         raise ValueError(f"eps = {eps} is not a finite number of at least 0")
-    ldr = _require_rows(residual, "residual", M, N) if residual is not None else 0
-    if h is None and residual is not None:
-        h = _new(x, (M, N), residual.dtype, stream)
-    ldh = 0
-    if h is not None:
-        ldh = _require_rows(h, "h", M, N, _FLOATS if residual is None else (residual.dtype,))
+    ldr = ldh = ldy = 0
+    rdtype = _FLOATS
+    if residual is not None:
+        ldr = _require_rows(residual, "residual", M, N)
+        rdtype = (residual.dtype,)
+        if h is None:
+            h = _new(x, (M, N), residual.dtype, stream)
+            ldh = N
+    if h is not None and ldh == 0:
+        ldh = _require_rows(h, "h", M, N, rdtype)
     qx = sx = None
     if int8 is None:
         if y is None:
@@ -940,15 +958,17 @@ def _norm(x, weight, eps, residual, h, y, ydtype, int8, stream):
         qx, sx = int8
         if qx is None:
             qx = _new(x, (M, N), torch.int8, stream)
+        else:
+            _require(qx, "qx", (torch.int8,), (M, N))
         if sx is None:
             sx = _new(x, (M,), torch.int16, stream)
-        _require(qx, "qx", (torch.int8,), (M, N))
-        _require(sx, "sx", _TWO_BYTE, (M,))
-        ldy = 0
+        else:
+            _require(sx, "sx", _TWO_BYTE, (M,))
     _on_current_device(x, weight, residual, h, y, qx, sx)
-    n = _Norm(_ptr(x), ldx, _ydt(x), _ptr(residual), ldr, _ydt(h) if h is not None else DT_F32,
-              _ptr(weight), eps, M, N, _ptr(h), ldh, _ptr(y), ldy,
-              _ydt(y) if y is not None else DT_F32, _ptr(qx), _ptr(sx))
+    n = _Norm(x.data_ptr(), ldx, _FLOAT_DT[x.dtype], _ptr(residual), ldr,
+              _FLOAT_DT[h.dtype] if h is not None else DT_F32, _ptr(weight), eps, M, N, _ptr(h),
+              ldh, _ptr(y), ldy, _FLOAT_DT[y.dtype] if y is not None else DT_F32, _ptr(qx),
+              _ptr(sx))
     _check(load().qlinear_rms_norm(ctypes.byref(n), _stream(stream)))
     return (y, h) if int8 is None else (qx, sx, h)
 
@@ -992,39 +1012,37 @@ def rms_norm_backward(dy, h, weight=None, eps=1e-6, dres=None, dx=None, dtype=to
     lddres = _require_rows(dres, "dres", M, N, (dx.dtype,)) if dres is not None else 0
     dw = _new(h, (N,), torch.float32, stream) if weight_grad else None
     _on_current_device(dy, h, weight, dres, dx, dw)
-    g = _NormGrad(_ptr(dy), lddy, _ydt(dy), _ptr(h), ldh, _ydt(h), _ptr(dres), lddres,
-                  _ptr(weight), eps, M, N, _ptr(dx), lddx, _ydt(dx), _ptr(dw))
+    g = _NormGrad(dy.data_ptr(), lddy, _FLOAT_DT[dy.dtype], h.data_ptr(), ldh,
+                  _FLOAT_DT[h.dtype], _ptr(dres), lddres, _ptr(weight), eps, M, N, dx.data_ptr(),
+                  lddx, _FLOAT_DT[dx.dtype], _ptr(dw))
     _check(load().qlinear_rms_norm_backward(ctypes.byref(g), _stream(stream)))
     return dx, dw
 
 
 def _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets, k_offsets, q_lens, k_lens):
-    """(_Attn, its tensors) of a masked attention's checked arguments."""
+    """(_Attn, its tensors, rows of q and of k) of a masked attention's checked arguments."""
     Hk, kT = H if kv_heads is None else kv_heads, T if kT is None else kT
     if H < 1 or Hk < 1 or H % Hk:
         raise ValueError(f"{H} query heads do not share {Hk} key heads")
     if B < 0 or T < 0 or kT < 0:
         raise ValueError(f"B = {B}, T = {T} or kT = {kT} is negative")
-    ld = []
-    for name, t, heads in (("q", q, H), ("k", k, Hk), ("v", v, Hk)):
-        _require(t, name, _BF16_BITS, min_cols=heads * dh)
-        # (a single row's stride may be anything: its length serves, in whole eights)
-        ld.append(t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8)
-    if v.shape[0] != k.shape[0]:
-        raise ValueError(f"v has {v.shape[0]} rows, k {k.shape[0]}")
+    ldq = _require_rows(q, "q", None, H * dh, _BF16_BITS, False, 8)
+    ldk = _require_rows(k, "k", None, Hk * dh, _BF16_BITS, False, 8)
+    qrows, krows = q.shape[0], k.shape[0]
+    ldv = _require_rows(v, "v", krows, Hk * dh, _BF16_BITS, False, 8)
     for name, t, n in (("q_offsets", q_offsets, B + 1), ("k_offsets", k_offsets, B + 1),
                        ("q_lens", q_lens, B), ("k_lens", k_lens, B)):
         if t is not None:
             _require(t, name, (torch.int64,), (n,))
-    if q_offsets is None and q.shape[0] < B * T:
-        raise ValueError(f"q has {q.shape[0]} rows, expected at least B * T = {B * T}")
-    if k_offsets is None and k.shape[0] < B * kT:
-        raise ValueError(f"k has {k.shape[0]} rows, expected at least B * kT = {B * kT}")
+    if q_offsets is None and qrows < B * T:
+        raise ValueError(f"q has {qrows} rows, expected at least B * T = {B * T}")
+    if k_offsets is None and krows < B * kT:
+        raise ValueError(f"k has {krows} rows, expected at least B * kT = {B * kT}")
     scale = 1.0 / float(dh) ** 0.5 if scale is None else float(scale)
-    a = _Attn(_ptr(q), ld[0], _ptr(k), ld[1], _ptr(v), ld[2], q.shape[0], k.shape[0],
+    a = _Attn(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, qrows, krows,
               _ptr(q_offsets), _ptr(k_offsets), _ptr(q_lens), _ptr(k_lens), B, T, kT, H, Hk, dh,
               causal, scale)
-    return a, (q, k, v, q_offsets, k_offsets, q_lens, k_lens)
+    return a, (q, k, v, q_offsets, k_offsets, q_lens, k_lens), qrows, krows
 
 
 def _attn_new(like, shape, dtype, stream, value):
@@ -1032,6 +1050,8 @@ def _attn_new(like, shape, dtype, stream, value):
     stay as they are) filled with it."""
     t = _new(like, shape, dtype, stream)
     if value is not None:
+        if stream is None:
+            return t.fill_(value)
         with torch.cuda.stream(stream):
             t.fill_(value)
     return t
@@ -1051,23 +1071,19 @@ def attention_forward(q, k, v, B, T, H, kv_heads=None, dh=64, kT=None, causal=Fa
     outputs made here: zeros and -inf).  O: row view [rows of q][>= H * dh], bf16 or
     fp32 (odtype where it is made here); lse: fp32 [H][rows of q], the logarithms of the
     row sums that attention_backward takes (None without with_lse).  Asynchronous."""
-    a, tensors = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets, k_offsets,
-                       q_lens, k_lens)
-    rows = q.shape[0]
+    a, tensors, rows, _ = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
+                                k_offsets, q_lens, k_lens)
     loose = q_offsets is not None or rows != B * T  # rows that may be of no sequence
     if O is None:
         O = _attn_new(q, (rows, H * dh), odtype, stream, 0.0 if loose else None)
-    _require(O, "O", _FLOATS, min_cols=H * dh)
-    if O.shape[0] != rows:
-        raise ValueError(f"O has {O.shape[0]} rows, expected {rows}")
-    if lse is None and with_lse:
-        lse = _attn_new(q, (H, rows), torch.float32, stream, -math.inf if loose else None)
+    ldo = _require_rows(O, "O", rows, H * dh, _FLOATS, False, 4)
     if lse is not None:
         _require(lse, "lse", (torch.float32,), (H, rows))
+    elif with_lse:
+        lse = _attn_new(q, (H, rows), torch.float32, stream, -math.inf if loose else None)
     _on_current_device(O, lse, *tensors)
-    ldo = O.stride(0) if rows > 1 else -(-O.shape[1] // 4) * 4
-    _check(load().qlinear_attention_forward(ctypes.byref(a), _ptr(O), ldo, _ydt(O), _ptr(lse),
-                                            _stream(stream)))
+    _check(load().qlinear_attention_forward(ctypes.byref(a), O.data_ptr(), ldo, _FLOAT_DT[O.dtype],
+                                            _ptr(lse), _stream(stream)))
     return O, lse
 
 
@@ -1085,38 +1101,36 @@ def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=No
     of one dtype (fp32 or bf16; dtype where they are made here), e.g. the columns of a
     fused QKV output's gradient.  Padding rows get zeros, rows of no sequence are not
     written (zeros in outputs made here).  Asynchronous."""
-    a, tensors = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets, k_offsets,
-                       q_lens, k_lens)
-    qrows, krows, wide, narrow = q.shape[0], k.shape[0], H * dh, a.Hk * dh
-    _require(O, "O", _FLOATS, min_cols=wide)
-    _require(dO, "dO", _BF16_BITS, min_cols=wide)
+    a, tensors, qrows, krows = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
+                                     k_offsets, q_lens, k_lens)
+    wide, narrow = H * dh, a.Hk * dh
+    ldo = _require_rows(O, "O", qrows, wide, _FLOATS, False, 4)
+    lddo = _require_rows(dO, "dO", qrows, wide, _BF16_BITS, False, 8)
     _require(lse, "lse", (torch.float32,), (H, qrows))
-    if O.shape[0] != qrows or dO.shape[0] != qrows:
-        raise ValueError(f"O has {O.shape[0]} rows, dO {dO.shape[0]}, expected {qrows}")
     if not kv_grads and (dk is not None or dv is not None):
         raise ValueError("dk and dv are given, but not asked for")
     if dtype not in _FLOATS:
         raise TypeError(f"gradients are float32 or bfloat16, not {dtype}")
-    given = [t for t in (dq, dk, dv) if t is not None]
-    dtype = given[0].dtype if given else dtype
-    zero = [0.0 if off is not None or rows != B * n else None  # rows that may be of no sequence
-            for off, rows, n in ((q_offsets, qrows, T), (k_offsets, krows, a.Tk))]
-    if dq is None:
-        dq = _attn_new(q, (qrows, wide), dtype, stream, zero[0])
-    if kv_grads:
-        dk = _attn_new(q, (krows, narrow), dtype, stream, zero[1]) if dk is None else dk
-        dv = _attn_new(q, (krows, narrow), dtype, stream, zero[1]) if dv is None else dv
-    for name, t, rows, cols in (("dq", dq, qrows, wide), ("dk", dk, krows, narrow),
-                                ("dv", dv, krows, narrow)):
+    for t in (dq, dk, dv):
         if t is not None:
-            _require(t, name, _FLOATS if name == "dq" else (dq.dtype,), min_cols=cols)
-            if t.shape[0] != rows:
-                raise ValueError(f"{name} has {t.shape[0]} rows, expected {rows}")
+            dtype = t.dtype
+            break
+    if dq is None:  # (zeros: rows that may be of no sequence)
+        dq = _attn_new(q, (qrows, wide), dtype, stream,
+                       0.0 if q_offsets is not None or qrows != B * T else None)
+    lddq = _require_rows(dq, "dq", qrows, wide, _FLOATS, False, 4)
+    lddk = lddv = 0
+    if kv_grads:
+        zero = 0.0 if k_offsets is not None or krows != B * a.Tk else None
+        if dk is None:
+            dk = _attn_new(q, (krows, narrow), dtype, stream, zero)
+        if dv is None:
+            dv = _attn_new(q, (krows, narrow), dtype, stream, zero)
+        lddk = _require_rows(dk, "dk", krows, narrow, (dq.dtype,), False, 4)
+        lddv = _require_rows(dv, "dv", krows, narrow, (dq.dtype,), False, 4)
     _on_current_device(O, lse, dO, dq, dk, dv, *tensors)
-    ld = lambda t, n: t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // n) * n
-    g = _AttnGrad(_ptr(O), ld(O, 4), _ydt(O), _ptr(lse), _ptr(dO), ld(dO, 8), _ptr(dq), _ptr(dk),
-                  _ptr(dv), ld(dq, 4), ld(dk, 4) if kv_grads else 0, ld(dv, 4) if kv_grads else 0,
-                  _ydt(dq))
+    g = _AttnGrad(O.data_ptr(), ldo, _FLOAT_DT[O.dtype], lse.data_ptr(), dO.data_ptr(), lddo,
+                  dq.data_ptr(), _ptr(dk), _ptr(dv), lddq, lddk, lddv, _FLOAT_DT[dq.dtype])
     _check(load().qlinear_attention_backward(ctypes.byref(a), ctypes.byref(g), _stream(stream)))
     return AttentionGrads(dq, dk, dv)
 
