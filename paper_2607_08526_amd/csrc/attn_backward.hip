@@ -10,13 +10,14 @@
 // dP: 7 products of dh flops per pair instead of 5.
 //
 // A wavefront keeps 32 rows of two tensors in registers as right operands (Q, dO; or K,
-// V); tiles of 32 rows of the other two (K, V; or Q, dO) come into LDS by direct loads, a
-// ring of BUFS of them.  S and dP of a tile are formed with the streamed rows as left
-// operand: a lane then holds 16 streamed rows of one kept row, just what the right operand
-// of the second products (transposed left operand: dQ^T += K^T dS^T, dV^T += dO^T P, dK^T
-// += Q^T dS) wants of P and dS, which are rounded to bf16 for it.  Matrix and vector units
-// run beside each other within a wavefront: P and dS of tile j are formed between the
-// matrix instructions of tile j + 1's S and dP; tile j's second products follow.
+// V); tiles of BT rows of the other two (K, V; or Q, dO) come into LDS by direct loads, a
+// ring of BUFS of them, and are taken in blocks of 32 rows.  S and dP of a block are
+// formed with the streamed rows as left operand: a lane then holds 16 streamed rows of one
+// kept row, just what the right operand of the second products (transposed left operand:
+// dQ^T += K^T dS^T, dV^T += dO^T P, dK^T += Q^T dS) wants of P and dS, which are rounded to
+// bf16 for it.  Matrix and vector units run beside each other within a wavefront: P and dS
+// of block i are formed between the matrix instructions of block i + 1's S and dP; block
+// i's second products follow.
 #include "attn.h"
 
 namespace qlk {
@@ -26,20 +27,19 @@ constexpr int THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 constexpr int KEEP = 128;  // kept rows of a workgroup
-constexpr int BT = 32;     // streamed rows of a tile
-// Where the queries of a workgroup see at most so many tiles of keys, d_i is formed as sum
+// Where the queries of a workgroup see at most so many keys, d_i is formed as sum
 // P_ij dP_ij in a pass of its own: the rounding of a bf16 O, harmless in a sum over many
 // keys, is not when a few make up the row (dq off by 0.0030 of its norm at 3 keys against
 // 0.0024, of which the output's rounding is 0.0017).
-constexpr int FEW_TILES = 4;
+constexpr int FEW_KEYS = 128;
 
-template <int D, bool KEYS, int BUFS>
+template <int D, bool KEYS, int BT, int BUFS>
 __global__ __launch_bounds__(THREADS)
 __attribute__((amdgpu_waves_per_eu(D == 128 && KEYS ? 1 : 2, 2)))
 void seq_attn_grad_kernel(const SeqAttnGrad a)
 {
     constexpr int TILE = BT * D * 2;  // bytes of a tile
-    constexpr int DT = D / 32, DS = D / 16;
+    constexpr int DT = D / 32, DS = D / 16, SUB = BT / 32;
     constexpr int BUF = 2 * TILE + (KEYS ? 1024 : 0);  // (the sums of 64 rows)
     __shared__ __align__(16) uint8_t lds[BUFS * BUF + (KEYS ? 16 : 0)];
     uint8_t *const zeros = lds + BUFS * BUF;
@@ -65,65 +65,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const int shift = K.len - Q.len;  // causal: query t sees the keys up to t + shift
     const float c = s.c;
 
-    // the kept row of this lane: its operands, and the streamed rows lo to hi that meet it
-    const int wrow = row0 + wave * 32, row = wrow + l32;
-    const int t = KEYS ? row : row / G, head = KEYS ? hk : hk * G + row - t * G;
-    const bool live = t < (KEYS ? K.len : Q.len);
-    bf16x8 x1[DS], x2[DS];
-    {
-        const uint16_t *p1 = KEYS ? s.k + (K.first + t) * s.ldk : s.q + (Q.first + t) * s.ldq;
-        const uint16_t *p2 = KEYS ? s.v + (K.first + t) * s.ldv : a.dO + (Q.first + t) * a.lddo;
-#pragma unroll
-        for (int i = 0; i < DS; ++i) {
-            u32x4 v1 = {0u, 0u, 0u, 0u}, v2 = v1;
-            if (live) {
-                v1 = *reinterpret_cast<const u32x4 *>(p1 + head * D + 16 * i + 8 * hf);
-                v2 = *reinterpret_cast<const u32x4 *>(p2 + head * D + 16 * i + 8 * hf);
-            }
-            x1[i] = __builtin_bit_cast(bf16x8, v1);
-            x2[i] = __builtin_bit_cast(bf16x8, v2);
-        }
-    }
-    const int lo = KEYS && s.causal ? t - shift : 0;
-    const int hi = !live ? -1 : KEYS ? Q.len - 1 : s.causal ? min(K.len - 1, t + shift) : K.len - 1;
-    // of a kept query: lse in powers of two, and d = sum dO O
-    float lse2 = INFINITY, delta = 0.0f;
-    if (!KEYS && live) {
-        const int64_t at = (Q.first + t) * a.ldo + head * D + 8 * hf;
-#pragma unroll
-        for (int i = 0; i < DS; ++i) {
-            float o[8];
-            if (a.obf16) {
-                const uint16_t *p = static_cast<const uint16_t *>(a.o) + at + 16 * i;
-                const u32x2 w[2] = {*reinterpret_cast<const u32x2 *>(p),
-                                    *reinterpret_cast<const u32x2 *>(p + 4)};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    o[2 * j] = __uint_as_float(w[j >> 1][j & 1] << 16);
-                    o[2 * j + 1] = __uint_as_float(w[j >> 1][j & 1] & 0xFFFF0000u);
-                }
-            } else {
-                const float *p = static_cast<const float *>(a.o) + at + 16 * i;
-                const f32x4_t w[2] = {*reinterpret_cast<const f32x4_t *>(p),
-                                      *reinterpret_cast<const f32x4_t *>(p + 4)};
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    o[j] = w[j >> 2][j & 3];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                delta = __builtin_fmaf((float)x2[i][j], o[j], delta);
-        }
-        const float l = a.lse[head * s.qrows + Q.first + t];
-        lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
-    }
-    auto halves = [](float x) {
-        float l, h;
-        both_halves(x, l, h);
-        return l + h;
-    };
-    if (!KEYS)
-        delta = halves(delta);
+    const int wrow = row0 + wave * 32;  // the wavefront's first row
     // tiles [first, first + tiles) of streamed rows, for keys of each head in turn
     int first = 0, tiles;
     if (KEYS) {
@@ -184,6 +126,78 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         }
     };
 
+    // The first tiles, before the kept rows (whose loads they pass on the way).
+    const bool few = !KEYS && tiles * BT <= FEW_KEYS;
+    auto fetch_first = [&] {
+        aim(j0);
+        fbuf = 0;
+#pragma unroll
+        for (int i = 0; i < BUFS - 1; ++i)
+            if (j0 + i < j1)
+                fetch();
+    };
+    if (j0 < j1 && !few)
+        fetch_first();
+
+    // the kept row of this lane: its operands, and the streamed rows lo to hi that meet it
+    const int row = wrow + l32;
+    const int t = KEYS ? row : row / G, head = KEYS ? hk : hk * G + row - t * G;
+    const bool live = t < (KEYS ? K.len : Q.len);
+    bf16x8 x1[DS], x2[DS];
+    {
+        const uint16_t *p1 = KEYS ? s.k + (K.first + t) * s.ldk : s.q + (Q.first + t) * s.ldq;
+        const uint16_t *p2 = KEYS ? s.v + (K.first + t) * s.ldv : a.dO + (Q.first + t) * a.lddo;
+#pragma unroll
+        for (int i = 0; i < DS; ++i) {
+            u32x4 v1 = {0u, 0u, 0u, 0u}, v2 = v1;
+            if (live) {
+                v1 = *reinterpret_cast<const u32x4 *>(p1 + head * D + 16 * i + 8 * hf);
+                v2 = *reinterpret_cast<const u32x4 *>(p2 + head * D + 16 * i + 8 * hf);
+            }
+            x1[i] = __builtin_bit_cast(bf16x8, v1);
+            x2[i] = __builtin_bit_cast(bf16x8, v2);
+        }
+    }
+    const int lo = KEYS && s.causal ? t - shift : 0;
+    const int hi = !live ? -1 : KEYS ? Q.len - 1 : s.causal ? min(K.len - 1, t + shift) : K.len - 1;
+    // of a kept query: lse in powers of two, and d = sum dO O
+    float lse2 = INFINITY, delta = 0.0f;
+    if (!KEYS && live) {
+        const int64_t at = (Q.first + t) * a.ldo + head * D + 8 * hf;
+#pragma unroll
+        for (int i = 0; i < DS; ++i) {
+            float o[8];
+            if (a.obf16) {
+                const uint16_t *p = static_cast<const uint16_t *>(a.o) + at + 16 * i;
+                const u32x2 w[2] = {*reinterpret_cast<const u32x2 *>(p),
+                                    *reinterpret_cast<const u32x2 *>(p + 4)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    o[2 * j] = __uint_as_float(w[j >> 1][j & 1] << 16);
+                    o[2 * j + 1] = __uint_as_float(w[j >> 1][j & 1] & 0xFFFF0000u);
+                }
+            } else {
+                const float *p = static_cast<const float *>(a.o) + at + 16 * i;
+                const f32x4_t w[2] = {*reinterpret_cast<const f32x4_t *>(p),
+                                      *reinterpret_cast<const f32x4_t *>(p + 4)};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    o[j] = w[j >> 2][j & 3];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                delta = __builtin_fmaf((float)x2[i][j], o[j], delta);
+        }
+        const float l = a.lse[head * s.qrows + Q.first + t];
+        lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
+    }
+    auto halves = [](float x) {
+        float l, h;
+        both_halves(x, l, h);
+        return l + h;
+    };
+    if (!KEYS)
+        delta = halves(delta);
     f32x16 acc1[DT], acc2[KEYS ? DT : 1];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -229,7 +243,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     constexpr bool BIAS = D == 128 || KEYS;
     auto bias = [&](int r0, Raw &x) {
         const int from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
-        if (r0 >= free_lo && r0 + BT - 1 <= free_hi) {
+        if (r0 >= free_lo && r0 + 31 <= free_hi) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 x.s[r] = 0.0f;
@@ -250,16 +264,18 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const uint32_t one = hf == 0 ? 0x3F80u : 0u, ones = one | one << 16;
     const bf16x8 ones_lse = __builtin_bit_cast(bf16x8, u32x4{ones, one, 0u, 0u});
     const bf16x8 ones_d = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, ones, one});
-    auto operand = [&](auto ic, const uint8_t *next, const uint8_t *prev) {
-        constexpr int I = decltype(ic)::value;
+    // (block NS of the tile in next, block PS of that in prev)
+    auto operand = [&](auto ic, auto nsc, auto psc, const uint8_t *next, const uint8_t *prev) {
+        constexpr int I = decltype(ic)::value, NS = decltype(nsc)::value, PS = decltype(psc)::value;
         if constexpr (I < SUMS) {
             return __builtin_bit_cast(
-                bf16x8, *reinterpret_cast<const u32x4 *>(hf ? zeros : next + 2 * TILE + l32 * 16));
+                bf16x8, *reinterpret_cast<const u32x4 *>(
+                            hf ? zeros : next + 2 * TILE + 512 * NS + l32 * 16));
         } else if constexpr (I < FIRST) {
-            return row_operand<D>(next + (I % 2) * TILE, l32, (I - SUMS) / 2, hf);
+            return row_operand<D>(next + (I % 2) * TILE, 32 * NS + l32, (I - SUMS) / 2, hf);
         } else {
             constexpr int k = I - FIRST, which = KEYS ? k % 2 : 0, m = KEYS ? k / 2 : k;
-            return transposed_operand<D>(prev + which * TILE, m / DT, m % DT, lane);
+            return transposed_operand<D>(prev + which * TILE, 2 * PS + m / DT, m % DT, lane);
         }
     };
     auto multiply = [&](auto ic, bf16x8 w, Raw &x, const Cooked &y) {
@@ -280,19 +296,21 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
                 acc1[m % DT] = mfma(w, y.ds[m / DT], acc1[m % DT]);
         }
     };
-    // The first products of tile j + 1 with the PAIRS steps of cook for tile j between them,
-    // then the second products of tile j; operands are read AHEAD of their instruction.
+    // The first products of the next block with the PAIRS steps of cook for this one between
+    // them, then this one's second products; operands are read AHEAD of their instruction.
     constexpr int AHEAD = 3, PAIRS = 8;
-    auto run = [&](auto maskc, const uint8_t *buf, const uint8_t *next, int r0, const Raw &cur,
-                   Raw &nxt, Cooked &now) {
+    auto run = [&](auto maskc, auto subc, const uint8_t *buf, const uint8_t *next, int r0,
+                   const Raw &cur, Raw &nxt, Cooked &now) {
+        constexpr auto ns = Index<(decltype(subc)::value + 1) % SUB>{};
         const int from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
         constexpr int N = FIRST + SECOND;
         bf16x8 w[AHEAD + 1];
-        each<AHEAD>([&](auto ic) { w[decltype(ic)::value] = operand(ic, next, buf); });
+        each<AHEAD>([&](auto ic) { w[decltype(ic)::value] = operand(ic, ns, subc, next, buf); });
         each<N>([&](auto ic) {
             constexpr int I = decltype(ic)::value;
             if constexpr (I + AHEAD < N)
-                w[(I + AHEAD) % (AHEAD + 1)] = operand(Index<I + AHEAD>{}, next, buf);
+                w[(I + AHEAD) % (AHEAD + 1)] =
+                    operand(Index<I + AHEAD>{}, ns, subc, next, buf);
             multiply(ic, w[I % (AHEAD + 1)], nxt, now);
             if constexpr (I < FIRST) {
                 constexpr int P0 = PAIRS * I / FIRST, P1 = PAIRS * (I + 1) / FIRST;
@@ -303,41 +321,46 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             }
         });
     };
-    auto first_products = [&](const uint8_t *buf, int r0, Raw &x) {
+    auto first_products = [&](auto subc, const uint8_t *buf, int r0, Raw &x) {
         if (BIAS)
             bias(r0, x);
         Cooked none;
-        each<FIRST>([&](auto ic) { multiply(ic, operand(ic, buf, buf), x, none); });
+        each<FIRST>([&](auto ic) { multiply(ic, operand(ic, subc, subc, buf, buf), x, none); });
     };
-    auto second_products = [&](const uint8_t *buf, const Cooked &y) {
+    auto second_products = [&](auto subc, const uint8_t *buf, const Cooked &y) {
         Raw none;
         each<SECOND>([&](auto ic) {
             constexpr int I = FIRST + decltype(ic)::value;
-            multiply(Index<I>{}, operand(Index<I>{}, buf, buf), none, y);
+            multiply(Index<I>{}, operand(Index<I>{}, subc, subc, buf, buf), none, y);
         });
     };
 
     if constexpr (!KEYS) {
-        if (tiles > 0 && tiles <= FEW_TILES) {
+        if (few && tiles > 0) {
             float d = 0.0f;
             aim(0);
-            for (int r0 = 0; r0 < tiles * BT; r0 += BT) {
+            for (int at = 0; at < tiles * BT; at += BT) {
                 fbuf = 0;
                 fetch();
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
-                Raw x;
-                first_products(lds, r0, x);
-                const int to = hi - r0 - 4 * hf;
+                each<SUB>([&](auto subc) {
+                    const int r0 = at + 32 * decltype(subc)::value;
+                    Raw x;
+                    first_products(subc, lds, r0, x);
+                    const int to = hi - r0 - 4 * hf;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[r], c, -lse2));
-                    if (8 * (r >> 2) + (r & 3) <= to)
-                        d = __builtin_fmaf(p, x.dp[r], d);
-                }
+                    for (int r = 0; r < 16; ++r) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[r], c, -lse2));
+                        if (8 * (r >> 2) + (r & 3) <= to)
+                            d = __builtin_fmaf(p, x.dp[r], d);
+                    }
+                });
                 __syncthreads();
             }
             delta = halves(d);
+            if (j0 < j1)
+                fetch_first();
         }
         if (live && part == 0 && hf == 0) {
             // -lse / scale and -d as three bf16 each (a query that sees no key: so low that
@@ -360,13 +383,13 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         }
     }
 
-    // At the start of step j the loads of tile j + 1 have landed (of those issued, up to tile
-    // j + BUFS - 2, later ones may be in flight) and every wavefront has finished step j -
-    // 1, so the buffer of tile j - 1 takes tile j + BUFS - 1.
+    // At the start of tile j the loads of tile j + 1 have landed (of those issued, up to tile
+    // j + BUFS - 2, later ones may be in flight) and every wavefront has finished tile j - 1,
+    // so its buffer takes tile j + BUFS - 1.
     static_assert(BUFS == 3 || BUFS == 4, "");
     Cooked y;
-    int r0 = 0, cbuf = 0;  // of tile j
-    auto step = [&](int j, const Raw &cur, Raw &nxt) {
+    int r0 = 0, cbuf = 0;  // this block's first row, this tile's buffer
+    auto begin = [&](int j) {
         if (BUFS == 4 && j + 2 < j1)
             __builtin_amdgcn_s_waitcnt(dma_vmcnt(LOADS));
         else
@@ -375,47 +398,57 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         __syncthreads();
         if (j + BUFS - 1 < j1)
             fetch();
-        const int nbuf = following(cbuf);
+    };
+    auto block = [&](auto subc, const Raw &cur, Raw &nxt) {
+        constexpr bool WITHIN = decltype(subc)::value + 1 < SUB;
+        const int nbuf = WITHIN ? cbuf : following(cbuf);
         // (the last tile of a head: the next one's first follows)
-        const int next = KEYS && r0 + BT >= Q.len ? first * BT : r0 + BT;
+        const int next = !WITHIN && KEYS && r0 + 32 >= Q.len ? first * BT : r0 + 32;
         if (BIAS)
             bias(next, nxt);
-        if (BIAS || (r0 >= free_lo && r0 + BT - 1 <= free_hi))
-            run(Flag<false>{}, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
+        if (BIAS || (r0 >= free_lo && r0 + 31 <= free_hi))
+            run(Flag<false>{}, subc, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
         else
-            run(Flag<true>{}, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
+            run(Flag<true>{}, subc, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
         cbuf = nbuf;
         r0 = next;
     };
     auto last = [&](const Raw &cur) {
         const int at = r0 + 4 * hf;
         each<PAIRS>([&](auto ic) { cook(Flag<!BIAS>{}, ic, lo - at, hi - at, cur, y); });
-        second_products(lds + cbuf, y);
+        second_products(Index<SUB - 1>{}, lds + cbuf, y);
     };
     if (j0 < j1) {
         Raw xa, xb;
         if (KEYS && tid == 0)
             *reinterpret_cast<u32x4 *>(zeros) = u32x4{0u, 0u, 0u, 0u};
-        aim(j0);
-        r0 = (first + ft) * BT;
-        fbuf = 0;
-#pragma unroll
-        for (int i = 0; i < BUFS - 1; ++i)
-            if (j0 + i < j1)
-                fetch();
+        r0 = (first + (KEYS ? j0 % tiles : j0)) * BT;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        first_products(lds, r0, xa);
+        first_products(Index<0>{}, lds, r0, xa);
         int j = j0;
-        for (; j + 2 < j1; j += 2) {
-            step(j, xa, xb);
-            step(j + 1, xb, xa);
-        }
-        if (j + 1 < j1) {
-            step(j, xa, xb);
+        if constexpr (SUB == 2) {
+            for (; j + 1 < j1; ++j) {
+                begin(j);
+                block(Index<0>{}, xa, xb);
+                block(Index<1>{}, xb, xa);
+            }
+            block(Index<0>{}, xa, xb);
             last(xb);
         } else {
-            last(xa);
+            for (; j + 2 < j1; j += 2) {
+                begin(j);
+                block(Index<0>{}, xa, xb);
+                begin(j + 1);
+                block(Index<0>{}, xb, xa);
+            }
+            if (j + 1 < j1) {
+                begin(j);
+                block(Index<0>{}, xa, xb);
+                last(xb);
+            } else {
+                last(xa);
+            }
         }
     }
 
@@ -484,6 +517,10 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
         *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + o) = v;
 }
 
+// Rows of a streamed tile: 64, half the barriers and waits of 32, where the LDS holds them
+// (two workgroups on a CU but for D = 128 and kept keys).
+constexpr int tile_rows(int D, bool keys) { return D == 64 || keys ? 64 : 32; }
+
 int64_t blocks(const SeqAttn &s, bool keys)
 {
     const int64_t rows = keys ? s.KT : (int64_t)s.T * (s.H / s.Hk);
@@ -495,8 +532,9 @@ hipError_t go(const SeqAttnGrad &a, hipStream_t stream)
 {
     const int parts = KEYS ? a.kparts : a.qparts;
     const unsigned grid = (unsigned)(blocks(a.s, KEYS) * parts);
+    constexpr int BT = tile_rows(D, KEYS);
     if (grid)
-        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, 4>), dim3(grid),
+        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, BT, BT == 64 ? 3 : 4>), dim3(grid),
                            dim3(THREADS), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts < 2 || !grid)
@@ -520,9 +558,9 @@ SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys, int cus)
         return (int)(most < 2 ? 1 : want < most ? want : most);
     };
     SeqAttnGradPlan p{1, 1};
-    p.qparts = parts(blocks(s, false), (s.KT + BT - 1) / BT);
+    p.qparts = parts(blocks(s, false), (s.KT + 31) / 32);
     if (keys)
-        p.kparts = parts(blocks(s, true), (s.T + BT - 1) / BT * (s.H / s.Hk));
+        p.kparts = parts(blocks(s, true), (s.T + 31) / 32 * (s.H / s.Hk));
     return p;
 }
 
