@@ -62,7 +62,7 @@ int qlinear_rms_norm(const ql_norm *n, hipStream_t stream);
  * on (NULL: 0), of dx's dtype.  dw fp32 [N] or NULL.  dx may be dy, h or dres in place
  * (same address, dtype and ld); other conventions as above.  Sums of a row in
  * fp64, of dw in fp32 in one fixed order.  Workspace with dw (per stream, as in
- * qlinear.h): at most 8 N bytes per CU.  M == 0 writes zeros to dw and nothing else. */
+ * qlinear.h): at most 12 N bytes per CU.  M == 0 writes zeros to dw and nothing else. */
 typedef struct {
     const void *dy;
     int64_t lddy;
@@ -129,7 +129,7 @@ typedef struct {
 /* O, and with lse (fp32 [H][q_rows], or NULL) what the backward pass takes.  O and lse
  * share no elements with an input (QL_ERR_INVALID).  Workspace (per stream, as in
  * qlinear.h) where few queries leave CUs idle: fp32 partial results of parts of the
- * keys, at most 40 MiB.  Asynchronous; B == 0 or Tq == 0 is a no-op. */
+ * keys, at most 80 MiB.  Asynchronous; B == 0 or Tq == 0 is a no-op. */
 int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, float *lse,
                               hipStream_t stream);
 
@@ -147,7 +147,7 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
  * shares elements with an input or another output (QL_ERR_INVALID; other columns of the
  * same rows may be: the gradients may be those of a fused QKV output).  Workspace (per
  * stream, as in qlinear.h): 16 H q_rows bytes, and fp32 partial sums where few rows leave
- * CUs idle, at most 80 MiB.  Asynchronous. */
+ * CUs idle, at most 160 MiB.  Asynchronous. */
 typedef struct {
     const void *o;
     int64_t ldo;

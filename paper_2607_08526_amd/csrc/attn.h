@@ -173,11 +173,15 @@ __device__ inline void in_agprs(f32x16 &v) { asm volatile("" : "+a"(v)); }
 __device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Workgroup p runs on XCD p % 8: each XCD takes a contiguous range of the grid's work,
-// so that the tiles which several workgroups read come into one L2.
-__device__ inline int xcd_order(int p, int grid)
+// so that the tiles which several workgroups read come into one L2.  Fold: where the
+// whole grid is on the GPU at once, two workgroups a CU, the second half of a range is
+// taken from its end, so that a CU's two are a long and a short one of causal blocks.
+__device__ inline int xcd_order(int p, int grid, int fold)
 {
     const int q = grid >> 3, r = grid & 7, xcd = p & 7, i = p >> 3;
-    return xcd < r ? xcd * (q + 1) + i : r * (q + 1) + (xcd - r) * q + i;
+    const int n = xcd < r ? q + 1 : q, first = xcd < r ? xcd * n : r * (q + 1) + (xcd - r) * q;
+    const int half = (n + 1) / 2;
+    return first + (fold && i >= half ? n - 1 - (i - half) : i);
 }
 
 }  // namespace qlk

@@ -18,6 +18,9 @@
 // bf16 for it.  Matrix and vector units run beside each other within a wavefront: P and dS
 // of block i are formed between the matrix instructions of block i + 1's S and dP; block
 // i's second products follow.
+#include <algorithm>
+#include <cmath>
+
 #include "attn.h"
 
 namespace qlk {
@@ -51,7 +54,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const int G = s.H / s.Hk, parts = KEYS ? a.kparts : a.qparts;
     const int rows = KEYS ? s.KT : s.T * G;  // kept, of a (sequence, key head)
     const int nb = (rows + KEEP - 1) / KEEP;
-    int L = xcd_order((int)blockIdx.x, (int)gridDim.x);
+    int L = xcd_order((int)blockIdx.x, (int)gridDim.x, s.fold);
     const int part = L % parts;
     L /= parts;
     const int unit = L / nb, b = unit / s.Hk, hk = unit - b * s.Hk;
@@ -527,11 +530,46 @@ int64_t blocks(const SeqAttn &s, bool keys)
     return (rows + KEEP - 1) / KEEP * s.B * s.Hk;
 }
 
-template <int D, bool KEYS>
-hipError_t go(const SeqAttnGrad &a, hipStream_t stream)
+// us of a launch (fitted to sweeps of 247 shapes in up to 8 numbers of parts; the choice
+// takes 1.01 times the best one's time on average, 1.07 at the ninth decile): its start
+// and end, a block of 32 streamed rows where a workgroup has its CU to itself, and where two
+// share it; by D = 64 and 128 of kept queries, then of kept keys.
+struct StepCost {
+    double start, alone, shared;
+};
+constexpr StepCost STEP[2][2] = {{{6.95, 0.41, 0.95}, {10.45, 0.73, 1.61}},
+                                 {{5.21, 0.64, 0.64}, {7.72, 0.97, 0.97}}};
+constexpr double JOIN_US = 2.0, JOIN_PART_US = 0.09;  // of adding parts up, and a part more
+constexpr double JOIN_RATE = 4.3e6;                   // bytes a us of their values
+
+double parts_us(const SeqAttn &s, bool keys, int parts)
 {
+    const StepCost &c = STEP[keys][s.dh == 128];
+    const bool two = s.dh == 64 || !keys;  // workgroups fit a CU
+    const int G = s.H / s.Hk;
+    const double w = (double)blocks(s, keys) * parts, slots = (two ? 2.0 : 1.0) * s.cus;
+    const double most = std::ceil((keys ? s.T : s.KT) / 32.0) * (keys ? G : 1);
+    const double mean = s.causal ? most / 2 + 2 * (keys ? G : 1) : most;
+    const double full = std::min(1.0, std::max(0.0, (w - s.cus) / s.cus));
+    const double step = two ? c.alone + (c.shared - c.alone) * full : c.alone;
+    auto steps = [&](double n) { return std::ceil(n / parts); };
+    double us = c.start + (s.causal ? std::max(steps(most) * c.alone,
+                                               steps(mean) * step * std::max(1.0, w / slots))
+                                    : steps(most) * step * std::ceil(w / slots));
+    if (parts > 1) {
+        const double rows = (keys ? 2.0 * s.KT : (double)s.T * G) * s.B * s.Hk;
+        us += JOIN_US + JOIN_PART_US * parts + parts * rows * s.dh * 8.0 / JOIN_RATE;
+    }
+    return us;
+}
+
+template <int D, bool KEYS>
+hipError_t go(const SeqAttnGrad &g, hipStream_t stream)
+{
+    SeqAttnGrad a = g;
     const int parts = KEYS ? a.kparts : a.qparts;
     const unsigned grid = (unsigned)(blocks(a.s, KEYS) * parts);
+    a.s.fold = grid <= 2 * (unsigned)a.s.cus;
     constexpr int BT = tile_rows(D, KEYS);
     if (grid)
         hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, BT, BT == 64 ? 3 : 4>), dim3(grid),
@@ -549,19 +587,31 @@ hipError_t go(const SeqAttnGrad &a, hipStream_t stream)
 
 }  // namespace
 
-SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys, int cus)
+// The number of parts estimated to be fastest.  Measured, us of dk and dv in 1 / 2 / 4 / 8 parts:
+// 250 keys of one head of 128 for 4 causal query heads 41.9 / 27.6 / 19.5 / 15.9; 432 keys, 3
+// sequences of 4 such 59.7 / 42.0 / 31.4 / 40.6; 778 causal keys, 3 of 8 of 64, one query head
+// each 21.5 / 31.1 / 30.6 / 38.6.
+SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys)
 {
-    auto parts = [&](int64_t wgs, int64_t tiles) {
-        if (wgs == 0 || wgs >= cus)
-            return 1;
-        const int64_t want = (cus + wgs - 1) / wgs, most = tiles / 8;
-        return (int)(most < 2 ? 1 : want < most ? want : most);
+    constexpr int PARTS[] = {1, 2, 3, 4, 6, 8, 12, 16};
+    constexpr int64_t MOST = 1024;  // workgroups of a launch in parts: they bound the workspace
+    auto choose = [&](bool k) {
+        const int64_t w = blocks(s, k);
+        const int64_t tiles = k ? ((int64_t)s.T + 63) / 64 * (s.H / s.Hk) : ((int64_t)s.KT + 63) / 64;
+        int best = 1;
+        double us = 0.0;
+        for (const int p : PARTS) {
+            if (p > 1 && (p > tiles || w * p > MOST))
+                break;
+            const double t = parts_us(s, k, p);
+            if (p == 1 || t < us) {
+                us = t;
+                best = p;
+            }
+        }
+        return best;
     };
-    SeqAttnGradPlan p{1, 1};
-    p.qparts = parts(blocks(s, false), (s.KT + 31) / 32);
-    if (keys)
-        p.kparts = parts(blocks(s, true), (s.T + 31) / 32 * (s.H / s.Hk));
-    return p;
+    return {choose(false), keys ? choose(true) : 1};
 }
 
 int64_t seq_attn_grad_workgroups(const SeqAttn &s, const SeqAttnGradPlan &p)

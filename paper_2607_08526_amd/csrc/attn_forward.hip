@@ -18,6 +18,9 @@
 // G heads fill G rows.  KG groups of wavefronts share out a tile's keys (KG = 4: one
 // wavefront of 32 rows each, for one token; merged through LDS at the end); beyond that
 // `splits` workgroups take parts of the keys and attn_join_kernel adds them up.
+#include <algorithm>
+#include <cmath>
+
 #include "attn.h"
 
 namespace qlk {
@@ -50,7 +53,7 @@ void seq_attn_kernel(const SeqAttnOut a)
     const SeqAttn &s = a.s;
     const int G = s.H / s.Hk;
     const int nq = (s.T * G + BQ - 1) / BQ;
-    int L = xcd_order((int)blockIdx.x, (int)gridDim.x);
+    int L = xcd_order((int)blockIdx.x, (int)gridDim.x, s.fold);
     const int part = L % a.splits;
     L /= a.splits;
     const int unit = L / nq, b = unit / s.Hk, hk = unit - b * s.Hk;
@@ -428,75 +431,124 @@ void seq_attn_kernel(const SeqAttnOut a)
             none ? -INFINITY : (mrun * c + __builtin_amdgcn_logf(lrun)) * LN2;
 }
 
-// The parts of a split, joined in order: a wavefront per (query, head).
+// The parts of a split, joined in order: 4 channels of a (query, head) a thread.
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(const SeqAttnOut a)
 {
-    constexpr int V = D / 64;
     const SeqAttn &s = a.s;
-    const int G = s.H / s.Hk, lane = (int)threadIdx.x & 63;
+    const int G = s.H / s.Hk;
     const int64_t rows = (int64_t)s.B * s.Hk * s.T * G;
-    const int64_t at = (int64_t)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
+    const int64_t i = (int64_t)blockIdx.x * 256 + (int)threadIdx.x, at = i / (D / 4);
+    const int ch = 4 * (int)(i % (D / 4));
     if (at >= rows)
         return;
     const int unit = (int)(at / (s.T * G)), row = (int)(at - (int64_t)unit * s.T * G);
     const int b = unit / s.Hk, t = row / G, head = (unit - b * s.Hk) * G + row - t * G;
+    const f32x2_t *const ml =
+        reinterpret_cast<const f32x2_t *>(a.part + a.splits * rows * D) + at;
+    const float *const po = a.part + at * D + ch;
+    // as in the kernel, part by part: 0 where a part saw no key
+    f32x2_t x = ml[0];
+    float m = x[0], l = x[1];
+    f32x4_t o = *reinterpret_cast<const f32x4_t *>(po);
+#pragma unroll 4
+    for (int p = 1; p < a.splits; ++p) {
+        x = ml[p * rows];
+        const f32x4_t op = *reinterpret_cast<const f32x4_t *>(po + p * rows * D);
+        const float mn = fmaxf(m, x[0]);
+        const float w0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - mn) * s.c);
+        const float w1 = x[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((x[0] - mn) * s.c);
+        m = mn;
+        l = w0 * l + w1 * x[1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            o[k] = w0 * o[k] + w1 * op[k];
+    }
     const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
     if (t >= Q.cap)
         return;
     const SeqRows K = seq_rows(s.k_off, s.k_len, s.krows, s.KT, b);
     const bool none = t >= Q.len || K.len == 0 || (s.causal && t + K.len - Q.len < 0);
-    const f32x2_t *const ml = reinterpret_cast<const f32x2_t *>(a.part + a.splits * rows * D);
-    float m = -INFINITY, l = 0.0f, o[V] = {};
-    for (int p = 0; p < a.splits; ++p)
-        m = fmaxf(m, ml[p * rows + at][0]);
-#pragma unroll 4
-    for (int p = 0; p < a.splits; ++p) {
-        const f32x2_t x = ml[p * rows + at];
-        const float w = x[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((x[0] - m) * s.c);
-        const float *const po = a.part + (p * rows + at) * D + lane * V;
-        l += w * x[1];
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            o[i] += w * po[i];
-    }
     const float inv = 1.0f / l;
-    const int64_t out = (Q.first + t) * a.ldo + head * D + lane * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float v = none ? 0.0f : o[i] * inv;
-        if (a.obf16)
-            static_cast<uint16_t *>(a.o)[out + i] = __builtin_bit_cast(uint16_t, (__bf16)v);
-        else
-            static_cast<float *>(a.o)[out + i] = v;
-    }
-    if (a.lse && lane == 0)
+    for (int k = 0; k < 4; ++k)
+        o[k] = none ? 0.0f : o[k] * inv;
+    const int64_t out = (Q.first + t) * a.ldo + head * D + ch;
+    if (a.obf16)
+        *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(a.o) + out) =
+            u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+    else
+        *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.o) + out) = o;
+    if (a.lse && ch == 0)
         a.lse[head * s.qrows + Q.first + t] =
             none ? -INFINITY : (m * s.c + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 int tile_rows(int groups) { return 128 / groups; }
 
+// us of a launch (fitted to sweeps of 398 shapes in up to 40 forms each; the choice takes
+// 1.015 times the best form's time on average, 1.06 at the ninth decile): its start and end,
+// 64 keys of a group of wavefronts where a workgroup has its CU to itself, and where two
+// share it.
+struct StepCost {
+    double start, alone, shared;
+};
+constexpr StepCost STEP[2][3] = {{{4.81, 0.80, 1.30}, {4.90, 0.87, 1.88}, {4.58, 1.34, 2.58}},
+                                 {{5.01, 1.37, 1.57}, {5.33, 1.58, 2.74}, {5.65, 2.22, 2.22}}};
+constexpr double JOIN_US = 2.0, JOIN_PART_US = 0.13;  // of joining parts, and a part more
+constexpr double JOIN_RATE = 1.9e6, KEY_RATE = 6.5e6;  // bytes a us: their values; keys
+
+double form_us(const SeqAttn &s, int groups, int splits)
+{
+    const int kind = groups == 4 ? 2 : groups - 1;
+    const StepCost &c = STEP[s.dh == 128][kind];
+    const bool two = s.dh == 64 || groups < 4;  // workgroups fit a CU
+    const double units = (double)s.B * s.Hk, rows = (double)s.T * (s.H / s.Hk);
+    const double w = std::ceil(rows / tile_rows(groups)) * units * splits;
+    const double slots = (two ? 2.0 : 1.0) * s.cus;
+    const double most = std::ceil(s.KT / 64.0);
+    // (causal: the longest of a launch's chains, and the average that fills its places)
+    const double mean =
+        s.causal ? std::max(1.0, (s.KT - 0.5 * std::min(s.T, s.KT)) / 64.0 + 0.5) : most;
+    auto steps = [&](double tiles) { return std::ceil(tiles / splits / groups); };
+    const double full = std::min(1.0, std::max(0.0, (w - s.cus) / s.cus));
+    const double step = two ? c.alone + (c.shared - c.alone) * full : c.alone;
+    const double rounds = s.causal ? std::max(1.0, w / slots) : std::ceil(w / slots);
+    double us = std::max(s.causal ? steps(most) * c.alone : 0.0, steps(mean) * step * rounds);
+    // (of two bounds near each other both count)
+    const double bytes_us = units * s.KT * s.dh * 4.0 / KEY_RATE;
+    const double a2 = us * us, b2 = bytes_us * bytes_us;
+    us = c.start + std::sqrt(std::sqrt(a2 * a2 + b2 * b2));
+    if (splits > 1)
+        us += JOIN_US + JOIN_PART_US * splits + splits * units * rows * (s.dh + 2) * 4.0 / JOIN_RATE;
+    return us;
+}
+
 }  // namespace
 
-SeqAttnPlan seq_attn_plan(const SeqAttn &s, int cus)
+// The form estimated to be fastest.  Measured, us in 1, 2 and 4 groups of unsplit and of
+// the best number of parts (queries x keys, heads): 1 x 5066, 8 sequences of 16 of 64 65.5 /
+// 43.7 / 41.4 and 34.9 / 32.2 / 31.2 (4 parts); 592 x 592, 3 of 8 of 64, causal 13.0 / 9.7 / -;
+// 215 x 215, 3 of 8 of 128, 4 query heads each 12.3 / 13.1 / -, in 2 parts 26.3 / 28.5 / -.
+SeqAttnPlan seq_attn_plan(const SeqAttn &s)
 {
-    const int64_t units = (int64_t)s.B * s.Hk, rows = (int64_t)s.T * (s.H / s.Hk);
-    const int64_t tiles = ((int64_t)s.KT + 63) / 64;
-    auto wgs = [&](int groups) {
-        return (rows + tile_rows(groups) - 1) / tile_rows(groups) * units;
-    };
-    SeqAttnPlan p{1, 1};
-    if (rows <= 32)
-        p.groups = 4;
-    else if (wgs(2) <= cus ? tiles >= 2 : wgs(2) <= 2 * (int64_t)cus && tiles >= 8)
-        p.groups = 2;
-    const int64_t w = wgs(p.groups), most = tiles / (2 * p.groups);
-    if (w < cus && most > 1) {
-        const int64_t want = (cus + w - 1) / w;
-        p.splits = (int)(want < most ? want : most);
-    }
-    return p;
+    constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96};
+    constexpr int64_t MOST = 1024;  // workgroups of a split launch: they bound the workspace
+    const int64_t rows = (int64_t)s.T * (s.H / s.Hk), tiles = ((int64_t)s.KT + 63) / 64;
+    SeqAttnPlan best{1, 1};
+    double us = 0.0;
+    for (int groups = 1; groups <= (rows <= 128 ? 4 : 2); groups *= 2)
+        for (const int splits : SPLITS) {
+            const SeqAttnPlan p{groups, splits};
+            if (splits > 1 && (splits > tiles || seq_attn_workgroups(s, p) > MOST))
+                break;
+            const double t = form_us(s, groups, splits);
+            if ((groups == 1 && splits == 1) || t < us) {
+                us = t;
+                best = p;
+            }
+        }
+    return best;
 }
 
 int64_t seq_attn_workgroups(const SeqAttn &s, const SeqAttnPlan &p)
@@ -510,8 +562,10 @@ size_t seq_attn_bytes(const SeqAttn &s, const SeqAttnPlan &p)
     return p.splits < 2 ? 0 : (size_t)p.splits * s.B * s.H * s.T * (s.dh + 2) * 4;
 }
 
-hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_t stream)
+hipError_t launch_seq_attn(const SeqAttnOut &out, const SeqAttnPlan &p, hipStream_t stream)
 {
+    SeqAttnOut a = out;
+    a.s.fold = seq_attn_workgroups(a.s, p) <= 2 * a.s.cus;
     const dim3 grid((unsigned)seq_attn_workgroups(a.s, p)), block(THREADS);
 #define QL_GO(D, KG, BK) \
     hipLaunchKernelGGL((seq_attn_kernel<D, KG, BK>), grid, block, 0, stream, a)
@@ -534,7 +588,7 @@ hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits < 2)
         return e;
-    const dim3 joins((unsigned)(((int64_t)a.s.B * a.s.H * a.s.T + 3) / 4));
+    const dim3 joins((unsigned)(((int64_t)a.s.B * a.s.H * a.s.T * (a.s.dh / 4) + 255) / 256));
     if (a.s.dh == 64)
         hipLaunchKernelGGL(attn_join_kernel<64>, joins, dim3(256), 0, stream, a);
     else

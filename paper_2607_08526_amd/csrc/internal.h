@@ -331,6 +331,8 @@ struct SeqAttn {
     int B, T, KT, H, Hk, dh;
     int causal;
     float c;  // scale * log2(e), > 0
+    int cus;
+    int fold;  // set by the launches (xcd_order in attn.h)
 };
 struct SeqAttnOut {
     SeqAttn s;
@@ -346,7 +348,7 @@ struct SeqAttnOut {
 struct SeqAttnPlan {
     int groups, splits;
 };
-SeqAttnPlan seq_attn_plan(const SeqAttn &s, int cus);
+SeqAttnPlan seq_attn_plan(const SeqAttn &s);
 size_t seq_attn_bytes(const SeqAttn &s, const SeqAttnPlan &p);  // workspace
 int64_t seq_attn_workgroups(const SeqAttn &s, const SeqAttnPlan &p);
 hipError_t launch_seq_attn(const SeqAttnOut &a, const SeqAttnPlan &p, hipStream_t stream);
@@ -373,7 +375,7 @@ struct SeqAttnGrad {
 struct SeqAttnGradPlan {
     int qparts, kparts;
 };
-SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys, int cus);
+SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys);
 size_t seq_attn_grad_bytes(const SeqAttn &s, const SeqAttnGradPlan &p);
 int64_t seq_attn_grad_workgroups(const SeqAttn &s, const SeqAttnGradPlan &p);
 hipError_t launch_seq_attn_grad(const SeqAttnGrad &a, hipStream_t stream);

@@ -24,6 +24,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
 typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
 
 __device__ inline uint32_t bf16_bits(float f)
@@ -31,41 +32,43 @@ __device__ inline uint32_t bf16_bits(float f)
     return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
 
-// values 8 g .. 8 g + 7 of a row (n of them; those past the row's end are 0)
+// Values 8 g .. 8 g + 7 of a row as they are in memory (n of them; those past the row's end
+// are 0), and as numbers: apart, so that a load may be in flight while others are used.
 template <bool BF16>
-__device__ inline void load8(const void *p, int64_t e, int n, float (&v)[8])
-{
-    if constexpr (BF16) {
-        const uint16_t *q = static_cast<const uint16_t *>(p) + e;
-        if (n >= 8) {
-            const u32x4 a = *reinterpret_cast<const u32x4_at2 *>(q);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[2 * j] = __uint_as_float(a[j] << 16);
-                v[2 * j + 1] = __uint_as_float(a[j] & 0xFFFF0000u);
+struct Eight {
+    u32x4 w[BF16 ? 1 : 2];
+
+    __device__ inline void load(const void *p, int64_t e, int n)
+    {
+        if constexpr (BF16) {
+            const uint16_t *q = static_cast<const uint16_t *>(p) + e;
+            if (n >= 8) {
+                w[0] = *reinterpret_cast<const u32x4_at2 *>(q);
+                return;
             }
-            return;
-        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = j < n ? __uint_as_float((uint32_t)q[j] << 16) : 0.0f;
-    } else {
-        const float *q = static_cast<const float *>(p) + e;
-        if (n >= 8) {
-            const f32x4 a = *reinterpret_cast<const f32x4_at4 *>(q);
-            const f32x4 b = *reinterpret_cast<const f32x4_at4 *>(q + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] = a[j];
-                v[4 + j] = b[j];
+            for (int j = 0; j < 4; ++j)
+                w[0][j] = (2 * j < n ? q[2 * j] : 0u) | (2 * j + 1 < n ? q[2 * j + 1] : 0u) << 16;
+        } else {
+            const uint32_t *q = static_cast<const uint32_t *>(p) + e;
+            if (n >= 8) {
+                w[0] = *reinterpret_cast<const u32x4_at4 *>(q);
+                w[1] = *reinterpret_cast<const u32x4_at4 *>(q + 4);
+                return;
             }
-            return;
-        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = j < n ? q[j] : 0.0f;
+            for (int j = 0; j < 8; ++j)
+                w[j / 4][j % 4] = j < n ? q[j] : 0u;
+        }
     }
-}
+    __device__ inline float operator[](int j) const
+    {
+        if constexpr (BF16)
+            return __uint_as_float(j % 2 ? w[0][j / 2] & 0xFFFF0000u : w[0][j / 2] << 16);
+        else
+            return __uint_as_float(w[j / 4][j % 4]);
+    }
+};
 
 __device__ inline void store8(void *p, bool bf16, int64_t e, int n, const float (&v)[8])
 {
@@ -128,22 +131,27 @@ template <bool XB, bool HB, int W, int R>
 __global__ __launch_bounds__(THREADS<W>) void norm_kernel(const NormArgs a)
 {
     constexpr int T = 64 * W;
-    __shared__ double ssum[W];
-    __shared__ uint32_t smax[W];
-    const int t = (int)threadIdx.x % T, wave = t >> 6;
-    const int64_t m = (int64_t)blockIdx.x * ROWS<W> + (int)threadIdx.x / T;
-    if (W < 4 && m >= a.M)
+    __shared__ double ssum[ROWS<W>][W];
+    __shared__ uint32_t smax[ROWS<W>][W];
+    const int t = (int)threadIdx.x % T, wave = t >> 6, slot = (int)threadIdx.x / T;
+    const int64_t m = (int64_t)blockIdx.x * ROWS<W> + slot;
+    const bool live = m < a.M;
+    if (W == 1 && !live)
         return;  // (a wavefront of its own: no barrier below)
-    const int N = a.N;
+    const int N = live ? a.N : 0;  // (a row past the last: nothing of it)
     float v[R][8];
     double s = 0.0;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int c = 8 * (t + i * T), n = N - c;
-        float r[8];
-        load8<XB>(a.x, m * a.ldx + c, n, v[i]);
+        Eight<XB> x;
+        x.load(a.x, m * a.ldx + c, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[i][j] = x[j];
         if (a.res) {
-            load8<HB>(a.res, m * a.ldr + c, n, r);
+            Eight<HB> r;
+            r.load(a.res, m * a.ldr + c, n);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 v[i][j] += r[j];
@@ -161,20 +169,20 @@ __global__ __launch_bounds__(THREADS<W>) void norm_kernel(const NormArgs a)
     s = wave_sum(s);
     if constexpr (W > 1) {
         if ((t & 63) == 0)
-            ssum[wave] = s;
+            ssum[slot][wave] = s;
         __syncthreads();
         s = 0.0;
 #pragma unroll
         for (int w = 0; w < W; ++w)
-            s += ssum[w];
+            s += ssum[slot][w];
     }
     const double rstd = inverse_sqrt(__builtin_fma(s, a.inv_n, a.eps));
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int c = 8 * (t + i * T), n = N - c;
-        float w[8];
+        Eight<false> w;
         if (a.weight)
-            load8<false>(a.weight, c, n, w);
+            w.load(a.weight, c, n);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const double u = (double)v[i][j] * rstd;
@@ -204,18 +212,18 @@ __global__ __launch_bounds__(THREADS<W>) void norm_kernel(const NormArgs a)
     }
     if constexpr (W > 1) {
         if ((t & 63) == 0)
-            smax[wave] = amax;
+            smax[slot][wave] = amax;
         __syncthreads();
-        amax = smax[0];
+        amax = smax[slot][0];
 #pragma unroll
         for (int w = 1; w < W; ++w)
-            amax = smax[w] > amax ? smax[w] : amax;
+            amax = smax[slot][w] > amax ? smax[slot][w] : amax;
     }
     uint32_t sbits = 0x7C00;
     if (amax < 0x7F800000u)
         sbits = scale_bits<127>(__uint_as_float(amax));
     const bool zero = sbits == 0x7C00 || sbits == 0;
-    if (t == 0)
+    if (t == 0 && live)
         a.sx[m] = (uint16_t)(sbits == 0x7C00 ? 0x7E00 : sbits);
     const float sc = zero ? 1.0f : f16_value(sbits);
     const float inv = inverse(sc), half_s = 0.5f * sc;
@@ -228,7 +236,7 @@ __global__ __launch_bounds__(THREADS<W>) void norm_kernel(const NormArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             q[j] = zero ? 0u : (uint32_t)nearest_code(v[i][j], sc, inv, half_s, 127) & 0xFFu;
-        *reinterpret_cast<uint2 *>(a.qx + m * N + c) =
+        *reinterpret_cast<uint2 *>(a.qx + m * a.N + c) =
             make_uint2(q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24,
                        q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24);
     }
@@ -241,31 +249,51 @@ template <bool YB, bool HB, bool DB, int W, int R>
 __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArgs a)
 {
     constexpr int T = 64 * W;
-    __shared__ double sums[2][W][2];
+    constexpr bool HOLD = R <= 2;  // registers for a row ahead and the weights
+    __shared__ double sums[2][ROWS<W>][W][2];
     __shared__ float shared_dw[W < 4 ? THREADS<W> : 1][8];
-    const int t = (int)threadIdx.x % T, wave = t >> 6;
+    const int t = (int)threadIdx.x % T, wave = t >> 6, slot = (int)threadIdx.x / T;
     const int N = a.N;
     float dw[R][8];
+    Eight<false> w[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i)
+    for (int i = 0; i < R; ++i) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             dw[i][j] = 0.0f;
-    int turn = 0;
-    for (int64_t m = (int64_t)blockIdx.x * ROWS<W> + (int)threadIdx.x / T; m < a.M;
-         m += (int64_t)gridDim.x * ROWS<W>, turn ^= 1) {
-        float v[R][8], dy[R][8], w[R][8];
+        if (HOLD && a.weight)
+            w[i].load(a.weight, 8 * (t + i * T), N - 8 * (t + i * T));
+    }
+    // the next row is loaded before this one's sums are waited for
+    Eight<HB> hs[2][R];
+    Eight<YB> ys[2][R];
+    Eight<DB> rs[2][R];
+    // (a row past the last, beside one that is there: nothing of it)
+    auto columns = [&](int64_t m) { return ROWS<W> > 1 && m >= a.M ? 0 : N; };
+    auto load = [&](int64_t m, int k) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int c = 8 * (t + i * T), n = columns(m) - c;
+            hs[k][i].load(a.h, m * a.ldh + c, n);
+            ys[k][i].load(a.dy, m * a.lddy + c, n);
+            if (HOLD && a.dres)
+                rs[k][i].load(a.dres, m * a.ldres + c, n);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * ROWS<W>;
+    auto row = [&](int64_t m, int k) {
+        if (HOLD && m - slot + step < a.M)
+            load(m + step, k ^ 1);
+        if (!HOLD)
+            load(m, k);
+        const Eight<HB>(&v)[R] = hs[k];
+        const Eight<YB>(&dy)[R] = ys[k];
+        const Eight<DB>(&d)[R] = rs[k];
         double s = 0.0, p = 0.0;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int c = 8 * (t + i * T), n = N - c;
-            load8<HB>(a.h, m * a.ldh + c, n, v[i]);
-            load8<YB>(a.dy, m * a.lddy + c, n, dy[i]);
-            if (a.weight)
-                load8<false>(a.weight, c, n, w[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i)
+            if (!HOLD && a.weight)
+                w[i].load(a.weight, 8 * (t + i * T), N - 8 * (t + i * T));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const double x = v[i][j], g = a.weight ? (double)dy[i][j] * (double)w[i][j]
@@ -273,45 +301,56 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
                 s = __builtin_fma(x, x, s);
                 p = __builtin_fma(x, g, p);
             }
+        }
         s = wave_sum(s);
         p = wave_sum(p);
         if constexpr (W > 1) {
             // (two turns' places: a wavefront that is a row ahead writes the other)
             if ((t & 63) == 0) {
-                sums[turn][wave][0] = s;
-                sums[turn][wave][1] = p;
+                sums[k][slot][wave][0] = s;
+                sums[k][slot][wave][1] = p;
             }
             __syncthreads();
             s = p = 0.0;
 #pragma unroll
-            for (int k = 0; k < W; ++k) {
-                s += sums[turn][k][0];
-                p += sums[turn][k][1];
+            for (int q = 0; q < W; ++q) {
+                s += sums[k][slot][q][0];
+                p += sums[k][slot][q][1];
             }
         }
         const double rstd = inverse_sqrt(__builtin_fma(s, a.inv_n, a.eps));
         const double mean = p * rstd * a.inv_n;  // of g u
         const float r32 = (float)rstd, k32 = (float)(mean * rstd);
+        const bool there = columns(m) > 0;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int c = 8 * (t + i * T), n = N - c;
-            float d[8], out[8];
-            if (a.dres)
-                load8<DB>(a.dres, m * a.ldres + c, n, d);
+            const int c = 8 * (t + i * T);
+            float out[8];
+            if (!HOLD && a.dres)
+                rs[k][i].load(a.dres, m * a.ldres + c, N - c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float u = v[i][j] * r32, g = a.weight ? dy[i][j] * w[i][j] : dy[i][j];
                 const float o = __builtin_fmaf(g, r32, -u * k32);
-                out[j] = a.dres ? d[j] + o : o;
-                dw[i][j] = __builtin_fmaf(dy[i][j], u, dw[i][j]);
+                out[j] = a.dres ? d[i][j] + o : o;
+                dw[i][j] = there ? __builtin_fmaf(dy[i][j], u, dw[i][j]) : dw[i][j];
             }
-            store8(a.dx, DB, m * a.lddx + c, n, out);
+            store8(a.dx, DB, m * a.lddx + c, columns(m) - c, out);
         }
+    };
+    // (by the workgroup's first row: its wavefronts meet at the sums of several)
+    int64_t m0 = (int64_t)blockIdx.x * ROWS<W>;
+    if (HOLD && m0 < a.M)
+        load(m0 + slot, 0);
+    for (; m0 < a.M; m0 += 2 * step) {
+        row(m0 + slot, 0);
+        if (m0 + step < a.M)
+            row(m0 + step + slot, 1);
     }
     if (!a.part)
         return;
     if constexpr (W < 4) {  // the rows that ran beside each other
-        static_assert(R == 1 && W == 1, "");
+        static_assert(R == 1, "");
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             shared_dw[threadIdx.x][j] = dw[0][j];
@@ -363,6 +402,8 @@ void forward(const NormArgs &a, hipStream_t s)
                        dim3((unsigned)((a.M + ROWS<W> - 1) / ROWS<W>)), dim3(THREADS<W>), 0, s, a)
     if (a.N <= 512)
         QL_GO(1, 1);
+    else if (a.N <= 1024)
+        QL_GO(2, 1);
     else if (a.N <= 2048)
         QL_GO(4, 1);
     else if (a.N <= 4096)
@@ -382,6 +423,8 @@ void backward(const NormGradArgs &a, int parts, hipStream_t s)
                        dim3(THREADS<W>), 0, s, a)
     if (a.N <= 512)
         QL_GO(1, 1);
+    else if (a.N <= 1024)
+        QL_GO(2, 1);
     else if (a.N <= 2048)
         QL_GO(4, 1);
     else if (a.N <= 4096)
@@ -404,11 +447,12 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Workgroups of the backward pass, and partial sums of dw: up to two per CU.
+// Workgroups of the backward pass, and partial sums of dw: up to three per CU (two and four
+// of 8192 x 2048 in fp32 take 42.4 and 45.2 us for 41.1).
 int norm_grad_parts(int64_t M, int N, int cus)
 {
-    const int64_t rows = N <= 512 ? 4 : 1, groups = (M + rows - 1) / rows;
-    const int64_t most = 2 * (int64_t)cus;
+    const int64_t rows = N <= 512 ? 4 : N <= 1024 ? 2 : 1, groups = (M + rows - 1) / rows;
+    const int64_t most = 3 * (int64_t)cus;
     return (int)(groups < most ? groups : most);
 }
 

@@ -110,6 +110,7 @@ SeqAttn seq_attn(const ql_attn &a)
     s.Hk = (int)a.Hk;
     s.dh = (int)a.dh;
     s.causal = a.causal != 0;
+    s.cus = current_cus();
     // (scale 0: so small that every power of it is 1; quotients by it stay finite)
     s.c = std::max(a.scale * 1.44269504088896340736f, 1e-30f);
     return s;
@@ -281,7 +282,7 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
     t.ldo = ldo;
     t.obf16 = odt == QL_DT_BF16;
     t.lse = lse;
-    const SeqAttnPlan plan = seq_attn_plan(t.s, current_cus());
+    const SeqAttnPlan plan = seq_attn_plan(t.s);
     if (seq_attn_workgroups(t.s, plan) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
     t.splits = plan.splits;
@@ -355,7 +356,7 @@ int qlinear_attention_backward(const ql_attn *a, const ql_attn_grad *g, hipStrea
     t.lddv = g->lddv;
     t.bf16 = g->dt == QL_DT_BF16;
     t.scale = a->scale;
-    const SeqAttnGradPlan plan = seq_attn_grad_plan(t.s, t.dk != nullptr, current_cus());
+    const SeqAttnGradPlan plan = seq_attn_grad_plan(t.s, t.dk != nullptr);
     if (seq_attn_grad_workgroups(t.s, plan) > MAX_WORKGROUPS)
         return QL_ERR_UNSUPPORTED;
     t.qparts = plan.qparts;

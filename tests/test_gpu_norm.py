@@ -12,7 +12,7 @@ EPS = 1e-6
 # rows, the longest; rows: one, fewer and more than the workgroups that run beside
 # each other
 SIZES = [(1, 1), (3, 7), (5, 33), (1, 512), (9, 511), (6, 513), (2, 1536), (67, 1000), (4, 2048),
-         (3, 2049), (2, 4095), (3, 4104), (2, 8191), (2, 8200), (2, 16384), (1300, 96)]
+         (3, 2049), (2, 4095), (3, 4104), (2, 8191), (2, 8200), (2, 16384), (1300, 96), (5, 513), (7, 1024), (4, 1025), (1601, 600)]
 
 
 @pytest.fixture(scope="module")
@@ -207,6 +207,21 @@ def test_backward_against_differences(gpu):
         e = rng.standard_normal(N)
         diff = (dyv * R.norm(hv, e, EPS)).sum()  # linear in the weight
         assert abs((host(dw) * e).sum() - diff) <= (ew * np.abs(e)).sum() + 1e-12
+
+
+@pytest.mark.parametrize("N", [96, 600, 1500])
+def test_backward_without_eps(gpu, N):
+    """eps = 0 and a number of rows that leaves places of the last workgroups empty: what
+    is not there adds nothing to dw."""
+    torch, ql = gpu
+    rng = np.random.default_rng(N)
+    for M in (1, 3, 3073):
+        dy, dyv = rows(torch, rng, M, N, torch.float32)
+        h, hv = rows(torch, rng, M, N, torch.float32)
+        dx, dw = ql.rms_norm_backward(dy, h, eps=0.0)
+        want_x, want_w, ex, ew = R.norm_grads(dyv, hv, 1.0, 0.0, 0.0)
+        within(host(dx), want_x, ex)
+        within(host(dw), want_w, ew)
 
 
 def test_no_rows(gpu):
