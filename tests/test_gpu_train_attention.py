@@ -111,7 +111,10 @@ FORWARD = [
     dict(B=1, T=65, H=2, kT=63), dict(B=1, T=107, H=6, Hk=2), dict(B=2, T=130, H=2, kT=257),
     dict(B=4, T=640, H=8), dict(B=1, T=1200, H=2), dict(B=2, T=300, H=32),
     dict(B=1, T=129, H=5, kT=1), dict(B=1, T=200, H=1, kT=4000), dict(B=3, T=33, H=40, kT=130),
+    dict(B=1, T=1, H=1, kT=344),
 ]
+# (parts of the keys where no wavefronts share them, D = 64)
+LARGE = dict(B=3, T=23, H=27, Hk=9, kT=10300)
 
 
 @pytest.mark.parametrize("dh", [64, 128])
@@ -142,6 +145,11 @@ def test_forward_lengths(gpu, shape, rows, causal, dh):
     padding rows hold does not matter."""
     torch, ql = gpu
     check_forward(torch, ql, Case(torch, **shape, rows=rows, causal=causal, dh=dh))
+
+
+def test_forward_large(gpu):
+    torch, ql = gpu
+    check_forward(torch, ql, Case(torch, **LARGE, rows="padded", klens=[10300, 1, 7777]))
 
 
 def test_forward_types_and_scales(gpu):

@@ -30,7 +30,7 @@ def lib():
 def test_exports(lib):
     src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
     names = set(re.findall(r"\b(qlinear_\w+)\s*\(", src))
-    assert len(names) >= 2
+    assert len(names) == 4
     for n in names:
         assert hasattr(lib, n) and n in ql.EXPORTS
 
@@ -41,7 +41,8 @@ def test_structures(tmp_path):
         pytest.skip("no host C compiler or HIP headers")
     src = ['#include <stdio.h>', '#include <stddef.h>', '#include "qlinear_train.h"',
            'int main(void) {']
-    pairs = [("ql_norm", ql._Norm), ("ql_norm_grad", ql._NormGrad), ("ql_attn", ql._Attn)]
+    pairs = [("ql_norm", ql._Norm), ("ql_norm_grad", ql._NormGrad), ("ql_attn", ql._Attn),
+             ("ql_attn_grad", ql._AttnGrad)]
     for name, cls in pairs:
         src.append(f'printf("%zu\\n", sizeof({name}));')
         src += [f'printf("%zu\\n", offsetof({name}, {f}));' for f, _ in cls._fields_]
@@ -232,3 +233,60 @@ def test_binding_refuses_attention():
                dict(O=q.half()), dict(lse=torch.zeros((4, 20), dtype=torch.bfloat16))):
         with pytest.raises(TypeError, match="dtype"):
             call(**kw)
+
+
+def attend_back(lib, **kw):
+    G = 0x10000000
+    g = dict(o=D, ldo=256, odt=BF16, lse=E, dO=G, lddo=256, dq=2 * G, dk=3 * G, dv=4 * G, lddq=256,
+             lddk=128, lddv=128, dt=BF16)
+    a = attn(**{k: v for k, v in kw.items() if k not in g})
+    g.update({k: v for k, v in kw.items() if k in g})
+    return lib.qlinear_attention_backward(ctypes.byref(a), ctypes.byref(ql._AttnGrad(**g)), None)
+
+
+def test_attention_backward_errors(lib):
+    G = 0x10000000
+    for kw, status in ATTN_ERRORS:
+        assert attend_back(lib, **kw) == status, kw
+    assert lib.qlinear_attention_backward(None, None, None) == INVALID
+    assert lib.qlinear_attention_backward(ctypes.byref(attn()), None, None) == INVALID
+    assert attend_back(lib, B=0) == OK
+    assert attend_back(lib, odt=2) == INVALID and attend_back(lib, dt=3) == INVALID
+    for p in ("o", "lse", "dO", "dq", "dk", "dv"):  # (dk and dv: both or neither)
+        assert attend_back(lib, **{p: None}) == INVALID, p
+    for ld, least in (("ldo", 252), ("lddo", 248), ("lddq", 252), ("lddk", 124), ("lddv", 124)):
+        assert attend_back(lib, **{ld: least}) == SHAPE, ld
+        assert attend_back(lib, **{ld: least + 10}) == ALIGN, ld
+        assert attend_back(lib, **{ld: 1 << 31}) == UNSUPPORTED, ld
+    assert attend_back(lib, lddo=1 << 24) == UNSUPPORTED
+    for kw in (dict(o=D + 4), dict(o=D + 8, odt=F32), dict(lse=E + 2), dict(dO=G + 8),
+               dict(dq=2 * G + 4), dict(dk=3 * G + 8, dt=F32), dict(dv=4 * G + 2)):
+        assert attend_back(lib, **kw) == ALIGN, kw
+    # outputs on inputs, on each other; columns of one buffer may lie beside each other
+    for out in ("dq", "dk", "dv"):
+        for at in (A, B, C, D, E, G, F, 2 * G if out != "dq" else 3 * G):
+            assert attend_back(lib, **{out: at, "k_lens": F}) == INVALID, (out, at)
+    wide = dict(lddq=512, lddk=512, lddv=512)
+    assert attend_back(lib, dk=2 * G + 2 * 256, dv=2 * G + 2 * 320, **wide) == INVALID
+    assert attend_back(lib, dk=2 * G + 2 * 448, dv=4 * G, **wide) == INVALID
+
+
+def test_binding_refuses_attention_backward():
+    q = torch.zeros((20, 256), dtype=torch.bfloat16)
+    k = v = torch.zeros((40, 128), dtype=torch.bfloat16)
+    lse = torch.zeros((4, 20))
+    call = lambda O=q, lse=lse, dO=q, **kw: ql.attention_backward(
+        q, k, v, O, lse, dO, 2, 10, 4, kv_heads=2, kT=20, **kw)
+    with pytest.raises(ValueError, match="device"):
+        call()
+    for kw, match in ((dict(O=q[:19]), "rows"), (dict(dO=q[:, :128]), "256 columns"),
+                      (dict(lse=lse[:3]), "shape"), (dict(dq=q[:4]), "rows"),
+                      (dict(dk=k[:4]), "rows"), (dict(dk=k, kv_grads=False), "asked")):
+        with pytest.raises(ValueError, match=match):
+            call(**kw)
+    for kw in (dict(O=q.half()), dict(dO=q.float()), dict(lse=lse.double()), dict(dq=q.half()),
+               dict(dq=q, dk=k.float())):
+        with pytest.raises(TypeError, match="dtype"):
+            call(**kw)
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        call(dtype=torch.float16)
