@@ -173,7 +173,10 @@ __device__ inline void in_agprs(f32x16 &v) { asm volatile("" : "+a"(v)); }
 __device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
 // Workgroup p runs on XCD p % 8: each XCD takes a contiguous range of the grid's work,
-// so that the tiles which several workgroups read come into one L2.  Fold: where the
+// so that the tiles which several workgroups read come into one L2 (sequences vary fastest
+// in it: each XCD has long and short ones.  Five packed clips of 387 to 645 tokens, 32
+// heads: with heads fastest the XCD of the longest has 1.5 times the work of the
+// average).  Fold: where the
 // whole grid is on the GPU at once, two workgroups a CU, the second half of a range is
 // taken from its end, so that a CU's two are a long and a short one of causal blocks.
 __device__ inline int xcd_order(int p, int grid, int fold)

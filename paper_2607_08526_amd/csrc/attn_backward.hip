@@ -57,7 +57,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     int L = xcd_order((int)blockIdx.x, (int)gridDim.x, s.fold);
     const int part = L % parts;
     L /= parts;
-    const int unit = L / nb, b = unit / s.Hk, hk = unit - b * s.Hk;
+    const int unit = L / nb, hk = unit / s.B, b = unit - hk * s.B;
     // causal: the longest first (the last queries, the first keys)
     const int blk = s.causal && !KEYS ? nb - 1 - (L - unit * nb) : L - unit * nb;
     const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
     if (at >= all)
         return;
     const int unit = (int)(at / rows), row = (int)(at - (int64_t)unit * rows);
-    const int b = unit / s.Hk, hk = unit - b * s.Hk;
+    const int hk = unit / s.B, b = unit - hk * s.B;
     const int t = KEYS ? row : row / G, head = KEYS ? hk : hk * G + row - t * G;
     const SeqRows R = KEYS ? seq_rows(s.k_off, s.k_len, s.krows, s.KT, b)
                            : seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);

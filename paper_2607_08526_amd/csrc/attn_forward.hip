@@ -56,7 +56,7 @@ void seq_attn_kernel(const SeqAttnOut a)
     int L = xcd_order((int)blockIdx.x, (int)gridDim.x, s.fold);
     const int part = L % a.splits;
     L /= a.splits;
-    const int unit = L / nq, b = unit / s.Hk, hk = unit - b * s.Hk;
+    const int unit = L / nq, hk = unit / s.B, b = unit - hk * s.B;
     // causal: the longest first, the last tiles of the grid are short
     const int qblk = s.causal ? nq - 1 - (L - unit * nq) : L - unit * nq;
     const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
@@ -443,7 +443,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const SeqAttnOut a)
     if (at >= rows)
         return;
     const int unit = (int)(at / (s.T * G)), row = (int)(at - (int64_t)unit * s.T * G);
-    const int b = unit / s.Hk, t = row / G, head = (unit - b * s.Hk) * G + row - t * G;
+    const int hk = unit / s.B, b = unit - hk * s.B;
+    const int t = row / G, head = hk * G + row - t * G;
     const f32x2_t *const ml =
         reinterpret_cast<const f32x2_t *>(a.part + a.splits * rows * D) + at;
     const float *const po = a.part + at * D + ch;

@@ -1097,8 +1097,8 @@ def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=No
                        stream=None):
     """The backward pass of attention_forward (its arguments, and the O and lse it
     returned) from dO, the gradient of O (bf16): AttentionGrads, k's and v's None without
-    kv_grads.  dq [rows of q][>= H * dh], dk and dv [rows of k][>= kv_heads * dh]: row views
-    of one dtype (fp32 or bf16; dtype where they are made here), e.g. the columns of a
+    kv_grads.  dq [rows of q][>= H * dh], dk and dv (both or neither) [rows of k][>= kv_heads
+    * dh]: row views of one dtype (fp32 or bf16; dtype where they are made here), e.g. the columns of a
     fused QKV output's gradient.  Padding rows get zeros, rows of no sequence are not
     written (zeros in outputs made here).  Asynchronous."""
     a, tensors, qrows, krows = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
@@ -1115,17 +1115,21 @@ def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=No
         if t is not None:
             dtype = t.dtype
             break
-    if dq is None:  # (zeros: rows that may be of no sequence)
-        dq = _attn_new(q, (qrows, wide), dtype, stream,
-                       0.0 if q_offsets is not None or qrows != B * T else None)
+    # (made here: in one piece where they are alike, as zeros where rows may be of no sequence)
+    qfill = 0.0 if q_offsets is not None or qrows != B * T else None
+    if kv_grads and dk is None and dv is None:
+        fill = 0.0 if k_offsets is not None or krows != B * a.Tk else None
+        if dq is None and qrows == krows and wide == narrow and fill == qfill:
+            dq, dk, dv = _attn_new(q, (3, qrows, wide), dtype, stream, fill).unbind(0)
+        else:
+            dk, dv = _attn_new(q, (2, krows, narrow), dtype, stream, fill).unbind(0)
+    if dq is None:
+        dq = _attn_new(q, (qrows, wide), dtype, stream, qfill)
     lddq = _require_rows(dq, "dq", qrows, wide, _FLOATS, False, 4)
     lddk = lddv = 0
     if kv_grads:
-        zero = 0.0 if k_offsets is not None or krows != B * a.Tk else None
-        if dk is None:
-            dk = _attn_new(q, (krows, narrow), dtype, stream, zero)
-        if dv is None:
-            dv = _attn_new(q, (krows, narrow), dtype, stream, zero)
+        if dk is None or dv is None:
+            raise ValueError("dk and dv: both or neither are given")
         lddk = _require_rows(dk, "dk", krows, narrow, (dq.dtype,), False, 4)
         lddv = _require_rows(dv, "dv", krows, narrow, (dq.dtype,), False, 4)
     _on_current_device(O, lse, dO, dq, dk, dv, *tensors)

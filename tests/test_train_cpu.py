@@ -281,11 +281,12 @@ def test_binding_refuses_attention_backward():
         call()
     for kw, match in ((dict(O=q[:19]), "rows"), (dict(dO=q[:, :128]), "256 columns"),
                       (dict(lse=lse[:3]), "shape"), (dict(dq=q[:4]), "rows"),
-                      (dict(dk=k[:4]), "rows"), (dict(dk=k, kv_grads=False), "asked")):
+                      (dict(dk=k[:4], dv=v), "rows"), (dict(dk=k), "neither"),
+                      (dict(dk=k, kv_grads=False), "asked")):
         with pytest.raises(ValueError, match=match):
             call(**kw)
     for kw in (dict(O=q.half()), dict(dO=q.float()), dict(lse=lse.double()), dict(dq=q.half()),
-               dict(dq=q, dk=k.float())):
+               dict(dq=q, dk=k.float(), dv=v)):
         with pytest.raises(TypeError, match="dtype"):
             call(**kw)
     with pytest.raises(TypeError, match="float32 or bfloat16"):
