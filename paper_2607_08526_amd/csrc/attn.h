@@ -172,19 +172,56 @@ __device__ inline void in_agprs(f32x16 &v) { asm volatile("" : "+a"(v)); }
 // The order of instructions stays as written across this point.
 __device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 
+// What a workgroup does: part `part` of block `blk` of rows (0: the longest of causal ones)
+// of key head and sequence `unit`.
+struct Work {
+    int part, blk, unit;
+};
+
 // Workgroup p runs on XCD p % 8: each XCD takes a contiguous range of the grid's work,
 // so that the tiles which several workgroups read come into one L2 (sequences vary fastest
 // in it: each XCD has long and short ones.  Five packed clips of 387 to 645 tokens, 32
 // heads: with heads fastest the XCD of the longest has 1.5 times the work of the
-// average).  Fold: where the
-// whole grid is on the GPU at once, two workgroups a CU, the second half of a range is
-// taken from its end, so that a CU's two are a long and a short one of causal blocks.
-__device__ inline int xcd_order(int p, int grid, int fold)
+// average).  Causal blocks, long and short: see order_work.
+__host__ __device__ inline Work work_of(const SeqAttn &s, int p, int grid, int parts, int nb)
 {
     const int q = grid >> 3, r = grid & 7, xcd = p & 7, i = p >> 3;
     const int n = xcd < r ? q + 1 : q, first = xcd < r ? xcd * n : r * (q + 1) + (xcd - r) * q;
     const int half = (n + 1) / 2;
-    return first + (fold && i >= half ? n - 1 - (i - half) : i);
+    const int L = first + (s.fold && i >= half ? n - 1 - (i - half) : i);
+    Work w;
+    int at = L / parts;
+    w.part = L - at * parts;
+    w.unit = at / nb;
+    w.blk = at - w.unit * nb;
+    if (s.group > 1) {
+        const int units = s.B * s.Hk / 8;  // of an XCD: first to first + units - 1
+        const int u0 = w.unit / units * units, g0 = (w.unit - u0) / s.group * s.group;
+        const int size = s.group < units - g0 ? s.group : units - g0;
+        at -= (u0 + g0) * nb;
+        w.blk = at / size;
+        w.unit = u0 + g0 + at - w.blk * size;
+    }
+    return w;
+}
+
+// The order of a launch of `blocks` workgroups for each of the B Hk units, `resident` of
+// them on a CU at a time.  Causal blocks take from next to nothing to twice the average.
+// Where all run at once, two on a CU, the second half of an XCD's range is taken from its
+// end: a CU's two are a long and a short one.  Where they do not, a unit's longest come
+// first, and the places that its short ones leave early take the next unit's long ones;
+// units that do not fill an XCD's places twice are taken together, as many as do, their
+// longest first.  4096 queries of 32 heads of 64, us forward, dq, dk and dv: 122 / 151 / 192
+// unit by unit, 108 / 134 / 167 four together; 2 sequences of 2048, 8 heads of 128 with 4
+// query heads each, dk and dv in 2 parts: 194 and, two together, 184.  (One workgroup on a
+// CU at a time, so nothing taken from the end: dk and dv of one such sequence 104, not 124.)
+inline void order_work(SeqAttn &s, int64_t blocks, int resident)
+{
+    const int64_t units = (int64_t)s.B * s.Hk, places = (int64_t)resident * s.cus / 8;
+    s.fold = s.causal && resident == 2 && blocks * units <= 8 * places;
+    s.group = 1;
+    if (s.causal && !s.fold && units % 8 == 0 && blocks > 0)
+        s.group = (int)((2 * places + blocks - 1) / blocks);
 }
 
 }  // namespace qlk

@@ -54,12 +54,10 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     const int G = s.H / s.Hk, parts = KEYS ? a.kparts : a.qparts;
     const int rows = KEYS ? s.KT : s.T * G;  // kept, of a (sequence, key head)
     const int nb = (rows + KEEP - 1) / KEEP;
-    int L = xcd_order((int)blockIdx.x, (int)gridDim.x, s.fold);
-    const int part = L % parts;
-    L /= parts;
-    const int unit = L / nb, hk = unit / s.B, b = unit - hk * s.B;
-    // causal: the longest first (the last queries, the first keys)
-    const int blk = s.causal && !KEYS ? nb - 1 - (L - unit * nb) : L - unit * nb;
+    const Work w = work_of(s, (int)blockIdx.x, (int)gridDim.x, parts, nb);
+    const int part = w.part, unit = w.unit, hk = unit / s.B, b = unit - hk * s.B;
+    // (the longest of causal blocks: the last queries, the first keys)
+    const int blk = s.causal && !KEYS ? nb - 1 - w.blk : w.blk;
     const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
     const SeqRows K = seq_rows(s.k_off, s.k_len, s.krows, s.KT, b);
     const int row0 = blk * KEEP;
@@ -523,6 +521,7 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
 // Rows of a streamed tile: 64, half the barriers and waits of 32, where the LDS holds them
 // (two workgroups on a CU but for D = 128 and kept keys).
 constexpr int tile_rows(int D, bool keys) { return D == 64 || keys ? 64 : 32; }
+constexpr int on_a_cu(int D, bool keys) { return D == 64 || !keys ? 2 : 1; }
 
 int64_t blocks(const SeqAttn &s, bool keys)
 {
@@ -545,7 +544,7 @@ constexpr double JOIN_RATE = 4.3e6;                   // bytes a us of their val
 double parts_us(const SeqAttn &s, bool keys, int parts)
 {
     const StepCost &c = STEP[keys][s.dh == 128];
-    const bool two = s.dh == 64 || !keys;  // workgroups fit a CU
+    const bool two = on_a_cu(s.dh, keys) == 2;
     const int G = s.H / s.Hk;
     const double w = (double)blocks(s, keys) * parts, slots = (two ? 2.0 : 1.0) * s.cus;
     const double most = std::ceil((keys ? s.T : s.KT) / 32.0) * (keys ? G : 1);
@@ -569,7 +568,8 @@ hipError_t go(const SeqAttnGrad &g, hipStream_t stream)
     SeqAttnGrad a = g;
     const int parts = KEYS ? a.kparts : a.qparts;
     const unsigned grid = (unsigned)(blocks(a.s, KEYS) * parts);
-    a.s.fold = grid <= 2 * (unsigned)a.s.cus;
+    if (grid)
+        order_work(a.s, grid / ((int64_t)a.s.B * a.s.Hk), on_a_cu(D, KEYS));
     constexpr int BT = tile_rows(D, KEYS);
     if (grid)
         hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, BT, BT == 64 ? 3 : 4>), dim3(grid),

@@ -53,12 +53,9 @@ void seq_attn_kernel(const SeqAttnOut a)
     const SeqAttn &s = a.s;
     const int G = s.H / s.Hk;
     const int nq = (s.T * G + BQ - 1) / BQ;
-    int L = xcd_order((int)blockIdx.x, (int)gridDim.x, s.fold);
-    const int part = L % a.splits;
-    L /= a.splits;
-    const int unit = L / nq, hk = unit / s.B, b = unit - hk * s.B;
-    // causal: the longest first, the last tiles of the grid are short
-    const int qblk = s.causal ? nq - 1 - (L - unit * nq) : L - unit * nq;
+    const Work w = work_of(s, (int)blockIdx.x, (int)gridDim.x, a.splits, nq);
+    const int part = w.part, unit = w.unit, hk = unit / s.B, b = unit - hk * s.B;
+    const int qblk = s.causal ? nq - 1 - w.blk : w.blk;
     const SeqRows Q = seq_rows(s.q_off, s.q_len, s.qrows, s.T, b);
     const SeqRows K = seq_rows(s.k_off, s.k_len, s.krows, s.KT, b);
     const int row0 = qblk * BQ;
@@ -486,6 +483,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(const SeqAttnOut a)
 }
 
 int tile_rows(int groups) { return 128 / groups; }
+int on_a_cu(const SeqAttn &s, int groups) { return s.dh == 64 || groups < 4 ? 2 : 1; }
 
 // us of a launch (fitted to sweeps of 398 shapes in up to 40 forms each; the choice takes
 // 1.015 times the best form's time on average, 1.06 at the ninth decile): its start and end,
@@ -503,7 +501,7 @@ double form_us(const SeqAttn &s, int groups, int splits)
 {
     const int kind = groups == 4 ? 2 : groups - 1;
     const StepCost &c = STEP[s.dh == 128][kind];
-    const bool two = s.dh == 64 || groups < 4;  // workgroups fit a CU
+    const bool two = on_a_cu(s, groups) == 2;
     const double units = (double)s.B * s.Hk, rows = (double)s.T * (s.H / s.Hk);
     const double w = std::ceil(rows / tile_rows(groups)) * units * splits;
     const double slots = (two ? 2.0 : 1.0) * s.cus;
@@ -566,8 +564,9 @@ size_t seq_attn_bytes(const SeqAttn &s, const SeqAttnPlan &p)
 hipError_t launch_seq_attn(const SeqAttnOut &out, const SeqAttnPlan &p, hipStream_t stream)
 {
     SeqAttnOut a = out;
-    a.s.fold = seq_attn_workgroups(a.s, p) <= 2 * a.s.cus;
-    const dim3 grid((unsigned)seq_attn_workgroups(a.s, p)), block(THREADS);
+    const int64_t workgroups = seq_attn_workgroups(a.s, p);
+    order_work(a.s, workgroups / ((int64_t)a.s.B * a.s.Hk), on_a_cu(a.s, p.groups));
+    const dim3 grid((unsigned)workgroups), block(THREADS);
 #define QL_GO(D, KG, BK) \
     hipLaunchKernelGGL((seq_attn_kernel<D, KG, BK>), grid, block, 0, stream, a)
     if (a.s.dh == 64) {

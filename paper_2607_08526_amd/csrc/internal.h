@@ -332,7 +332,7 @@ struct SeqAttn {
     int causal;
     float c;  // scale * log2(e), > 0
     int cus;
-    int fold;  // set by the launches (xcd_order in attn.h)
+    int fold, group;  // set by the launches (order_work in attn.h)
 };
 struct SeqAttnOut {
     SeqAttn s;

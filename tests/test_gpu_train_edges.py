@@ -10,7 +10,7 @@ import pytest
 import block_ref as BR
 import train_ref as R
 from test_gpu_norm import host, within
-from test_gpu_train_attention import Case, compare
+from test_gpu_train_attention import Case, check_backward, check_forward, compare
 
 pytestmark = pytest.mark.gpu
 
@@ -374,3 +374,15 @@ def test_long_cache(gpu):
     # (bf16 probability, the exponential's and the sum's last steps)
     assert (np.abs(got[:4] - want) <= want * (R.BF16 + 1e-5)).all() and (got[4:] == 0).all()
     assert abs(float(lse) - np.log(total)) <= 1e-5
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("rows", ["padded", "packed"])
+def test_causal_over_many_heads(gpu, rows, dh):
+    """More (sequence, head) pairs than run at once, short and long ones: those of an XCD
+    are taken in groups, the last of them smaller."""
+    torch, ql = gpu
+    lens = [1 + 37 * b % 130 for b in range(25)]
+    c = Case(torch, 25, 130, 32, dh=dh, causal=True, rows=rows, lens=lens)
+    check_forward(torch, ql, c)
+    check_backward(torch, ql, c)

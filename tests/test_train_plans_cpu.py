@@ -36,7 +36,7 @@ def probe(tmp_path_factory):
 
     def run(kind, cases):
         lines = [f"{kind} {c['B']} {c['T']} {c.get('kT', c['T'])} {c['H']} {c.get('Hk', c['H'])} "
-                 f"{c['dh']} {int(c['causal'])}" for c in cases]
+                 f"{c['dh']} {int(c['causal'])} {c.get('more', '')}" for c in cases]
         r = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True,
                            timeout=120)
         assert r.returncode == 0, r.stderr[-2000:]
@@ -94,3 +94,29 @@ def test_plans_of_measured_calls(probe):
     got = probe("bwd", [case(1, 4096, 4096, 32, 32, 64), case(1, 2048, 2048, 32, 8, 128, True),
                         case(3, 778, 778, 8, 8, 64, True)])
     assert [g[:2] for g in got] == [(1, 1), (1, 4), (1, 1)]
+
+
+def test_order_of_work(probe):
+    """Every part of every block of every unit is some workgroup's, once, in any order."""
+    rng = random.Random(5)
+    cases = []
+    while len(cases) < 300:
+        B, Hk = rng.choice([1, 1, 2, 3, 8, 25]), rng.choice([1, 2, 5, 8, 16, 32])
+        parts, blocks = rng.choice([1, 1, 2, 3, 8]), rng.randint(1, 70)
+        if B * Hk * parts * blocks <= 6000:
+            cases.append(dict(B=B, T=1, H=Hk, Hk=Hk, dh=64, causal=rng.random() < 0.7,
+                              more=f"{parts} {blocks} {rng.choice([1, 2])}", size=(parts, blocks)))
+    seen = set()
+    for c, (fold, group, *work) in zip(cases, probe("work", cases)):
+        parts, blocks = c["size"]
+        units = c["B"] * c["Hk"]
+        work = list(zip(work[::3], work[1::3], work[2::3]))
+        assert sorted(work) == [(p, b, u) for p in range(parts) for b in range(blocks)
+                                for u in range(units)], c
+        assert c["causal"] or (fold, group) == (0, 1)
+        seen.add((fold, group > 1, group > 1 and units // 8 % group > 0 and units // 8 > group))
+        if group > 1:  # of an XCD's units that are taken together, the longest first
+            for xcd in range(8):
+                blks = [b for _, b, _ in work[xcd::8]][: parts * blocks * min(group, units // 8)]
+                assert blks == sorted(blks), c
+    assert seen >= {(0, False, False), (1, False, False), (0, True, False), (0, True, True)}
