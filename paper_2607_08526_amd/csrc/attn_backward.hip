@@ -18,6 +18,20 @@
 // bf16 for it.  Matrix and vector units run beside each other within a wavefront: P and dS
 // of block i are formed between the matrix instructions of block i + 1's S and dP; block
 // i's second products follow.
+//
+// What bounds it, measured in us, dq / dk and dv: 4096 queries and keys of 32 heads of 64
+// 215 / 270, of 16 heads of 128 199 / 285: 960 to 1040 TFLOP/s of dq's three products and
+// the four of dk and dv.  Matrix cores are busy in 0.5 (dq) and 0.6 of a CU's cycles, vector
+// instructions in 0.6, and the clock falls as these shares rise.  One causal sequence of
+// 2048, 8 key heads of 128 with 4 query heads each: 77 / 100 and 12 for adding up 4 parts,
+// where half of the time without a mask is 55 / 75 and 8: a grid that the GPU holds at once,
+// as forward.  Five packed sequences of 387 to 645, 32 heads of 64: 44 / 52, launches of 960
+// workgroups for 512 places, of 7 to 11 tiles each: their first loads and last stores weigh
+// as much as a third of these.
+//
+// Both launches in one, or one that adds dq up by atomics, would save two of seven products;
+// the one needs the registers of both (two accumulators of D x 32 more), the other gives
+// sums whose order changes.
 #include <algorithm>
 #include <cmath>
 
@@ -258,9 +272,9 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     };
     // The matrix instructions of a step: S and dP of the tile in next (for kept keys they
     // start with -lse / scale and -d of the streamed queries, three bf16 each that add up
-    // to 24 bits: as products with ones, where reading them from LDS in the accumulators'
-    // layout, 16 values a lane, would take as long as reading the tiles' rows), then the
-    // second products of the tile in prev.
+    // to 24 bits: as products with ones, two matrix instructions and LDS reads a block, where
+    // reading them in the accumulators' layout, 16 values a lane each, takes eight reads and
+    // 32 registers), then the second products of the tile in prev.
     constexpr int SUMS = KEYS ? 2 : 0, FIRST = SUMS + 2 * DS, SECOND = (KEYS ? 4 : 2) * DT;
     const uint32_t one = hf == 0 ? 0x3F80u : 0u, ones = one | one << 16;
     const bf16x8 ones_lse = __builtin_bit_cast(bf16x8, u32x4{ones, one, 0u, 0u});
@@ -485,7 +499,8 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     }
 }
 
-// Partial sums added in order, 4 channels a thread (blockIdx.y: dk, dv).
+// Partial sums added in order, 4 channels a thread (blockIdx.y: dk, dv).  4 parts of 16384
+// rows of 128 for both: 12 us, 6.2 TB/s, much of it from the last-level cache.
 template <int D, bool KEYS>
 __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a)
 {

@@ -10,14 +10,31 @@
 // scores of one query), then O^T += V^T P^T with P^T straight from the score
 // registers; a lane's query never changes, so its maximum, sum, mask and rescaling
 // are its own.  Tiles of keys come in by direct-to-LDS loads, two buffers each for K
-// and V, one tile apart; the scores of tile j + 1 are formed between the maximum of
-// tile j and its value product.
+// and V, one tile apart.  Matrix and vector units run beside each other within a
+// wavefront: the softmax of tile j is placed, a few instructions at a time, between the
+// matrix instructions that form the scores of tile j + 1 and the value product of tile
+// j - 1.  (In the compiler's order one unit waits for the other: 200 us for 183 of the first
+// case below, 118 for 62 of the causal one with 128 channels.)
 //
 // Rows of a tile are (query, head of the group) pairs, i = t G + g for the G query
 // heads of a key head: each K and V tile is read once for all of them, and one token's
 // G heads fill G rows.  KG groups of wavefronts share out a tile's keys (KG = 4: one
 // wavefront of 32 rows each, for one token; merged through LDS at the end); beyond that
 // `splits` workgroups take parts of the keys and attn_join_kernel adds them up.
+//
+// What bounds it, measured in us: 4096 queries and keys of 32 heads of 64 170 to 180, 760
+// to 810 TFLOP/s, by the vector instructions that a score takes (they are active in 0.65 of
+// a CU's cycles, the matrix cores in 0.40; LDS in 0.20, without conflicts); of 16 heads of
+// 128, twice the matrix work for a score, 149, 920 TFLOP/s.  2 causal sequences of 4096, 32
+// heads of 64: 180.  One causal sequence of 2048, 8 key heads of 128 with 4 query heads
+// each: 60 to 63, where half of the time without a mask is 42: a grid that the GPU holds at
+// once, so the start and end of a launch and what its CUs' last blocks leave idle (two groups
+// of wavefronts take as long; two parts of the keys 59 and 17 for the join).  One token of 8
+// sequences over up to 8192 keys: 47, 4.4 TB/s, by HBM.
+//
+// Two workgroups a CU, 256 registers a lane: with three the compiler spills (D = 64, tiles of
+// 32 keys: 350 us for 170).  Tiles of 64 keys for D = 64; 32 for D = 128 (64, with one
+// workgroup a CU: 68 for 60).  Plain stores: non-temporal ones took as long.
 #include <algorithm>
 #include <cmath>
 
@@ -428,7 +445,8 @@ void seq_attn_kernel(const SeqAttnOut a)
             none ? -INFINITY : (mrun * c + __builtin_amdgcn_logf(lrun)) * LN2;
 }
 
-// The parts of a split, joined in order: 4 channels of a (query, head) a thread.
+// The parts of a split, joined in order: 4 channels of a (query, head) a thread.  (Latency:
+// 4 parts of 256 rows of 128 take 4.8 us.)
 template <int D>
 __global__ __launch_bounds__(256) void attn_join_kernel(const SeqAttnOut a)
 {

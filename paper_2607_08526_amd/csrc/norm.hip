@@ -13,7 +13,12 @@
 //
 // Bound: HBM; at few rows the latency of one load and of the row's reduction.  A
 // row's values stay in registers between the sum and the output (W wavefronts of
-// R groups of 8 columns per lane), so each is read once.
+// R groups of 8 columns per lane), so each is read once.  Measured, us:
+//   forward, 2048 rows of 2048, fp32 x, r and h, bf16 y (59 MB): 12.2, 4.8 TB/s (a copy of
+//   4 GiB: 4.4 to 5.1); 1290 rows of 1536, bf16 x, fp32 r and h, int8 y (22 MB): 9.6, a
+//   row's two reductions and its latency; one row: 2.5, a launch
+//   backward, 8192 rows of 2048, bf16 dy, fp32 h, dres and dx (235 MB): 41 and 4.7 for the
+//   sum of dw, 5.1 TB/s; 107 rows of 1024: 4.3 and 3.4, two launches
 #include "codes.h"
 #include "internal.h"
 
@@ -370,8 +375,9 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
     }
 }
 
-// dw[c] = the sum of part[0 .. parts)[c]: 64 columns a workgroup, every 16th part a
-// wavefront
+// dw[c] = the sum of part[0 .. parts)[c], in one order (so that results repeat): 64 columns
+// a workgroup, every 16th part a wavefront.  768 parts of 2048 columns: 4.7 us, most of it
+// the launch and the latency of 48 loads, eight in flight.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, int parts, int N,
                                                        float *dw)
 {
