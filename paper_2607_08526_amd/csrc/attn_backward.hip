@@ -107,8 +107,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     constexpr int LOADS = 2 * TileLoad<D, BT, THREADS>::N + (KEYS ? 1 : 0);  // a tile's
     // The tile that is loaded next: tile ft of head fh, its rows' first bytes and number,
     // and its buffer.  (Counted on from tile to tile: scalar instructions take their turn
-    // with the others of a wavefront, and a division and four products a tile took 0.3 of
-    // the time of a step.)
+    // with the others of a wavefront, a division and four products a tile among them.)
     int ft, fh, fleft, fbuf = 0;
     const uint8_t *f1, *f2;
     const float *fsums;
