@@ -102,14 +102,15 @@ int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream);
  * lens (device, [B]) the first lens[b] of these rows are the sequence's and the others
  * padding: never read, written as zeros (lse: -infinity).  Rows of no sequence stay as
  * they are.  Offsets and lens are read on the device; values that lie outside of a
- * tensor or a sequence's place are cut to it.  Sequences that share query rows (for the
- * backward pass: key rows) give what the last writer leaves.
+ * tensor or a sequence's place are cut to it.  Sequences that share query rows (in the
+ * backward pass, query or key rows) leave one of their results there, or a mixture.
  *
  * q, k, v: bf16, 16-byte aligned, rows of ldq, ldk, ldv elements (% 8 == 0, < 2^24).  O:
- * fp32 (16-byte aligned) or bf16 (8-byte), rows of ldo (% 4 == 0).  scale >= 0, finite.
- * The probabilities enter the product with V rounded to bf16, sums are fp32.  A value
- * that is not finite in a row which only the causal mask hides may reach queries of
- * the same tile (0 * infinity).  Sizes: B * H * Tq, B * Hk * Tk < 2^31, B * Hk *
+ * fp32 (16-byte aligned) or bf16 (8-byte), rows of ldo (% 4 == 0).  scale: 0 (taken as
+ * 1e-30) or 1e-30 to 2.3e38; scores times log2(e) that leave fp32's range give NaN.  The
+ * probabilities enter the product with V rounded to bf16, sums are fp32.  A value that is
+ * not finite in a row which only the causal mask hides may reach queries of the same
+ * tile (0 * infinity).  Sizes: B * H * Tq, B * Hk * Tk < 2^31, Tk <= 2^30, B * Hk *
  * ceil(Tq * H / Hk / 32) < 2^24 (QL_ERR_UNSUPPORTED). */
 typedef struct {
     const uint16_t *q;

@@ -58,17 +58,19 @@ bool share_bytes(const Rows &a, const Rows &b)
 // (backward: there is work for the keys without queries too)
 int check_attn(const ql_attn *a, bool backward)
 {
-    if (!a || !(a->scale >= 0.0f) || a->scale > 3e38f)
+    // (scale log2(e) is finite, and no other than 0 is smaller than seq_attn takes it)
+    if (!a || !(a->scale >= 0.0f) || a->scale > 2.3e38f || (a->scale > 0.0f && a->scale < 1e-30f))
         return QL_ERR_INVALID;
     if (a->B < 0 || a->Tq < 0 || a->Tk < 0 || a->H <= 0 || a->Hk <= 0 || a->H % a->Hk ||
         a->q_rows < 0 || a->k_rows < 0)
         return QL_ERR_SHAPE;
-    if ((a->dh != 64 && a->dh != 128) || a->B >= I31 || a->Tq >= I31 || a->Tk >= I31 ||
+    if ((a->dh != 64 && a->dh != 128) || a->B >= I31 || a->Tq >= I31 || a->Tk > I31 / 2 ||
         a->H >= 1 << 16 || a->q_rows >= I31 || a->k_rows >= I31 || a->ldq >= 1 << 24 ||
         a->ldk >= 1 << 24 || a->ldv >= 1 << 24)
         return QL_ERR_UNSUPPORTED;
     const int64_t rows = a->Tq * (a->H / a->Hk);  // of a key head's queries
-    // (each factor is below 2^31 and 2^16: no product overflows)
+    // (each factor is below 2^31 and 2^16: no product overflows.  Rows are at most 2^29 then,
+    // and keys 2^30: the kernels add them in 32 bits)
     if (a->B * a->H >= I31 || (a->Tq && a->B * a->H >= (I31 + a->Tq - 1) / a->Tq) ||
         (a->Tk && a->B * a->Hk >= (I31 + a->Tk - 1) / a->Tk) ||
         a->B * a->Hk * ((rows + 31) / 32) > MAX_WORKGROUPS)

@@ -291,3 +291,16 @@ def test_binding_refuses_attention_backward():
             call(**kw)
     with pytest.raises(TypeError, match="float32 or bfloat16"):
         call(dtype=torch.float16)
+
+
+@pytest.mark.parametrize("change, want", [
+    # scale log2(e) past fp32's range; so small that it would be taken as another
+    (dict(scale=3e38), INVALID), (dict(scale=2.4e38), INVALID), (dict(scale=9e-31), INVALID),
+    (dict(scale=1e-40), INVALID),
+    # tiles' ends past 2^31
+    (dict(B=1, Tk=(1 << 30) + 1, k_rows=(1 << 30) + 1), UNSUPPORTED),
+    (dict(B=1, H=1, Hk=1, Tk=(1 << 31) - 1, k_rows=(1 << 31) - 1), UNSUPPORTED),
+], ids=str)
+def test_attention_far_ends(lib, change, want):
+    assert attend(lib, **change) == want
+    assert attend_back(lib, **change) == want
