@@ -44,11 +44,13 @@ constexpr int THREADS = 256;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 constexpr int KEEP = 128;  // kept rows of a workgroup
-// Where the queries of a workgroup see at most so many keys, d_i is formed as sum
-// P_ij dP_ij in a pass of its own: the rounding of a bf16 O, harmless in a sum over many
-// keys, is not when a few make up the row (dq off by 0.0030 of its norm at 3 keys against
-// 0.0024, of which the output's rounding is 0.0017).
-constexpr int FEW_KEYS = 128;
+// Where a workgroup streams at most so many rows, its sums, of few terms each, take what
+// rounding averages out in longer ones: P and dS enter the products as two bf16, 16 bits of
+// them, and d_i is formed as sum P_ij dP_ij in a pass of its own, not from a bf16 O.  Tiles
+// are loaded a ring at a time and nothing overlaps (107 queries and keys of 48 heads of 64: dk
+// and dv in 10.1 us, 8.2 with P and dS as one bf16 each and overlapped; dq 10.3 and 10.7).  (dq at 2 to 3 keys was off by 0.0027 to 0.0030 of its norm, where
+// the output's own rounding is 0.0017.)
+constexpr int FEW = 128;
 
 template <int D, bool KEYS, int BT, int BUFS>
 __global__ __launch_bounds__(THREADS)
@@ -140,18 +142,17 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         }
     };
 
-    // The first tiles, before the kept rows (whose loads they pass on the way).
-    const bool few = !KEYS && tiles * BT <= FEW_KEYS;
-    auto fetch_first = [&] {
-        aim(j0);
-        fbuf = 0;
-#pragma unroll
-        for (int i = 0; i < BUFS - 1; ++i)
-            if (j0 + i < j1)
-                fetch();
-    };
-    if (j0 < j1 && !few)
-        fetch_first();
+    // The first tiles, before the kept rows (whose loads they pass on the way); where they
+    // are few, all (of dq those of other parts too: d is a sum over them)
+    static_assert(KEYS || FEW / BT <= BUFS, "");
+    const bool few = (KEYS ? (int64_t)(Q.len - first * BT) * G : tiles * BT) <= FEW;
+    const int l0 = few && !KEYS ? 0 : j0;
+    const int l1 = few && !KEYS ? tiles : min(j1, j0 + (few ? BUFS : BUFS - 1));
+    if (l0 < l1) {
+        aim(l0);
+        for (int j = l0; j < l1; ++j)
+            fetch();
+    }
 
     // the kept row of this lane: its operands, and the streamed rows lo to hi that meet it
     const int row = wrow + l32;
@@ -231,10 +232,10 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     };
     // Values 2 I and 2 I + 1 of a lane: streamed rows r0 + 8 (r / 4) + 4 hf + r % 4, r = 2 I
     // and 2 I + 1; from, to: lo and hi less r0 + 4 hf.
-    auto cook = [&](auto maskc, auto ic, int from, int to, const Raw &x, Cooked &y) {
+    auto probability = [&](auto maskc, auto ic, int from, int to, const Raw &x, float (&p)[2],
+                           float (&ds)[2]) {
         constexpr bool MASK = decltype(maskc)::value;
         constexpr int I = decltype(ic)::value;
-        float p[2], ds[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int r = 2 * I + k, at = 8 * (r >> 2) + (r & 3);
@@ -243,14 +244,34 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
                 p[k] = at <= to && (!KEYS || at >= from) ? p[k] : 0.0f;
             ds[k] = p[k] * (KEYS ? x.dp[r] : x.dp[r] - delta);
         }
-        auto put = [](bf16x8 &v, int i, uint32_t w) {
-            u32x4 u = __builtin_bit_cast(u32x4, v);
-            u[i] = w;
-            v = __builtin_bit_cast(bf16x8, u);
-        };
+    };
+    auto put = [](bf16x8 &v, int i, uint32_t w) {
+        u32x4 u = __builtin_bit_cast(u32x4, v);
+        u[i] = w;
+        v = __builtin_bit_cast(bf16x8, u);
+    };
+    auto cook = [&](auto maskc, auto ic, int from, int to, const Raw &x, Cooked &y) {
+        constexpr int I = decltype(ic)::value;
+        float p[2], ds[2];
+        probability(maskc, ic, from, to, x, p, ds);
         if constexpr (KEYS)
             put(y.p[I / 4], I % 4, pack_bf16(p[0], p[1]));
         put(y.ds[I / 4], I % 4, pack_bf16(ds[0], ds[1]));
+    };
+    // (as two bf16 each: y and what it leaves)
+    auto cook_both = [&](auto ic, int from, int to, const Raw &x, Cooked &y, Cooked &rest) {
+        constexpr int I = decltype(ic)::value;
+        float p[2], ds[2];
+        probability(Flag<true>{}, ic, from, to, x, p, ds);
+        auto split = [&](bf16x8 &v, bf16x8 &w, const float (&f)[2]) {
+            const uint32_t hi = pack_bf16(f[0], f[1]);
+            put(v, I % 4, hi);
+            put(w, I % 4, pack_bf16(f[0] - __uint_as_float(hi << 16),
+                                    f[1] - __uint_as_float(hi & 0xFFFF0000u)));
+        };
+        if constexpr (KEYS)
+            split(y.p[I / 4], rest.p[I / 4], p);
+        split(y.ds[I / 4], rest.ds[I / 4], ds);
     };
     // D = 128 (one code for every tile, or the accumulators' registers run out): the mask
     // is what a tile's scores start from, 0 or -infinity.
@@ -349,19 +370,20 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         });
     };
 
+    if (KEYS && tid == 0)
+        *reinterpret_cast<u32x4 *>(zeros) = u32x4{0u, 0u, 0u, 0u};
+    if (l0 < l1 && few) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    }
     if constexpr (!KEYS) {
         if (few && tiles > 0) {
             float d = 0.0f;
-            aim(0);
-            for (int at = 0; at < tiles * BT; at += BT) {
-                fbuf = 0;
-                fetch();
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                __syncthreads();
+            for (int j = 0; j < tiles; ++j)
                 each<SUB>([&](auto subc) {
-                    const int r0 = at + 32 * decltype(subc)::value;
+                    const int r0 = j * BT + 32 * decltype(subc)::value;
                     Raw x;
-                    first_products(subc, lds, r0, x);
+                    first_products(subc, lds + j * BUF, r0, x);
                     const int to = hi - r0 - 4 * hf;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
@@ -370,11 +392,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
                             d = __builtin_fmaf(p, x.dp[r], d);
                     }
                 });
-                __syncthreads();
-            }
             delta = halves(d);
-            if (j0 < j1)
-                fetch_first();
         }
         if (live && part == 0 && hf == 0) {
             // -lse / scale and -d as three bf16 each (a query that sees no key: so low that
@@ -395,6 +413,10 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             *reinterpret_cast<u32x4 *>(a.sums + (head * s.qrows + Q.first + t) * 4) =
                 u32x4{w[0], w[1], w[2], w[3]};
         }
+        // a query of one key: its probability is 1 for any score, dS is 0 (not what
+        // rounding leaves of it)
+        if (hi == 0)
+            lse2 = INFINITY;
     }
 
     // At the start of tile j the loads of tile j + 1 have landed (of those issued, up to tile
@@ -432,10 +454,29 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         each<PAIRS>([&](auto ic) { cook(Flag<!BIAS>{}, ic, lo - at, hi - at, cur, y); });
         second_products(Index<SUB - 1>{}, lds + cbuf, y);
     };
-    if (j0 < j1) {
+    if (few) {
+        for (int j = j0; j < j1; ++j) {
+            if (KEYS && j > j0 && (j - j0) % BUFS == 0) {
+                __syncthreads();
+                for (int i = j; i < min(j1, j + BUFS); ++i)
+                    fetch();
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+            }
+            each<SUB>([&](auto subc) {
+                const uint8_t *const buf = lds + (j - l0) % BUFS * BUF;
+                const int at = (first + (KEYS ? j % tiles : j)) * BT + 32 * decltype(subc)::value;
+                const int from = lo - at - 4 * hf, to = hi - at - 4 * hf;
+                Raw x;
+                Cooked rest;
+                first_products(subc, buf, at, x);
+                each<PAIRS>([&](auto ic) { cook_both(ic, from, to, x, y, rest); });
+                second_products(subc, buf, y);
+                second_products(subc, buf, rest);
+            });
+        }
+    } else if (j0 < j1) {
         Raw xa, xb;
-        if (KEYS && tid == 0)
-            *reinterpret_cast<u32x4 *>(zeros) = u32x4{0u, 0u, 0u, 0u};
         r0 = (first + (KEYS ? j0 % tiles : j0)) * BT;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
@@ -491,7 +532,8 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             }
     };
     if constexpr (KEYS) {
-        store(acc1, a.dk, a.lddk, a.part, a.scale);
+        // (of a single key: dS is 0, as for its queries)
+        store(acc1, a.dk, a.lddk, a.part, K.len == 1 ? 0.0f : a.scale);
         store(acc2, a.dv, a.lddv, a.part + (int64_t)parts * s.B * s.Hk * rows * D, 1.0f);
     } else {
         store(acc1, a.dq, a.lddq, a.part, a.scale);

@@ -386,3 +386,69 @@ def test_causal_over_many_heads(gpu, rows, dh):
     c = Case(torch, 25, 130, 32, dh=dh, causal=True, rows=rows, lens=lens)
     check_forward(torch, ql, c)
     check_backward(torch, ql, c)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("how", [
+    dict(B=1, T=1, H=2, Hk=1), dict(B=2, T=1, H=2, causal=True), dict(B=1, T=300, H=4, kT=1),
+    dict(B=3, T=5, H=4, Hk=2, lens=[1, 5, 1], rows="packed"),
+    dict(B=2, T=150, H=2, lens=[150, 1], rows="padded", causal=True),
+    dict(B=1, T=700, H=8, Hk=1, kT=1, lens=[690], klens=[1], rows="padded"),
+], ids=str)
+def test_one_key_has_no_gradient(gpu, how, dh):
+    """The softmax of one key is 1 for any score: dq and dk are 0, not what rounding leaves."""
+    torch, ql = gpu
+    c = Case(torch, **how, dh=dh, size=3.0)
+    _, _, g = check_backward(torch, ql, c, torch.float32)
+    for s in c.seqs:
+        n, m = s.n, s.m
+        alone = [i for i in range(n) if (i + m - n == 0 if c.how["causal"] else m == 1)]
+        assert m > 1 or alone
+        assert (host(g.q)[[s.q + i for i in alone]] == 0).all()
+        if m == 1:
+            assert (host(g.k)[s.k] == 0).all()
+            assert (host(g.v)[s.k] != 0).any()
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("T, kT, G", [(2, 2, 1), (2, 2, 2), (1, 77, 2), (5, 3, 1), (22, 22, 1),
+                                      (40, 100, 2), (64, 64, 2), (128, 128, 1), (97, 33, 1),
+                                      (128, 1, 1), (1, 128, 1), (2, 2, 4), (5, 50, 7),
+                                      (1, 20, 64)])
+def test_few_rows_precisely(gpu, T, kT, G, causal, dh):
+    """Gradients of few queries and keys, which the outputs' own type rounds but nothing else
+    does: P and dS as two bf16 each (2^-16, and the fp32 roundings before them), the scores'
+    and dP's sums of dh fp32 terms, lse and d as these leave them."""
+    torch, ql = gpu
+    c = Case(torch, 1, T, 2 * G, Hk=2, kT=kT, dh=dh, causal=causal)
+    O, lse = ql.attention_forward(c.q, c.k, c.v, *c.shape, **c.how)
+    g = ql.attention_backward(c.q, c.k, c.v, O, lse, c.dO, *c.shape, dtype=torch.float32, **c.how)
+    q, k, v, dO = (host(t).astype(np.float64) for t in (c.q, c.k, c.v, c.dO))
+    u = 2.0 ** -24
+    heads = lambda x, h: x[:, h * dh: (h + 1) * dh]
+    for hk in range(2):
+        dk, dv, ek, ev = (np.zeros((kT, dh)) for _ in range(4))
+        K, V = heads(k, hk), heads(v, hk)
+        for h in range(hk * G, (hk + 1) * G):
+            Q, W = heads(q, h), heads(dO, h)
+            S, Sa = c.scale * Q @ K.T, c.scale * abs(Q) @ abs(K).T
+            if causal:
+                S[np.arange(kT)[None, :] > np.arange(T)[:, None] + kT - T] = -np.inf
+            with np.errstate(invalid="ignore"):
+                P = np.exp(S - S.max(1, keepdims=True))
+                P = np.nan_to_num(P / P.sum(1, keepdims=True))
+            dP, dPa = W @ V.T, abs(W) @ abs(V).T
+            d, da = (P * dP).sum(1, keepdims=True), (P * dPa).sum(1, keepdims=True)
+            dS = P * (dP - d)
+            eP = 2 * (dh + 8) * u * Sa.max(1, keepdims=True) + 2.0 ** -20
+            eS = abs(dS) * (1.1 * 2.0 ** -16 + eP) + P * ((dh + 8 + kT) * u * (dPa + da) + eP * da)
+            eV = P * (1.1 * 2.0 ** -16 + eP)
+            want, bound = c.scale * dS @ K, c.scale * (eS + kT * u * abs(dS)) @ abs(K)
+            assert (abs(heads(host(g.q), h) - want) <= bound + 1e-37).all()
+            dk += c.scale * dS.T @ Q
+            ek += c.scale * (eS + 2 * G * T * u * abs(dS)).T @ abs(Q)
+            dv += P.T @ W
+            ev += (eV + 2 * G * T * u * P).T @ abs(W)
+        assert (abs(heads(host(g.k), hk) - dk) <= ek + 1e-37).all()
+        assert (abs(heads(host(g.v), hk) - dv) <= ev + 1e-37).all()
