@@ -61,7 +61,7 @@ int qlinear_rms_norm(const ql_norm *n, hipStream_t stream);
  * dx, the gradient of x and of res alike; dres: the one that arrives at h from further
  * on (NULL: 0), of dx's dtype.  dw fp32 [N] or NULL.  dx may be dy, h or dres in place
  * (same address, dtype and ld); other conventions as above.  Sums of a row in
- * fp64, of dw in fp32 in one fixed order.  Workspace with dw (per stream, as in
+ * fp64; dw in one fixed order, fp32 over some of the rows and fp64 over these sums.  Workspace with dw (per stream, as in
  * qlinear.h): at most 12 N bytes per CU.  M == 0 writes zeros to dw and nothing else. */
 typedef struct {
     const void *dy;

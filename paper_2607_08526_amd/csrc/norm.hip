@@ -375,16 +375,17 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
     }
 }
 
-// dw[c] = the sum of part[0 .. parts)[c], in one order (so that results repeat): 64 columns
-// a workgroup, every 16th part a wavefront.  768 parts of 2048 columns: 4.7 us, most of it
+// dw[c] = the sum of part[0 .. parts)[c], in fp64 and one order (so that results repeat): 64
+// columns a workgroup, every 16th part a wavefront.  (fp64 within the parts too would take
+// the registers of a row ahead: 8192 rows of 2048 46.5 us for 41.)  768 parts of 2048 columns: 4.7 us, most of it
 // the launch and the latency of 48 loads, eight in flight.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, int parts, int N,
                                                        float *dw)
 {
-    __shared__ float sums[16][64];
+    __shared__ double sums[16][64];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     const int c = (int)blockIdx.x * 64 + lane;
-    float s = 0.0f;
+    double s = 0.0;
     if (c < N) {
 #pragma unroll 8
         for (int p = wave; p < parts; p += 16)
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, int pa
 #pragma unroll
     for (int w = 1; w < 16; ++w)
         s += sums[w][lane];
-    dw[c] = s;
+    dw[c] = (float)s;
 }
 
 template <bool XB, bool HB>
