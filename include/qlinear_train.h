@@ -61,8 +61,9 @@ int qlinear_rms_norm(const ql_norm *n, hipStream_t stream);
  * dx, the gradient of x and of res alike; dres: the one that arrives at h from further
  * on (NULL: 0), of dx's dtype.  dw fp32 [N] or NULL.  dx may be dy, h or dres in place
  * (same address, dtype and ld); other conventions as above.  Sums of a row in
- * fp64; dw in one fixed order, fp32 over some of the rows and fp64 over these sums.  Workspace with dw (per stream, as in
- * qlinear.h): at most 12 N bytes per CU.  M == 0 writes zeros to dw and nothing else. */
+ * fp64; dw in one fixed order, fp32 over some of the rows and fp64 over these sums.
+ * Workspace with dw (per stream, as in qlinear.h): at most 12 N bytes per CU.  M == 0
+ * writes zeros to dw and nothing else. */
 typedef struct {
     const void *dy;
     int64_t lddy;
@@ -141,8 +142,9 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
  *     dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i
  *
  * (K_j and V_j: summed over the query heads that share them.)  The probabilities are
- * formed again from lse; P and dS enter the products rounded to bf16, sums are fp32 in
- * one fixed order.  dO: bf16, 16-byte aligned, rows of lddo (% 8 == 0, < 2^24).  dq, dk,
+ * formed again from lse; P and dS enter the products rounded to bf16 (in sums over few
+ * rows as two bf16), sums are fp32 in one fixed order.  A query that sees one key has dS =
+ * 0.  dO: bf16, 16-byte aligned, rows of lddo (% 8 == 0, < 2^24).  dq, dk,
  * dv: dtype dt, aligned and strided as O; dk and dv both or neither.  Rows as above:
  * padding rows of q (k, v) get zeros in dq (dk, dv), those of no sequence stay.  No output
  * shares elements with an input or another output (QL_ERR_INVALID; other columns of the

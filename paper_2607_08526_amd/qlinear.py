@@ -1063,7 +1063,8 @@ def attention_forward(q, k, v, B, T, H, kv_heads=None, dh=64, kT=None, causal=Fa
     """(O, lse): masked softmax attention of B sequences of up to T queries and kT
     keys (None: T).  q, k, v: bf16 (or int16 bit patterns) row views with unit column
     stride; H query heads of dh (64 or 128) channels share kv_heads key heads (None:
-    H).  causal: query i of n sees the keys up to i + m - n of m.  A sequence's rows: T
+    H).  scale: of the scores (None: 1 / sqrt(dh)).  causal: query i of n sees the keys up to
+    i + m - n of m.  A sequence's rows: T
     (kT) from b * T on, or with offsets (int64 [B + 1] on the device) those between its
     offset and the next, at most T (kT); with lens (int64 [B] on the device) only the
     first of them are live, the others padding (never read; O zero, lse -inf).  A query
@@ -1097,9 +1098,9 @@ def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=No
                        stream=None):
     """The backward pass of attention_forward (its arguments, and the O and lse it
     returned) from dO, the gradient of O (bf16): AttentionGrads, k's and v's None without
-    kv_grads.  dq [rows of q][>= H * dh], dk and dv (both or neither) [rows of k][>= kv_heads
-    * dh]: row views of one dtype (fp32 or bf16; dtype where they are made here), e.g. the columns of a
-    fused QKV output's gradient.  Padding rows get zeros, rows of no sequence are not
+    kv_grads.  dq [rows of q][>= H * dh], dk and dv (both or neither) [rows of
+    k][>= kv_heads * dh]: row views of one dtype (fp32 or bf16; dtype where they are made
+    here), e.g. the columns of a fused QKV output's gradient.  Padding rows get zeros, rows of no sequence are not
     written (zeros in outputs made here).  Asynchronous."""
     a, tensors, qrows, krows = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
                                      k_offsets, q_lens, k_lens)
