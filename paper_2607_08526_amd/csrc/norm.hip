@@ -325,7 +325,12 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
         }
         const double rstd = inverse_sqrt(__builtin_fma(s, a.inv_n, a.eps));
         const double mean = p * rstd * a.inv_n;  // of g u
-        const float r32 = (float)rstd, k32 = (float)(mean * rstd);
+        // rstd = r 2^e, so that u = v rstd is of size 1 where rstd itself leaves fp32 (rows of
+        // subnormals, of the largest numbers): scaling by 2^e is exact, the other roundings
+        // are those of products with an fp32 rstd
+        const int e = __builtin_amdgcn_frexp_exp(rstd);
+        const double r64 = __builtin_amdgcn_frexp_mant(rstd);
+        const float r32 = (float)r64, k32 = (float)(mean * r64);
         const bool there = columns(m) > 0;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -335,8 +340,9 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
                 rs[k][i].load(a.dres, m * a.ldres + c, N - c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float u = v[i][j] * r32, g = a.weight ? dy[i][j] * w[i][j] : dy[i][j];
-                const float o = __builtin_fmaf(g, r32, -u * k32);
+                const float u = __builtin_ldexpf(v[i][j], e) * r32;
+                const float g = a.weight ? dy[i][j] * w[i][j] : dy[i][j];
+                const float o = __builtin_ldexpf(__builtin_fmaf(g, r32, -u * k32), e);
                 out[j] = a.dres ? d[i][j] + o : o;
                 dw[i][j] = there ? __builtin_fmaf(dy[i][j], u, dw[i][j]) : dw[i][j];
             }
