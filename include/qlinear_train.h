@@ -29,8 +29,9 @@ extern "C" {
  * qlinear_quantize_act gives them for the fp32 y (N % 32 == 0, qx 16-byte aligned).
  * h, y, and qx with sx may each be NULL, not all.  h or y may be x or res in place
  * (same address, dtype and ld); no output shares elements with another argument
- * otherwise (QL_ERR_INVALID; other columns of the same rows may be).  eps >= 0.
- * N <= 16384, M < 2^24 (QL_ERR_UNSUPPORTED).  Asynchronous; M == 0 is a no-op. */
+ * otherwise (QL_ERR_INVALID; other columns of the same rows may be).  eps >= 0; a row of
+ * zeros has y = 0, also with eps = 0.  N <= 16384, M < 2^24 (QL_ERR_UNSUPPORTED).
+ * Asynchronous; M == 0 is a no-op. */
 typedef struct {
     const void *x;
     int64_t ldx;
@@ -58,6 +59,7 @@ int qlinear_rms_norm(const ql_norm *n, hipStream_t stream);
  *     dx = dres + r (g - u mean(g u)),  dw = sum over rows of dy u,
  *          r = 1 / sqrt(mean(h^2) + eps),  u = h r,  g = dy weight
  *
+ * (r = 0 for a row of zeros with eps = 0: dx = dres, and nothing for dw.)
  * dx, the gradient of x and of res alike; dres: the one that arrives at h from further
  * on (NULL: 0), of dx's dtype.  dw fp32 [N] or NULL.  dx may be dy, h or dres in place
  * (same address, dtype and ld); other conventions as above.  Sums of a row in

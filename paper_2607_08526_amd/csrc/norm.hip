@@ -114,9 +114,12 @@ __device__ inline double wave_sum(double s)
 }
 
 // 1 / sqrt(x) for x >= 0: the hardware's estimate (2^-26 or better) and two Newton steps;
-// 0, infinities and NaN as the estimate has them
+// infinities and NaN as the estimate has them.  0 for 0, a row of zeros and eps = 0: it has no
+// direction u, and 0 as such (not 0 * infinity) keeps it out of the others' dw.
 __device__ inline double inverse_sqrt(double x)
 {
+    if (x == 0.0)
+        return 0.0;
     double r = __builtin_amdgcn_rsq(x);
     if (x > 0.0 && x < __builtin_inf()) {
 #pragma unroll
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(THREADS<W>) void norm_kernel(const NormArgs a)
         return;
 
     // act_quant's scale and codes of the row (|y| bit patterns compare like the
-    // values; columns past the row's end are 0, or NaN where rstd is infinite: out)
+    // values; columns past the row's end are 0, or NaN where rstd is: out)
     uint32_t amax = 0;
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -331,7 +334,6 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
         const int e = __builtin_amdgcn_frexp_exp(rstd);
         const double r64 = __builtin_amdgcn_frexp_mant(rstd);
         const float r32 = (float)r64, k32 = (float)(mean * r64);
-        const bool there = columns(m) > 0;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int c = 8 * (t + i * T);
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
                 const float g = a.weight ? dy[i][j] * w[i][j] : dy[i][j];
                 const float o = __builtin_ldexpf(__builtin_fmaf(g, r32, -u * k32), e);
                 out[j] = a.dres ? d[i][j] + o : o;
-                dw[i][j] = there ? __builtin_fmaf(dy[i][j], u, dw[i][j]) : dw[i][j];
+                dw[i][j] = __builtin_fmaf(dy[i][j], u, dw[i][j]);
             }
             store8(a.dx, DB, m * a.lddx + c, columns(m) - c, out);
         }

@@ -979,8 +979,8 @@ def rms_norm(x, weight=None, eps=1e-6, residual=None, h=None, y=None, ydtype=tor
     residual, h and y: fp32 or bf16 row views [M][N] with unit column stride (y of
     ydtype where it is made here, h of residual's dtype; None without residual unless it
     is given); weight fp32 [N] or None.  y is formed from the fp32 sum, before its
-    rounding to h's dtype.  h or y may be x or residual itself.  N <= 16384.
-    Asynchronous."""
+    rounding to h's dtype (0 for a row of zeros, also with eps = 0).  h or y may be x or
+    residual itself.  N <= 16384.  Asynchronous."""
     return _norm(x, weight, eps, residual, h, y, ydtype, None, stream)
 
 
@@ -996,8 +996,8 @@ def rms_norm_backward(dy, h, weight=None, eps=1e-6, dres=None, dx=None, dtype=to
     """(dx, dw): the backward pass of rms_norm from dy, the gradient of y, and h as it
     was kept.  dx, the gradient of x and of residual alike: with dres, the gradient that
     arrives at h from further on, added (of dx's dtype; dtype where dx is made here);
-    dx may be dy, h or dres itself.  dw fp32 [N], None without weight_grad.
-    Asynchronous."""
+    dx may be dy, h or dres itself.  dw fp32 [N], None without weight_grad.  A row of
+    zeros with eps = 0 gives dx = dres and nothing to dw.  Asynchronous."""
     if not isinstance(h, torch.Tensor) or h.dim() != 2:
         raise ValueError("h must be a 2-D tensor [M][N]")
     M, N = h.shape
