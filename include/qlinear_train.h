@@ -111,9 +111,10 @@ int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream);
  * q, k, v: bf16, 16-byte aligned, rows of ldq, ldk, ldv elements (% 8 == 0, < 2^24).  O:
  * fp32 (16-byte aligned) or bf16 (8-byte), rows of ldo (% 4 == 0).  scale: 0 (taken as
  * 1e-30) or 1e-30 to 2.3e38; scores times log2(e) that leave fp32's range give NaN.  The
- * probabilities enter the product with V rounded to bf16, sums are fp32.  A value that is
- * not finite in a row which only the causal mask hides may reach queries of the same
- * tile (0 * infinity).  Sizes: B * H * Tq, B * Hk * Tk < 2^31, Tk <= 2^30, B * Hk *
+ * probabilities enter the product with V rounded to bf16, sums are fp32.  Values that are not
+ * finite keep to what they are part of, but not under a causal mask alone: there a key
+ * may reach queries up to 255 before those that see it, and in the backward pass a query
+ * the gradients of keys up to 255 behind those it sees (0 * infinity).  Sizes: B * H * Tq, B * Hk * Tk < 2^31, Tk <= 2^30, B * Hk *
  * ceil(Tq * H / Hk / 32) < 2^24 (QL_ERR_UNSUPPORTED). */
 typedef struct {
     const uint16_t *q;

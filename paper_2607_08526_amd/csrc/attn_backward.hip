@@ -294,18 +294,18 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     // start with -lse / scale and -d of the streamed queries, three bf16 each that add up
     // to 24 bits: as products with ones, two matrix instructions and LDS reads a block, where
     // reading them in the accumulators' layout, 16 values a lane each, takes eight reads and
-    // 32 registers), then the second products of the tile in prev.
+    // 32 registers; each with zeros beside it, not the other: a d that is not finite must not
+    // reach P), then the second products of the tile in prev.
     constexpr int SUMS = KEYS ? 2 : 0, FIRST = SUMS + 2 * DS, SECOND = (KEYS ? 4 : 2) * DT;
     const uint32_t one = hf == 0 ? 0x3F80u : 0u, ones = one | one << 16;
-    const bf16x8 ones_lse = __builtin_bit_cast(bf16x8, u32x4{ones, one, 0u, 0u});
-    const bf16x8 ones_d = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, ones, one});
+    const bf16x8 ones3 = __builtin_bit_cast(bf16x8, u32x4{ones, one, 0u, 0u});
     // (block NS of the tile in next, block PS of that in prev)
     auto operand = [&](auto ic, auto nsc, auto psc, const uint8_t *next, const uint8_t *prev) {
         constexpr int I = decltype(ic)::value, NS = decltype(nsc)::value, PS = decltype(psc)::value;
         if constexpr (I < SUMS) {
-            return __builtin_bit_cast(
-                bf16x8, *reinterpret_cast<const u32x4 *>(
-                            hf ? zeros : next + 2 * TILE + 512 * NS + l32 * 16));
+            const u32x2 x = *reinterpret_cast<const u32x2 *>(
+                hf ? zeros : next + 2 * TILE + 512 * NS + l32 * 16 + 8 * I);
+            return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], 0u, 0u});
         } else if constexpr (I < FIRST) {
             return row_operand<D>(next + (I % 2) * TILE, 32 * NS + l32, (I - SUMS) / 2, hf);
         } else {
@@ -319,10 +319,10 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             const f32x16 zero = {};
             constexpr int i = (I - SUMS) / 2;
             if constexpr (I % 2 == 0)
-                x.s = mfma(w, I < SUMS ? ones_lse : x1[I < SUMS ? 0 : i],
+                x.s = mfma(w, I < SUMS ? ones3 : x1[I < SUMS ? 0 : i],
                            I == 0 && !BIAS ? zero : x.s);
             else
-                x.dp = mfma(w, I < SUMS ? ones_d : x2[I < SUMS ? 0 : i], I == 1 ? zero : x.dp);
+                x.dp = mfma(w, I < SUMS ? ones3 : x2[I < SUMS ? 0 : i], I == 1 ? zero : x.dp);
         } else {
             constexpr int k = I - FIRST, m = KEYS ? k / 2 : k;
             if constexpr (KEYS && k % 2)
