@@ -146,8 +146,13 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
  *
  * (K_j and V_j: summed over the query heads that share them.)  The probabilities are
  * formed again from lse; P and dS enter the products rounded to bf16 (in sums over few
- * rows as two bf16), sums are fp32 in one fixed order.  A query that sees one key has dS =
- * 0.  dO: bf16, 16-byte aligned, rows of lddo (% 8 == 0, < 2^24).  dq, dk,
+ * rows as two bf16), sums are fp32 in one fixed order.  <dO, O> is as exact as the O that
+ * was kept (over up to 128 keys it is formed anew): where a row's probability is that of a
+ * few keys, dS is much smaller than its terms and a bf16 O is most of its error.  Errors
+ * of dq and dk relative to their norm, of bf16 gradients: scores of a spread of 1, 4, 10
+ * and 30 up to 0.0025, 0.0038, 0.0059 and 0.0075 with a bf16 O, 0.0025, 0.0030, 0.0034 and
+ * 0.0034 with an fp32 O (the gradients' own rounding: 0.0017).  dq of a query that sees
+ * one key, and dk of a sequence's only key, are 0.  dO: bf16, 16-byte aligned, rows of lddo (% 8 == 0, < 2^24).  dq, dk,
  * dv: dtype dt, aligned and strided as O; dk and dv both or neither.  Rows as above:
  * padding rows of q (k, v) get zeros in dq (dk, dv), those of no sequence stay.  No output
  * shares elements with an input or another output (QL_ERR_INVALID; other columns of the

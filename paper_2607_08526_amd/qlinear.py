@@ -1070,7 +1070,8 @@ def attention_forward(q, k, v, B, T, H, kv_heads=None, dh=64, kT=None, causal=Fa
     first of them are live, the others padding (never read; O zero, lse -inf).  A query
     that sees no key gives zeros and -inf too.  Rows of no sequence are not written (in
     outputs made here: zeros and -inf).  O: row view [rows of q][>= H * dh], bf16 or
-    fp32 (odtype where it is made here); lse: fp32 [H][rows of q], the logarithms of the
+    fp32 (odtype where it is made here; the probabilities are rounded to bf16 before the
+    product with v either way); lse: fp32 [H][rows of q], the logarithms of the
     row sums that attention_backward takes (None without with_lse).  Asynchronous."""
     a, tensors, rows, _ = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
                                 k_offsets, q_lens, k_lens)
@@ -1100,8 +1101,12 @@ def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=No
     returned) from dO, the gradient of O (bf16): AttentionGrads, k's and v's None without
     kv_grads.  dq [rows of q][>= H * dh], dk and dv (both or neither) [rows of
     k][>= kv_heads * dh]: row views of one dtype (fp32 or bf16; dtype where they are made
-    here), e.g. the columns of a fused QKV output's gradient.  Padding rows get zeros, rows of no sequence are not
-    written (zeros in outputs made here).  Asynchronous."""
+    here), e.g. the columns of a fused QKV output's gradient.  Padding rows get zeros,
+    rows of no sequence are not written (zeros in outputs made here).  dq, dk and dv made
+    here may be views of one allocation, which any of them keeps alive.  Where a row's
+    probability is that of a few keys (scores of a spread of 4 and more), an O kept in
+    fp32 (attention_forward's odtype) makes dq and dk up to twice as exact as one in
+    bf16.  Asynchronous."""
     a, tensors, qrows, krows = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
                                      k_offsets, q_lens, k_lens)
     wide, narrow = H * dh, a.Hk * dh
