@@ -166,9 +166,6 @@ __device__ inline void both_halves(float x, float &lo, float &hi)
     hi = __uint_as_float(r[1]);
 }
 
-// Accumulators that stay in the accumulation registers
-__device__ inline void in_agprs(f32x16 &v) { asm volatile("" : "+a"(v)); }
-
 // The order of instructions stays as written across this point.
 __device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 

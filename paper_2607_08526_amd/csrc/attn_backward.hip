@@ -20,13 +20,13 @@
 // i's second products follow.
 //
 // What is rounded to bf16, and why: P and dS, as the matrix instructions take them (fp32
-// would take 16 times as long; two bf16 each, as for few rows, 11 products for 7); d is as
+// would take 16 times as long; two bf16 each, as for few rows, 10 products for 7); d is as
 // exact as the caller's O.  Off by a row's d error times sum P K, dq has 0.0024 of its norm for
 // scores of a spread of 1 and either O; at a spread of 10 a bf16 O makes it 0.0059, an fp32
 // one 0.0034.  d could be made exact from this kernel's own sums (the rest that a row's
 // dS leave, 0 in exact arithmetic), but dq's correction takes sum P K: a fourth product
-// and D x 32 more accumulators, or a second pass over the keys, a quarter of dq's time or
-// more for every caller, where an fp32 O costs its bytes.
+// beside three and D x 32 more accumulators, or a second pass over the keys, for every
+// caller, where an fp32 O costs its bytes.
 //
 // What bounds it, measured in us, dq / dk and dv: 4096 queries and keys of 32 heads of 64
 // 215 / 270, of 16 heads of 128 199 / 285: 960 to 1040 TFLOP/s of dq's three products and

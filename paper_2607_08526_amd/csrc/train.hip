@@ -284,9 +284,9 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
     t.ldo = ldo;
     t.obf16 = odt == QL_DT_BF16;
     t.lse = lse;
+    // (no more workgroups than MAX_WORKGROUPS: check_attn bounds those of 32 rows, the fewest
+    // of any form, and forms in parts have few)
     const SeqAttnPlan plan = seq_attn_plan(t.s);
-    if (seq_attn_workgroups(t.s, plan) > MAX_WORKGROUPS)
-        return QL_ERR_UNSUPPORTED;
     t.splits = plan.splits;
     uint8_t *ws = nullptr;
     bool own = false;
