@@ -114,8 +114,9 @@ int qlinear_rms_norm_backward(const ql_norm_grad *g, hipStream_t stream);
  * probabilities enter the product with V rounded to bf16, sums are fp32.  Values that are not
  * finite keep to what they are part of, but not under a causal mask alone: there a key
  * may reach queries up to 255 before those that see it, and in the backward pass a query
- * the gradients of keys up to 255 behind those it sees (0 * infinity).  Sizes: B * H * Tq, B * Hk * Tk < 2^31, Tk <= 2^30, B * Hk *
- * ceil(Tq * H / Hk / 32) < 2^24 (QL_ERR_UNSUPPORTED). */
+ * the gradients of keys up to 255 behind those it sees (0 * infinity).  Sizes: B * H * Tq,
+ * B * Hk * Tk < 2^31, Tk <= 2^30, B * Hk * ceil(Tq * H / Hk / 32) < 2^24, in the backward
+ * pass B * Hk * ceil(Tk / 128) < 2^24 too (QL_ERR_UNSUPPORTED). */
 typedef struct {
     const uint16_t *q;
     int64_t ldq;
@@ -152,9 +153,9 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
  * of dq and dk relative to their norm, of bf16 gradients: scores of a spread of 1, 4, 10
  * and 30 up to 0.0025, 0.0038, 0.0059 and 0.0075 with a bf16 O, 0.0025, 0.0030, 0.0034 and
  * 0.0034 with an fp32 O (the gradients' own rounding: 0.0017).  dq of a query that sees
- * one key, and dk of a sequence's only key, are 0.  dO: bf16, 16-byte aligned, rows of lddo (% 8 == 0, < 2^24).  dq, dk,
- * dv: dtype dt, aligned and strided as O; dk and dv both or neither.  Rows as above:
- * padding rows of q (k, v) get zeros in dq (dk, dv), those of no sequence stay.  No output
+ * one key, and dk of a sequence's only key, are 0.  dO: bf16, 16-byte aligned, rows of
+ * lddo (% 8 == 0, < 2^24).  dq, dk, dv: dtype dt, aligned and strided as O; dk and dv both
+ * or neither.  Rows as above: padding rows of q (k, v) get zeros in dq (dk, dv), those of no sequence stay.  No output
  * shares elements with an input or another output (QL_ERR_INVALID; other columns of the
  * same rows may be: the gradients may be those of a fused QKV output).  Workspace (per
  * stream, as in qlinear.h): 16 H q_rows bytes, and fp32 partial sums where few rows leave

@@ -57,8 +57,9 @@ constexpr int KEEP = 128;  // kept rows of a workgroup
 // rounding averages out in longer ones: P and dS enter the products as two bf16, 16 bits of
 // them, and d_i is formed as sum P_ij dP_ij in a pass of its own, not from a bf16 O.  Tiles
 // are loaded a ring at a time and nothing overlaps (107 queries and keys of 48 heads of 64: dk
-// and dv in 10.1 us, 8.2 with P and dS as one bf16 each and overlapped; dq 10.3 and 10.7).  (dq at 2 to 3 keys was off by 0.0027 to 0.0030 of its norm, where
-// the output's own rounding is 0.0017.)
+// and dv in 10.1 us, 8.2 with P and dS as one bf16 each and overlapped; dq 10.3 and 10.7).
+// (With one bf16 each, dq at 2 to 3 keys was off by 0.0027 to 0.0030 of its norm, where the
+// output's own rounding is 0.0017.)
 constexpr int FEW = 128;
 
 template <int D, bool KEYS, int BT, int BUFS>
@@ -575,7 +576,8 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
     for (int p = 1; p < parts; ++p)
         v += *reinterpret_cast<const f32x4_t *>(part + p * all * D);
     void *const out = !KEYS ? a.dq : blockIdx.y ? a.dv : a.dk;
-    const int64_t o = (R.first + t) * (!KEYS ? a.lddq : blockIdx.y ? a.lddv : a.lddk) + head * D + ch;
+    const int64_t ld = !KEYS ? a.lddq : blockIdx.y ? a.lddv : a.lddk;
+    const int64_t o = (R.first + t) * ld + head * D + ch;
     if (a.bf16)
         *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(out) + o) =
             u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
@@ -584,7 +586,9 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
 }
 
 // Rows of a streamed tile: 64, half the barriers and waits of 32, where the LDS holds them
-// (two workgroups on a CU but for D = 128 and kept keys).
+// (two workgroups on a CU but for D = 128 and kept keys).  Registers: 220 and 230 (dq, dk and
+// dv) of 256 for D = 64; for D = 128 dq takes all 256, with 14 values spilled outside of the
+// loop over tiles, and kept keys 361 of the 512 that a workgroup alone on its CU has.
 constexpr int tile_rows(int D, bool keys) { return D == 64 || keys ? 64 : 32; }
 constexpr int on_a_cu(int D, bool keys) { return D == 64 || !keys ? 2 : 1; }
 
@@ -662,7 +666,8 @@ SeqAttnGradPlan seq_attn_grad_plan(const SeqAttn &s, bool keys)
     constexpr int64_t MOST = 1024;  // workgroups of a launch in parts: they bound the workspace
     auto choose = [&](bool k) {
         const int64_t w = blocks(s, k);
-        const int64_t tiles = k ? ((int64_t)s.T + 63) / 64 * (s.H / s.Hk) : ((int64_t)s.KT + 63) / 64;
+        const int64_t tiles =
+            k ? ((int64_t)s.T + 63) / 64 * (s.H / s.Hk) : ((int64_t)s.KT + 63) / 64;
         int best = 1;
         double us = 0.0;
         for (const int p : PARTS) {

@@ -32,9 +32,11 @@
 // of wavefronts take as long; two parts of the keys 59 and 17 for the join).  One token of 8
 // sequences over up to 8192 keys: 47, 4.4 TB/s, by HBM.
 //
-// Two workgroups a CU, 256 registers a lane: with three the compiler spills (D = 64, tiles of
-// 32 keys: 350 us for 170).  Tiles of 64 keys for D = 64; 32 for D = 128 (64, with one
-// workgroup a CU: 68 for 60).  Plain stores: non-temporal ones took as long.
+// Two workgroups a CU, 256 registers a lane, all of them taken (10 values spilled for D = 64,
+// 7 and 3 for D = 128 in one and two groups, outside of the loop over tiles): with three
+// workgroups the compiler spills within it (D = 64, tiles of 32 keys: 350 us for 170).  Tiles
+// of 64 keys for D = 64; 32 for D = 128 (64, with one workgroup a CU: 68 for 60).  Plain
+// stores: non-temporal ones took as long.
 #include <algorithm>
 #include <cmath>
 
@@ -537,7 +539,8 @@ double form_us(const SeqAttn &s, int groups, int splits)
     const double a2 = us * us, b2 = bytes_us * bytes_us;
     us = c.start + std::sqrt(std::sqrt(a2 * a2 + b2 * b2));
     if (splits > 1)
-        us += JOIN_US + JOIN_PART_US * splits + splits * units * rows * (s.dh + 2) * 4.0 / JOIN_RATE;
+        us += JOIN_US + JOIN_PART_US * splits +
+              splits * units * rows * (s.dh + 2) * 4.0 / JOIN_RATE;
     return us;
 }
 
@@ -549,6 +552,7 @@ double form_us(const SeqAttn &s, int groups, int splits)
 // 215 x 215, 3 of 8 of 128, 4 query heads each 12.3 / 13.1 / -, in 2 parts 26.3 / 28.5 / -.
 SeqAttnPlan seq_attn_plan(const SeqAttn &s)
 {
+    // (96: as far as the sweeps went; one sequence with one key head stays below the CUs)
     constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96};
     constexpr int64_t MOST = 1024;  // workgroups of a split launch: they bound the workspace
     const int64_t rows = (int64_t)s.T * (s.H / s.Hk), tiles = ((int64_t)s.KT + 63) / 64;

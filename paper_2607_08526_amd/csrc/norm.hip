@@ -14,11 +14,13 @@
 // Bound: HBM; at few rows the latency of one load and of the row's reduction.  A
 // row's values stay in registers between the sum and the output (W wavefronts of
 // R groups of 8 columns per lane), so each is read once.  Measured, us:
-//   forward, 2048 rows of 2048, fp32 x, r and h, bf16 y (59 MB): 12.2, 4.8 TB/s (a copy of
-//   4 GiB: 4.4 to 5.1); 1290 rows of 1536, bf16 x, fp32 r and h, int8 y (22 MB): 9.6, a
-//   row's two reductions and its latency; one row: 2.5, a launch
-//   backward, 8192 rows of 2048, bf16 dy, fp32 h, dres and dx (235 MB): 41 and 4.7 for the
-//   sum of dw, 5.1 TB/s; 107 rows of 1024: 4.3 and 3.4, two launches
+//   forward, fp32 x, r and h, bf16 y, every call on other rows than the last ones: 8192 rows
+//   of 2048 (235 MB) 45, 5.2 TB/s (a copy of 4 GiB: 4.4 to 5.1); 2048 rows 15.2, 3.9 TB/s, and
+//   12.2 where three sets of them in turn are partly in the last-level cache; 1290 rows of
+//   1536, bf16 x, int8 y (22 MB): 9.6, a row's two reductions and its latency; one row:
+//   2.5, a launch
+//   backward, 8192 rows of 2048, bf16 dy, fp32 h, dres and dx (235 MB): 41 to 44 and 4.7 for
+//   the sum of dw, 5.1 TB/s; 107 rows of 1024: 4.3 and 3.4, two launches
 #include "codes.h"
 #include "internal.h"
 
@@ -385,8 +387,8 @@ __global__ __launch_bounds__(THREADS<W>) void norm_grad_kernel(const NormGradArg
 
 // dw[c] = the sum of part[0 .. parts)[c], in fp64 and one order (so that results repeat): 64
 // columns a workgroup, every 16th part a wavefront.  (fp64 within the parts too would take
-// the registers of a row ahead: 8192 rows of 2048 46.5 us for 41.)  768 parts of 2048 columns: 4.7 us, most of it
-// the launch and the latency of 48 loads, eight in flight.
+// the registers of a row ahead: 8192 rows of 2048 46.5 us for 41.)  768 parts of 2048
+// columns: 4.7 us, most of it the launch and the latency of 48 loads, eight in flight.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, int parts, int N,
                                                        float *dw)
 {
@@ -409,6 +411,14 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, int pa
     dw[c] = (float)s;
 }
 
+// Wavefronts and groups of 8 columns a lane by the columns (us from HBM, forward of fp32 rows
+// with bf16 y / backward of bf16 dy with dw):
+//   2048 rows of 4096: 4 and 2 28.2 / 33.5, 8 and 1 26.3 / 34.9
+//   2048 rows of 8192: 8 and 2 48.3 / 60.5, 16 and 1 47.7 / 92.5, 4 and 4 51.4 / 70.7
+//   1024 rows of 16384: 16 and 2 52.3 / 202, 8 and 4 53.2 / 85.8
+// (Backward, 16 wavefronts leave 128 registers a lane, and values are spilled.)  The backward
+// pass of more than 8192 columns holds no row ahead and loads weights and dres in every
+// row: 2.7 TB/s; up to 8192 columns 3.5 to 4.7.
 template <bool XB, bool HB>
 void forward(const NormArgs &a, hipStream_t s)
 {

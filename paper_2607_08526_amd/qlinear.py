@@ -687,7 +687,9 @@ def attention(q, k, v, B, T, H, dh=64, scale=None, O=None, odtype=torch.float32,
     """Softmax self-attention over each sequence's T keys.  q, k, v: bf16 (or
     int16 bit patterns) 2-D row views [B*T][>= H*dh] with unit column stride
     (e.g. column slices of a fused QKV output).  Returns O [B*T][H*dh] fp32
-    or bf16.  Asynchronous."""
+    or bf16.  dh = 64; for masks, sequences of unlike lengths, shared key heads, heads
+    of 128, gradients, or more than about 1000 tokens: attention_forward.
+    Asynchronous."""
     for name, t in (("q", q), ("k", k), ("v", v)):
         _require(t, name, _BF16_BITS, min_cols=H * dh)
         if t.shape[0] != B * T:
@@ -1063,16 +1065,20 @@ def attention_forward(q, k, v, B, T, H, kv_heads=None, dh=64, kT=None, causal=Fa
     """(O, lse): masked softmax attention of B sequences of up to T queries and kT
     keys (None: T).  q, k, v: bf16 (or int16 bit patterns) row views with unit column
     stride; H query heads of dh (64 or 128) channels share kv_heads key heads (None:
-    H).  scale: of the scores (None: 1 / sqrt(dh)).  causal: query i of n sees the keys up to
-    i + m - n of m.  A sequence's rows: T
-    (kT) from b * T on, or with offsets (int64 [B + 1] on the device) those between its
-    offset and the next, at most T (kT); with lens (int64 [B] on the device) only the
-    first of them are live, the others padding (never read; O zero, lse -inf).  A query
+    H).  scale: of the scores (None: 1 / sqrt(dh)).  causal: query i of n sees the keys
+    up to i + m - n of m.  A sequence's rows: T (kT) from b * T on, or with offsets (int64
+    [B + 1] on the device) those between its offset and the next, at most T (kT); with
+    lens (int64 [B] on the device) only the first of them are live, the others padding
+    (never read; O zero, lse -inf).  A query
     that sees no key gives zeros and -inf too.  Rows of no sequence are not written (in
     outputs made here: zeros and -inf).  O: row view [rows of q][>= H * dh], bf16 or
     fp32 (odtype where it is made here; the probabilities are rounded to bf16 before the
     product with v either way); lse: fp32 [H][rows of q], the logarithms of the
-    row sums that attention_backward takes (None without with_lse).  Asynchronous."""
+    row sums that attention_backward takes (None without with_lse).  Asynchronous.
+
+    Of unmasked sequences of one length with heads of 64, attention is the faster up to
+    about 1000 tokens (fewer host steps, and 20 us for 21 on the device at 2 x 645 tokens,
+    24 heads), this beyond (174 us for 182 at 4096 tokens, 32 heads)."""
     a, tensors, rows, _ = _attn(q, k, v, B, T, H, kv_heads, dh, kT, causal, scale, q_offsets,
                                 k_offsets, q_lens, k_lens)
     loose = q_offsets is not None or rows != B * T  # rows that may be of no sequence
@@ -1102,7 +1108,8 @@ def attention_backward(q, k, v, O, lse, dO, B, T, H, kv_heads=None, dh=64, kT=No
     kv_grads.  dq [rows of q][>= H * dh], dk and dv (both or neither) [rows of
     k][>= kv_heads * dh]: row views of one dtype (fp32 or bf16; dtype where they are made
     here), e.g. the columns of a fused QKV output's gradient.  Padding rows get zeros,
-    rows of no sequence are not written (zeros in outputs made here).  dq, dk and dv made
+    rows of no sequence are not written (zeros in outputs made here).  Probabilities and
+    dS are rounded to bf16 before their products.  dq, dk and dv made
     here may be views of one allocation, which any of them keeps alive.  Where a row's
     probability is that of a few keys (scores of a spread of 4 and more), an O kept in
     fp32 (attention_forward's odtype) makes dq and dk up to twice as exact as one in

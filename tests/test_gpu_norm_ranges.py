@@ -45,8 +45,8 @@ def test_backward_of_any_size(gpu, N, size):
     for hd in (torch.float32, torch.bfloat16):
         if hd == torch.bfloat16 and size < -130:  # (below its smallest steps)
             continue
-        h, hv = put(torch, rng.uniform(1.0, 4.0, (M, N)) * rng.choice([-1, 1], (M, N)) * 2.0 ** size,
-                    hd)
+        x = rng.uniform(1.0, 4.0, (M, N)) * rng.choice([-1, 1], (M, N))
+        h, hv = put(torch, x * 2.0 ** size, hd)
         w, wv = put(torch, 1 + 0.3 * rng.standard_normal(N))
         dy, dyv = put(torch, rng.standard_normal((M, N)))
         _, dw = ql.rms_norm_backward(dy, h, w, 0.0)

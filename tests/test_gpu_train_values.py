@@ -63,12 +63,13 @@ def test_values_keep_to_their_rows(gpu, lens, klens, bad, dh):
             hit = [1] if keys else [2, 3]
             clean = [h for h in range(Hk if keys else H) if h not in hit]
             for h in clean:
-                assert same(torch, x, want[name], here, slice(h * width, (h + 1) * width)), (n, name)
+                cols = slice(h * width, (h + 1) * width)
+                assert same(torch, x, want[name], here, cols), (n, name)
             for h in hit:
                 cols = slice(h * width, (h + 1) * width)
                 if query and not keys:  # the query's own row alone, of its own head
                     for r in [i for i in range(first, first + n_rows) if i != row or h != head]:
-                        assert same(torch, x, want[name], slice(r, r + 1), cols), (n, name, r - first)
+                        assert same(torch, x, want[name], slice(r, r + 1), cols), (n, name, r)
                     touched = x[row: row + 1, cols] if h == head else None
                     if n == "dO" and name in ("O", "lse"):
                         touched = None
@@ -117,14 +118,15 @@ def test_reach_of_what_the_causal_mask_hides(gpu, shift, bad, dh):
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("causal", [False, True])
-@pytest.mark.parametrize("how", [dict(lens=[200, 50, 131]), dict(lens=[130, 1, 64], klens=[9, 700, 64])],
-                         ids=str)
+@pytest.mark.parametrize("how", [dict(lens=[200, 50, 131]),
+                                 dict(lens=[130, 1, 64], klens=[9, 700, 64])], ids=str)
 def test_sequences_alone(gpu, how, causal, dh):
     """Each sequence of a packed batch as it is on its own (its parts of the keys may be
     others: each is off by its bound)."""
     torch, ql = gpu
     lens, klens = how["lens"], how.get("klens", how["lens"])
-    c = Case(torch, 3, max(lens), 4, Hk=2, dh=dh, kT=max(klens), rows="packed", causal=causal, **how)
+    c = Case(torch, 3, max(lens), 4, Hk=2, dh=dh, kT=max(klens), rows="packed", causal=causal,
+             **how)
     got, bounds = both(ql, c), c.want(grads=True)
     for s in c.seqs:
         q, k = slice(s.q, s.q + s.n), slice(s.k, s.k + s.m)
@@ -150,7 +152,8 @@ def clamped(offsets, lens, rows, T):
 
 
 BAD = [([0, 10 ** 12, -5, 2], None), ([150, 0, 150, 150], None), ([-7, -3, -1, -1], None),
-       ([40, 90, 60, 100], [10 ** 15, -1, 7]), ([0, 30, 30, 5 * 10 ** 18], [-(10 ** 18), 3, 10 ** 9])]
+       ([40, 90, 60, 100], [10 ** 15, -1, 7]),
+       ([0, 30, 30, 5 * 10 ** 18], [-(10 ** 18), 3, 10 ** 9])]
 
 
 @pytest.mark.parametrize("dh", [64, 128])
