@@ -147,7 +147,7 @@ int qlinear_attention_forward(const ql_attn *a, void *o, int64_t ldo, int odt, f
  *
  * (K_j and V_j: summed over the query heads that share them.)  The probabilities are
  * formed again from lse; P and dS enter the products rounded to bf16 (in sums over few
- * rows as two bf16), sums are fp32 in one fixed order.  <dO, O> is as exact as the O that
+ * rows, and for outputs of few, as two bf16), sums are fp32 in one fixed order.  <dO, O> is as exact as the O that
  * was kept (over up to 128 keys it is formed anew): where a row's probability is that of a
  * few keys, dS is much smaller than its terms and a bf16 O is most of its error.  Errors
  * of dq and dk relative to their norm, of bf16 gradients: scores of a spread of 1, 4, 10

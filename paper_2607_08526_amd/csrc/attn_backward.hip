@@ -62,9 +62,17 @@ constexpr int KEEP = 128;  // kept rows of a workgroup
 // output's own rounding is 0.0017.)
 constexpr int FEW = 128;
 
-template <int D, bool KEYS, int BT, int BUFS>
+// The same where the outputs have few rows, of all sequences and heads together (TWO): their
+// roundings do not average out over the output either (dq of one query over 479 keys, 4
+// heads of 4 sequences, was off by 0.0025 of its norm; 0.0017 so).  The tiles overlap as in
+// longer outputs, and each second product is taken twice: in launches that leave most CUs
+// idle.  (us, as one and as two bf16: dq of 5 queries over 3000 keys, 2 heads of 64 10.7 and
+// 11.3, of one over 8192, 8 sequences of 32 heads of 128 on 8 63 and 72; dk and dv of 8 keys
+// under 700 queries of 8 heads of 128 on one 21.0 and 24.2.)
+constexpr int FEW_OUT = 2048;
+template <int D, bool KEYS, int BT, int BUFS, bool TWO>
 __global__ __launch_bounds__(THREADS)
-__attribute__((amdgpu_waves_per_eu(D == 128 && KEYS ? 1 : 2, 2)))
+__attribute__((amdgpu_waves_per_eu(D == 128 && (KEYS || TWO) ? 1 : 2, 2)))
 void seq_attn_grad_kernel(const SeqAttnGrad a)
 {
     constexpr int TILE = BT * D * 2;  // bytes of a tile
@@ -260,19 +268,18 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         u[i] = w;
         v = __builtin_bit_cast(bf16x8, u);
     };
-    auto cook = [&](auto maskc, auto ic, int from, int to, const Raw &x, Cooked &y) {
+    // (as two bf16 each with `two`: y and what it leaves)
+    auto cook = [&](auto maskc, auto twoc, auto ic, int from, int to, const Raw &x, Cooked &y,
+                    Cooked &rest) {
         constexpr int I = decltype(ic)::value;
         float p[2], ds[2];
         probability(maskc, ic, from, to, x, p, ds);
-        if constexpr (KEYS)
-            put(y.p[I / 4], I % 4, pack_bf16(p[0], p[1]));
-        put(y.ds[I / 4], I % 4, pack_bf16(ds[0], ds[1]));
-    };
-    // (as two bf16 each: y and what it leaves)
-    auto cook_both = [&](auto ic, int from, int to, const Raw &x, Cooked &y, Cooked &rest) {
-        constexpr int I = decltype(ic)::value;
-        float p[2], ds[2];
-        probability(Flag<true>{}, ic, from, to, x, p, ds);
+        if constexpr (!decltype(twoc)::value) {
+            if constexpr (KEYS)
+                put(y.p[I / 4], I % 4, pack_bf16(p[0], p[1]));
+            put(y.ds[I / 4], I % 4, pack_bf16(ds[0], ds[1]));
+            return;
+        }
         auto split = [&](bf16x8 &v, bf16x8 &w, const float (&f)[2]) {
             const uint32_t hi = pack_bf16(f[0], f[1]);
             put(v, I % 4, hi);
@@ -323,7 +330,8 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             return transposed_operand<D>(prev + which * TILE, 2 * PS + m / DT, m % DT, lane);
         }
     };
-    auto multiply = [&](auto ic, bf16x8 w, Raw &x, const Cooked &y) {
+    auto multiply = [&](auto twoc, auto ic, bf16x8 w, Raw &x, const Cooked &y,
+                        const Cooked &rest) {
         constexpr int I = decltype(ic)::value;
         if constexpr (I < FIRST) {
             const f32x16 zero = {};
@@ -335,17 +343,18 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
                 x.dp = mfma(w, I < SUMS ? ones3 : x2[I < SUMS ? 0 : i], I == 1 ? zero : x.dp);
         } else {
             constexpr int k = I - FIRST, m = KEYS ? k / 2 : k;
-            if constexpr (KEYS && k % 2)
-                acc2[m % DT] = mfma(w, y.p[KEYS ? m / DT : 0], acc2[KEYS ? m % DT : 0]);
-            else
-                acc1[m % DT] = mfma(w, y.ds[m / DT], acc1[m % DT]);
+            constexpr bool second = KEYS && k % 2;
+            f32x16 &acc = second ? acc2[KEYS ? m % DT : 0] : acc1[m % DT];
+            acc = mfma(w, second ? y.p[KEYS ? m / DT : 0] : y.ds[m / DT], acc);
+            if constexpr (decltype(twoc)::value)
+                acc = mfma(w, second ? rest.p[KEYS ? m / DT : 0] : rest.ds[m / DT], acc);
         }
     };
     // The first products of the next block with the PAIRS steps of cook for this one between
     // them, then this one's second products; operands are read AHEAD of their instruction.
     constexpr int AHEAD = 3, PAIRS = 8;
     auto run = [&](auto maskc, auto subc, const uint8_t *buf, const uint8_t *next, int r0,
-                   const Raw &cur, Raw &nxt, Cooked &now) {
+                   const Raw &cur, Raw &nxt, Cooked &now, Cooked &rest) {
         constexpr auto ns = Index<(decltype(subc)::value + 1) % SUB>{};
         const int from = lo - r0 - 4 * hf, to = hi - r0 - 4 * hf;
         constexpr int N = FIRST + SECOND;
@@ -356,11 +365,12 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
             if constexpr (I + AHEAD < N)
                 w[(I + AHEAD) % (AHEAD + 1)] =
                     operand(Index<I + AHEAD>{}, ns, subc, next, buf);
-            multiply(ic, w[I % (AHEAD + 1)], nxt, now);
+            multiply(Flag<TWO>{}, ic, w[I % (AHEAD + 1)], nxt, now, rest);
             if constexpr (I < FIRST) {
                 constexpr int P0 = PAIRS * I / FIRST, P1 = PAIRS * (I + 1) / FIRST;
                 each<P1 - P0>([&](auto pc) {
-                    cook(maskc, Index<P0 + decltype(pc)::value>{}, from, to, cur, now);
+                    cook(maskc, Flag<TWO>{}, Index<P0 + decltype(pc)::value>{}, from, to, cur,
+                         now, rest);
                 });
                 keep_order();
             }
@@ -370,13 +380,16 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         if (BIAS)
             bias(r0, x);
         Cooked none;
-        each<FIRST>([&](auto ic) { multiply(ic, operand(ic, subc, subc, buf, buf), x, none); });
+        each<FIRST>([&](auto ic) {
+            multiply(Flag<false>{}, ic, operand(ic, subc, subc, buf, buf), x, none, none);
+        });
     };
-    auto second_products = [&](auto subc, const uint8_t *buf, const Cooked &y) {
+    auto second_products = [&](auto twoc, auto subc, const uint8_t *buf, const Cooked &y,
+                               const Cooked &rest) {
         Raw none;
         each<SECOND>([&](auto ic) {
             constexpr int I = FIRST + decltype(ic)::value;
-            multiply(Index<I>{}, operand(Index<I>{}, subc, subc, buf, buf), none, y);
+            multiply(twoc, Index<I>{}, operand(Index<I>{}, subc, subc, buf, buf), none, y, rest);
         });
     };
 
@@ -433,7 +446,7 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
     // j + BUFS - 2, later ones may be in flight) and every wavefront has finished tile j - 1,
     // so its buffer takes tile j + BUFS - 1.
     static_assert(BUFS == 3 || BUFS == 4, "");
-    Cooked y;
+    Cooked y, rest;
     int r0 = 0, cbuf = 0;  // this block's first row, this tile's buffer
     auto begin = [&](int j) {
         if (BUFS == 4 && j + 2 < j1)
@@ -453,16 +466,18 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
         if (BIAS)
             bias(next, nxt);
         if (BIAS || (r0 >= free_lo && r0 + 31 <= free_hi))
-            run(Flag<false>{}, subc, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
+            run(Flag<false>{}, subc, lds + cbuf, lds + nbuf, r0, cur, nxt, y, rest);
         else
-            run(Flag<true>{}, subc, lds + cbuf, lds + nbuf, r0, cur, nxt, y);
+            run(Flag<true>{}, subc, lds + cbuf, lds + nbuf, r0, cur, nxt, y, rest);
         cbuf = nbuf;
         r0 = next;
     };
     auto last = [&](const Raw &cur) {
         const int at = r0 + 4 * hf;
-        each<PAIRS>([&](auto ic) { cook(Flag<!BIAS>{}, ic, lo - at, hi - at, cur, y); });
-        second_products(Index<SUB - 1>{}, lds + cbuf, y);
+        each<PAIRS>([&](auto ic) {
+            cook(Flag<!BIAS>{}, Flag<TWO>{}, ic, lo - at, hi - at, cur, y, rest);
+        });
+        second_products(Flag<TWO>{}, Index<SUB - 1>{}, lds + cbuf, y, rest);
     };
     if (few) {
         for (int j = j0; j < j1; ++j) {
@@ -478,11 +493,12 @@ void seq_attn_grad_kernel(const SeqAttnGrad a)
                 const int at = (first + (KEYS ? j % tiles : j)) * BT + 32 * decltype(subc)::value;
                 const int from = lo - at - 4 * hf, to = hi - at - 4 * hf;
                 Raw x;
-                Cooked rest;
                 first_products(subc, buf, at, x);
-                each<PAIRS>([&](auto ic) { cook_both(ic, from, to, x, y, rest); });
-                second_products(subc, buf, y);
-                second_products(subc, buf, rest);
+                each<PAIRS>([&](auto ic) {
+                    cook(Flag<true>{}, Flag<true>{}, ic, from, to, x, y, rest);
+                });
+                second_products(Flag<false>{}, subc, buf, y, y);
+                second_products(Flag<false>{}, subc, buf, rest, rest);
             });
         }
     } else if (j0 < j1) {
@@ -590,12 +606,21 @@ __global__ __launch_bounds__(256) void attn_grad_join_kernel(const SeqAttnGrad a
 // dv) of 256 for D = 64; for D = 128 dq takes all 256, with 14 values spilled outside of the
 // loop over tiles, and kept keys 361 of the 512 that a workgroup alone on its CU has.
 constexpr int tile_rows(int D, bool keys) { return D == 64 || keys ? 64 : 32; }
-constexpr int on_a_cu(int D, bool keys) { return D == 64 || !keys ? 2 : 1; }
+constexpr int on_a_cu(int D, bool keys, bool two) { return D == 64 || !(keys || two) ? 2 : 1; }
+
+int64_t kept(const SeqAttn &s, bool keys)
+{
+    return keys ? s.KT : (int64_t)s.T * (s.H / s.Hk);
+}
+
+bool few_out(const SeqAttn &s, bool keys)
+{
+    return kept(s, keys) * s.B * s.Hk <= FEW_OUT;
+}
 
 int64_t blocks(const SeqAttn &s, bool keys)
 {
-    const int64_t rows = keys ? s.KT : (int64_t)s.T * (s.H / s.Hk);
-    return (rows + KEEP - 1) / KEEP * s.B * s.Hk;
+    return (kept(s, keys) + KEEP - 1) / KEEP * s.B * s.Hk;
 }
 
 // us of a launch (fitted to sweeps of 247 shapes in up to 8 numbers of parts; the choice
@@ -613,7 +638,7 @@ constexpr double JOIN_RATE = 4.3e6;                   // bytes a us of their val
 double parts_us(const SeqAttn &s, bool keys, int parts)
 {
     const StepCost &c = STEP[keys][s.dh == 128];
-    const bool two = on_a_cu(s.dh, keys) == 2;
+    const bool two = on_a_cu(s.dh, keys, few_out(s, keys)) == 2;
     const int G = s.H / s.Hk;
     const double w = (double)blocks(s, keys) * parts, slots = (two ? 2.0 : 1.0) * s.cus;
     const double most = std::ceil((keys ? s.T : s.KT) / 32.0) * (keys ? G : 1);
@@ -637,17 +662,20 @@ hipError_t go(const SeqAttnGrad &g, hipStream_t stream)
     SeqAttnGrad a = g;
     const int parts = KEYS ? a.kparts : a.qparts;
     const unsigned grid = (unsigned)(blocks(a.s, KEYS) * parts);
+    const bool two = few_out(a.s, KEYS);
     if (grid)
-        order_work(a.s, grid / ((int64_t)a.s.B * a.s.Hk), on_a_cu(D, KEYS));
-    constexpr int BT = tile_rows(D, KEYS);
-    if (grid)
-        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, BT, BT == 64 ? 3 : 4>), dim3(grid),
+        order_work(a.s, grid / ((int64_t)a.s.B * a.s.Hk), on_a_cu(D, KEYS, two));
+    constexpr int BT = tile_rows(D, KEYS), BUFS = BT == 64 ? 3 : 4;
+    if (grid && two)
+        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, BT, BUFS, true>), dim3(grid),
+                           dim3(THREADS), 0, stream, a);
+    else if (grid)
+        hipLaunchKernelGGL((seq_attn_grad_kernel<D, KEYS, BT, BUFS, false>), dim3(grid),
                            dim3(THREADS), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts < 2 || !grid)
         return e;
-    const int64_t rows = KEYS ? a.s.KT : (int64_t)a.s.T * (a.s.H / a.s.Hk);
-    const int64_t threads = (int64_t)a.s.B * a.s.Hk * rows * (D / 4);
+    const int64_t threads = (int64_t)a.s.B * a.s.Hk * kept(a.s, KEYS) * (D / 4);
     hipLaunchKernelGGL((attn_grad_join_kernel<D, KEYS>),
                        dim3((unsigned)((threads + 255) / 256), KEYS ? 2 : 1), dim3(256), 0, stream,
                        a);
